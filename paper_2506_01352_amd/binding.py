@@ -32,6 +32,22 @@ class tahq_naive_config(C.Structure):
     ]
 
 
+class tahq_mx4_config(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "rows", "cols", "ld", "dtype", "transform", "scale_rule")]
+
+
+class tahq_mx4_matmul_config(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "m", "n", "k", "ldc", "out_dtype", "accumulate")]
+
+
+class tahq_norm_config(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("rows", C.c_uint32), ("cols", C.c_uint32), ("dtype", C.c_uint32), ("gate_rows", C.c_uint32),
+        ("eps", C.c_float), ("residual_scale", C.c_float),
+        ("accumulate", C.c_uint32), ("transform", C.c_uint32), ("scale_rule", C.c_uint32),
+    ]
+
+
 _lib = None
 
 
@@ -95,6 +111,23 @@ def _load():
     L.tahq_naive_encode.argtypes = [PN, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     L.tahq_naive_decode.restype = C.c_int
     L.tahq_naive_decode.argtypes = [PN, C.c_void_p, C.c_size_t, C.c_void_p, C.c_uint32, C.c_void_p]
+    V, Z, PX, PM, PB = C.c_void_p, C.c_size_t, C.POINTER(tahq_mx4_config), C.POINTER(tahq_mx4_matmul_config), C.POINTER(tahq_norm_config)
+    for name, result, arguments in (
+            ("tahq_mx4_config_default", None, [PX]),
+            ("tahq_mx4_packed_size", Z, [C.c_uint32, C.c_uint32]),
+            ("tahq_mx4_quantize", C.c_int, [PX, V, V, Z, V, Z, V]),
+            ("tahq_mx4_dequantize", C.c_int, [PX, V, Z, V, V]),
+            ("tahq_mx4_matmul_config_default", None, [PM]),
+            ("tahq_mx4_matmul_workspace_size", Z, [PM]),
+            ("tahq_mx4_matmul", C.c_int, [PM, V, Z, V, Z, V, V, Z, V]),
+            ("tahq_mx4_linear_workspace_size", Z, [PX, PM]),
+            ("tahq_mx4_linear", C.c_int, [PX, PM, V, V, Z, V, V, Z, V]),
+            ("tahq_norm_config_default", None, [PB]),
+            ("tahq_norm_forward", C.c_int, [PB, V, V, V, V, V, V, V, V, Z, V, V]),
+            ("tahq_norm_workspace_size", Z, [PB]),
+            ("tahq_norm_backward", C.c_int, [PB] + [V] * 14 + [Z, V])):
+        f = getattr(L, name)
+        f.restype, f.argtypes = result, arguments
     _lib = L
     return L
 
@@ -346,3 +379,306 @@ class Codec:
     def decode(self, stream=None):
         tahq_decode(self.cfg, self.packed, self.out, self.out_dtype, stream)
         return self.out
+
+
+# ---- microscaled 4-bit matrices (include/tahq_mx4.h)
+
+MX4_FLOOR, MX4_COVER = 0, 1
+
+
+def tahq_mx4_config_default():
+    cfg = tahq_mx4_config()
+    _load().tahq_mx4_config_default(C.byref(cfg))
+    return cfg
+
+
+def make_mx4_config(rows, cols, dtype, ld=0, transform=0, scale_rule=MX4_FLOOR):
+    cfg = tahq_mx4_config_default()
+    cfg.rows, cfg.cols, cfg.dtype, cfg.ld, cfg.transform, cfg.scale_rule = rows, cols, dtype, ld, transform, scale_rule
+    return cfg
+
+
+def tahq_mx4_packed_size(rows, cols):
+    return int(_load().tahq_mx4_packed_size(rows, cols))
+
+
+def _strided_elements(rows, cols, ld):
+    """Elements from the first to the last one of a [rows, cols] tensor of row stride ld."""
+    return (rows - 1) * (ld or cols) + cols if rows and cols else 0
+
+
+def _rows_ptr(t, ld):
+    """Device address of a row-major tensor whose rows may lie `ld` elements apart: contiguous, or a two-dimensional view that says so."""
+    if t is None or isinstance(t, int):
+        return t
+    if not t.is_contiguous():
+        assert t.is_cuda and t.dim() == 2 and t.stride(1) == 1 and t.stride(0) == ld, "device tensor, rows of unit stride, ld apart"
+        return t.data_ptr()
+    return _dev_ptr(t)
+
+
+def _check_rows(where, name, t, rows, cols, ld, dtype):
+    """_check_tensor for a tensor of rows that lie `ld` elements apart; a view is checked by its own shape."""
+    if t is None or isinstance(t, int):
+        return
+    if t.is_contiguous():
+        _check_tensor(where, name, t, _strided_elements(rows, cols, ld), dtype)
+    elif dtype in _ESIZE and (t.element_size() != _ESIZE[dtype] or t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols):
+        raise ValueError(f"{where}: {name} is a {tuple(t.shape)} view of {t.element_size()}-byte elements, the configuration needs "
+                         f"[{rows}, {cols}] of {_ESIZE[dtype]}")
+
+
+def tahq_mx4_quantize(cfg, d_in, d_packed=None, d_packed_t=None, stream=None):
+    """[rows, cols] -> packed along rows (d_packed) and / or along columns (d_packed_t), read once."""
+    _check_rows("tahq_mx4_quantize", "d_in", d_in, cfg.rows, cfg.cols, cfg.ld, cfg.dtype)
+    rc = (_lib or _load()).tahq_mx4_quantize(C.byref(cfg), _rows_ptr(d_in, cfg.ld), _dev_ptr(d_packed), _nbytes(d_packed),
+                                             _dev_ptr(d_packed_t), _nbytes(d_packed_t), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_mx4_quantize")
+
+
+def tahq_mx4_dequantize(cfg, d_packed, d_out, stream=None):
+    _check_rows("tahq_mx4_dequantize", "d_out", d_out, cfg.rows, cfg.cols, cfg.ld, cfg.dtype)
+    rc = (_lib or _load()).tahq_mx4_dequantize(C.byref(cfg), _dev_ptr(d_packed), _nbytes(d_packed), _rows_ptr(d_out, cfg.ld),
+                                               _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_mx4_dequantize")
+
+
+def tahq_mx4_matmul_config_default():
+    cfg = tahq_mx4_matmul_config()
+    _load().tahq_mx4_matmul_config_default(C.byref(cfg))
+    return cfg
+
+
+def make_mx4_matmul_config(m, n, k, out_dtype, ldc=0, accumulate=0):
+    cfg = tahq_mx4_matmul_config_default()
+    cfg.m, cfg.n, cfg.k, cfg.out_dtype, cfg.ldc, cfg.accumulate = m, n, k, out_dtype, ldc, accumulate
+    return cfg
+
+
+def tahq_mx4_matmul_workspace_size(cfg):
+    return int(_load().tahq_mx4_matmul_workspace_size(C.byref(cfg)))
+
+
+def tahq_mx4_matmul(cfg, d_a, d_b, d_c, d_workspace=None, stream=None):
+    """C[m, n] (+)= A[m, k] B[n, k]^T of packed matrices."""
+    _check_rows("tahq_mx4_matmul", "d_c", d_c, cfg.m, cfg.n, cfg.ldc, cfg.out_dtype)
+    rc = (_lib or _load()).tahq_mx4_matmul(C.byref(cfg), _dev_ptr(d_a), _nbytes(d_a), _dev_ptr(d_b), _nbytes(d_b), _rows_ptr(d_c, cfg.ldc),
+                                           _dev_ptr(d_workspace), _nbytes(d_workspace), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_mx4_matmul")
+
+
+def tahq_mx4_linear_workspace_size(x, cfg):
+    return int(_load().tahq_mx4_linear_workspace_size(C.byref(x), C.byref(cfg)))
+
+
+def tahq_mx4_linear(x, cfg, d_x, d_b, d_y, d_workspace, stream=None):
+    """y[m, n] (+)= quantized(x)[m, k] B[n, k]^T, x in fp32 or bf16."""
+    _check_rows("tahq_mx4_linear", "d_x", d_x, x.rows, x.cols, x.ld, x.dtype)
+    _check_rows("tahq_mx4_linear", "d_y", d_y, cfg.m, cfg.n, cfg.ldc, cfg.out_dtype)
+    rc = (_lib or _load()).tahq_mx4_linear(C.byref(x), C.byref(cfg), _rows_ptr(d_x, x.ld), _dev_ptr(d_b), _nbytes(d_b),
+                                           _rows_ptr(d_y, cfg.ldc), _dev_ptr(d_workspace), _nbytes(d_workspace), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_mx4_linear")
+
+
+def _bytes_on(device, size):
+    import torch
+    return torch.empty(max(size, 16), dtype=torch.uint8, device=device)
+
+
+def _torch_dtype(dtype):
+    import torch
+    return torch.float32 if dtype == F32 else torch.bfloat16
+
+
+class Mx4Tensor:
+    """Buffers of one tensor's packed form, along its rows and if asked along its columns, and of its values back."""
+
+    def __init__(self, cfg, transposed=False, device="cuda:0"):
+        import torch
+        if tahq_mx4_packed_size(cfg.rows, cfg.cols) == 0:
+            raise TahqError(2, "tahq_mx4_packed_size")
+        self.cfg = cfg
+        self.packed = _bytes_on(device, tahq_mx4_packed_size(cfg.rows, cfg.cols))
+        self.packed_t = _bytes_on(device, tahq_mx4_packed_size(cfg.cols, cfg.rows)) if transposed else None
+        self._values = make_mx4_config(cfg.rows, cfg.cols, cfg.dtype, 0, cfg.transform, cfg.scale_rule)
+        self._values_t = make_mx4_config(cfg.cols, cfg.rows, cfg.dtype, 0, cfg.transform, cfg.scale_rule)
+        kind = _torch_dtype(cfg.dtype)
+        self.out = torch.empty(cfg.rows, cfg.cols, dtype=kind, device=device)
+        self.out_t = torch.empty(cfg.cols, cfg.rows, dtype=kind, device=device) if transposed else None
+
+    def quantize(self, d_in, stream=None):
+        tahq_mx4_quantize(self.cfg, d_in, self.packed, self.packed_t, stream)
+        return (self.packed,) if self.packed_t is None else (self.packed, self.packed_t)
+
+    def dequantize(self, stream=None):
+        """The values of the packed forms: (x,), or (x, x transposed)."""
+        tahq_mx4_dequantize(self._values, self.packed, self.out, stream)
+        if self.packed_t is None:
+            return (self.out,)
+        tahq_mx4_dequantize(self._values_t, self.packed_t, self.out_t, stream)
+        return self.out, self.out_t
+
+
+class Mx4Linear:
+    """A linear layer y = x W^T in mx4 for a fixed number of tokens: W packed once, buffers for x, y and, for training, for the
+    backward pass.  `weight`: [n, k], fp32 or bf16, which is also the dtype of x, y and their gradients; grad_w is fp32."""
+
+    def __init__(self, weight, tokens, transform=0, scale_rule=MX4_FLOOR, training=False, accumulate=0):
+        import torch
+        n, k = weight.shape
+        device, dtype = weight.device, F32 if weight.dtype == torch.float32 else BF16
+        self.training = training
+        self._x = make_mx4_config(tokens, k, dtype, 0, transform, scale_rule)
+        self._dy = make_mx4_config(tokens, n, dtype, 0, transform, scale_rule)
+        self._w = make_mx4_config(n, k, dtype, 0, transform, scale_rule)
+        self._forward = make_mx4_matmul_config(tokens, n, k, dtype)
+        self._dx = make_mx4_matmul_config(tokens, k, n, dtype)
+        self._dw = make_mx4_matmul_config(n, k, tokens, F32, 0, accumulate)
+        if not tahq_mx4_linear_workspace_size(self._x, self._forward):
+            raise TahqError(2, "tahq_mx4_linear_workspace_size")
+        self.weight = _bytes_on(device, tahq_mx4_packed_size(n, k))
+        self.y = torch.empty(tokens, n, dtype=weight.dtype, device=device)
+        need = tahq_mx4_linear_workspace_size(self._x, self._forward)
+        self.weight_t = self.x_t = None
+        if training:
+            self.weight_t = _bytes_on(device, tahq_mx4_packed_size(k, n))
+            self.x, self.x_t = _bytes_on(device, tahq_mx4_packed_size(tokens, k)), _bytes_on(device, tahq_mx4_packed_size(k, tokens))
+            self.dy, self.dy_t = _bytes_on(device, tahq_mx4_packed_size(tokens, n)), _bytes_on(device, tahq_mx4_packed_size(n, tokens))
+            self.grad_x = torch.empty(tokens, k, dtype=weight.dtype, device=device)
+            self.grad_w = torch.zeros(n, k, dtype=torch.float32, device=device)
+            need = max([need] + [tahq_mx4_matmul_workspace_size(c) for c in (self._forward, self._dx, self._dw)])
+        self.workspace = _bytes_on(device, need)
+        self.update(weight)
+
+    def update(self, weight, stream=None):
+        """Pack W, e.g. after an optimizer's step."""
+        tahq_mx4_quantize(self._w, weight, self.weight, self.weight_t, stream)
+
+    def forward(self, x, stream=None):
+        """y; in training x is kept along its tokens for the weight's gradient."""
+        if not self.training:
+            tahq_mx4_linear(self._x, self._forward, x, self.weight, self.y, self.workspace, stream)
+            return self.y
+        tahq_mx4_quantize(self._x, x, self.x, self.x_t, stream)
+        return self.product(self.x, stream)
+
+    def product(self, x_packed, stream=None):
+        """y of an x that is packed already, e.g. by BlockNorm."""
+        tahq_mx4_matmul(self._forward, x_packed, self.weight, self.y, self.workspace, stream)
+        return self.y
+
+    def backward(self, grad_y, stream=None):
+        """(gradient of x, gradient of W); the latter is added to with accumulate = 1."""
+        tahq_mx4_quantize(self._dy, grad_y, self.dy, self.dy_t, stream)
+        tahq_mx4_matmul(self._dx, self.dy, self.weight_t, self.grad_x, self.workspace, stream)
+        tahq_mx4_matmul(self._dw, self.dy_t, self.x_t, self.grad_w, self.workspace, stream)
+        return self.grad_x, self.grad_w
+
+
+# ---- norms before and after a block (include/tahq_norm.h)
+
+NORM_MAX_COLS = 8192
+
+
+def tahq_norm_config_default():
+    cfg = tahq_norm_config()
+    _load().tahq_norm_config_default(C.byref(cfg))
+    return cfg
+
+
+def make_norm_config(rows, cols, dtype, gate_rows=0, eps=1e-6, residual_scale=1.0, accumulate=0, transform=0, scale_rule=MX4_FLOOR):
+    cfg = tahq_norm_config_default()
+    cfg.rows, cfg.cols, cfg.dtype, cfg.gate_rows, cfg.eps, cfg.residual_scale = rows, cols, dtype, gate_rows, eps, residual_scale
+    cfg.accumulate, cfg.transform, cfg.scale_rule = accumulate, transform, scale_rule
+    return cfg
+
+
+def _gate_groups(cfg):
+    return -(-cfg.rows // cfg.gate_rows) if cfg.gate_rows else 0
+
+
+def _check_norm(where, cfg, tensors, weights, gate):
+    for name, t in tensors.items():
+        _check_tensor(where, name, t, cfg.rows * cfg.cols, cfg.dtype)
+    for name, t in weights.items():
+        _check_tensor(where, name, t, cfg.cols, cfg.dtype)
+    _check_tensor(where, "d_gate", gate, _gate_groups(cfg) * cfg.cols, cfg.dtype)
+
+
+def tahq_norm_forward(cfg, d_residual, d_block, d_w_post, d_gate, d_w_pre, d_residual_out, d_h=None, d_h_mx4=None, d_stats=None,
+                      stream=None):
+    """r' = residual_scale r + gate RMSNorm(block) w_post and h = RMSNorm(r') w_pre; halves may be None, see include/tahq_norm.h."""
+    _check_norm("tahq_norm_forward", cfg, {"d_residual": d_residual, "d_block": d_block, "d_residual_out": d_residual_out, "d_h": d_h},
+                {"d_w_post": d_w_post, "d_w_pre": d_w_pre}, d_gate)
+    _check_tensor("tahq_norm_forward", "d_stats", d_stats, 2 * cfg.rows, F32)
+    rc = (_lib or _load()).tahq_norm_forward(
+        C.byref(cfg), _dev_ptr(d_residual), _dev_ptr(d_block), _dev_ptr(d_w_post), _dev_ptr(d_gate), _dev_ptr(d_w_pre),
+        _dev_ptr(d_residual_out), _dev_ptr(d_h), _dev_ptr(d_h_mx4), _nbytes(d_h_mx4), _dev_ptr(d_stats), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_norm_forward")
+
+
+def tahq_norm_workspace_size(cfg):
+    return int(_load().tahq_norm_workspace_size(C.byref(cfg)))
+
+
+def tahq_norm_backward(cfg, d_grad_residual_out, d_grad_h, d_block, d_w_post, d_gate, d_residual_out, d_w_pre, d_stats,
+                       d_grad_residual, d_grad_block, d_grad_w_post, d_grad_gate, d_grad_w_pre, d_workspace, stream=None):
+    _check_norm("tahq_norm_backward", cfg,
+                {"d_grad_residual_out": d_grad_residual_out, "d_grad_h": d_grad_h, "d_block": d_block, "d_residual_out": d_residual_out,
+                 "d_grad_residual": d_grad_residual, "d_grad_block": d_grad_block}, {"d_w_post": d_w_post, "d_w_pre": d_w_pre}, d_gate)
+    for name, t, n in (("d_stats", d_stats, 2 * cfg.rows), ("d_grad_w_post", d_grad_w_post, cfg.cols),
+                       ("d_grad_w_pre", d_grad_w_pre, cfg.cols), ("d_grad_gate", d_grad_gate, _gate_groups(cfg) * cfg.cols)):
+        _check_tensor("tahq_norm_backward", name, t, n, F32)
+    rc = (_lib or _load()).tahq_norm_backward(
+        C.byref(cfg), _dev_ptr(d_grad_residual_out), _dev_ptr(d_grad_h), _dev_ptr(d_block), _dev_ptr(d_w_post), _dev_ptr(d_gate),
+        _dev_ptr(d_residual_out), _dev_ptr(d_w_pre), _dev_ptr(d_stats), _dev_ptr(d_grad_residual), _dev_ptr(d_grad_block),
+        _dev_ptr(d_grad_w_post), _dev_ptr(d_grad_gate), _dev_ptr(d_grad_w_pre), _dev_ptr(d_workspace), _nbytes(d_workspace),
+        _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_norm_backward")
+
+
+class BlockNorm:
+    """Buffers of one configuration's norms.  mx4: h leaves as a packed matrix; otherwise in the configuration's dtype."""
+
+    def __init__(self, cfg, mx4=False, device="cuda:0"):
+        import torch
+        need = tahq_norm_workspace_size(cfg)
+        if need == 0:
+            raise TahqError(2, "tahq_norm_workspace_size")
+        self.cfg, self.mx4, kind = cfg, mx4, _torch_dtype(cfg.dtype)
+        shape = (cfg.rows, cfg.cols)
+        self.residual_out = torch.empty(shape, dtype=kind, device=device)
+        self.h = _bytes_on(device, tahq_mx4_packed_size(*shape)) if mx4 else torch.empty(shape, dtype=kind, device=device)
+        self.stats = torch.empty(2, cfg.rows, dtype=torch.float32, device=device)
+        self._need, self._device, self.workspace = need, device, None
+
+    def forward(self, residual, block, w_post, gate, w_pre, stream=None):
+        """(r', h); block, w_post and gate may be None, or w_pre."""
+        h = None if w_pre is None else self.h
+        tahq_norm_forward(self.cfg, residual, block, w_post, gate, w_pre, self.residual_out, None if self.mx4 else h,
+                          h if self.mx4 else None, self.stats, stream)
+        return self.residual_out, h
+
+    def backward(self, grad_residual_out, grad_h, block, w_post, gate, residual_out, w_pre, stats, stream=None):
+        """Gradients of residual, block, w_post, gate and w_pre by name; None for what there is not."""
+        import torch
+        if self.workspace is None:
+            cfg, device = self.cfg, self._device
+            self.workspace = _bytes_on(device, self._need)
+            self.grad_residual, self.grad_block = (torch.empty_like(self.residual_out) for _ in range(2))
+            self.grad_w_post, self.grad_w_pre = (torch.zeros(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
+            self.grad_gate = torch.zeros(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
+        got = {"grad_residual": self.grad_residual, "grad_block": None, "grad_w_post": None, "grad_gate": None, "grad_w_pre": None}
+        if block is not None:
+            got.update(grad_block=self.grad_block, grad_w_post=self.grad_w_post, grad_gate=self.grad_gate)
+        if grad_h is not None:
+            got["grad_w_pre"] = self.grad_w_pre
+        tahq_norm_backward(self.cfg, grad_residual_out, grad_h, block, w_post, gate, residual_out, w_pre, stats, got["grad_residual"],
+                           got["grad_block"], got["grad_w_post"], got["grad_gate"], got["grad_w_pre"], self.workspace, stream)
+        return got

@@ -6,7 +6,7 @@ import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("tahq.hip", "tahq_rank_quant.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("tahq.hip", "tahq_rank_quant.hip", "tahq_mx4.hip", "tahq_norm.hip")]
 LIB = os.path.join(HERE, "libtahq.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

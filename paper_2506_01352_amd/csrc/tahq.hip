@@ -42,8 +42,6 @@ std::mutex g_scratch_mutex;
 void *g_scratch_ptr[kMaxDevices];
 
 
-inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
 constexpr uint32_t kMaxGridY = 65535;
 
 inline uint32_t blocks_for(uint64_t threads) { return (uint32_t)((threads + 255) / 256); }

@@ -1,9 +1,7 @@
 // What the translation units of the library share on the host: launches, dispatch, the plan of the small tensors' launch.
 #pragma once
+#include "tahq_enqueue.hpp"
 #include "tahq_rank_quant.hpp"
-
-#include <tuple>
-#include <utility>
 
 namespace tahq {
 
@@ -17,31 +15,6 @@ inline void dispatch(uint32_t G, bool bf16, Args... args)
     else if (G == 64) { if (bf16) F<64, true>::run(args...); else F<64, false>::run(args...); }
     else { if (bf16) F<128, true>::run(args...); else F<128, false>::run(args...); }
 }
-
-// Kernel launches of one call: each launch returns its own status (the thread's sticky "last error", which may
-// belong to the caller's earlier work, is neither read nor cleared), and after a failure nothing more is enqueued.
-struct Enqueue {
-    hipStream_t stream;
-    hipError_t status = hipSuccess;
-
-    template <typename... P, typename... A>
-    void operator()(void (*kernel)(P...), dim3 grid, dim3 block, A... args)
-    {
-        static_assert(sizeof...(P) == sizeof...(A), "one argument per kernel parameter");
-        if (status != hipSuccess) return;
-        std::tuple<P...> values(static_cast<P>(args)...);
-        status = launch(kernel, grid, block, values, std::index_sequence_for<P...>{});
-    }
-    tahq_status result() const { return status == hipSuccess ? TAHQ_OK : TAHQ_ERR_HIP; }
-
-private:
-    template <typename... P, size_t... I>
-    hipError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, std::tuple<P...> &values, std::index_sequence<I...>)
-    {
-        void *ptrs[] = {static_cast<void *>(&std::get<I>(values))...};
-        return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, block, ptrs, 0, stream);
-    }
-};
 
 // Fewer wavefronts than the chip has vector units (256 compute units of four), at the usual number of lanes per tile: the launch
 // takes as long as one lane does, and tiles are spread over more lanes, as long as those make no more wavefronts per vector

@@ -1,0 +1,188 @@
+// Layout and numerics of packed mx4 matrices (include/tahq_mx4.h), shared by the quantizer, the products and the norm that
+// quantizes its output.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tahq_mx4.h"
+
+namespace tahq {
+
+constexpr float kRoot32 = 0.17677669529663687f;            // fp32(1 / sqrt(32))
+constexpr uint32_t kCover = 0x3fffffu;                     // see block_scale
+
+// Rows and columns come in units of the matrix instruction's operand, 32 rows x 64 columns; a lane's four scale bytes belong to
+// four such units side by side, so that one register serves 256 columns (the instruction picks the byte).
+struct Mx4Layout {
+    uint32_t rb, kb, kc;
+    __host__ __device__ Mx4Layout(uint32_t rows, uint32_t cols) : rb((rows + 31) / 32), kb((cols + 63) / 64), kc((cols + 255) / 256) {}
+    __host__ __device__ uint64_t scales() const { return (uint64_t)rb * kb * 1024; }
+    __host__ __device__ uint64_t total() const { return scales() + (uint64_t)rb * kc * 256; }
+    // 16 bytes of codes, and the scale's byte, of row r's block b
+    __host__ __device__ uint64_t code(uint32_t r, uint32_t b) const
+    {
+        return ((uint64_t)(r / 32) * kb + b / 2) * 1024 + (b % 2) * 512 + (r % 32) * 16;
+    }
+    __host__ __device__ uint64_t scale(uint32_t r, uint32_t b) const
+    {
+        return scales() + ((uint64_t)(r / 32) * kc + b / 8) * 256 + (b % 2) * 128 + (r % 32) * 4 + b / 2 % 4;
+    }
+};
+
+// ---------------------------------------------------------------- loads
+
+// Eight consecutive elements as fp32.  Rows need no alignment beyond their elements': a 16-byte load may start anywhere.
+template <bool BF16>
+__device__ __forceinline__ void load8(const void *base, uint64_t at, float (&x)[8])
+{
+    if constexpr (BF16) {
+        uint32_t w[4];
+        __builtin_memcpy(w, static_cast<const uint16_t *>(base) + at, 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+        __builtin_memcpy(x, static_cast<const float *>(base) + at, 32);
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ float load1(const void *base, uint64_t at)
+{
+    if constexpr (BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(base)[at] << 16);
+    else return static_cast<const float *>(base)[at];
+}
+// Of eight elements the first `valid`, the others 0.  EIGHTS: `valid` is 8 or more, or not above 0.
+template <bool BF16, bool EIGHTS>
+__device__ __forceinline__ void load8(const void *base, uint64_t at, int64_t valid, float (&x)[8])
+{
+    if (valid >= 8) {
+        load8<BF16>(base, at, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = !EIGHTS && i < valid ? load1<BF16>(base, at + i) : 0.0f;
+    }
+}
+
+// two fp32 to bf16, nearest even (v_cvt_pk_bf16_f32)
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
+{
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    const pair p = {(__bf16)lo, (__bf16)hi};
+    return __builtin_bit_cast(uint32_t, p);
+}
+template <bool BF16>
+__device__ __forceinline__ void store1(void *base, uint64_t at, float x)
+{
+    if constexpr (BF16) static_cast<uint16_t *>(base)[at] = (uint16_t)two_bf16(x, 0.0f);
+    else static_cast<float *>(base)[at] = x;
+}
+template <bool BF16, bool EIGHTS>
+__device__ __forceinline__ void store8(void *base, uint64_t at, int64_t valid, const float (&x)[8])
+{
+    if (valid >= 8) {
+        if constexpr (BF16) {
+            const uint32_t w[4] = {two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7])};
+            __builtin_memcpy(static_cast<uint16_t *>(base) + at, w, 16);
+        } else {
+            __builtin_memcpy(static_cast<float *>(base) + at, x, 32);
+        }
+    } else if constexpr (!EIGHTS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) store1<BF16>(base, at + i, x[i]);
+    }
+}
+
+// ---------------------------------------------------------------- a block
+
+// the value of the lane whose number differs in bit 0 (CTRL 0xb1) or bit 1 (0x4e): quad permutations
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL>
+__device__ __forceinline__ float quadf(float v) { return __uint_as_float(quad<CTRL>(__float_as_uint(v))); }
+
+// butterflies h = 1, 2, .. N/2 on the N elements of one lane
+template <int N>
+__device__ __forceinline__ void butterfly(float (&x)[N])
+{
+#pragma unroll
+    for (int h = 1; h < N; h *= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (!(i & h)) {
+                const float a = x[i], b = x[i + h];
+                x[i] = a + b;
+                x[i + h] = a - b;
+            }
+}
+// a block whose four lanes hold eight elements each
+__device__ __forceinline__ void rotate_quad(float (&x)[8])
+{
+    butterfly(x);
+    const uint32_t lane = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float o = quadf<0xb1>(x[i]);
+        x[i] = lane & 1 ? o - x[i] : x[i] + o;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float o = quadf<0x4e>(x[i]);
+        x[i] = (lane & 2 ? o - x[i] : x[i] + o) * kRoot32;
+    }
+}
+
+// The scale byte of a block from the bits of its largest magnitude (as an integer the largest, too; infinities and NaN are above
+// all others).  The exponent field less 2; the cover rule counts a magnitude above 1.5 * 2^e, i.e. above 6 units, to the next
+// exponent: adding 0x3fffff to the bits carries into the exponent exactly for a fraction above 0x400000.
+__device__ __forceinline__ uint32_t block_scale(uint32_t top, uint32_t cover)
+{
+    const uint32_t e = (top + cover) >> 23;
+    const uint32_t s = e > 2 ? e - 2 : 0;
+    return top >= 0x7f800000u ? 255u : s;
+}
+// 2^(s - 127), as the conversion takes it
+__device__ __forceinline__ float scale_value(uint32_t s) { return __uint_as_float(s ? s << 23 : 0x400000u); }
+
+// eight elements to codes, low half of the first byte first
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], uint32_t s)
+{
+    const float v = scale_value(s);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], v, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], v, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], v, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], v, 3);
+    return s == 255u ? 0u : w;
+}
+
+// A block of which four neighbouring lanes hold eight elements each: its codes (this lane's) and scale byte
+template <bool ROTATE>
+__device__ __forceinline__ uint32_t quantize_quad(float (&x)[8], uint32_t cover, uint32_t &s)
+{
+    if constexpr (ROTATE) rotate_quad(x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = max(top, quad<0xb1>(top));
+    top = max(top, quad<0x4e>(top));
+    s = block_scale(top, cover);
+    return codes8(x, s);
+}
+
+// the magnitude a code stands for, times its block's scale; `scale` of a block of NaN is NaN
+__device__ __forceinline__ float code_value(uint32_t code, float scale)
+{
+    // 0, .5: subnormal grid; otherwise exponent (code >> 1 & 3), fraction bit code & 1
+    const uint32_t m = code & 7u;
+    const float v = m < 2 ? 0.5f * (float)m : __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22);
+    return (code & 8u ? -v : v) * scale;
+}
+__device__ __forceinline__ float dequant_scale(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : scale_value(s); }
+
+}  // namespace tahq

@@ -1,0 +1,143 @@
+// Quantization to mx4 along rows, along columns or both from one read, and back.
+//
+// Both are bound by memory: an element takes 2 or 4 bytes to read, 17/32 of a byte to write per orientation, and about ten vector
+// instructions.
+#pragma once
+#include "tahq_mx4_common.hpp"
+
+namespace tahq {
+
+constexpr uint32_t kQuantRows = 64, kQuantCols = 256, kQuantThreads = 256;
+
+// A workgroup takes a tile of 64 rows x 256 columns.  Along rows: a lane loads 16 bytes of bf16 (32 of fp32), neighbours in a row
+// next to each other, and four lanes share a block; the tile is two units of rows x four of columns, 8 KB of codes, which
+// are put in order in LDS and leave in whole lines.  Along columns: the tile passes through LDS once, and a lane takes two columns of 32
+// rows, i.e. two whole blocks, whose 16-byte codes are neighbours in the transposed matrix.
+template <bool BF16, bool ROW, bool COL, bool ROTATE>
+__global__ __launch_bounds__(kQuantThreads)
+void k_mx4_quantize(const void *in, uint8_t *packed, uint8_t *packed_t, uint32_t rows, uint32_t cols, uint64_t ld,
+                    uint32_t cover, uint32_t tiles_x)
+{
+    constexpr uint32_t RUN = 512 + 32;              // a half unit of codes in LDS: the skew spreads a wavefront's words over the banks
+    constexpr int ES = BF16 ? 2 : 4;
+    __shared__ __attribute__((aligned(16))) uint8_t codes[ROW ? 16 * RUN : 16];
+    __shared__ __attribute__((aligned(16))) uint32_t scale_words[ROW ? 128 : 4];
+    __shared__ __attribute__((aligned(16))) uint8_t tile[COL ? kQuantRows * kQuantCols * ES : 16];
+    const uint32_t tid = threadIdx.x;
+    const uint32_t r0 = blockIdx.x / tiles_x * kQuantRows, c0 = blockIdx.x % tiles_x * kQuantCols;
+    const uint32_t chunk = tid % 32, row = tid / 32;
+    const int64_t valid = (int64_t)cols - c0 - 8 * chunk;
+
+    float x[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t r = r0 + row + 8 * i;
+        load8<BF16, false>(in, (uint64_t)r * ld + c0 + 8 * chunk, r < rows ? valid : 0, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t r = row + 8 * i;                                    // in the tile
+        if constexpr (COL) store8<BF16, true>(tile, r * kQuantCols + 8 * chunk, 8, x[i]);   // exact: these were bf16
+        if constexpr (ROW) {
+            uint32_t s;
+            const uint32_t w = quantize_quad<ROTATE>(x[i], cover, s);
+            const uint32_t unit = r / 32 * 4 + chunk / 8, half = chunk / 4 % 2;
+            *reinterpret_cast<uint32_t *>(codes + (unit * 2 + half) * RUN + r % 32 * 16 + chunk % 4 * 4) = w;
+            if (chunk % 4 == 0)
+                reinterpret_cast<uint8_t *>(scale_words)[(r / 32 * 64 + half * 32 + r % 32) * 4 + chunk / 8] = (uint8_t)s;
+        }
+    }
+    __syncthreads();
+    if constexpr (ROW) {
+        const Mx4Layout L(rows, cols);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t at = (i * kQuantThreads + tid) * 16, unit = at / 1024;
+            const uint32_t rb = r0 / 32 + unit / 4, kb = c0 / 64 + unit % 4;
+            if (rb < L.rb && kb < L.kb)
+                *reinterpret_cast<uint4 *>(packed + ((uint64_t)rb * L.kb + kb) * 1024 + at % 1024) =
+                    *reinterpret_cast<const uint4 *>(codes + at / 512 * RUN + at % 512);
+        }
+        if (tid < 128) {
+            const uint32_t rb = r0 / 32 + tid / 64;
+            if (rb < L.rb)
+                reinterpret_cast<uint32_t *>(packed + L.scales())[((uint64_t)rb * L.kc + c0 / 256) * 64 + tid % 64] = scale_words[tid];
+        }
+    }
+    if constexpr (COL) {
+        // two columns x 32 rows: blocks r0/32 + tid/128 of rows c0 + 2 * (tid % 128) of the transposed matrix
+        const Mx4Layout L(cols, rows);
+        const uint32_t c = c0 + 2 * (tid % 128), b = r0 / 32 + tid / 128;
+        float y[2][32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const uint32_t at = (tid / 128 * 32 + i) * kQuantCols + 2 * (tid % 128);
+            if constexpr (BF16) {
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(tile + 2 * at);
+                y[0][i] = __uint_as_float(w << 16);
+                y[1][i] = __uint_as_float(w & 0xffff0000u);
+            } else {
+                const float2 w = *reinterpret_cast<const float2 *>(tile + 4 * at);
+                y[0][i] = w.x;
+                y[1][i] = w.y;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (ROTATE) {
+                butterfly(y[j]);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) y[j][i] *= kRoot32;
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(y[j][i]) & 0x7fffffffu);
+            const uint32_t s = block_scale(top, cover);
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float part[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) part[i] = y[j][8 * q + i];
+                w[q] = codes8(part, s);
+            }
+            if (c + j < 32 * L.rb) {                                       // rows behind `cols` hold zeros, as the tile does
+                if (b / 2 < L.kb) *reinterpret_cast<uint4 *>(packed_t + L.code(c + j, b)) = make_uint4(w[0], w[1], w[2], w[3]);
+                packed_t[L.scale(c + j, b)] = (uint8_t)s;                  // also of the blocks that fill up the last four
+            }
+        }
+    }
+}
+
+// Values of a packed matrix.  A workgroup takes 32 rows x 256 columns, 4 KB of codes; four lanes share a block, as above.
+template <bool BF16, bool ROTATE>
+__global__ __launch_bounds__(kQuantThreads)
+void k_mx4_dequantize(const uint8_t *packed, void *out, uint32_t rows, uint32_t cols, uint64_t ld, uint32_t tiles_x)
+{
+    const Mx4Layout L(rows, cols);
+    const uint32_t tid = threadIdx.x;
+    const uint32_t r0 = blockIdx.x / tiles_x * 32, c0 = blockIdx.x % tiles_x * kQuantCols;
+    const uint32_t chunk = tid % 32, row = tid / 32;
+    const int64_t valid = (int64_t)cols - c0 - 8 * chunk;
+    const uint32_t b = c0 / 32 + chunk / 4;
+    uint32_t w[4];
+    uint8_t s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t r = r0 + row + 8 * i;                               // below 32 * L.rb
+        w[i] = b / 2 < L.kb ? *reinterpret_cast<const uint32_t *>(packed + L.code(r, b) + chunk % 4 * 4) : 0u;
+        s[i] = packed[L.scale(r, b)];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t r = r0 + row + 8 * i;
+        const float v = dequant_scale(s[i]);
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = code_value(w[i] >> (4 * j), v);
+        if constexpr (ROTATE) rotate_quad(x);
+        if (r < rows) store8<BF16, false>(out, (uint64_t)r * ld + c0 + 8 * chunk, valid, x);
+    }
+}
+
+}  // namespace tahq

@@ -1,0 +1,179 @@
+// Entry points of the block norms (include/tahq_norm.h): validation, plan, launches.
+#include "tahq_enqueue.hpp"
+#include "tahq_norm.h"
+#include "tahq_norm_kernels.hpp"
+
+using namespace tahq;
+
+namespace {
+
+tahq_status check(const tahq_norm_config *c)
+{
+    if (!c) return TAHQ_ERR_NULL;
+    if (c->struct_size != sizeof *c) return TAHQ_ERR_INVALID_ARG;
+    if (c->rows == 0 || c->rows >= 0x80000000u || c->cols == 0 || c->dtype > TAHQ_BF16) return TAHQ_ERR_INVALID_ARG;
+    if (!(c->eps > 0.0f) || !(c->eps <= 3.4028234663852886e38f)) return TAHQ_ERR_INVALID_ARG;
+    if (!(__builtin_fabsf(c->residual_scale) <= 3.4028234663852886e38f)) return TAHQ_ERR_INVALID_ARG;
+    if (c->accumulate > 1 || c->transform > 1 || c->scale_rule > TAHQ_MX4_COVER) return TAHQ_ERR_INVALID_ARG;
+    if (c->cols > TAHQ_NORM_MAX_COLS) return TAHQ_ERR_UNSUPPORTED;
+    return TAHQ_OK;
+}
+
+NormShape shape_of(const tahq_norm_config *c)
+{
+    // a gate row for more tokens than there are is one for all of them
+    return {c->rows, c->cols, c->gate_rows < c->rows ? c->gate_rows : c->rows, c->eps, c->residual_scale};
+}
+
+template <bool BF16, bool EIGHTS, typename Run>
+void launch_forward(uint32_t vectors, Run run)
+{
+    if (vectors <= 1) run(k_norm_forward<BF16, EIGHTS, 256, 1>);
+    else if (vectors <= 2) run(k_norm_forward<BF16, EIGHTS, 256, 2>);
+    else run(k_norm_forward<BF16, EIGHTS, 256, 4>);
+}
+template <typename Run>
+void launch_forward(const tahq_norm_config *c, Run run)
+{
+    const uint32_t vectors = (c->cols + 2047) / 2048;
+    const bool eights = c->cols % 8 == 0;
+    if (c->dtype == TAHQ_BF16) eights ? launch_forward<true, true>(vectors, run) : launch_forward<true, false>(vectors, run);
+    else eights ? launch_forward<false, true>(vectors, run) : launch_forward<false, false>(vectors, run);
+}
+
+template <bool BF16, bool EIGHTS, typename Run>
+void launch_backward(uint32_t threads, Run run)
+{
+    if (threads == 256) run(k_norm_backward<BF16, EIGHTS, 256, 1>);
+    else if (threads == 512) run(k_norm_backward<BF16, EIGHTS, 512, 1>);
+    else run(k_norm_backward<BF16, EIGHTS, 1024, 1>);
+}
+template <typename Run>
+void launch_backward(const tahq_norm_config *c, uint32_t threads, Run run)
+{
+    const bool eights = c->cols % 8 == 0;
+    if (c->dtype == TAHQ_BF16) eights ? launch_backward<true, true>(threads, run) : launch_backward<true, false>(threads, run);
+    else eights ? launch_backward<false, true>(threads, run) : launch_backward<false, false>(threads, run);
+}
+
+// Backward: threads per row, eight channels to each, and the workgroups that share the rows
+struct BackwardPlan {
+    uint32_t threads, rows_each, workgroups;
+    uint64_t workspace;
+};
+BackwardPlan plan_backward(const tahq_norm_config *c)
+{
+    BackwardPlan p;
+    p.threads = c->cols <= 2048 ? 256 : c->cols <= 4096 ? 512 : 1024;
+    const uint32_t most = 512 * (1024 / p.threads) < 1024 ? 512 * (1024 / p.threads) : 1024;
+    p.rows_each = (c->rows + most - 1) / most;
+    if (p.rows_each < 8) p.rows_each = 8;
+    p.workgroups = (c->rows + p.rows_each - 1) / p.rows_each;
+    p.workspace = (uint64_t)p.workgroups * c->cols * 4 * (c->gate_rows ? 4 : 2);
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+void tahq_norm_config_default(tahq_norm_config *cfg)
+{
+    if (!cfg) return;
+    *cfg = tahq_norm_config{};
+    cfg->struct_size = (uint32_t)sizeof *cfg;
+    cfg->dtype = TAHQ_BF16;
+    cfg->eps = 1e-6f;
+    cfg->residual_scale = 1.0f;
+}
+
+tahq_status tahq_norm_forward(const tahq_norm_config *cfg, const void *d_residual, const void *d_block, const void *d_w_post,
+                              const void *d_gate, const void *d_w_pre, void *d_residual_out, void *d_h, void *d_h_mx4,
+                              size_t h_mx4_capacity, float *d_stats, tahq_stream stream)
+{
+    const tahq_status rc = check(cfg);
+    if (rc != TAHQ_OK) return rc;
+    if (!d_residual) return TAHQ_ERR_NULL;
+    if (d_block) {
+        if (!d_w_post || !d_residual_out || (cfg->gate_rows && !d_gate)) return TAHQ_ERR_NULL;
+        if (!cfg->gate_rows && d_gate) return TAHQ_ERR_INVALID_ARG;
+    } else if (d_w_post || d_gate) {
+        return TAHQ_ERR_INVALID_ARG;
+    }
+    if (d_w_pre) {
+        if (!d_h && !d_h_mx4) return TAHQ_ERR_NULL;
+    } else {
+        if (d_h || d_h_mx4) return TAHQ_ERR_INVALID_ARG;
+        if (!d_residual_out) return TAHQ_ERR_NULL;
+    }
+    if (d_h_mx4 && h_mx4_capacity < tahq_mx4_packed_size(cfg->rows, cfg->cols)) return TAHQ_ERR_BUFFER_TOO_SMALL;
+    for (const void *p : {d_residual, d_block, d_w_post, d_gate, d_w_pre, (const void *)d_residual_out, (const void *)d_h, (const void *)d_h_mx4, (const void *)d_stats})
+        if (misaligned(p)) return TAHQ_ERR_MISALIGNED;
+    const NormShape s = shape_of(cfg);
+    const uint32_t cover = cfg->scale_rule == TAHQ_MX4_COVER ? kCover : 0u;
+    const uint32_t total = d_h_mx4 ? 32 * ((cfg->rows + 31) / 32) : cfg->rows;
+    const uint32_t rows_each = total >= 8192 ? 8 : 1;
+    const dim3 grid((total + rows_each - 1) / rows_each);
+    Enqueue q{(hipStream_t)stream};
+    auto run = [&](auto kernel) {
+        q(kernel, grid, dim3(256), d_residual, d_block, d_w_post, d_block ? d_gate : nullptr, d_w_pre, d_residual_out, d_h,
+          static_cast<uint8_t *>(d_h_mx4), d_stats, s, cover, cfg->transform, rows_each);
+    };
+    launch_forward(cfg, run);
+    return q.result();
+}
+
+size_t tahq_norm_workspace_size(const tahq_norm_config *cfg)
+{
+    return check(cfg) == TAHQ_OK ? (size_t)plan_backward(cfg).workspace : 0;
+}
+
+tahq_status tahq_norm_backward(const tahq_norm_config *cfg, const void *d_grad_residual_out, const void *d_grad_h,
+                               const void *d_block, const void *d_w_post, const void *d_gate, const void *d_residual_out,
+                               const void *d_w_pre, const float *d_stats, void *d_grad_residual, void *d_grad_block,
+                               float *d_grad_w_post, float *d_grad_gate, float *d_grad_w_pre, void *d_workspace,
+                               size_t workspace_capacity, tahq_stream stream)
+{
+    const tahq_status rc = check(cfg);
+    if (rc != TAHQ_OK) return rc;
+    if (!d_grad_residual || !d_workspace || (!d_grad_residual_out && !d_grad_h)) return TAHQ_ERR_NULL;
+    if ((d_block || d_grad_h) && !d_stats) return TAHQ_ERR_NULL;
+    if (d_block) {
+        if (!d_w_post || !d_grad_block || !d_grad_w_post) return TAHQ_ERR_NULL;
+        if (cfg->gate_rows ? !d_gate || !d_grad_gate : false) return TAHQ_ERR_NULL;
+        if (!cfg->gate_rows && (d_gate || d_grad_gate)) return TAHQ_ERR_INVALID_ARG;
+    } else if (d_w_post || d_gate || d_grad_block || d_grad_w_post || d_grad_gate) {
+        return TAHQ_ERR_INVALID_ARG;
+    }
+    if (d_grad_h) {
+        if (!d_w_pre || !d_residual_out || !d_grad_w_pre) return TAHQ_ERR_NULL;
+    } else if (d_w_pre || d_grad_w_pre) {
+        return TAHQ_ERR_INVALID_ARG;
+    }
+    const BackwardPlan p = plan_backward(cfg);
+    if (workspace_capacity < p.workspace) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
+    for (const void *x : {d_grad_residual_out, d_grad_h, d_block, d_w_post, d_gate, d_residual_out, d_w_pre, (const void *)d_stats,
+                          (const void *)d_grad_residual, (const void *)d_grad_block, (const void *)d_grad_w_post,
+                          (const void *)d_grad_gate, (const void *)d_grad_w_pre, (const void *)d_workspace})
+        if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
+    const NormShape s = shape_of(cfg);
+    const uint64_t each = (uint64_t)p.workgroups * cfg->cols;
+    float *ws = static_cast<float *>(d_workspace);
+    const NormPartials parts = {ws, ws + each, ws + 2 * each};
+    const void *gate = d_block ? d_gate : nullptr;
+    Enqueue q{(hipStream_t)stream};
+    auto run = [&](auto kernel) {
+        q(kernel, dim3(p.workgroups), dim3(p.threads), d_grad_residual_out, d_grad_h, d_block, d_w_post, gate, d_residual_out, d_w_pre,
+          d_stats, d_grad_residual, d_grad_block, d_grad_gate, parts, s, p.rows_each, cfg->accumulate);
+    };
+    launch_backward(cfg, p.threads, run);
+    const uint32_t groups = gate ? (cfg->rows + s.gate_rows - 1) / s.gate_rows : 0;
+    if (d_block || d_grad_h) {
+        const uint32_t slots = groups < 64 ? groups : 64;
+        q(k_norm_reduce, dim3((cfg->cols + 63) / 64, 2 + slots), dim3(256), parts, d_grad_w_post, d_grad_w_pre, d_grad_gate, cfg->cols,
+          p.workgroups, cfg->rows, s.gate_rows, p.rows_each, groups, cfg->accumulate);
+    }
+    return q.result();
+}
+
+}  // extern "C"

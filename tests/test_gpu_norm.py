@@ -1,0 +1,196 @@
+"""The norms around a block through the C ABI against their 64-bit definition, forward and backward."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_01352_amd as tahq
+from oracle import mx4, norm64
+
+pytestmark = pytest.mark.gpu
+
+KINDS = {"f32": (tahq.F32, torch.float32), "bf16": (tahq.BF16, torch.bfloat16)}
+EPS, ALPHA = 1e-6, 0.8125
+UNIT = 2.0 ** -24           # half a unit in the last place of an fp32 number
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}      # of 24 and 8 significant bits
+
+
+def _tensors(rows, cols, gate_rows, halves, kind, seed=1):
+    g = torch.Generator().manual_seed(seed)
+    make = lambda *s: torch.randn(*s, generator=g)      # noqa: E731
+    t = {"residual": make(rows, cols), "block": make(rows, cols) * torch.exp(2 * make(rows, 1)), "w_post": 1 + 0.2 * make(cols),
+         "w_pre": 1 + 0.2 * make(cols), "gate": make(-(-rows // gate_rows), cols) if gate_rows else None,
+         "grad_residual_out": 1e-4 * make(rows, cols), "grad_h": 1e-4 * make(rows, cols)}
+    if rows > 2:
+        t["block"][1] = 0
+        t["residual"][1] = 0
+        t["block"][2] *= 1e-12                          # the statistics are eps
+    if halves == "pre":
+        t.update(block=None, w_post=None, gate=None)
+    if halves == "post":
+        t.update(w_pre=None, grad_h=None)
+    return {n: None if v is None else v.to(KINDS[kind][1]) for n, v in t.items()}
+
+
+def _np(v):
+    return None if v is None else v.double().cpu().numpy()
+
+
+def _cuda(t):
+    return {n: None if v is None else v.cuda() for n, v in t.items()}
+
+
+SHAPES = [(1, 1), (1, 8), (2, 7), (3, 257), (33, 96), (5, 1600), (40, 2047), (17, 2048), (9, 4100), (70, 8192), (600, 33), (8200, 64)]
+
+
+def _gates(rows, halves):
+    return (0,) if halves == "pre" else sorted({0, 1, 7, rows, rows + 3})
+
+
+@pytest.mark.parametrize("rows, cols", SHAPES)
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+@pytest.mark.parametrize("halves", ("both", "post", "pre"))
+def test_forward(rows, cols, kind, halves):
+    """Off by: a sum of squares of `cols` terms in fp32, 32 of them in a row and the rest in a tree, and a handful of roundings."""
+    for gate_rows in _gates(rows, halves):
+        t = _tensors(rows, cols, gate_rows, halves, kind)
+        d = _cuda(t)
+        cfg = tahq.make_norm_config(rows, cols, KINDS[kind][0], gate_rows, EPS, ALPHA)
+        out = torch.full((rows + 1, cols), 7.0, dtype=KINDS[kind][1], device="cuda")
+        h = torch.full((rows + 1, cols), 7.0, dtype=KINDS[kind][1], device="cuda") if halves != "post" else None
+        stats = torch.full((2 * rows + 1,), 7.0, device="cuda")
+        tahq.tahq_norm_forward(cfg, d["residual"], d["block"], d["w_post"], d["gate"], d["w_pre"], out, h, None, stats)
+        torch.cuda.synchronize()
+        n = {k: _np(v) for k, v in t.items()}
+        want, want_h, rb, rr = norm64.forward(n["residual"], n["block"], n["w_post"], n["gate"], n["w_pre"], gate_rows, float(np.float32(EPS)), ALPHA)
+        size = np.abs(ALPHA * n["residual"])
+        if halves != "pre":
+            size = size + np.abs(want - ALPHA * n["residual"])
+        off = 64 * UNIT * size + HALF[kind] * np.abs(want) + 1e-38
+        assert (np.abs(_np(out)[:rows] - want) <= off).all()
+        s = stats.cpu().double().numpy()
+        assert (np.abs(s[:rows] - rb) <= 64 * UNIT * rb).all()
+        assert s[2 * rows] == 7.0 and (_np(out)[rows] == 7.0).all()
+        if h is None:
+            assert (s[rows:2 * rows] == 0).all()
+            continue
+        # cancellation between the residual and the block goes through to the row's mean square
+        spread = np.sqrt((np.square(size).mean(1) + EPS) / (np.square(want).mean(1) + EPS))
+        assert (np.abs(s[rows:2 * rows] - rr) <= 192 * UNIT * rr * spread).all()
+        off = (256 * UNIT * spread[:, None] * (np.abs(want_h) + np.abs(size * rr[:, None] * n["w_pre"]))) + HALF[kind] * np.abs(want_h) + 1e-38
+        assert (np.abs(_np(h)[:rows] - want_h) <= off).all() and (_np(h)[rows] == 7.0).all()
+
+
+@pytest.mark.parametrize("rows, cols", [(1, 1), (1, 1600), (33, 96), (40, 2047), (70, 8192), (64, 256), (8200, 64)])
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+@pytest.mark.parametrize("transform, rule", [(0, tahq.MX4_FLOOR), (1, tahq.MX4_COVER)])
+def test_h_in_mx4_is_quantized_h(rows, cols, kind, transform, rule):
+    """The packed h of an fp32 norm is the quantizer's of the fp32 h, byte for byte; that of a bf16 norm is quantized before rounding,
+    which the same norm of the same numbers held in fp32 shows."""
+    t = _tensors(rows, cols, 1, "both", kind)
+    wide = {n: None if v is None else v.float().cuda() for n, v in t.items()}
+    d = _cuda(t)
+    size = tahq.tahq_mx4_packed_size(rows, cols)
+    got = []
+    for dtype, x in ((KINDS[kind][0], d), (tahq.F32, wide)):
+        cfg = tahq.make_norm_config(rows, cols, dtype, 1, EPS, ALPHA, 0, transform, rule)
+        packed = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(x["residual"])
+        h = torch.empty_like(x["residual"])
+        tahq.tahq_norm_forward(cfg, x["residual"], x["block"], x["w_post"], x["gate"], x["w_pre"], out, h if dtype == tahq.F32 else None, packed, None)
+        got.append(packed)
+    torch.cuda.synchronize()
+    want = mx4.quantize(h.cpu().numpy(), transform, rule)
+    for packed in got:
+        p = packed.cpu().numpy()
+        assert (p[size:] == 0xA5).all() and (p[:size] == want).all()
+
+
+@pytest.mark.parametrize("rows, cols", SHAPES)
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+@pytest.mark.parametrize("halves", ("both", "post", "pre"))
+def test_backward(rows, cols, kind, halves):
+    """Every output within 128 roundings of the magnitudes of its terms, and one for every row of a sum over rows."""
+    for gate_rows in _gates(rows, halves):
+        t = _tensors(rows, cols, gate_rows, halves, kind)
+        n = {k: _np(v) for k, v in t.items()}
+        out, _, rb, rr = norm64.forward(n["residual"], n["block"], n["w_post"], n["gate"], n["w_pre"], gate_rows, EPS, ALPHA)
+        t["residual_out"] = torch.from_numpy(out).to(KINDS[kind][1]) if halves != "post" else None
+        stats = torch.from_numpy(np.stack((rb, rr))).float()
+        want = norm64.backward(n["grad_residual_out"], n["grad_h"], n["block"], n["w_post"], n["gate"], _np(t["residual_out"]), n["w_pre"],
+                               *stats.double().numpy(), gate_rows, ALPHA)
+        d = _cuda(t)
+        for accumulate in (0, 1):
+            cfg = tahq.make_norm_config(rows, cols, KINDS[kind][0], gate_rows, EPS, ALPHA, accumulate)
+            big = lambda: torch.full((rows + 1, cols), 7.0, dtype=KINDS[kind][1], device="cuda")      # noqa: E731
+            gr, gb = big(), big() if halves != "pre" else None
+            gw = {w: torch.full((cols,), 0.5, device="cuda") for w in ("w_post", "w_pre") if t[w] is not None}
+            gg = torch.full_like(d["gate"], 0.5, dtype=torch.float32) if gate_rows and halves != "pre" else None
+            need = tahq.tahq_norm_workspace_size(cfg)
+            ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+            tahq.tahq_norm_backward(cfg, d["grad_residual_out"], d["grad_h"], d["block"], d["w_post"], d["gate"], d["residual_out"], d["w_pre"],
+                                    stats.cuda(), gr, gb, gw.get("w_post"), gg, gw.get("w_pre"), ws)
+            torch.cuda.synchronize()
+            assert (ws[need:] == 0xA5).all() and (gr[rows] == 7.0).all() and (gb is None or (gb[rows] == 7.0).all())
+            got = {"grad_residual": gr[:rows], "grad_block": gb if gb is None else gb[:rows], "grad_gate": gg,
+                   **{"grad_" + w: v for w, v in gw.items()}}
+            for name, g in got.items():
+                if g is None:
+                    assert name not in want
+                    continue
+                w, size, g = want[name], want[name + "_size"], _np(g)
+                small = name in ("grad_residual", "grad_block")
+                before = 0.5 if accumulate and not small else 0.0
+                off = (128 + (0 if small else rows)) * UNIT * (size + before) + (HALF[kind] * np.abs(w) if small else 0) + 1e-38
+                assert (np.abs(g - (w + before)) <= off).all(), (name, gate_rows, accumulate)
+
+
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+def test_without_a_gradient_of_the_residual(kind):
+    rows, cols = 50, 320
+    t = _tensors(rows, cols, 0, "both", kind)
+    d = _cuda(t)
+    cfg = tahq.make_norm_config(rows, cols, KINDS[kind][0], 0, EPS, ALPHA)
+    a, b = tahq.BlockNorm(cfg), tahq.BlockNorm(cfg)
+    out, _ = a.forward(d["residual"], d["block"], d["w_post"], None, d["w_pre"])
+    rest = (d["grad_h"], d["block"], d["w_post"], None, out, d["w_pre"], a.stats)
+    got, want = a.backward(None, *rest), b.backward(torch.zeros_like(out), *rest)
+    assert all(torch.equal(got[n], want[n]) for n in want if want[n] is not None)
+
+
+def test_the_residual_stream_may_be_updated_in_place():
+    rows, cols = 300, 1600
+    d = _cuda(_tensors(rows, cols, 100, "both", "bf16"))
+    cfg = tahq.make_norm_config(rows, cols, tahq.BF16, 100, EPS, ALPHA)
+    norm = tahq.BlockNorm(cfg)
+    want, want_h = norm.forward(d["residual"], d["block"], d["w_post"], d["gate"], d["w_pre"])
+    r, h = d["residual"].clone(), torch.empty_like(want_h)
+    tahq.tahq_norm_forward(cfg, r, d["block"], d["w_post"], d["gate"], d["w_pre"], r, h)
+    assert torch.equal(r, want) and torch.equal(h, want_h)
+
+
+def test_infinities_and_nan_stay_in_their_rows():
+    rows, cols = 20, 512
+    t = _tensors(rows, cols, 1, "both", "f32")
+    t["block"][3, 5], t["residual"][7, 0] = float("nan"), float("inf")
+    norm = tahq.BlockNorm(tahq.make_norm_config(rows, cols, tahq.F32, 1, EPS, ALPHA), mx4=True)
+    d = _cuda(t)
+    out, packed = norm.forward(d["residual"], d["block"], d["w_post"], d["gate"], d["w_pre"])
+    torch.cuda.synchronize()
+    bad = {3, 7}
+    finite = out.isfinite().all(1).cpu().numpy()
+    assert [i for i in range(rows) if not finite[i]] == sorted(bad)
+    _, scales = mx4.unpack(packed.cpu().numpy(), rows, cols)
+    assert (scales[[i for i in range(rows) if i not in bad]] < 255).all() and (scales[3] == 255).all()
+
+
+def test_sums_over_tokens_are_the_same_every_time():
+    rows, cols = 5000, 640
+    d = _cuda(_tensors(rows, cols, 700, "both", "bf16"))
+    norm = tahq.BlockNorm(tahq.make_norm_config(rows, cols, tahq.BF16, 700, EPS, ALPHA))
+    out, _ = norm.forward(d["residual"], d["block"], d["w_post"], d["gate"], d["w_pre"])
+    first = None
+    for _ in range(3):
+        got = norm.backward(d["grad_residual_out"], d["grad_h"], d["block"], d["w_post"], d["gate"], out, d["w_pre"], norm.stats)
+        got = {n: v.clone() for n, v in got.items()}
+        assert first is None or all(torch.equal(first[n], got[n]) for n in got)
+        first = got
