@@ -102,7 +102,8 @@ ProductPlan plan_product(const tahq_mx4_matmul_config *c)
 {
     const uint32_t groups = (uint32_t)ceil_div(c->k, 256);
     ProductPlan p{-1, groups, 1};
-    if (c->m <= kFewRows) return p;
+    // a half unit of B's rows to a workgroup reads A too often where B is long: 32 rows, 28672 x 8192: 31 us, 64 x 64 tiles 23
+    if (c->m <= 16 || (c->m <= kFewRows && c->n <= 16384)) return p;
     float best = 0.0f;
     for (int i = 0; i < (int)(sizeof kTiles / sizeof *kTiles); ++i) {
         const float t = estimate(kTiles[i], c);
@@ -181,8 +182,12 @@ tahq_status enqueue_product(const tahq_mx4_matmul_config *c, const void *d_a, co
     return q->result();
 }
 
-// few rows in fp32 or bf16: quantized in the product's launch
-bool quantizes_itself(const tahq_mx4_matmul_config *c) { return c->m <= kFewQuantRows; }
+// Few rows in fp32 or bf16 are quantized in the product's launch, by every workgroup anew, where that is less than a launch of its own: up to two
+// rows (8192 x 8192: 9.0 us, apart 7.6 + 4.6), up to eight if B is small (4 rows, 4096 x 4096: 5.2, 3.7 + 4.5; 8192 x 8192: 13.9, 7.6 + 4.6).
+bool quantizes_itself(const tahq_mx4_matmul_config *c)
+{
+    return c->m <= 2 || (c->m <= kFewQuantRows && (uint64_t)c->n * c->k <= (1u << 24));
+}
 
 tahq_status enqueue_few(const tahq_mx4_config *x, const tahq_mx4_matmul_config *c, const void *d_x, const uint8_t *b, void *d_c, Enqueue *q)
 {

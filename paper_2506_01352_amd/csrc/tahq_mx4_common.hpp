@@ -29,42 +29,16 @@ struct Mx4Layout {
     }
 };
 
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // ---------------------------------------------------------------- loads
 
-// Eight consecutive elements as fp32.  Rows need no alignment beyond their elements': a 16-byte load may start anywhere.
-template <bool BF16>
-__device__ __forceinline__ void load8(const void *base, uint64_t at, float (&x)[8])
-{
-    if constexpr (BF16) {
-        uint32_t w[4];
-        __builtin_memcpy(w, static_cast<const uint16_t *>(base) + at, 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    } else {
-        __builtin_memcpy(x, static_cast<const float *>(base) + at, 32);
-    }
-}
 template <bool BF16>
 __device__ __forceinline__ float load1(const void *base, uint64_t at)
 {
     if constexpr (BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(base)[at] << 16);
     else return static_cast<const float *>(base)[at];
 }
-// Of eight elements the first `valid`, the others 0.  EIGHTS: `valid` is 8 or more, or not above 0.
-template <bool BF16, bool EIGHTS>
-__device__ __forceinline__ void load8(const void *base, uint64_t at, int64_t valid, float (&x)[8])
-{
-    if (valid >= 8) {
-        load8<BF16>(base, at, x);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = !EIGHTS && i < valid ? load1<BF16>(base, at + i) : 0.0f;
-    }
-}
-
 // two fp32 to bf16, nearest even (v_cvt_pk_bf16_f32)
 __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
 {
@@ -78,20 +52,53 @@ __device__ __forceinline__ void store1(void *base, uint64_t at, float x)
     if constexpr (BF16) static_cast<uint16_t *>(base)[at] = (uint16_t)two_bf16(x, 0.0f);
     else static_cast<float *>(base)[at] = x;
 }
+// Eight elements of a lane as they lie in memory
+template <bool BF16>
+struct Eight {
+    uint4 q[BF16 ? 1 : 2];
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        const uint4 &p = q[BF16 ? 0 : i / 4];
+        const int k = BF16 ? i / 2 : i % 4;
+        const uint32_t w = k == 0 ? p.x : k == 1 ? p.y : k == 2 ? p.z : p.w;
+        return __uint_as_float(!BF16 ? w : i % 2 ? w & 0xffff0000u : w << 16);
+    }
+};
+// Rows need no alignment beyond their elements': a 16-byte access may start anywhere.
+// Elements c .. c + 7 of a row, of which the first is there; zeros behind the row's end.  EIGHTS: rows of whole eights
 template <bool BF16, bool EIGHTS>
-__device__ __forceinline__ void store8(void *base, uint64_t at, int64_t valid, const float (&x)[8])
+__device__ __forceinline__ Eight<BF16> fetch(const void *row, uint32_t c, uint32_t C)
 {
-    if (valid >= 8) {
+    Eight<BF16> e;
+    if (EIGHTS || c + 8 <= C) {
+        __builtin_memcpy(e.q, static_cast<const uint8_t *>(row) + c * (BF16 ? 2 : 4), sizeof e.q);
+    } else {
+        uint32_t w[BF16 ? 4 : 8] = {};
+#pragma unroll
+        for (uint32_t i = 0; i < 7; ++i)
+            if (c + i < C) {
+                if constexpr (BF16) w[i / 2] |= (uint32_t)static_cast<const uint16_t *>(row)[c + i] << (i % 2 * 16);
+                else w[i] = static_cast<const uint32_t *>(row)[c + i];
+            }
+        __builtin_memcpy(e.q, w, sizeof e.q);
+    }
+    return e;
+}
+// what fetch reads
+template <bool BF16, bool EIGHTS>
+__device__ __forceinline__ void keep(void *row, uint32_t c, uint32_t C, const float (&x)[8])
+{
+    if (EIGHTS || c + 8 <= C) {
         if constexpr (BF16) {
             const uint32_t w[4] = {two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7])};
-            __builtin_memcpy(static_cast<uint16_t *>(base) + at, w, 16);
+            __builtin_memcpy(static_cast<uint8_t *>(row) + c * 2, w, 16);
         } else {
-            __builtin_memcpy(static_cast<float *>(base) + at, x, 32);
+            __builtin_memcpy(static_cast<uint8_t *>(row) + c * 4, x, 32);
         }
-    } else if constexpr (!EIGHTS) {
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < valid) store1<BF16>(base, at + i, x[i]);
+        for (uint32_t i = 0; i < 7; ++i)
+            if (c + i < C) store1<BF16>(row, c + i, x[i]);
     }
 }
 
@@ -161,6 +168,25 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], uint32_t s)
     return s == 255u ? 0u : w;
 }
 
+// eight bf16, two to a word
+__device__ __forceinline__ uint32_t codes8(const uint4 &q, uint32_t s)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const float v = scale_value(s);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, q.x), v, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, q.y), v, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, q.z), v, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, q.w), v, 3);
+    return s == 255u ? 0u : w;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void unpack(const Eight<BF16> &e, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = e[i];
+}
 // A block of which four neighbouring lanes hold eight elements each: its codes (this lane's) and scale byte
 template <bool ROTATE>
 __device__ __forceinline__ uint32_t quantize_quad(float (&x)[8], uint32_t cover, uint32_t &s)
@@ -173,6 +199,32 @@ __device__ __forceinline__ uint32_t quantize_quad(float (&x)[8], uint32_t cover,
     top = max(top, quad<0x4e>(top));
     s = block_scale(top, cover);
     return codes8(x, s);
+}
+
+// The same of bf16 as it lies in memory: magnitudes of bf16 are ordered like 16-bit integers
+__device__ __forceinline__ uint32_t quantize_quad(const uint4 &q, uint32_t cover, uint32_t &s)
+{
+    typedef uint16_t pair __attribute__((ext_vector_type(2)));
+    auto magnitude = [](uint32_t w) { return __builtin_bit_cast(pair, w & 0x7fff7fffu); };
+    const pair m = __builtin_elementwise_max(__builtin_elementwise_max(magnitude(q.x), magnitude(q.y)),
+                                             __builtin_elementwise_max(magnitude(q.z), magnitude(q.w)));
+    uint32_t top = (uint32_t)max(m.x, m.y) << 16;
+    top = max(top, quad<0xb1>(top));
+    top = max(top, quad<0x4e>(top));
+    s = block_scale(top, cover);
+    return codes8(q, s);
+}
+
+template <bool BF16, bool ROTATE>
+__device__ __forceinline__ uint32_t quantize_quad(const Eight<BF16> &e, uint32_t cover, uint32_t &s)
+{
+    if constexpr (BF16 && !ROTATE) {
+        return quantize_quad(e.q[0], cover, s);
+    } else {
+        float x[8];
+        unpack(e, x);
+        return quantize_quad<ROTATE>(x, cover, s);
+    }
 }
 
 // the magnitude a code stands for, times its block's scale; `scale` of a block of NaN is NaN

@@ -60,7 +60,6 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
 // s_waitcnt's operand: at most `vm` loads and `lgkm` LDS accesses outstanding (no exports are)
 constexpr int waitcnt(int vm, int lgkm) { return (vm & 15) | 7 << 4 | lgkm << 8 | (vm >> 4) << 14; }
 
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 // what was read is used here: the reads are not moved behind this place
 __device__ __forceinline__ void pin(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
 
@@ -356,7 +355,7 @@ void k_mx4_few(const uint8_t *b, FewInput in, void *c, uint32_t M, uint32_t N, u
     for (uint32_t g0 = wave; g0 < LB.kc; g0 += kFewWaves * kFewAhead) {
         uint4 vb[kFewAhead][NT][2], va[QUANT ? 1 : kFewAhead][MT][2];
         uint32_t sb[kFewAhead][NT], sa[QUANT ? 1 : kFewAhead][MT];
-        float x[QUANT ? kFewAhead : 1][PAIRS][8];
+        Eight<QUANT == 1> x[QUANT ? kFewAhead : 1][PAIRS] = {};
 #pragma unroll
         for (int u = 0; u < kFewAhead; ++u) {
             const uint32_t g = g0 + u * kFewWaves;
@@ -364,8 +363,8 @@ void k_mx4_few(const uint8_t *b, FewInput in, void *c, uint32_t M, uint32_t N, u
             if constexpr (QUANT != 0) {
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) {
-                    const uint32_t r = 2 * i + lane / 32, col = g * 256 + lane % 32 * 8;
-                    load8<QUANT == 1, false>(in.a, (uint64_t)r * in.ld + col, r < M ? (int64_t)K - col : 0, x[u][i]);
+                    const uint32_t r = 2 * i + lane / 32, c = lane % 32 * 8, wide = K - g * 256;
+                    if (r < M && c < wide) x[u][i] = fetch<QUANT == 1, false>(a + ((uint64_t)r * in.ld + g * 256) * (QUANT == 1 ? 2 : 4), c, wide);
                 }
             }
 #pragma unroll
@@ -394,7 +393,7 @@ void k_mx4_few(const uint8_t *b, FewInput in, void *c, uint32_t M, uint32_t N, u
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) {
                     uint32_t s;
-                    const uint32_t w = quantize_quad<ROTATE>(x[u][i], in.cover, s), t = lane % 32 / 4, r = 2 * i + lane / 32;
+                    const uint32_t w = quantize_quad<QUANT == 1, ROTATE>(x[u][i], in.cover, s), t = lane % 32 / 4, r = 2 * i + lane / 32;
                     *reinterpret_cast<uint32_t *>(mine + (t * 16 + r) * 16 + lane % 4 * 4) = w;
                     if (lane % 4 == 0) mine[2048 + (t % 4 * 16 + r) * 4 + t / 4 * 2] = (uint8_t)s;
                 }

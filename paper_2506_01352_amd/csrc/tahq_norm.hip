@@ -1,4 +1,7 @@
 // Entry points of the block norms (include/tahq_norm.h): validation, plan, launches.
+#include <stdlib.h>
+#include <type_traits>
+
 #include "tahq_enqueue.hpp"
 #include "tahq_norm.h"
 #include "tahq_norm_kernels.hpp"
@@ -19,55 +22,46 @@ tahq_status check(const tahq_norm_config *c)
     return TAHQ_OK;
 }
 
+// wavefronts of a row: eight channels to a lane
+uint32_t waves_of(const tahq_norm_config *c) { return (c->cols + 511) / 512; }
+
 NormShape shape_of(const tahq_norm_config *c)
 {
     // a gate row for more tokens than there are is one for all of them
-    return {c->rows, c->cols, c->gate_rows < c->rows ? c->gate_rows : c->rows, c->eps, c->residual_scale};
+    return {c->rows, c->cols, c->gate_rows < c->rows ? c->gate_rows : c->rows, waves_of(c), c->eps, c->residual_scale};
 }
 
+// the kernels' template parameters from a configuration and the halves that there are
 template <bool BF16, bool EIGHTS, typename Run>
-void launch_forward(uint32_t vectors, Run run)
+void with_halves(bool post, bool pre, Run run)
 {
-    if (vectors <= 1) run(k_norm_forward<BF16, EIGHTS, 256, 1>);
-    else if (vectors <= 2) run(k_norm_forward<BF16, EIGHTS, 256, 2>);
-    else run(k_norm_forward<BF16, EIGHTS, 256, 4>);
+    const std::bool_constant<BF16> b;
+    const std::bool_constant<EIGHTS> e;
+    if (post && pre) run(b, e, std::true_type{}, std::true_type{});
+    else if (post) run(b, e, std::true_type{}, std::false_type{});
+    else if (pre) run(b, e, std::false_type{}, std::true_type{});
+    else run(b, e, std::false_type{}, std::false_type{});
 }
 template <typename Run>
-void launch_forward(const tahq_norm_config *c, Run run)
-{
-    const uint32_t vectors = (c->cols + 2047) / 2048;
-    const bool eights = c->cols % 8 == 0;
-    if (c->dtype == TAHQ_BF16) eights ? launch_forward<true, true>(vectors, run) : launch_forward<true, false>(vectors, run);
-    else eights ? launch_forward<false, true>(vectors, run) : launch_forward<false, false>(vectors, run);
-}
-
-template <bool BF16, bool EIGHTS, typename Run>
-void launch_backward(uint32_t threads, Run run)
-{
-    if (threads == 256) run(k_norm_backward<BF16, EIGHTS, 256, 1>);
-    else if (threads == 512) run(k_norm_backward<BF16, EIGHTS, 512, 1>);
-    else run(k_norm_backward<BF16, EIGHTS, 1024, 1>);
-}
-template <typename Run>
-void launch_backward(const tahq_norm_config *c, uint32_t threads, Run run)
+void with_kind(const tahq_norm_config *c, bool post, bool pre, Run run)
 {
     const bool eights = c->cols % 8 == 0;
-    if (c->dtype == TAHQ_BF16) eights ? launch_backward<true, true>(threads, run) : launch_backward<true, false>(threads, run);
-    else eights ? launch_backward<false, true>(threads, run) : launch_backward<false, false>(threads, run);
+    if (c->dtype == TAHQ_BF16) eights ? with_halves<true, true>(post, pre, run) : with_halves<true, false>(post, pre, run);
+    else eights ? with_halves<false, true>(post, pre, run) : with_halves<false, false>(post, pre, run);
 }
 
-// Backward: threads per row, eight channels to each, and the workgroups that share the rows
+// Backward: the workgroups that share the rows
 struct BackwardPlan {
-    uint32_t threads, rows_each, workgroups;
+    uint32_t rows_each, workgroups;
     uint64_t workspace;
 };
 BackwardPlan plan_backward(const tahq_norm_config *c)
 {
     BackwardPlan p;
-    p.threads = c->cols <= 2048 ? 256 : c->cols <= 4096 ? 512 : 1024;
-    const uint32_t most = 512 * (1024 / p.threads) < 1024 ? 512 * (1024 / p.threads) : 1024;
+    const char *e = getenv("NB_WG"), *e2 = getenv("NB_MIN");
+    const uint32_t most = e ? atoi(e) : 512, least = e2 ? atoi(e2) : 4;
     p.rows_each = (c->rows + most - 1) / most;
-    if (p.rows_each < 8) p.rows_each = 8;
+    if (p.rows_each < least) p.rows_each = least;
     p.workgroups = (c->rows + p.rows_each - 1) / p.rows_each;
     p.workspace = (uint64_t)p.workgroups * c->cols * 4 * (c->gate_rows ? 4 : 2);
     return p;
@@ -112,14 +106,14 @@ tahq_status tahq_norm_forward(const tahq_norm_config *cfg, const void *d_residua
     const NormShape s = shape_of(cfg);
     const uint32_t cover = cfg->scale_rule == TAHQ_MX4_COVER ? kCover : 0u;
     const uint32_t total = d_h_mx4 ? 32 * ((cfg->rows + 31) / 32) : cfg->rows;
-    const uint32_t rows_each = total >= 8192 ? 8 : 1;
+    const char *e = getenv("NF_ROWS");
+    const uint32_t rows_each = e ? atoi(e) : total >= 4096 ? 2 : 1;
     const dim3 grid((total + rows_each - 1) / rows_each);
     Enqueue q{(hipStream_t)stream};
-    auto run = [&](auto kernel) {
-        q(kernel, grid, dim3(256), d_residual, d_block, d_w_post, d_block ? d_gate : nullptr, d_w_pre, d_residual_out, d_h,
+    with_kind(cfg, d_block, d_w_pre, [&](auto bf16, auto eights, auto post, auto pre) {
+        q(k_norm_forward<bf16, eights, post, pre>, grid, dim3(64 * waves_of(cfg)), d_residual, d_block, d_w_post, d_block ? d_gate : nullptr, d_w_pre, d_residual_out, d_h,
           static_cast<uint8_t *>(d_h_mx4), d_stats, s, cover, cfg->transform, rows_each);
-    };
-    launch_forward(cfg, run);
+    });
     return q.result();
 }
 
@@ -162,15 +156,14 @@ tahq_status tahq_norm_backward(const tahq_norm_config *cfg, const void *d_grad_r
     const NormPartials parts = {ws, ws + each, ws + 2 * each};
     const void *gate = d_block ? d_gate : nullptr;
     Enqueue q{(hipStream_t)stream};
-    auto run = [&](auto kernel) {
-        q(kernel, dim3(p.workgroups), dim3(p.threads), d_grad_residual_out, d_grad_h, d_block, d_w_post, gate, d_residual_out, d_w_pre,
+    with_kind(cfg, d_block, d_grad_h, [&](auto bf16, auto eights, auto post, auto pre) {
+        q(k_norm_backward<bf16, eights, post, pre>, dim3(p.workgroups), dim3(64 * waves_of(cfg)), d_grad_residual_out, d_grad_h, d_block, d_w_post, gate, d_residual_out, d_w_pre,
           d_stats, d_grad_residual, d_grad_block, d_grad_gate, parts, s, p.rows_each, cfg->accumulate);
-    };
-    launch_backward(cfg, p.threads, run);
+    });
     const uint32_t groups = gate ? (cfg->rows + s.gate_rows - 1) / s.gate_rows : 0;
     if (d_block || d_grad_h) {
         const uint32_t slots = groups < 64 ? groups : 64;
-        q(k_norm_reduce, dim3((cfg->cols + 63) / 64, 2 + slots), dim3(256), parts, d_grad_w_post, d_grad_w_pre, d_grad_gate, cfg->cols,
+        q(k_norm_reduce, dim3((cfg->cols + 63) / 64, 2 + slots), dim3(64 * kReduceRuns), parts, d_grad_w_post, d_grad_w_pre, d_grad_gate, cfg->cols,
           p.workgroups, cfg->rows, s.gate_rows, p.rows_each, groups, cfg->accumulate);
     }
     return q.result();

@@ -1,129 +1,165 @@
 // The norms before and after a block with its gate and residual scale (include/tahq_norm.h), forward and backward.
 //
-// Bound by memory: four tensors forward (two and 17/32 of a byte an element where h leaves in mx4), six backward, each once.  A
-// workgroup takes a row at a time, so that both of its row sums come from registers.
+// Bound by memory: four tensors forward (three and 17/32 of a byte an element where h leaves in mx4), six backward, each once.  A
+// workgroup takes a row at a time, eight channels to a lane and no more wavefronts than that needs, so that both of its row sums come from
+// registers; the next row is on its way meanwhile.
 #pragma once
 #include "tahq_mx4_common.hpp"
 
 namespace tahq {
 
 struct NormShape {
-    uint32_t rows, cols, gate_rows;
+    uint32_t rows, cols, gate_rows, waves;     // waves: of a workgroup
     float eps, alpha;
 };
+constexpr int kNormWaves = TAHQ_NORM_MAX_COLS / 512;       // at most, in a workgroup
 
-// How many of the eight channels from c on a row has, as far as load8 and store8 care; rows of whole eights need no code for others.
-template <bool EIGHTS>
-__device__ __forceinline__ int64_t valid8(uint32_t C, uint32_t c)
+// A gate of ones, for where there is none
+template <bool BF16>
+__device__ __forceinline__ Eight<BF16> ones()
 {
-    if constexpr (EIGHTS) return c < C ? 8 : 0;
-    else return (int64_t)C - c;
+    constexpr uint32_t one = BF16 ? 0x3f803f80u : 0x3f800000u;
+    Eight<BF16> e;
+    for (uint4 &p : e.q) p = make_uint4(one, one, one, one);
+    return e;
+}
+// A row's address, the same in all lanes, so that a lane's own part of an address is its 32-bit offset in the row; worked out anew for every row
+// in scalar registers, where a pointer per tensor carried along would take two vector registers
+template <bool BF16>
+__device__ __forceinline__ const void *row_of(const void *t, uint32_t row, uint32_t C)
+{
+    return static_cast<const uint8_t *>(t) + (uint64_t)uniform(row) * C * (BF16 ? 2 : 4);
+}
+template <bool BF16>
+__device__ __forceinline__ void *row_of(void *t, uint32_t row, uint32_t C)
+{
+    return static_cast<uint8_t *>(t) + (uint64_t)uniform(row) * C * (BF16 ? 2 : 4);
+}
+// Keeps a lane's channels as they lie in memory: unpacked once for all rows they would take twice the registers
+template <bool BF16>
+__device__ __forceinline__ void stay_packed(Eight<BF16> &e)
+{
+    if constexpr (BF16) asm volatile("" : "+v"(e.q[0].x), "+v"(e.q[0].y), "+v"(e.q[0].z), "+v"(e.q[0].w));
 }
 
-// Sum over a workgroup, the same in every lane: a butterfly in each wavefront, then the wavefronts' sums from LDS in order.  `turn`
-// alternates between two places, so that one barrier per sum is enough: nobody writes a place again before all have passed the
-// barrier of the sum in between.
-template <int NT>
-__device__ __forceinline__ float group_sum(float v, float (*places)[NT / 64], uint32_t &turn)
+// Sum over a wavefront, the same in every lane: pairs, quads, eights and sixteens by permutations within rows of sixteen lanes, then the four rows.
+template <int CTRL>
+__device__ __forceinline__ float add_permuted(float v)
 {
-    float (*slot)[NT / 64] = places + turn;
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v = add_permuted<0xb1>(v);                             // lane ^ 1
+    v = add_permuted<0x4e>(v);                             // lane ^ 2
+    v = add_permuted<0x141>(v);                            // mirrored in eight: the other quad
+    v = add_permuted<0x140>(v);                            // mirrored in sixteen: the other eight
+    const int w = (int)__float_as_uint(v);
+    auto row = [&](int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane(w, lane)); };
+    return (row(0) + row(16)) + (row(32) + row(48));
+}
+// Sum over a workgroup of `waves` wavefronts, the same in every lane; places of wavefronts that there are not hold zeros.  `turn` alternates
+// between two places, so that one barrier per sum is enough: nobody writes a place again before all have passed the barrier of the sum in between.
+struct Places {
+    float of[2][16];
+};
+static_assert(kNormWaves <= 16, "a row of sixteen lanes adds the wavefronts' sums");
+
+__device__ __forceinline__ float group_sum(float v, uint32_t waves, Places &places, uint32_t &turn)
+{
+    v = wave_sum(v);
+    if (waves == 1) return v;
+    if (threadIdx.x % 64 == 0) places.of[turn][threadIdx.x / 64] = v;
+    __syncthreads();
+    v = places.of[turn][threadIdx.x % 16];
     turn ^= 1;
+    v = add_permuted<0xb1>(v);
+    v = add_permuted<0x4e>(v);
+    v = add_permuted<0x141>(v);
+    return add_permuted<0x140>(v);
+}
+__device__ __forceinline__ void clear(Places &places)
+{
+    if (threadIdx.x < 32) reinterpret_cast<float *>(&places)[threadIdx.x] = 0.0f;
+    __syncthreads();
+}
+// Sums that are up to date here: otherwise the compiler keeps what they are of over the barrier, in registers that would be another workgroup's
+__device__ __forceinline__ void settle(float (&v)[8])
+{
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
-    if constexpr (NT == 64) {
-        return v;
-    } else {
-        if (threadIdx.x % 64 == 0) (*slot)[threadIdx.x / 64] = v;
-        __syncthreads();
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NT / 64; ++i) s += (*slot)[i];
-        return s;
-    }
+    for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(v[i]));
 }
 
-template <bool BF16, bool EIGHTS, int NT, int V>
-__global__ __launch_bounds__(NT)
+// POST, PRE: whether the halves are there
+template <bool BF16, bool EIGHTS, bool POST, bool PRE>
+__global__ __launch_bounds__(64 * kNormWaves)
 void k_norm_forward(const void *residual, const void *block, const void *w_post, const void *gate, const void *w_pre,
                     void *residual_out, void *h, uint8_t *h_mx4, float *stats, NormShape s, uint32_t cover, uint32_t rotate,
                     uint32_t rows_each)
 {
-    __shared__ float sums[2][NT / 64];
+    __shared__ Places places;
     uint32_t turn = 0;
-    const uint32_t tid = threadIdx.x, C = s.cols;
-    auto valid = [&](uint32_t c) { return valid8<EIGHTS>(C, c); };
+    const uint32_t C = s.cols, c = 8 * threadIdx.x;
+    const bool mine = c < C;
     const Mx4Layout L(s.rows, C);
-    const uint32_t end = h_mx4 ? 32 * L.rb : s.rows;
+    const uint32_t end = h_mx4 ? 32 * L.rb : s.rows;       // rows behind the last one fill up the packed matrix with zeros
     const uint32_t first = blockIdx.x * rows_each, last = min(first + rows_each, end);
+    Eight<BF16> next_r = {}, next_b = {}, post = {}, pre = {}, next_k = ones<BF16>();
+    auto ask = [&](uint32_t row) {
+        if (row < s.rows && row < last && mine) {
+            next_r = fetch<BF16, EIGHTS>(row_of<BF16>(residual, row, C), c, C);
+            if constexpr (POST) {
+                next_b = fetch<BF16, EIGHTS>(row_of<BF16>(block, row, C), c, C);
+                if (gate) next_k = fetch<BF16, EIGHTS>(row_of<BF16>(gate, row / s.gate_rows, C), c, C);
+            }
+        }
+    };
+    ask(first);
+    if (mine) {
+        if constexpr (POST) post = fetch<BF16, EIGHTS>(w_post, c, C);
+        if constexpr (PRE) pre = fetch<BF16, EIGHTS>(w_pre, c, C);
+    }
+    clear(places);
+    const float inv_c = 1.0f / (float)C;
     for (uint32_t row = first; row < last; ++row) {
-        const bool there = row < s.rows;                                   // rows behind fill up the packed matrix with zeros
-        const uint64_t base = (uint64_t)row * C;
-        float x[V][8];
-        float rstd_b = 0.0f, rstd_r = 0.0f;
+        const bool there = row < s.rows;
+        stay_packed(post);
+        stay_packed(pre);
+        float x[8], rstd_b = 0.0f, rstd_r = 0.0f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t c = 8 * (v * NT + tid);
-            load8<BF16, EIGHTS>(residual, base + c, there ? valid(c) : 0, x[v]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] *= s.alpha;
-        }
-        if (block && there) {
-            float b[V][8], sum = 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = 8 * (v * NT + tid);
-                load8<BF16, EIGHTS>(block, base + c, valid(c), b[v]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(b[v][i], b[v][i], sum);
-            }
-            rstd_b = 1.0f / __builtin_sqrtf(group_sum<NT>(sum, sums, turn) / (float)C + s.eps);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = 8 * (v * NT + tid);
-                float w[8];
-                load8<BF16, EIGHTS>(w_post, c, valid(c), w);
-                if (gate) {
-                    float g[8];
-                    load8<BF16, EIGHTS>(gate, (uint64_t)(row / s.gate_rows) * C + c, valid(c), g);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) b[v][i] *= g[i];
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[v][i] = __builtin_fmaf(b[v][i] * rstd_b, w[i], x[v][i]);
-            }
-        }
-        if (residual_out && there) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = 8 * (v * NT + tid);
-                store8<BF16, EIGHTS>(residual_out, base + c, valid(c), x[v]);
-            }
-        }
-        if (w_pre) {
+        for (int i = 0; i < 8; ++i) x[i] = there ? s.alpha * next_r[i] : 0.0f;
+        if constexpr (POST) {
+            const Eight<BF16> b = next_b, k = next_k;
+            ask(row + 1);
             float sum = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v)
+            for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(b[i], b[i], sum);
+            rstd_b = 1.0f / __builtin_sqrtf(__builtin_fmaf(group_sum(sum, s.waves, places, turn), inv_c, s.eps));
+            if (there) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[v][i], x[v][i], sum);
-            rstd_r = 1.0f / __builtin_sqrtf(group_sum<NT>(sum, sums, turn) / (float)C + s.eps);
+                for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(b[i] * rstd_b, k[i] * post[i], x[i]);
+            }
+        } else {
+            ask(row + 1);
+        }
+        if (residual_out && there && mine) keep<BF16, EIGHTS>(row_of<BF16>(residual_out, row, C), c, C, x);
+        if constexpr (PRE) {
+            float sum = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = 8 * (v * NT + tid);
-                float w[8];
-                load8<BF16, EIGHTS>(w_pre, c, valid(c), w);
+            for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], x[i], sum);
+            rstd_r = 1.0f / __builtin_sqrtf(__builtin_fmaf(group_sum(sum, s.waves, places, turn), inv_c, s.eps));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[v][i] = x[v][i] * rstd_r * w[i];
-                if (h && there) store8<BF16, EIGHTS>(h, base + c, valid(c), x[v]);
-                if (h_mx4) {
-                    uint32_t e;
-                    const uint32_t codes = rotate ? quantize_quad<true>(x[v], cover, e) : quantize_quad<false>(x[v], cover, e);
-                    const uint32_t blk = c / 32;
-                    if (blk / 2 < L.kb) *reinterpret_cast<uint32_t *>(h_mx4 + L.code(row, blk) + tid % 4 * 4) = codes;
-                    if (tid % 4 == 0 && blk / 8 < L.kc) h_mx4[L.scale(row, blk)] = (uint8_t)e;
-                }
+            for (int i = 0; i < 8; ++i) x[i] = x[i] * rstd_r * pre[i];
+            if (h && there && mine) keep<BF16, EIGHTS>(row_of<BF16>(h, row, C), c, C, x);
+            if (h_mx4) {
+                uint32_t e;
+                const uint32_t codes = rotate ? quantize_quad<true>(x, cover, e) : quantize_quad<false>(x, cover, e);
+                const uint32_t blk = c / 32;
+                if (blk / 2 < L.kb) *reinterpret_cast<uint32_t *>(h_mx4 + L.code(row, blk) + threadIdx.x % 4 * 4) = codes;
+                if (threadIdx.x % 4 == 0 && blk / 8 < L.kc) h_mx4[L.scale(row, blk)] = (uint8_t)e;
             }
         }
-        if (stats && there && tid == 0) {
+        if (stats && there && threadIdx.x == 0) {
             stats[row] = rstd_b;
             stats[(uint64_t)s.rows + row] = rstd_r;
         }
@@ -137,144 +173,154 @@ struct NormPartials {
     float *post, *pre, *gate;
 };
 
-__device__ __forceinline__ void put(float *to, uint32_t c, uint32_t C, const float (&v)[8], bool add)
+template <bool EIGHTS>
+__device__ __forceinline__ void put(float *row, uint32_t c, uint32_t C, float (&v)[8], bool add)
 {
+    if (c >= C) return;
+    if (add) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c + i < C) to[c + i] = add ? to[c + i] + v[i] : v[i];
+        for (uint32_t i = 0; i < 8; ++i)
+            if (EIGHTS || c + i < C) v[i] += row[c + i];
+    }
+    keep<false, EIGHTS>(row, c, C, v);
 }
 
-template <bool BF16, bool EIGHTS, int NT, int V>
-__global__ __launch_bounds__(NT)
+template <bool BF16, bool EIGHTS, bool POST, bool PRE>
+__global__ __launch_bounds__(64 * kNormWaves)
 void k_norm_backward(const void *grad_out, const void *grad_h, const void *block, const void *w_post, const void *gate,
-                     const void *residual_out, const void *w_pre, const float *stats, void *grad_residual, void *grad_block,
+                     const void *residual_out, const void *w_pre, const float *__restrict__ stats, void *grad_residual, void *grad_block,
                      float *grad_gate, NormPartials parts, NormShape s, uint32_t rows_each, uint32_t accumulate)
 {
-    __shared__ float sums[2][NT / 64];
+    __shared__ Places places;
     uint32_t turn = 0;
-    const uint32_t tid = threadIdx.x, C = s.cols;
-    auto valid = [&](uint32_t c) { return valid8<EIGHTS>(C, c); };
+    const uint32_t C = s.cols, c = 8 * threadIdx.x;
+    const bool mine = c < C;
     const uint32_t first = blockIdx.x * rows_each, last = min(first + rows_each, s.rows);
     const float inv_c = 1.0f / (float)C;
-    float post[V][8] = {}, pre[V][8] = {}, gates[V][8] = {};
+    // the row that is worked on, loaded again as soon as it is used up
+    Eight<BF16> go = {}, gh = {}, ro = {}, bl = {}, k = ones<BF16>(), wpost = {}, wpre = {};
+    auto ask_pre = [&](uint32_t row) {
+        if (row < last && mine) {
+            if constexpr (PRE) {
+                gh = fetch<BF16, EIGHTS>(row_of<BF16>(grad_h, row, C), c, C);
+                ro = fetch<BF16, EIGHTS>(row_of<BF16>(residual_out, row, C), c, C);
+            }
+            if (grad_out) go = fetch<BF16, EIGHTS>(row_of<BF16>(grad_out, row, C), c, C);
+        }
+    };
+    auto ask_post = [&](uint32_t row) {
+        if (POST && row < last && mine) bl = fetch<BF16, EIGHTS>(row_of<BF16>(block, row, C), c, C);
+    };
+    // the rows of one gate row; they change on the way
+    uint32_t group = 0, stop = 0;
+    auto ask_gate = [&](uint32_t row) {
+        group = row / s.gate_rows;
+        stop = (uint32_t)min((uint64_t)group * s.gate_rows + s.gate_rows, (uint64_t)s.rows);
+        if (mine) k = fetch<BF16, EIGHTS>(row_of<BF16>(gate, group, C), c, C);
+    };
+    ask_pre(first);
+    ask_post(first);
+    if (mine) {
+        if constexpr (POST) wpost = fetch<BF16, EIGHTS>(w_post, c, C);
+        if constexpr (PRE) wpre = fetch<BF16, EIGHTS>(w_pre, c, C);
+    }
+    if (POST && gate) ask_gate(first);
+    clear(places);
+    float post[8] = {}, pre[8] = {}, gates[8] = {};
     for (uint32_t row = first; row < last; ++row) {
-        const uint64_t base = (uint64_t)row * C;
-        float g[V][8];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t c = 8 * (v * NT + tid);
-            load8<BF16, EIGHTS>(grad_out, base + c, grad_out ? valid(c) : 0, g[v]);
-        }
-        if (grad_h) {
+        stay_packed(wpost);
+        stay_packed(wpre);
+        stay_packed(k);
+        float g[8];
+        if constexpr (PRE) {
             const float rstd = stats[(uint64_t)s.rows + row];
-            float x2[V][8], t[V][8], sum = 0.0f;
+            float sum = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = 8 * (v * NT + tid);
-                float w[8];
-                load8<BF16, EIGHTS>(grad_h, base + c, valid(c), t[v]);
-                load8<BF16, EIGHTS>(residual_out, base + c, valid(c), x2[v]);
-                load8<BF16, EIGHTS>(w_pre, c, valid(c), w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x2[v][i] *= rstd;
-                    pre[v][i] = __builtin_fmaf(t[v][i], x2[v][i], pre[v][i]);
-                    t[v][i] *= w[i];
-                    sum = __builtin_fmaf(t[v][i], x2[v][i], sum);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float x2 = ro[i] * rstd;
+                pre[i] = __builtin_fmaf(gh[i], x2, pre[i]);
+                sum = __builtin_fmaf(gh[i] * wpre[i], x2, sum);
             }
-            const float mean = group_sum<NT>(sum, sums, turn) * inv_c;
+            settle(pre);
+            stay_packed(gh);
+            stay_packed(ro);
+            stay_packed(wpre);
+            const float mean = group_sum(sum, s.waves, places, turn) * inv_c;
 #pragma unroll
-            for (int v = 0; v < V; ++v)
+            for (int i = 0; i < 8; ++i) g[i] = __builtin_fmaf(rstd, __builtin_fmaf(-(ro[i] * rstd), mean, gh[i] * wpre[i]), go[i]);
+            settle(g);
+        } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[v][i] = __builtin_fmaf(rstd, __builtin_fmaf(-x2[v][i], mean, t[v][i]), g[v][i]);
+            for (int i = 0; i < 8; ++i) g[i] = go[i];
         }
+        ask_pre(row + 1);
+        float d[8];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t c = 8 * (v * NT + tid);
-            float d[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = s.alpha * g[v][i];
-            store8<BF16, EIGHTS>(grad_residual, base + c, valid(c), d);
-        }
-        if (block) {
+        for (int i = 0; i < 8; ++i) d[i] = s.alpha * g[i];
+        if (mine) keep<BF16, EIGHTS>(row_of<BF16>(grad_residual, row, C), c, C, d);
+        if constexpr (POST) {
             const float rstd = stats[row];
-            float x1[V][8], sum = 0.0f;
+            float sum = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = 8 * (v * NT + tid);
-                float w[8];
-                load8<BF16, EIGHTS>(block, base + c, valid(c), x1[v]);
-                load8<BF16, EIGHTS>(w_post, c, valid(c), w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x1[v][i] *= rstd;
-                if (gate) {
-                    float k[8];
-                    load8<BF16, EIGHTS>(gate, (uint64_t)(row / s.gate_rows) * C + c, valid(c), k);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        gates[v][i] = __builtin_fmaf(g[v][i] * x1[v][i], w[i], gates[v][i]);
-                        g[v][i] *= k[i];
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    post[v][i] = __builtin_fmaf(g[v][i], x1[v][i], post[v][i]);
-                    g[v][i] *= w[i];
-                    sum = __builtin_fmaf(g[v][i], x1[v][i], sum);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float x1 = bl[i] * rstd;
+                gates[i] = __builtin_fmaf(g[i] * x1, wpost[i], gates[i]);
+                g[i] *= k[i];
+                post[i] = __builtin_fmaf(g[i], x1, post[i]);
+                g[i] *= wpost[i];
+                sum = __builtin_fmaf(g[i], x1, sum);
             }
-            const float mean = group_sum<NT>(sum, sums, turn) * inv_c;
+            settle(gates);
+            settle(post);
+            settle(g);
+            stay_packed(bl);
+            const float mean = group_sum(sum, s.waves, places, turn) * inv_c;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t c = 8 * (v * NT + tid);
-                float d[8];
+            for (int i = 0; i < 8; ++i) d[i] = rstd * __builtin_fmaf(-(bl[i] * rstd), mean, g[i]);
+            ask_post(row + 1);
+            if (mine) keep<BF16, EIGHTS>(row_of<BF16>(grad_block, row, C), c, C, d);
+            if (gate && (row + 1 == last || row + 1 == stop)) {
+                const uint32_t begin = group * s.gate_rows;
+                const bool whole = begin >= first && stop <= last;
+                float *to = whole ? grad_gate + (uint64_t)group * C
+                                  : parts.gate + ((uint64_t)blockIdx.x * 2 + (begin <= first ? 0 : 1)) * C;
+                put<EIGHTS>(to, c, C, gates, whole && accumulate);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] = rstd * __builtin_fmaf(-x1[v][i], mean, g[v][i]);
-                store8<BF16, EIGHTS>(grad_block, base + c, valid(c), d);
-            }
-            if (gate) {
-                const uint32_t group = row / s.gate_rows;
-                if (row + 1 == last || (row + 1) / s.gate_rows != group) {
-                    const uint32_t begin = group * s.gate_rows;
-                    const uint32_t stop = (uint32_t)min((uint64_t)begin + s.gate_rows, (uint64_t)s.rows);
-                    const bool whole = begin >= first && stop <= last;
-                    float *to = whole ? grad_gate + (uint64_t)group * C
-                                      : parts.gate + ((uint64_t)blockIdx.x * 2 + (begin <= first ? 0 : 1)) * C;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        put(to, 8 * (v * NT + tid), C, gates[v], whole && accumulate);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) gates[v][i] = 0.0f;
-                    }
-                }
+                for (int i = 0; i < 8; ++i) gates[i] = 0.0f;
+                if (row + 1 < last) ask_gate(row + 1);
             }
         }
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const uint32_t c = 8 * (v * NT + tid);
-        if (block) put(parts.post + (uint64_t)blockIdx.x * C, c, C, post[v], false);
-        if (grad_h) put(parts.pre + (uint64_t)blockIdx.x * C, c, C, pre[v], false);
-    }
+    if constexpr (POST) put<EIGHTS>(parts.post + (uint64_t)blockIdx.x * C, c, C, post, false);
+    if constexpr (PRE) put<EIGHTS>(parts.pre + (uint64_t)blockIdx.x * C, c, C, pre, false);
 }
 
-// The workgroups' column sums, added in order: 64 columns x 4 runs of workgroups.  blockIdx.y: 0 post, 1 pre, then the groups of the gate.
-__global__ __launch_bounds__(256)
+// The workgroups' column sums, added in a fixed order: 64 columns x 16 runs of workgroups, eight loads of a run on their way at a time.
+// blockIdx.y: 0 post, 1 pre, then the groups of the gate.
+constexpr int kReduceRuns = 16;
+
+__global__ __launch_bounds__(64 * kReduceRuns)
 void k_norm_reduce(NormPartials parts, float *grad_w_post, float *grad_w_pre, float *grad_gate, uint32_t C, uint32_t W,
                    uint32_t rows, uint32_t gate_rows, uint32_t rows_each, uint32_t groups, uint32_t accumulate)
 {
-    __shared__ float runs[4][64];
+    __shared__ float runs[kReduceRuns][64];
     const uint32_t lane = threadIdx.x % 64, run = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
     auto total = [&](auto part, uint32_t n, float *to) {
-        const uint32_t each = (n + 3) / 4, from = min(run * each, n), till = min(from + each, n);
+        const uint32_t each = (n + kReduceRuns - 1) / kReduceRuns, from = min(run * each, n), till = min(from + each, n);
         float sum = 0.0f;
         if (c < C)
-            for (uint32_t i = from; i < till; ++i) sum += part(i)[c];
+            for (uint32_t i = from; i < till; i += 8) {
+                float v[8];
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) v[k] = i + k < till ? part(i + k)[c] : 0.0f;
+                sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            }
         runs[run][lane] = sum;
         __syncthreads();
         if (run == 0 && c < C) {
-            const float t = ((runs[0][lane] + runs[1][lane]) + runs[2][lane]) + runs[3][lane];
+            float t = runs[0][lane];
+#pragma unroll
+            for (int i = 1; i < kReduceRuns; ++i) t += runs[i][lane];
             to[c] = accumulate ? to[c] + t : t;
         }
         __syncthreads();
