@@ -494,6 +494,15 @@ def _torch_dtype(dtype):
     return torch.float32 if dtype == F32 else torch.bfloat16
 
 
+def _input_of(where, name, t, elements, dtype):
+    """Device address of a class's input: a contiguous device tensor of `dtype` with `elements` elements at least.  What a call on a few tokens
+    takes is mostly what it costs the host, so the classes look at an input once and keep their own buffers' addresses at hand."""
+    if t.dtype is not dtype or t.numel() < elements or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype} on {t.device}"
+                         f"{'' if t.is_contiguous() else ', not contiguous'}: {elements} contiguous elements of {dtype} on the GPU are needed")
+    return t.data_ptr()
+
+
 class Mx4Tensor:
     """Buffers of one tensor's packed form, along its rows and if asked along its columns, and of its values back."""
 
@@ -552,6 +561,10 @@ class Mx4Linear:
             self.grad_w = torch.zeros(n, k, dtype=torch.float32, device=device)
             need = max([need] + [tahq_mx4_matmul_workspace_size(c) for c in (self._forward, self._dx, self._dw)])
         self.workspace = _bytes_on(device, need)
+        self._kind = weight.dtype
+        self._kept = {k: getattr(self, k) for k in ("dy", "dy_t", "weight_t", "x_t", "workspace")} if training else {}
+        self._linear = (C.byref(self._x), C.byref(self._forward))
+        self._own = (self.weight.data_ptr(), self.weight.numel(), self.y.data_ptr(), self.workspace.data_ptr(), self.workspace.numel())
         self.update(weight)
 
     def update(self, weight, stream=None):
@@ -561,7 +574,10 @@ class Mx4Linear:
     def forward(self, x, stream=None):
         """y; in training x is kept along its tokens for the weight's gradient."""
         if not self.training:
-            tahq_mx4_linear(self._x, self._forward, x, self.weight, self.y, self.workspace, stream)
+            d_x = _input_of("Mx4Linear.forward", "x", x, self._x.rows * self._x.cols, self._kind)
+            rc = _lib.tahq_mx4_linear(*self._linear, d_x, *self._own, _stream_handle(stream))
+            if rc != 0:
+                raise TahqError(rc, "tahq_mx4_linear")
             return self.y
         tahq_mx4_quantize(self._x, x, self.x, self.x_t, stream)
         return self.product(self.x, stream)
@@ -573,9 +589,20 @@ class Mx4Linear:
 
     def backward(self, grad_y, stream=None):
         """(gradient of x, gradient of W); the latter is added to with accumulate = 1."""
-        tahq_mx4_quantize(self._dy, grad_y, self.dy, self.dy_t, stream)
-        tahq_mx4_matmul(self._dx, self.dy, self.weight_t, self.grad_x, self.workspace, stream)
-        tahq_mx4_matmul(self._dw, self.dy_t, self.x_t, self.grad_w, self.workspace, stream)
+        if not self.training:
+            raise ValueError("Mx4Linear.backward: the layer was not made with training=True")
+        d_dy = _input_of("Mx4Linear.backward", "grad_y", grad_y, self._dy.rows * self._dy.cols, self._kind)
+        at, size = {k: t.data_ptr() for k, t in self._kept.items()}, {k: t.numel() for k, t in self._kept.items()}
+        handle = _stream_handle(stream)
+        for name, call in (
+                ("tahq_mx4_quantize", (C.byref(self._dy), d_dy, at["dy"], size["dy"], at["dy_t"], size["dy_t"])),
+                ("tahq_mx4_matmul", (C.byref(self._dx), at["dy"], size["dy"], at["weight_t"], size["weight_t"], self.grad_x.data_ptr(),
+                                     at["workspace"], size["workspace"])),
+                ("tahq_mx4_matmul", (C.byref(self._dw), at["dy_t"], size["dy_t"], at["x_t"], size["x_t"], self.grad_w.data_ptr(),
+                                     at["workspace"], size["workspace"]))):
+            rc = getattr(_lib, name)(*call, handle)
+            if rc != 0:
+                raise TahqError(rc, name)
         return self.grad_x, self.grad_w
 
 
@@ -657,13 +684,23 @@ class BlockNorm:
         self.h = _bytes_on(device, tahq_mx4_packed_size(*shape)) if mx4 else torch.empty(shape, dtype=kind, device=device)
         self.stats = torch.empty(2, cfg.rows, dtype=torch.float32, device=device)
         self._need, self._device, self.workspace = need, device, None
+        self._kind, self._sizes = kind, (cfg.rows * cfg.cols, cfg.cols, _gate_groups(cfg) * cfg.cols)
+        h = self.h.data_ptr()
+        self._own = (self.residual_out.data_ptr(), None if mx4 else h, h if mx4 else None, self.h.numel() if mx4 else 0)
 
     def forward(self, residual, block, w_post, gate, w_pre, stream=None):
         """(r', h); block, w_post and gate may be None, or w_pre."""
-        h = None if w_pre is None else self.h
-        tahq_norm_forward(self.cfg, residual, block, w_post, gate, w_pre, self.residual_out, None if self.mx4 else h,
-                          h if self.mx4 else None, self.stats, stream)
-        return self.residual_out, h
+        where, kind, (n, cols, gates) = "BlockNorm.forward", self._kind, self._sizes
+        rc = _lib.tahq_norm_forward(
+            C.byref(self.cfg), _input_of(where, "residual", residual, n, kind),
+            None if block is None else _input_of(where, "block", block, n, kind),
+            None if w_post is None else _input_of(where, "w_post", w_post, cols, kind),
+            None if gate is None else _input_of(where, "gate", gate, gates, kind),
+            None if w_pre is None else _input_of(where, "w_pre", w_pre, cols, kind),
+            *(self._own if w_pre is not None else (self._own[0], None, None, 0)), self.stats.data_ptr(), _stream_handle(stream))
+        if rc != 0:
+            raise TahqError(rc, "tahq_norm_forward")
+        return self.residual_out, None if w_pre is None else self.h
 
     def backward(self, grad_residual_out, grad_h, block, w_post, gate, residual_out, w_pre, stats, stream=None):
         """Gradients of residual, block, w_post, gate and w_pre by name; None for what there is not."""
@@ -674,11 +711,22 @@ class BlockNorm:
             self.grad_residual, self.grad_block = (torch.empty_like(self.residual_out) for _ in range(2))
             self.grad_w_post, self.grad_w_pre = (torch.zeros(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
             self.grad_gate = torch.zeros(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
+        # in the order of the call's arguments
         got = {"grad_residual": self.grad_residual, "grad_block": None, "grad_w_post": None, "grad_gate": None, "grad_w_pre": None}
         if block is not None:
             got.update(grad_block=self.grad_block, grad_w_post=self.grad_w_post, grad_gate=self.grad_gate)
         if grad_h is not None:
             got["grad_w_pre"] = self.grad_w_pre
-        tahq_norm_backward(self.cfg, grad_residual_out, grad_h, block, w_post, gate, residual_out, w_pre, stats, got["grad_residual"],
-                           got["grad_block"], got["grad_w_post"], got["grad_gate"], got["grad_w_pre"], self.workspace, stream)
+        where, kind, (n, cols, gates) = "BlockNorm.backward", self._kind, self._sizes
+
+        def at(name, t, elements, dtype=kind):
+            return None if t is None else _input_of(where, name, t, elements, dtype)
+
+        rc = _lib.tahq_norm_backward(
+            C.byref(self.cfg), at("grad_residual_out", grad_residual_out, n), at("grad_h", grad_h, n), at("block", block, n),
+            at("w_post", w_post, cols), at("gate", gate, gates), at("residual_out", residual_out, n), at("w_pre", w_pre, cols),
+            at("stats", stats, 2 * self.cfg.rows, torch.float32), *(None if t is None else t.data_ptr() for t in got.values()),
+            self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))
+        if rc != 0:
+            raise TahqError(rc, "tahq_norm_backward")
         return got

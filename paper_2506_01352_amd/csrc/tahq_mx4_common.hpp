@@ -64,41 +64,74 @@ struct Eight {
         return __uint_as_float(!BF16 ? w : i % 2 ? w & 0xffff0000u : w << 16);
     }
 };
-// Rows need no alignment beyond their elements': a 16-byte access may start anywhere.
-// Elements c .. c + 7 of a row, of which the first is there; zeros behind the row's end.  EIGHTS: rows of whole eights
+// Rows need no alignment beyond their elements': a 16-byte access may start anywhere.  EIGHTS: rows of whole eights.
+// Elements c .. c + 7 of a row of C, of which the first is there; zeros behind the row's end.  `more`: seven elements behind it can be read, too, as they
+// can in all rows but the last: a row's end then takes no more loads than the rest of it (norms of 16384 x 2047 bf16, which wait for a row's
+// last wavefront: backward 172 -> 118 us, forward 112 -> 84).
 template <bool BF16, bool EIGHTS>
-__device__ __forceinline__ Eight<BF16> fetch(const void *row, uint32_t c, uint32_t C)
+__device__ __forceinline__ Eight<BF16> fetch(const void *row, uint32_t c, uint32_t C, bool more)
 {
+    constexpr uint32_t ES = BF16 ? 2 : 4, WORDS = BF16 ? 4 : 8;
     Eight<BF16> e;
-    if (EIGHTS || c + 8 <= C) {
-        __builtin_memcpy(e.q, static_cast<const uint8_t *>(row) + c * (BF16 ? 2 : 4), sizeof e.q);
-    } else {
-        uint32_t w[BF16 ? 4 : 8] = {};
+    if (EIGHTS || more || c + 8 <= C) {
+        __builtin_memcpy(e.q, static_cast<const uint8_t *>(row) + c * ES, sizeof e.q);
+        if (!EIGHTS && c + 8 > C) {
+            uint32_t w[WORDS];
+            __builtin_memcpy(w, e.q, sizeof w);
 #pragma unroll
-        for (uint32_t i = 0; i < 7; ++i)
-            if (c + i < C) {
-                if constexpr (BF16) w[i / 2] |= (uint32_t)static_cast<const uint16_t *>(row)[c + i] << (i % 2 * 16);
-                else w[i] = static_cast<const uint32_t *>(row)[c + i];
+            for (uint32_t i = 0; i < WORDS; ++i) {
+                if constexpr (BF16) w[i] = c + 2 * i + 1 < C ? w[i] : c + 2 * i < C ? w[i] & 0xffffu : 0u;
+                else w[i] = c + i < C ? w[i] : 0u;
             }
-        __builtin_memcpy(e.q, w, sizeof e.q);
+            __builtin_memcpy(e.q, w, sizeof w);
+        }
+        return e;
     }
+    asm volatile("");                                      // keeps the two ways apart: joined, both would go element by element
+    uint32_t w[WORDS] = {};
+#pragma unroll
+    for (uint32_t i = 0; i < 7; ++i)
+        if (c + i < C) {
+            if constexpr (BF16) w[i / 2] |= (uint32_t)static_cast<const uint16_t *>(row)[c + i] << (i % 2 * 16);
+            else w[i] = static_cast<const uint32_t *>(row)[c + i];
+        }
+    __builtin_memcpy(e.q, w, sizeof e.q);
     return e;
 }
+// Whether seven elements behind row r's end are still in the tensor
+__device__ __forceinline__ bool more_behind(uint32_t r, uint32_t rows, uint64_t ld) { return r + 7 < rows || (r + 1 < rows && ld >= 7); }
 // what fetch reads
 template <bool BF16, bool EIGHTS>
 __device__ __forceinline__ void keep(void *row, uint32_t c, uint32_t C, const float (&x)[8])
 {
+    constexpr uint32_t ES = BF16 ? 2 : 4, WORDS = BF16 ? 4 : 8;
+    uint8_t *to = static_cast<uint8_t *>(row) + c * ES;
+    uint32_t w[WORDS];
+#pragma unroll
+    for (uint32_t i = 0; i < WORDS; ++i) w[i] = BF16 ? two_bf16(x[2 * i % 8], x[(2 * i + 1) % 8]) : __float_as_uint(x[i]);
     if (EIGHTS || c + 8 <= C) {
-        if constexpr (BF16) {
-            const uint32_t w[4] = {two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7])};
-            __builtin_memcpy(static_cast<uint8_t *>(row) + c * 2, w, 16);
-        } else {
-            __builtin_memcpy(static_cast<uint8_t *>(row) + c * 4, x, 32);
+        __builtin_memcpy(to, w, sizeof w);
+        return;
+    }
+    asm volatile("");
+    if constexpr (BF16) {
+        const uint32_t left = C - c;                       // 1 .. 7: four, two and one of them
+        if (left & 4) {
+            __builtin_memcpy(to, w, 8);
+            to += 8;
+            w[0] = w[2];
+            w[1] = w[3];
         }
+        if (left & 2) {
+            __builtin_memcpy(to, w, 4);
+            to += 4;
+            w[0] = w[1];
+        }
+        if (left & 1) *reinterpret_cast<uint16_t *>(to) = (uint16_t)w[0];
     } else {
 #pragma unroll
         for (uint32_t i = 0; i < 7; ++i)
-            if (c + i < C) store1<BF16>(row, c + i, x[i]);
+            if (c + i < C) __builtin_memcpy(to + 4 * i, w + i, 4);
     }
 }
 
@@ -227,14 +260,15 @@ __device__ __forceinline__ uint32_t quantize_quad(const Eight<BF16> &e, uint32_t
     }
 }
 
-// the magnitude a code stands for, times its block's scale; `scale` of a block of NaN is NaN
-__device__ __forceinline__ float code_value(uint32_t code, float scale)
+// the numbers that eight codes and their block's scale byte stand for
+__device__ __forceinline__ void values8(uint32_t w, uint32_t s, float (&x)[8])
 {
-    // 0, .5: subnormal grid; otherwise exponent (code >> 1 & 3), fraction bit code & 1
-    const uint32_t m = code & 7u;
-    const float v = m < 2 ? 0.5f * (float)m : __uint_as_float((126u + (m >> 1)) << 23 | (m & 1u) << 22);
-    return (code & 8u ? -v : v) * scale;
+    typedef float pair __attribute__((ext_vector_type(2)));
+    const float v = scale_value(s);
+    const pair p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, v, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, v, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, v, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, v, 3)};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s == 255u ? __uint_as_float(0x7fc00000u) : i % 2 ? p[i / 2].y : p[i / 2].x;
 }
-__device__ __forceinline__ float dequant_scale(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : scale_value(s); }
 
 }  // namespace tahq

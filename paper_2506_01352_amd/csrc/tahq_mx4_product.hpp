@@ -364,7 +364,7 @@ void k_mx4_few(const uint8_t *b, FewInput in, void *c, uint32_t M, uint32_t N, u
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) {
                     const uint32_t r = 2 * i + lane / 32, c = lane % 32 * 8, wide = K - g * 256;
-                    if (r < M && c < wide) x[u][i] = fetch<QUANT == 1, false>(a + ((uint64_t)r * in.ld + g * 256) * (QUANT == 1 ? 2 : 4), c, wide);
+                    if (r < M && c < wide) x[u][i] = fetch<QUANT == 1, false>(a + ((uint64_t)r * in.ld + g * 256) * (QUANT == 1 ? 2 : 4), c, wide, more_behind(r, M, in.ld));
                 }
             }
 #pragma unroll

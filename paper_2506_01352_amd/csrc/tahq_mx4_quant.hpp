@@ -102,7 +102,7 @@ void k_mx4_quantize(const void *in, uint8_t *packed, uint8_t *packed_t, uint32_t
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t r = r0 + row + 8 * i;
-        if (r < rows && 8 * chunk < wide) x[i] = fetch<BF16, false>(static_cast<const uint8_t *>(in) + ((uint64_t)r * ld + c0) * ES, 8 * chunk, wide);
+        if (r < rows && 8 * chunk < wide) x[i] = fetch<BF16, false>(static_cast<const uint8_t *>(in) + ((uint64_t)r * ld + c0) * ES, 8 * chunk, wide, more_behind(r, rows, ld));
     }
     uint32_t w[8] = {}, s[8] = {};
 #pragma unroll
@@ -157,6 +157,22 @@ void k_mx4_quantize(const void *in, uint8_t *packed, uint8_t *packed_t, uint32_t
     }
 }
 
+// The 32 fp32 of a block that four lanes hold eight each of: lanes trade halves, so that each of the two stores writes 64 bytes in a row
+__device__ __forceinline__ void keep_block(float *to, const float (&x)[8])
+{
+    const uint32_t lane = threadIdx.x % 4;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = half ? quadf<0xfa>(x[i]) : quadf<0x50>(x[i]), b = half ? quadf<0xfa>(x[4 + i]) : quadf<0x50>(x[4 + i]);
+            v[i] = lane % 2 ? b : a;
+        }
+        __builtin_memcpy(to + 16 * half + 4 * lane, v, 16);
+    }
+}
+
 // Values of a packed matrix.  A workgroup takes 32 rows x 256 columns, 4 KB of codes; four lanes share a block, as above.
 template <bool BF16, bool ROTATE>
 __global__ __launch_bounds__(kQuantThreads)
@@ -179,11 +195,15 @@ void k_mx4_dequantize(const uint8_t *packed, void *out, uint32_t rows, uint32_t 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t r = r0 + row + 8 * i;
-        const float v = dequant_scale(s[i]);
         float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = code_value(w[i] >> (4 * j), v);
+        values8(w[i], s[i], x);
         if constexpr (ROTATE) rotate_quad(x);
+        if constexpr (!BF16) {
+            if (r < rows && 8 * (chunk | 3) + 8 <= wide) {
+                keep_block(static_cast<float *>(out) + (uint64_t)r * ld + c0 + 32 * (chunk / 4), x);
+                continue;
+            }
+        }
         if (r < rows && 8 * chunk < wide) keep<BF16, false>(static_cast<uint8_t *>(out) + ((uint64_t)r * ld + c0) * (BF16 ? 2 : 4), 8 * chunk, wide, x);
     }
 }

@@ -1,5 +1,4 @@
 // Entry points of the block norms (include/tahq_norm.h): validation, plan, launches.
-#include <stdlib.h>
 #include <type_traits>
 
 #include "tahq_enqueue.hpp"
@@ -50,7 +49,19 @@ void with_kind(const tahq_norm_config *c, bool post, bool pre, Run run)
     else eights ? with_halves<false, true>(post, pre, run) : with_halves<false, false>(post, pre, run);
 }
 
-// Backward: the workgroups that share the rows
+// Forward: rows that a workgroup takes one after another.  Two where there are many (8192 x 4096, one row: 45 us, two: 42.7, eight: 47); eight where a
+// workgroup of more than twelve wavefronts has a compute unit to itself and only the next row on its way keeps memory busy (2048 x 8192: one
+// 36, two 31, eight 28); one where there are few.
+uint32_t forward_rows(const tahq_norm_config *c, uint32_t rows)
+{
+    if (waves_of(c) > 12) return rows >= 2048 ? 8 : 1;
+    return rows >= 4096 ? 2 : 1;
+}
+
+// Backward: the workgroups that share the rows.  A compute unit holds sixteen wavefronts of up to 128 registers, so `most` workgroups at once; as many of
+// those as leave no compute unit with more rows than another need have (2331 rows: 10 with one or two workgroups each, 12 with three or four).  Two
+// rounds of workgroups of unlike length cost more than their column sums: 32768 x 5120, ten wavefronts: 256 workgroups 455 us, 409 534, 512
+// 458; 32768 x 1024, two: 512 152, 1024 111, 2048 101.
 struct BackwardPlan {
     uint32_t rows_each, workgroups;
     uint64_t workspace;
@@ -58,10 +69,16 @@ struct BackwardPlan {
 BackwardPlan plan_backward(const tahq_norm_config *c)
 {
     BackwardPlan p;
-    const char *e = getenv("NB_WG"), *e2 = getenv("NB_MIN");
-    const uint32_t most = e ? atoi(e) : 512, least = e2 ? atoi(e2) : 4;
-    p.rows_each = (c->rows + most - 1) / most;
-    if (p.rows_each < least) p.rows_each = least;
+    const uint32_t most = waves_of(c) > 1 ? 16 / waves_of(c) : 8;          // of one wavefront eight: 32768 x 512, 2048 in all 47 us, 4096 71
+    uint64_t least = ~0ull;
+    p.rows_each = 0;
+    for (uint32_t k = most; k > 0; --k) {
+        const uint32_t each = (uint32_t)(((uint64_t)c->rows + 256 * k - 1) / (256 * k));
+        if ((uint64_t)k * each < least) {
+            least = (uint64_t)k * each;
+            p.rows_each = each;
+        }
+    }
     p.workgroups = (c->rows + p.rows_each - 1) / p.rows_each;
     p.workspace = (uint64_t)p.workgroups * c->cols * 4 * (c->gate_rows ? 4 : 2);
     return p;
@@ -106,8 +123,7 @@ tahq_status tahq_norm_forward(const tahq_norm_config *cfg, const void *d_residua
     const NormShape s = shape_of(cfg);
     const uint32_t cover = cfg->scale_rule == TAHQ_MX4_COVER ? kCover : 0u;
     const uint32_t total = d_h_mx4 ? 32 * ((cfg->rows + 31) / 32) : cfg->rows;
-    const char *e = getenv("NF_ROWS");
-    const uint32_t rows_each = e ? atoi(e) : total >= 4096 ? 2 : 1;
+    const uint32_t rows_each = forward_rows(cfg, total);
     const dim3 grid((total + rows_each - 1) / rows_each);
     Enqueue q{(hipStream_t)stream};
     with_kind(cfg, d_block, d_w_pre, [&](auto bf16, auto eights, auto post, auto pre) {
@@ -163,8 +179,9 @@ tahq_status tahq_norm_backward(const tahq_norm_config *cfg, const void *d_grad_r
     const uint32_t groups = gate ? (cfg->rows + s.gate_rows - 1) / s.gate_rows : 0;
     if (d_block || d_grad_h) {
         const uint32_t slots = groups < 64 ? groups : 64;
-        q(k_norm_reduce, dim3((cfg->cols + 63) / 64, 2 + slots), dim3(64 * kReduceRuns), parts, d_grad_w_post, d_grad_w_pre, d_grad_gate, cfg->cols,
-          p.workgroups, cfg->rows, s.gate_rows, p.rows_each, groups, cfg->accumulate);
+        const uint32_t width = cfg->cols <= 2048 ? 16 : 64;
+        q(k_norm_reduce, dim3((cfg->cols + width - 1) / width, 2 + slots), dim3(kReduceLanes), parts, d_grad_w_post, d_grad_w_pre, d_grad_gate, cfg->cols,
+          p.workgroups, cfg->rows, s.gate_rows, p.rows_each, groups, cfg->accumulate, width);
     }
     return q.result();
 }

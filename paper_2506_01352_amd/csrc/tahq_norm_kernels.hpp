@@ -107,17 +107,17 @@ void k_norm_forward(const void *residual, const void *block, const void *w_post,
     Eight<BF16> next_r = {}, next_b = {}, post = {}, pre = {}, next_k = ones<BF16>();
     auto ask = [&](uint32_t row) {
         if (row < s.rows && row < last && mine) {
-            next_r = fetch<BF16, EIGHTS>(row_of<BF16>(residual, row, C), c, C);
+            next_r = fetch<BF16, EIGHTS>(row_of<BF16>(residual, row, C), c, C, more_behind(row, s.rows, C));
             if constexpr (POST) {
-                next_b = fetch<BF16, EIGHTS>(row_of<BF16>(block, row, C), c, C);
-                if (gate) next_k = fetch<BF16, EIGHTS>(row_of<BF16>(gate, row / s.gate_rows, C), c, C);
+                next_b = fetch<BF16, EIGHTS>(row_of<BF16>(block, row, C), c, C, more_behind(row, s.rows, C));
+                if (gate) next_k = fetch<BF16, EIGHTS>(row_of<BF16>(gate, row / s.gate_rows, C), c, C, false);
             }
         }
     };
     ask(first);
     if (mine) {
-        if constexpr (POST) post = fetch<BF16, EIGHTS>(w_post, c, C);
-        if constexpr (PRE) pre = fetch<BF16, EIGHTS>(w_pre, c, C);
+        if constexpr (POST) post = fetch<BF16, EIGHTS>(w_post, c, C, false);
+        if constexpr (PRE) pre = fetch<BF16, EIGHTS>(w_pre, c, C, false);
     }
     clear(places);
     const float inv_c = 1.0f / (float)C;
@@ -202,27 +202,27 @@ void k_norm_backward(const void *grad_out, const void *grad_h, const void *block
     auto ask_pre = [&](uint32_t row) {
         if (row < last && mine) {
             if constexpr (PRE) {
-                gh = fetch<BF16, EIGHTS>(row_of<BF16>(grad_h, row, C), c, C);
-                ro = fetch<BF16, EIGHTS>(row_of<BF16>(residual_out, row, C), c, C);
+                gh = fetch<BF16, EIGHTS>(row_of<BF16>(grad_h, row, C), c, C, more_behind(row, s.rows, C));
+                ro = fetch<BF16, EIGHTS>(row_of<BF16>(residual_out, row, C), c, C, more_behind(row, s.rows, C));
             }
-            if (grad_out) go = fetch<BF16, EIGHTS>(row_of<BF16>(grad_out, row, C), c, C);
+            if (grad_out) go = fetch<BF16, EIGHTS>(row_of<BF16>(grad_out, row, C), c, C, more_behind(row, s.rows, C));
         }
     };
     auto ask_post = [&](uint32_t row) {
-        if (POST && row < last && mine) bl = fetch<BF16, EIGHTS>(row_of<BF16>(block, row, C), c, C);
+        if (POST && row < last && mine) bl = fetch<BF16, EIGHTS>(row_of<BF16>(block, row, C), c, C, more_behind(row, s.rows, C));
     };
     // the rows of one gate row; they change on the way
     uint32_t group = 0, stop = 0;
     auto ask_gate = [&](uint32_t row) {
         group = row / s.gate_rows;
         stop = (uint32_t)min((uint64_t)group * s.gate_rows + s.gate_rows, (uint64_t)s.rows);
-        if (mine) k = fetch<BF16, EIGHTS>(row_of<BF16>(gate, group, C), c, C);
+        if (mine) k = fetch<BF16, EIGHTS>(row_of<BF16>(gate, group, C), c, C, false);
     };
     ask_pre(first);
     ask_post(first);
     if (mine) {
-        if constexpr (POST) wpost = fetch<BF16, EIGHTS>(w_post, c, C);
-        if constexpr (PRE) wpre = fetch<BF16, EIGHTS>(w_pre, c, C);
+        if constexpr (POST) wpost = fetch<BF16, EIGHTS>(w_post, c, C, false);
+        if constexpr (PRE) wpre = fetch<BF16, EIGHTS>(w_pre, c, C, false);
     }
     if (POST && gate) ask_gate(first);
     clear(places);
@@ -295,18 +295,18 @@ void k_norm_backward(const void *grad_out, const void *grad_h, const void *block
     if constexpr (PRE) put<EIGHTS>(parts.pre + (uint64_t)blockIdx.x * C, c, C, pre, false);
 }
 
-// The workgroups' column sums, added in a fixed order: 64 columns x 16 runs of workgroups, eight loads of a run on their way at a time.
-// blockIdx.y: 0 post, 1 pre, then the groups of the gate.
-constexpr int kReduceRuns = 16;
+// The workgroups' column sums, added in a fixed order by blocks of 1024 lanes: `width` columns (64; 16 where there are few, to have more blocks) x
+// 1024 / width runs of workgroups, eight loads of a run on their way at a time.  blockIdx.y: 0 post, 1 pre, then the groups of the gate.
+constexpr uint32_t kReduceLanes = 1024;
 
-__global__ __launch_bounds__(64 * kReduceRuns)
+__global__ __launch_bounds__(kReduceLanes)
 void k_norm_reduce(NormPartials parts, float *grad_w_post, float *grad_w_pre, float *grad_gate, uint32_t C, uint32_t W,
-                   uint32_t rows, uint32_t gate_rows, uint32_t rows_each, uint32_t groups, uint32_t accumulate)
+                   uint32_t rows, uint32_t gate_rows, uint32_t rows_each, uint32_t groups, uint32_t accumulate, uint32_t width)
 {
-    __shared__ float runs[kReduceRuns][64];
-    const uint32_t lane = threadIdx.x % 64, run = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    __shared__ float sums[kReduceLanes];
+    const uint32_t lane = threadIdx.x % width, run = threadIdx.x / width, runs = kReduceLanes / width, c = blockIdx.x * width + lane;
     auto total = [&](auto part, uint32_t n, float *to) {
-        const uint32_t each = (n + kReduceRuns - 1) / kReduceRuns, from = min(run * each, n), till = min(from + each, n);
+        const uint32_t each = (n + runs - 1) / runs, from = min(run * each, n), till = min(from + each, n);
         float sum = 0.0f;
         if (c < C)
             for (uint32_t i = from; i < till; i += 8) {
@@ -315,14 +315,13 @@ void k_norm_reduce(NormPartials parts, float *grad_w_post, float *grad_w_pre, fl
                 for (uint32_t k = 0; k < 8; ++k) v[k] = i + k < till ? part(i + k)[c] : 0.0f;
                 sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
             }
-        runs[run][lane] = sum;
+        sums[threadIdx.x] = sum;
         __syncthreads();
-        if (run == 0 && c < C) {
-            float t = runs[0][lane];
-#pragma unroll
-            for (int i = 1; i < kReduceRuns; ++i) t += runs[i][lane];
-            to[c] = accumulate ? to[c] + t : t;
+        for (uint32_t half = kReduceLanes / 2; half >= width; half /= 2) {
+            if (threadIdx.x < half) sums[threadIdx.x] += sums[threadIdx.x + half];
+            __syncthreads();
         }
+        if (run == 0 && c < C) to[c] = accumulate ? to[c] + sums[lane] : sums[lane];
         __syncthreads();
     };
     if (blockIdx.y == 0) {
