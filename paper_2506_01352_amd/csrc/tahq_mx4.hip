@@ -68,15 +68,16 @@ constexpr uint32_t kFewRows = 32, kFewQuantRows = 8;
 
 // Time of a product on 256 compute units, in us, with tiles of tm x tn of which `per_cu` are on a compute unit at once: `start` for each that one takes after
 // another, `each` byte of results, and for 256 columns `alone` while a unit has one tile and not all units have one, `loaded` for each tile of a
-// unit's once they have.  (All units at work slow down: 256 x 256 tiles 1.2 -> 1.77 us; the clock gives way.)  Fitted to 115 shapes from
-// 33 x 512 x 512 to 8192^3: what it chooses takes 0.7 % longer on average than the best of the five.
+// unit's once they have.  (All units at work slow down: 256 x 256 tiles 1.37 -> 1.77 us; the clock gives way.)  Fitted to 253 shapes from
+// 33 x 512 x 512 to 8192^3, both types of C: what it chooses takes 0.4 % longer on average than the best of the six.  The last kind has two teams
+// to a tile: 64 x 8192 x 8192 11.4 -> 9.6 us, 512 x 2048 x 8192 11.1 -> 10.1; two teams for larger tiles and four for these gained nothing more.
 struct TileKind {
     uint32_t tm, tn, per_cu;
     float start, alone, loaded;
 };
 constexpr TileKind kTiles[] = {
-    {256, 256, 1, 5.6f, 1.2f, 1.77f}, {256, 128, 2, 3.9f, 0.74f, 1.02f}, {128, 128, 2, 3.1f, 0.43f, 0.568f},
-    {64, 128, 3, 2.75f, 0.32f, 0.36f}, {64, 64, 4, 2.84f, 0.275f, 0.219f}};
+    {256, 256, 1, 5.6f, 1.37f, 1.77f},  {256, 128, 2, 4.18f, 0.687f, 1.08f}, {128, 128, 2, 2.68f, 0.43f, 0.584f},
+    {64, 128, 3, 2.75f, 0.32f, 0.36f}, {64, 64, 4, 2.84f, 0.275f, 0.248f},  {64, 64, 2, 3.3f, 0.22f, 0.24f}};
 constexpr float kEachByte = 4e-5f;
 
 uint64_t tiles_of(const TileKind &t, const tahq_mx4_matmul_config *c) { return ceil_div(c->m, t.tm) * ceil_div(c->n, t.tn); }
@@ -112,11 +113,12 @@ ProductPlan plan_product(const tahq_mx4_matmul_config *c)
             best = t;
         }
     }
-    // A long sum in few of the smallest tiles: runs of 16 groups and more, as many as there are compute units for.  512 x 512 x 16384: 19.2 us in
-    // one run, 13.9 in four; x 8192: 10.0 and 11.1.
+    // A long sum in few of the smallest tiles: runs of 16 groups and more, as many as there are compute units for.  512 x 512 x 16384: 15.8 us
+    // in one run of two teams, 13.9 in four; with 32 groups, x 8192, 9.0 and 11.1.
     const uint64_t tiles = tiles_of(kTiles[p.kind], c);
-    if (p.kind == 4 && groups >= 48 && tiles <= 128) {
+    if (p.kind >= 4 && groups >= 48 && tiles <= 64) {
         const uint32_t by_units = (uint32_t)(256 / tiles), by_length = groups / 16;
+        p.kind = 4;
         p.run = (uint32_t)ceil_div(groups, by_units < by_length ? by_units : by_length);
         p.parts = (uint32_t)ceil_div(groups, p.run);
     }
@@ -130,24 +132,24 @@ uint64_t product_workspace(const tahq_mx4_matmul_config *c)
 
 uint64_t ldc_of(const tahq_mx4_matmul_config *c) { return c->ldc ? c->ldc : c->n; }
 
-template <int WM, int WN, int MF, int NF, int NB, int PER_CU>
+template <int WM, int WN, int MF, int NF, int NB, int KS, int PER_CU>
 void launch_tiles(const tahq_mx4_matmul_config *c, const ProductPlan &p, const uint8_t *a, const uint8_t *b, void *d_c, void *d_workspace, Enqueue *q)
 {
     const uint32_t tiles_m = (uint32_t)ceil_div(c->m, 32 * WM * MF), tiles_n = (uint32_t)ceil_div(c->n, 32 * WN * NF);
     auto run = [&](auto kernel, void *to) {
-        (*q)(kernel, dim3(tiles_m * tiles_n, p.parts), dim3(64 * WM * WN), a, b, to, c->m, c->n, c->k, ldc_of(c), c->accumulate, tiles_m, tiles_n, p.run);
+        (*q)(kernel, dim3(tiles_m * tiles_n, p.parts), dim3(64 * WM * WN * KS), a, b, to, c->m, c->n, c->k, ldc_of(c), c->accumulate, tiles_m, tiles_n, p.run);
     };
-    if constexpr (MF == 1 && NF == 1) {
+    if constexpr (MF == 1 && NF == 1 && KS == 1) {
         if (p.parts > 1) {
-            run(k_mx4_tiles<WM, WN, MF, NF, NB, PER_CU, 2>, d_workspace);
+            run(k_mx4_tiles<WM, WN, MF, NF, NB, KS, PER_CU, 2>, d_workspace);
             const dim3 grid((uint32_t)ceil_div((uint64_t)c->m * c->n, 1024));
             (*q)(c->out_dtype == TAHQ_BF16 ? k_mx4_sum_parts<true> : k_mx4_sum_parts<false>, grid, dim3(256), static_cast<const float *>(d_workspace),
                  d_c, c->m, c->n, ldc_of(c), c->accumulate, p.parts);
             return;
         }
     }
-    if (c->out_dtype == TAHQ_BF16) run(k_mx4_tiles<WM, WN, MF, NF, NB, PER_CU, 1>, d_c);
-    else run(k_mx4_tiles<WM, WN, MF, NF, NB, PER_CU, 0>, d_c);
+    if (c->out_dtype == TAHQ_BF16) run(k_mx4_tiles<WM, WN, MF, NF, NB, KS, PER_CU, 1>, d_c);
+    else run(k_mx4_tiles<WM, WN, MF, NF, NB, KS, PER_CU, 0>, d_c);
 }
 
 template <int MT, int NT, int QUANT, bool ROTATE, int PAIRS>
@@ -170,11 +172,12 @@ tahq_status enqueue_product(const tahq_mx4_matmul_config *c, const void *d_a, co
     const uint8_t *a = static_cast<const uint8_t *>(d_a), *b = static_cast<const uint8_t *>(d_b);
     if (p.kind >= 0 && tiles_of(kTiles[p.kind], c) > kMaxGrid) return TAHQ_ERR_UNSUPPORTED;
     switch (p.kind) {
-    case 0: launch_tiles<2, 2, 4, 4, 4, 1>(c, p, a, b, d_c, d_workspace, q); break;
-    case 1: launch_tiles<2, 2, 4, 2, 3, 2>(c, p, a, b, d_c, d_workspace, q); break;
-    case 2: launch_tiles<2, 2, 2, 2, 4, 2>(c, p, a, b, d_c, d_workspace, q); break;
-    case 3: launch_tiles<2, 2, 1, 2, 4, 3>(c, p, a, b, d_c, d_workspace, q); break;
-    case 4: launch_tiles<2, 2, 1, 1, 4, 4>(c, p, a, b, d_c, d_workspace, q); break;
+    case 0: launch_tiles<2, 2, 4, 4, 4, 1, 1>(c, p, a, b, d_c, d_workspace, q); break;
+    case 1: launch_tiles<2, 2, 4, 2, 3, 1, 2>(c, p, a, b, d_c, d_workspace, q); break;
+    case 2: launch_tiles<2, 2, 2, 2, 4, 1, 2>(c, p, a, b, d_c, d_workspace, q); break;
+    case 3: launch_tiles<2, 2, 1, 2, 4, 1, 3>(c, p, a, b, d_c, d_workspace, q); break;
+    case 4: launch_tiles<2, 2, 1, 1, 4, 1, 4>(c, p, a, b, d_c, d_workspace, q); break;
+    case 5: launch_tiles<2, 2, 1, 1, 4, 2, 2>(c, p, a, b, d_c, d_workspace, q); break;
     default:
         if (c->m <= 16) launch_few<1, 1, 0, false, 1>(c, {a, 0, 0}, b, d_c, q);
         else launch_few<2, 2, 0, false, 1>(c, {a, 0, 0}, b, d_c, q);

@@ -98,30 +98,34 @@ __device__ __forceinline__ void store16(void *c, uint64_t at, uint32_t valid, ui
 // read is loaded over.  Reads and loads are spread between the matrix instructions.
 //   Columns behind the last unit: the last unit's codes again, with the scales that fill up a group of 256, which are 2^-127 on both sides: the
 // products are nothing beside 2^-149, the smallest fp32 number.
+//   KS: teams of WM * WN wavefronts that share the tile's columns, each with stages of its own, where there are too few tiles for two to a compute
+// unit: one wavefront to a vector unit waits more than it multiplies.
 //   OUT: 0 fp32, 1 bf16, 2 fp32 parts of a sum over k in gridDim.y runs of `run` groups of 256 columns.
-template <int WM, int WN, int MF, int NF, int NB, int PER_CU, int OUT>
-__global__ __launch_bounds__(64 * WM * WN, PER_CU)
+template <int WM, int WN, int MF, int NF, int NB, int KS, int PER_CU, int OUT>
+__global__ __launch_bounds__(64 * WM * WN * KS, PER_CU * KS)
 void k_mx4_tiles(const uint8_t *a, const uint8_t *b, void *c, uint32_t M, uint32_t N, uint32_t K, uint64_t ldc, uint32_t accumulate,
                  uint32_t tiles_m, uint32_t tiles_n, uint32_t run)
 {
     constexpr int UM = WM * MF, ROWS = UM + WN * NF, W = WM * WN;        // units of rows of A, of both, in a stage
     constexpr int CODES = ROWS * 2048, SCALES = ROWS * 256;
     constexpr int EACH = ROWS * 2 / W, EACH_S = (ROWS + W - 1) / W, PRODUCTS = MF * NF;
+    static_assert(KS == 1 || NB == 4, "teams' scales lie side by side");
     static_assert(ROWS * 2 % W == 0, "the same number of loads in every wavefront");
     // a variable for each stage: the compiler then knows which loads a read has to wait for
-    __shared__ __attribute__((aligned(1024))) uint8_t s0[CODES], s1[CODES], s2[CODES], s3[NB == 4 ? CODES : 16];
-    __shared__ __attribute__((aligned(256))) uint8_t t0[NB == 4 ? SCALES : 2 * SCALES], t1[NB == 4 ? SCALES : 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t s0[KS * CODES], s1[KS * CODES], s2[KS * CODES], s3[NB == 4 ? KS * CODES : 16];
+    __shared__ __attribute__((aligned(256))) uint8_t t0[KS * (NB == 4 ? SCALES : 2 * SCALES)], t1[NB == 4 ? KS * SCALES : 16];
+    const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64 % W), team = KS == 1 ? 0 : uniform(threadIdx.x / 64 / W);
     uint8_t *const codes[4] = {s0, s1, s2, s3};
     // where the scales of the group of 256 columns with stage s are; s is `at` and a multiple of the unrolled stages
     auto scale_words = [&](int at, uint32_t s) { return NB == 4 ? (at / 2 % 2 ? t1 : t0) : t0 + s / 2 % 2 * SCALES; };
     constexpr int TURN = NB == 3 ? 3 : 2;                    // groups of 256 columns that bring the buffers round
 
     const Mx4Layout LA(M, K), LB(N, K);
-    const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
     uint32_t tm, tn;
     tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
-    const uint32_t first = blockIdx.y * run;                 // group of 256 columns
-    const uint32_t groups = min(run, LA.kc - first);
+    // groups of 256 columns: a team's first one, how many it has, and how many all of them take their turn for
+    const uint32_t in_run = min(run, LA.kc - blockIdx.y * run), groups = (in_run + KS - 1) / KS;
+    const uint32_t first = blockIdx.y * run + team * groups, own = in_run > team * groups ? min(groups, in_run - team * groups) : 0;
 
     // this wavefront's share of a stage; units behind the last row are not there: the last one again, whose results are not stored
     const uint8_t *from[EACH], *from_s[EACH_S];
@@ -134,17 +138,17 @@ void k_mx4_tiles(const uint8_t *a, const uint8_t *b, void *c, uint32_t M, uint32
 #pragma unroll
     for (int j = 0; j < EACH_S; ++j) {
         const uint32_t i = min(wave * EACH_S + j, (uint32_t)ROWS - 1);
-        from_s[j] = (i < UM ? a + LA.scales() : b + LB.scales()) + ((uint64_t)row_unit(i) * LA.kc + first) * 256;
+        from_s[j] = (i < UM ? a + LA.scales() : b + LB.scales()) + (uint64_t)row_unit(i) * LA.kc * 256;
     }
     // load j of stage `stage`, the `at`-th of the unrolled ones: codes, then with the first of two stages the scales
     auto issue = [&](int at, uint32_t stage, int j) {
         if (j < EACH) {
             const uint32_t unit = wave * EACH + j, kb = uniform(min(4 * first + 2 * stage + unit % 2, LA.kb - 1));
-            __builtin_amdgcn_global_load_lds((GlobalPtr)(from[j] + (uint64_t)kb * 1024 + lane * 16), (LdsPtr)(codes[at % NB] + unit * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((GlobalPtr)(from[j] + (uint64_t)kb * 1024 + lane * 16), (LdsPtr)(codes[at % NB] + (team * CODES + unit * 1024)), 16, 0, 0);
         } else {
-            const uint32_t unit = min(wave * EACH_S + j - EACH, (uint32_t)ROWS - 1), group = uniform(min(stage / 2, groups - 1));
+            const uint32_t unit = min(wave * EACH_S + j - EACH, (uint32_t)ROWS - 1), group = uniform(min(first + stage / 2, LA.kc - 1));
             __builtin_amdgcn_global_load_lds((GlobalPtr)(from_s[j - EACH] + (uint64_t)group * 256 + lane * 4),
-                                             (LdsPtr)(scale_words(at, stage) + unit * 256), 4, 0, 0);
+                                             (LdsPtr)(scale_words(at, stage) + (team * SCALES + unit * 256)), 4, 0, 0);
         }
     };
     // all wavefronts have the operands that they asked for, and their loads but the last `behind`
@@ -159,8 +163,8 @@ void k_mx4_tiles(const uint8_t *a, const uint8_t *b, void *c, uint32_t M, uint32
     uint32_t sc[MF + NF], next_sc[MF + NF];
     const uint32_t wm = wave / WN * MF, wn = UM + wave % WN * NF;        // this wavefront's units in a stage
     auto unit_at = [&](int i) { return i < MF ? wm + i : wn + i - MF; };
-    auto operand = [&](const uint8_t *s, int kb, int i) { return *reinterpret_cast<const uint4 *>(s + unit_at(i) * 2048 + kb * 1024 + lane * 16); };
-    auto scale = [&](const uint8_t *s, int i) { return *reinterpret_cast<const uint32_t *>(s + unit_at(i) * 256 + lane * 4); };
+    auto operand = [&](const uint8_t *s, int kb, int i) { return *reinterpret_cast<const uint4 *>(s + (team * CODES + unit_at(i) * 2048 + kb * 1024 + lane * 16)); };
+    auto scale = [&](const uint8_t *s, int i) { return *reinterpret_cast<const uint32_t *>(s + (team * SCALES + unit_at(i) * 256 + lane * 4)); };
 
 #pragma unroll
     for (int at = 0; at < NB; ++at)
@@ -169,8 +173,8 @@ void k_mx4_tiles(const uint8_t *a, const uint8_t *b, void *c, uint32_t M, uint32
     arrived(std::integral_constant<int, (NB - 1) * EACH + (NB - 1) / 2 * EACH_S>{});
 #pragma unroll
     for (int i = 0; i < MF + NF; ++i) {
-        sc[i] = scale(t0, i);
-        v[0][i] = operand(s0, 0, i);
+        sc[i] = KS == 1 || own ? scale(scale_words(0, 0), i) : 0;
+        v[0][i] = operand(codes[0], 0, i);
     }
     __builtin_amdgcn_s_waitcnt(waitcnt(63, 0));
 
@@ -203,7 +207,7 @@ void k_mx4_tiles(const uint8_t *a, const uint8_t *b, void *c, uint32_t M, uint32
 #pragma unroll
         for (int i = 0; i < MF + NF; ++i) {
             pin(v[0][i]);
-            if (ODD) sc[i] = next_sc[i];
+            if (ODD) sc[i] = KS == 1 || (s + 1) / 2 < own ? next_sc[i] : 0;
         }
     };
     auto group = [&](auto at, uint32_t s) {
@@ -225,6 +229,43 @@ void k_mx4_tiles(const uint8_t *a, const uint8_t *b, void *c, uint32_t M, uint32
     }
     // loads to LDS that nobody reads are waited for, too: the results pass through LDS, so that rows of C are written a line at a time
     arrived(std::integral_constant<int, 0>{});
+    if constexpr (KS > 1) {
+        // the teams' sums to the first one, which adds them in order: a piece is 16 numbers of every lane of a team
+        constexpr int PIECE = W * 4096, EACH_STAGE = KS * CODES / PIECE;
+        static_assert(NB == 4 && (KS - 1) * PRODUCTS <= NB * EACH_STAGE, "all pieces fit");
+        uint8_t *const stages[4] = {s0, s1, s2, s3};
+        auto piece = [&](int from, int p) {
+            const int at = (from - 1) * PRODUCTS + p;
+            return reinterpret_cast<float4 *>(stages[at / EACH_STAGE] + at % EACH_STAGE * PIECE + wave * 4096) + lane;
+        };
+#pragma unroll
+        for (int from = 1; from < KS; ++from)
+            if (team == (uint32_t)from)
+#pragma unroll
+                for (int p = 0; p < PRODUCTS; ++p)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float16v &x = acc[p / NF][p % NF];
+                        piece(from, p)[q * 64] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                    }
+        __syncthreads();
+        if (team == 0)
+#pragma unroll
+            for (int from = 1; from < KS; ++from)
+#pragma unroll
+                for (int p = 0; p < PRODUCTS; ++p)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float4 x = piece(from, p)[q * 64];
+                        float16v &to = acc[p / NF][p % NF];
+                        to[4 * q] += x.x;
+                        to[4 * q + 1] += x.y;
+                        to[4 * q + 2] += x.z;
+                        to[4 * q + 3] += x.w;
+                    }
+        __syncthreads();
+        if (team != 0) return;
+    }
     if constexpr (OUT == 2) c = static_cast<float *>(c) + (uint64_t)blockIdx.y * M * N;
     if (OUT == 1 && accumulate) {                            // sums are added in fp32, which the rows in LDS are not
 #pragma unroll
