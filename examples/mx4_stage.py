@@ -1,0 +1,101 @@
+"""One training step over a pipeline-stage boundary, both stages in one process: what the library's parts do next to each other.
+
+    python examples/mx4_stage.py [--batch 2] [--seq 512] [--hidden 1600] [--features 1600]
+
+Sending stage    r' = a r + g RMSNorm(b) w_post (the post half of the norms), encoded by the activation codec at 3.8 bits
+Receiving stage  decoded; h = RMSNorm(r') w_pre (the pre half); y = h W^T with h and W in mx4, rotated by blocks of 32
+Backward         gradients of h and W from that of y, both products in mx4; gradient of r' through the pre half; encoded by the 8-bit
+                 fixed-point codec; gradients of r, b, the gate and w_post through the post half at the sending stage
+Inference        one token: both halves in one launch whose h leaves in mx4, and the product
+
+Prints the bytes on the wire and every result's distance from the same step in 64 bits (2-norm of the difference over that of the result)."""
+import argparse
+import os
+import sys
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+import torch  # noqa: E402
+
+import paper_2506_01352_amd as tahq  # noqa: E402
+import workloads  # noqa: E402
+
+RESIDUAL_SCALE, EPS, GRADIENT_SCALE = 0.8125, 1e-6, 2.0 ** 20
+
+
+def rms_norm(v, w):
+    return v * torch.rsqrt(v.square().mean(-1, keepdim=True) + EPS) * w
+
+
+def off(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+def run(batch=2, seq=512, hidden=1600, features=1600, seed=7):
+    tokens = batch * seq
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)      # noqa: E731
+    _, raw = workloads.generate(3, batch=batch, seq=seq)
+    base = torch.from_numpy(raw.view("int16").reshape(tokens, -1)).cuda().view(torch.bfloat16)[:, :hidden]
+    r = torch.nn.functional.pad(base, (0, hidden - base.shape[1])).contiguous()
+    b, weight = normal(tokens, hidden), normal(features, hidden) * hidden ** -0.5
+    w_post, w_pre, gate = 1 + 0.1 * normal(hidden), 1 + 0.1 * normal(hidden), 0.5 + 0.1 * normal(batch, hidden)
+    grad_y = normal(tokens, features) * 1e-5
+
+    # ---- sending stage
+    norm = tahq.make_norm_config(tokens, hidden, tahq.BF16, gate_rows=seq, eps=EPS, residual_scale=RESIDUAL_SCALE)
+    post = tahq.BlockNorm(norm)
+    out, _ = post.forward(r, b, w_post, gate, None)
+    codec = tahq.Codec(tahq.make_config(batch, seq, hidden, 64, tahq.BF16, 3.8))
+    stream = codec.encode(out)
+
+    # ---- receiving stage
+    received = codec.decode().view(tokens, hidden)
+    plain = tahq.make_norm_config(tokens, hidden, tahq.BF16, eps=EPS)            # the pre half alone: nothing is scaled
+    pre = tahq.BlockNorm(plain)
+    _, h = pre.forward(received, None, None, None, w_pre)
+    layer = tahq.Mx4Linear(weight, tokens, transform=1, scale_rule=tahq.MX4_COVER, training=True)
+    y = layer.forward(h)
+
+    # ---- backward
+    grad_h, grad_w = layer.backward(grad_y)
+    back = pre.backward(None, grad_h, None, None, None, received, w_pre, pre.stats)
+    naive = tahq.make_naive_config(batch, seq, hidden, tahq.BF16, 8, GRADIENT_SCALE)
+    wire = torch.empty(tahq.tahq_naive_packed_size(naive), dtype=torch.uint8, device="cuda")
+    grad_out = torch.empty_like(out)
+    tahq.tahq_naive_encode(naive, back["grad_residual"], wire)
+    tahq.tahq_naive_decode(naive, wire, grad_out, tahq.BF16)
+    grads = post.backward(grad_out, None, b, w_post, gate, None, None, post.stats)
+
+    # ---- one token at inference: both halves, h in mx4
+    one = tahq.BlockNorm(tahq.make_norm_config(1, hidden, tahq.BF16, 1, EPS, RESIDUAL_SCALE, 0, 1, tahq.MX4_COVER), mx4=True)
+    single = tahq.Mx4Linear(weight, 1, transform=1, scale_rule=tahq.MX4_COVER)
+    _, h1 = one.forward(r[:1], b[:1], w_post, gate[:1], w_pre)
+    y1 = single.product(h1)
+    torch.cuda.synchronize()
+
+    # ---- the same in 64 bits, nothing quantized
+    t = {n: v.double().requires_grad_() for n, v in (("r", r), ("b", b), ("w_post", w_post), ("w_pre", w_pre), ("gate", gate), ("w", weight))}
+    true_out = RESIDUAL_SCALE * t["r"] + t["gate"].repeat_interleave(seq, 0) * rms_norm(t["b"], t["w_post"])
+    true_y = rms_norm(true_out, t["w_pre"]) @ t["w"].t()
+    true_y.backward(grad_y.double())
+    errors = {"r'": off(out, true_out.detach()), "r' received": off(received, true_out.detach()), "y": off(y, true_y.detach()),
+              "gradient of W": off(grad_w, t["w"].grad), "gradient of w_pre": off(back["grad_w_pre"], t["w_pre"].grad),
+              "gradient of r": off(grads["grad_residual"], t["r"].grad), "gradient of b": off(grads["grad_block"], t["b"].grad),
+              "gradient of the gate": off(grads["grad_gate"], t["gate"].grad), "gradient of w_post": off(grads["grad_w_post"], t["w_post"].grad),
+              "y of one token": off(y1, true_y.detach()[:1])}
+    return {"activation bytes": stream.numel(), "gradient bytes": wire.numel(), "bf16 bytes": 2 * tokens * hidden, "errors": errors}
+
+
+def main():
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    for name, value in (("batch", 2), ("seq", 512), ("hidden", 1600), ("features", 1600)):
+        ap.add_argument("--" + name, type=int, default=value)
+    got = run(**vars(ap.parse_args()))
+    print(f"on the wire: activations {got['activation bytes']} bytes, gradients {got['gradient bytes']}, in bf16 {got['bf16 bytes']} each")
+    for name, value in got["errors"].items():
+        print(f"{name:22s} off by {value:.4f}")
+
+
+if __name__ == "__main__":
+    main()
