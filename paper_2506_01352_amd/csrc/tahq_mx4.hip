@@ -47,7 +47,7 @@ void launch_quantize(const tahq_mx4_config *c, const void *d_in, uint8_t *p, uin
 tahq_status enqueue_quantize(const tahq_mx4_config *c, const void *d_in, void *d_packed, void *d_packed_t, Enqueue *q)
 {
     // along columns the last four units of 64 rows are filled up: their scale bytes are written, too
-    const uint64_t tiles_y = d_packed_t ? ceil_div(c->rows, 256) * 4 : ceil_div(c->rows, kQuantRows);
+    const uint64_t tiles_y = d_packed_t ? ceil_div(c->rows, 256) * (256 / kQuantRows) : ceil_div(c->rows, kQuantRows);
     const uint64_t tiles_x = ceil_div(c->cols, kQuantCols);
     if (tiles_x * tiles_y > kMaxGrid) return TAHQ_ERR_UNSUPPORTED;
     uint8_t *p = static_cast<uint8_t *>(d_packed), *pt = static_cast<uint8_t *>(d_packed_t);
