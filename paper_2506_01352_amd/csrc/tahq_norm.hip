@@ -128,7 +128,7 @@ tahq_status tahq_norm_forward(const tahq_norm_config *cfg, const void *d_residua
     Enqueue q{(hipStream_t)stream};
     with_kind(cfg, d_block, d_w_pre, [&](auto bf16, auto eights, auto post, auto pre) {
         q(k_norm_forward<bf16, eights, post, pre>, grid, dim3(64 * waves_of(cfg)), d_residual, d_block, d_w_post, d_block ? d_gate : nullptr, d_w_pre, d_residual_out, d_h,
-          static_cast<uint8_t *>(d_h_mx4), d_stats, s, cover, cfg->transform, rows_each);
+          static_cast<uint8_t *>(d_h_mx4), d_stats, s, cover, cfg->transform, rows_each, 256 / rows_each);
     });
     return q.result();
 }

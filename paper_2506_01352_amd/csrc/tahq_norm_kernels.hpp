@@ -95,7 +95,7 @@ template <bool BF16, bool EIGHTS, bool POST, bool PRE>
 __global__ __launch_bounds__(64 * kNormWaves)
 void k_norm_forward(const void *residual, const void *block, const void *w_post, const void *gate, const void *w_pre,
                     void *residual_out, void *h, uint8_t *h_mx4, float *stats, NormShape s, uint32_t cover, uint32_t rotate,
-                    uint32_t rows_each)
+                    uint32_t rows_each, uint32_t together)
 {
     __shared__ Places places;
     uint32_t turn = 0;
@@ -103,7 +103,12 @@ void k_norm_forward(const void *residual, const void *block, const void *w_post,
     const bool mine = c < C;
     const Mx4Layout L(s.rows, C);
     const uint32_t end = h_mx4 ? 32 * L.rb : s.rows;       // rows behind the last one fill up the packed matrix with zeros
-    const uint32_t first = blockIdx.x * rows_each, last = min(first + rows_each, end);
+    // The workgroups of 256 rows in another order, so that a unit's rows, whose codes lie side by side in a line, are on one XCD and merge in its
+    // L2: 8192 x 4096 bf16 to mx4 57 -> 52 us, to h and mx4 58 -> 51.  `together`, workgroups for 256 rows, is a power of two.
+    uint32_t place = blockIdx.x;
+    const uint32_t in = place & (together - 1);
+    if (h_mx4 && place - in + together <= gridDim.x) place += in % 8 * (together / 8) + in / 8 - in;
+    const uint32_t first = place * rows_each, last = min(first + rows_each, end);
     Eight<BF16> next_r = {}, next_b = {}, post = {}, pre = {}, next_k = ones<BF16>();
     auto ask = [&](uint32_t row) {
         if (row < s.rows && row < last && mine) {
