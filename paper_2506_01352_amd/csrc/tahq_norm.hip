@@ -83,6 +83,15 @@ BackwardPlan plan_backward(const tahq_norm_config *c)
     p.workspace = (uint64_t)p.workgroups * c->cols * 4 * (c->gate_rows ? 4 : 2);
     return p;
 }
+// Workgroups that take the rows of a span in turn: where the six tensors are larger than the last cache, as many as the gate allows.  In turn and
+// side by side: 32768 x 5120 bf16 378 us and 441, 16384 x 1600 57 and 67, 8192 x 4096 fp32 147 and 160 (but 2048 x 8192 with four rows of a gate 95
+// and 87); of 100 MB, 8192 x 1024 bf16, 20.6 and 18.9, with four rows of a gate 24.6 and 20.2.
+uint32_t backward_team(const tahq_norm_config *c, const BackwardPlan &p, uint32_t gate_rows)
+{
+    if ((uint64_t)c->rows * c->cols * (c->dtype == TAHQ_BF16 ? 12 : 24) < (256u << 20)) return 1;
+    const uint32_t most = gate_rows / p.rows_each;
+    return gate_rows == c->rows || most > p.workgroups ? p.workgroups : most ? most : 1;
+}
 
 }  // namespace
 
@@ -171,17 +180,18 @@ tahq_status tahq_norm_backward(const tahq_norm_config *cfg, const void *d_grad_r
     float *ws = static_cast<float *>(d_workspace);
     const NormPartials parts = {ws, ws + each, ws + 2 * each};
     const void *gate = d_block ? d_gate : nullptr;
+    const uint32_t team = backward_team(cfg, p, gate ? s.gate_rows : cfg->rows);
     Enqueue q{(hipStream_t)stream};
     with_kind(cfg, d_block, d_grad_h, [&](auto bf16, auto eights, auto post, auto pre) {
         q(k_norm_backward<bf16, eights, post, pre>, dim3(p.workgroups), dim3(64 * waves_of(cfg)), d_grad_residual_out, d_grad_h, d_block, d_w_post, gate, d_residual_out, d_w_pre,
-          d_stats, d_grad_residual, d_grad_block, d_grad_gate, parts, s, p.rows_each, cfg->accumulate);
+          d_stats, d_grad_residual, d_grad_block, d_grad_gate, parts, s, p.rows_each, team, cfg->accumulate);
     });
     const uint32_t groups = gate ? (cfg->rows + s.gate_rows - 1) / s.gate_rows : 0;
     if (d_block || d_grad_h) {
         const uint32_t slots = groups < 64 ? groups : 64;
         const uint32_t width = cfg->cols <= 2048 ? 16 : 64;
         q(k_norm_reduce, dim3((cfg->cols + width - 1) / width, 2 + slots), dim3(kReduceLanes), parts, d_grad_w_post, d_grad_w_pre, d_grad_gate, cfg->cols,
-          p.workgroups, cfg->rows, s.gate_rows, p.rows_each, groups, cfg->accumulate, width);
+          p.workgroups, cfg->rows, s.gate_rows, p.rows_each, team, groups, cfg->accumulate, width);
     }
     return q.result();
 }

@@ -171,9 +171,23 @@ void k_norm_forward(const void *residual, const void *block, const void *w_post,
     }
 }
 
+// Teams of workgroups share a span of rows, `rows_each` for each workgroup, and take them in turn, so that what all of them work on at a time lies
+// close together in memory.  Where there is a gate, a span is no longer than the rows that share one of its rows, so that it has rows of two of these
+// groups at most; in a team of one workgroup it may have any number of them.
+struct NormSpan {
+    uint32_t base, last, first, step;          // rows base .. last - 1; this workgroup's: first, first + step, .., one at least
+    __device__ __forceinline__ NormSpan(uint32_t wg, uint32_t workgroups, uint32_t team, uint32_t rows_each, uint32_t rows)
+    {
+        const uint32_t member = wg % team;
+        base = (wg - member) * rows_each;
+        step = min(team, workgroups - (wg - member));
+        last = min(base + step * rows_each, rows);
+        first = base + member;
+    }
+};
 // Column sums of a workgroup's rows, in the workspace: post [W][C], pre [W][C], gate [W][2][C].  A group of rows that share a row of
 // the gate and lie in one workgroup has its sum written at once; of a group that several workgroups have rows of, each keeps its part: in slot 0
-// if the workgroup's first row is in the group, in slot 1 otherwise.
+// if the first row of its span is in the group, in slot 1 otherwise.
 struct NormPartials {
     float *post, *pre, *gate;
 };
@@ -194,13 +208,14 @@ template <bool BF16, bool EIGHTS, bool POST, bool PRE>
 __global__ __launch_bounds__(64 * kNormWaves)
 void k_norm_backward(const void *grad_out, const void *grad_h, const void *block, const void *w_post, const void *gate,
                      const void *residual_out, const void *w_pre, const float *__restrict__ stats, void *grad_residual, void *grad_block,
-                     float *grad_gate, NormPartials parts, NormShape s, uint32_t rows_each, uint32_t accumulate)
+                     float *grad_gate, NormPartials parts, NormShape s, uint32_t rows_each, uint32_t team, uint32_t accumulate)
 {
     __shared__ Places places;
     uint32_t turn = 0;
     const uint32_t C = s.cols, c = 8 * threadIdx.x;
     const bool mine = c < C;
-    const uint32_t first = blockIdx.x * rows_each, last = min(first + rows_each, s.rows);
+    const NormSpan span(blockIdx.x, gridDim.x, team, rows_each, s.rows);
+    const uint32_t first = span.first, last = span.last, step = span.step;
     const float inv_c = 1.0f / (float)C;
     // the row that is worked on, loaded again as soon as it is used up
     Eight<BF16> go = {}, gh = {}, ro = {}, bl = {}, k = ones<BF16>(), wpost = {}, wpre = {};
@@ -232,7 +247,7 @@ void k_norm_backward(const void *grad_out, const void *grad_h, const void *block
     if (POST && gate) ask_gate(first);
     clear(places);
     float post[8] = {}, pre[8] = {}, gates[8] = {};
-    for (uint32_t row = first; row < last; ++row) {
+    for (uint32_t row = first; row < last; row += step) {
         stay_packed(wpost);
         stay_packed(wpre);
         stay_packed(k);
@@ -258,7 +273,7 @@ void k_norm_backward(const void *grad_out, const void *grad_h, const void *block
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = go[i];
         }
-        ask_pre(row + 1);
+        ask_pre(row + step);
         float d[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = s.alpha * g[i];
@@ -282,19 +297,27 @@ void k_norm_backward(const void *grad_out, const void *grad_h, const void *block
             const float mean = group_sum(sum, s.waves, places, turn) * inv_c;
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = rstd * __builtin_fmaf(-(bl[i] * rstd), mean, g[i]);
-            ask_post(row + 1);
+            ask_post(row + step);
             if (mine) keep<BF16, EIGHTS>(row_of<BF16>(grad_block, row, C), c, C, d);
-            if (gate && (row + 1 == last || row + 1 == stop)) {
+            if (gate && (row + step >= last || row + step >= stop)) {
                 const uint32_t begin = group * s.gate_rows;
-                const bool whole = begin >= first && stop <= last;
+                const bool whole = team == 1 && begin >= first && stop <= last;
                 float *to = whole ? grad_gate + (uint64_t)group * C
-                                  : parts.gate + ((uint64_t)blockIdx.x * 2 + (begin <= first ? 0 : 1)) * C;
+                                  : parts.gate + ((uint64_t)blockIdx.x * 2 + (begin <= span.base ? 0 : 1)) * C;
                 put<EIGHTS>(to, c, C, gates, whole && accumulate);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) gates[i] = 0.0f;
-                if (row + 1 < last) ask_gate(row + 1);
+                if (row + step < last) ask_gate(row + step);
             }
         }
+    }
+    if (POST && gate && team > 1) {
+        // groups of the span that none of this workgroup's rows are in: their parts are zeros, as `gates` is now
+        const uint32_t next = (uint32_t)min((uint64_t)(span.base / s.gate_rows + 1) * s.gate_rows, (uint64_t)s.rows);      // the second group's first row
+        if (first >= next)
+            put<EIGHTS>(parts.gate + (uint64_t)blockIdx.x * 2 * C, c, C, gates, false);
+        if (first < next && next < last && next + (step - (next - first) % step) % step >= last)
+            put<EIGHTS>(parts.gate + ((uint64_t)blockIdx.x * 2 + 1) * C, c, C, gates, false);
     }
     if constexpr (POST) put<EIGHTS>(parts.post + (uint64_t)blockIdx.x * C, c, C, post, false);
     if constexpr (PRE) put<EIGHTS>(parts.pre + (uint64_t)blockIdx.x * C, c, C, pre, false);
@@ -306,7 +329,7 @@ constexpr uint32_t kReduceLanes = 1024;
 
 __global__ __launch_bounds__(kReduceLanes)
 void k_norm_reduce(NormPartials parts, float *grad_w_post, float *grad_w_pre, float *grad_gate, uint32_t C, uint32_t W,
-                   uint32_t rows, uint32_t gate_rows, uint32_t rows_each, uint32_t groups, uint32_t accumulate, uint32_t width)
+                   uint32_t rows, uint32_t gate_rows, uint32_t rows_each, uint32_t team, uint32_t groups, uint32_t accumulate, uint32_t width)
 {
     __shared__ float sums[kReduceLanes];
     const uint32_t lane = threadIdx.x % width, run = threadIdx.x / width, runs = kReduceLanes / width, c = blockIdx.x * width + lane;
@@ -334,16 +357,19 @@ void k_norm_reduce(NormPartials parts, float *grad_w_post, float *grad_w_pre, fl
     } else if (blockIdx.y == 1) {
         if (grad_w_pre) total([&](uint32_t i) { return parts.pre + (uint64_t)i * C; }, W, grad_w_pre);
     } else {
-        // groups in more than one workgroup: each of them holds the last row in front of some workgroup's first
-        const uint32_t stride = gridDim.y - 2;
+        // Groups in more than one workgroup: each of them holds the last row in front of some workgroup's first.  Teams of several have at most as
+        // many groups as there are workgroups, and none is written yet.
+        const uint32_t stride = gridDim.y - 2, span = team * rows_each;
         const bool by_group = groups <= W;
         const uint32_t count = by_group ? groups : W - 1;
         for (uint32_t i = blockIdx.y - 2; i < count; i += stride) {
             const uint32_t group = by_group ? i : ((i + 1) * rows_each - 1) / gate_rows;
             const uint32_t begin = group * gate_rows, stop = (uint32_t)min((uint64_t)begin + gate_rows, (uint64_t)rows);
-            const uint32_t w0 = begin / rows_each, w1 = (stop - 1) / rows_each;
-            if (w0 == w1 || (!by_group && w0 != i)) continue;
-            total([&](uint32_t j) { return parts.gate + ((uint64_t)(w0 + j) * 2 + (j == 0 && begin > w0 * rows_each ? 1 : 0)) * C; },
+            const uint32_t w0 = begin / span * team, w1 = min((stop - 1) / span * team + team, W) - 1;
+            if (team == 1 && (w0 == w1 || (!by_group && w0 != i))) continue;
+            // slot 1 in those whose span begins before the group
+            const uint32_t late = begin > w0 * rows_each ? team : 0;
+            total([&](uint32_t j) { return parts.gate + ((uint64_t)(w0 + j) * 2 + (j < late ? 1 : 0)) * C; },
                   w1 - w0 + 1, grad_gate + (uint64_t)group * C);
         }
     }

@@ -194,3 +194,28 @@ def test_sums_over_tokens_are_the_same_every_time():
         got = {n: v.clone() for n, v in got.items()}
         assert first is None or all(torch.equal(first[n], got[n]) for n in got)
         first = got
+
+
+@pytest.mark.parametrize("rows, cols, gate_rows", [(5000, 64, g) for g in (2, 3, 4, 9, 500, 4999)]
+                         + [(45000, 250, g) for g in (21, 45, 50, 1000, 20011, 44999)] + [(2060, 5500, g) for g in (9, 20, 700)])
+def test_gradients_summed_over_groups_of_rows(rows, cols, gate_rows):
+    """Groups of rows shorter and longer than a workgroup's share, and such that few rows of the next one are in it: as test_backward's sums."""
+    t = _tensors(rows, cols, gate_rows, "both", "f32")
+    n = {k: _np(v) for k, v in t.items()}
+    out, _, rb, rr = norm64.forward(n["residual"], n["block"], n["w_post"], n["gate"], n["w_pre"], gate_rows, EPS, ALPHA)
+    t["residual_out"] = torch.from_numpy(out).float()
+    stats = torch.from_numpy(np.stack((rb, rr))).float()
+    want = norm64.backward(n["grad_residual_out"], n["grad_h"], n["block"], n["w_post"], n["gate"], _np(t["residual_out"]), n["w_pre"],
+                           *stats.double().numpy(), gate_rows, ALPHA)
+    d = _cuda(t)
+    cfg = tahq.make_norm_config(rows, cols, tahq.F32, gate_rows, EPS, ALPHA)
+    gr, gb = (torch.full((rows, cols), 7.0, device="cuda") for _ in range(2))
+    gw, gp, gg = (torch.full_like(v, 0.5) for v in (d["w_post"], d["w_pre"], d["gate"]))
+    ws = torch.full((tahq.tahq_norm_workspace_size(cfg),), 0xFF, dtype=torch.uint8, device="cuda")       # NaN in what is not written
+    tahq.tahq_norm_backward(cfg, d["grad_residual_out"], d["grad_h"], d["block"], d["w_post"], d["gate"], d["residual_out"], d["w_pre"],
+                            stats.cuda(), gr, gb, gw, gg, gp, ws)
+    torch.cuda.synchronize()
+    for name, g in {"grad_residual": gr, "grad_block": gb, "grad_gate": gg, "grad_w_post": gw, "grad_w_pre": gp}.items():
+        w, size, small = want[name], want[name + "_size"], name in ("grad_residual", "grad_block")
+        off = (128 + (0 if small else rows)) * UNIT * size + (HALF["f32"] * np.abs(w) if small else 0) + 1e-38
+        assert (np.abs(_np(g) - w) <= off).all(), name
