@@ -58,10 +58,11 @@ uint32_t forward_rows(const tahq_norm_config *c, uint32_t rows)
     return rows >= 4096 ? 2 : 1;
 }
 
-// Backward: the workgroups that share the rows.  A compute unit holds sixteen wavefronts of up to 128 registers, so `most` workgroups at once; as many of
-// those as leave no compute unit with more rows than another need have (2331 rows: 10 with one or two workgroups each, 12 with three or four).  Two
-// rounds of workgroups of unlike length cost more than their column sums (teams of one): 32768 x 5120, ten wavefronts: 256 workgroups 455 us, 409 534, 512
-// 458; 32768 x 1024, two: 512 152, 1024 111, 2048 101.
+// Backward: the workgroups that share the rows.  A compute unit holds sixteen wavefronts of up to 128 registers, so `most` workgroups at once; more than one
+// round of workgroups of unlike length costs more than it gives (rows side by side: 32768 x 5120, ten wavefronts: 256 workgroups 455 us, 409 534, 512
+// 458; 32768 x 1024, two: 512 152, 1024 111, 2048 101).  What counts below that, in rows of a compute unit: the rows of the unit with most of them, a third of a
+// workgroup's rows, which nobody hides, and a row for every 256 workgroups, whose column sums are added afterwards.  Both kernels, fp32 with one row of
+// a gate, by a workgroup's rows: 777 x 1600 one 20.7 us, four 15.3; 4096 x 1600 four 35.6, eight 31.2, sixteen 33.3; 2331 x 1600 five 22.3, ten 23.7.
 struct BackwardPlan {
     uint32_t rows_each, workgroups;
     uint64_t workspace;
@@ -70,12 +71,13 @@ BackwardPlan plan_backward(const tahq_norm_config *c)
 {
     BackwardPlan p;
     const uint32_t most = waves_of(c) > 1 ? 16 / waves_of(c) : 8;          // of one wavefront eight: 32768 x 512, 2048 in all 47 us, 4096 71
-    uint64_t least = ~0ull;
+    float least = 0.0f;
     p.rows_each = 0;
     for (uint32_t k = most; k > 0; --k) {
-        const uint32_t each = (uint32_t)(((uint64_t)c->rows + 256 * k - 1) / (256 * k));
-        if ((uint64_t)k * each < least) {
-            least = (uint64_t)k * each;
+        const uint32_t each = (uint32_t)(((uint64_t)c->rows + 256 * k - 1) / (256 * k)), workgroups = (uint32_t)(((uint64_t)c->rows + each - 1) / each);
+        const float cost = (float)each * ((float)((workgroups + 255) / 256) + 0.3f) + (float)workgroups / 256;
+        if (!p.rows_each || cost < least) {
+            least = cost;
             p.rows_each = each;
         }
     }
