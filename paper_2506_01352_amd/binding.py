@@ -686,18 +686,20 @@ class BlockNorm:
         self._need, self._device, self.workspace = need, device, None
         self._kind, self._sizes = kind, (cfg.rows * cfg.cols, cfg.cols, _gate_groups(cfg) * cfg.cols)
         h = self.h.data_ptr()
-        self._own = (self.residual_out.data_ptr(), None if mx4 else h, h if mx4 else None, self.h.numel() if mx4 else 0)
+        out, stats, self._cfg = self.residual_out.data_ptr(), self.stats.data_ptr(), C.byref(cfg)
+        self._own = (out, None if mx4 else h, h if mx4 else None, self.h.numel() if mx4 else 0, stats)
+        self._own_post = (out, None, None, 0, stats)
 
     def forward(self, residual, block, w_post, gate, w_pre, stream=None):
         """(r', h); block, w_post and gate may be None, or w_pre."""
         where, kind, (n, cols, gates) = "BlockNorm.forward", self._kind, self._sizes
         rc = _lib.tahq_norm_forward(
-            C.byref(self.cfg), _input_of(where, "residual", residual, n, kind),
+            self._cfg, _input_of(where, "residual", residual, n, kind),
             None if block is None else _input_of(where, "block", block, n, kind),
             None if w_post is None else _input_of(where, "w_post", w_post, cols, kind),
             None if gate is None else _input_of(where, "gate", gate, gates, kind),
             None if w_pre is None else _input_of(where, "w_pre", w_pre, cols, kind),
-            *(self._own if w_pre is not None else (self._own[0], None, None, 0)), self.stats.data_ptr(), _stream_handle(stream))
+            *(self._own if w_pre is not None else self._own_post), _stream_handle(stream))
         if rc != 0:
             raise TahqError(rc, "tahq_norm_forward")
         return self.residual_out, None if w_pre is None else self.h
@@ -723,7 +725,7 @@ class BlockNorm:
             return None if t is None else _input_of(where, name, t, elements, dtype)
 
         rc = _lib.tahq_norm_backward(
-            C.byref(self.cfg), at("grad_residual_out", grad_residual_out, n), at("grad_h", grad_h, n), at("block", block, n),
+            self._cfg, at("grad_residual_out", grad_residual_out, n), at("grad_h", grad_h, n), at("block", block, n),
             at("w_post", w_post, cols), at("gate", gate, gates), at("residual_out", residual_out, n), at("w_pre", w_pre, cols),
             at("stats", stats, 2 * self.cfg.rows, torch.float32), *(None if t is None else t.data_ptr() for t in got.values()),
             self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))
