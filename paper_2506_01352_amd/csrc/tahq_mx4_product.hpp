@@ -102,7 +102,7 @@ __device__ __forceinline__ void store16(void *c, uint64_t at, uint32_t valid, ui
 // unit: one wavefront to a vector unit waits more than it multiplies.
 //   OUT: 0 fp32, 1 bf16, 2 fp32 parts of a sum over k in gridDim.y runs of `run` groups of 256 columns.
 //   Measured, 256 x 256 tiles: 8192 x 8192 x 8192 252 to 278 us, 4.2 PFLOP/s of the 8.7 that the instruction alone reaches; 407 k cycles, in 262 k of
-// which the matrix cores work.  The clock gives way to power: matrices of zeros take the same cycles at 1.5 times the clock (6.4 PFLOP/s).
+// which the matrix cores work.  The clock gives way to power: matrices of zeros reach 6.4 PFLOP/s.
 // Small products wait: 2048 x 1600 x 1600 8.0 us (1.3 PFLOP/s), launch, first loads and last stores being about 4 of them.
 template <int WM, int WN, int MF, int NF, int NB, int KS, int PER_CU, int OUT>
 __global__ __launch_bounds__(64 * WM * WN * KS, PER_CU * KS)
