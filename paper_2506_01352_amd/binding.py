@@ -407,12 +407,14 @@ def _strided_elements(rows, cols, ld):
     return (rows - 1) * (ld or cols) + cols if rows and cols else 0
 
 
-def _rows_ptr(t, ld):
-    """Device address of a row-major tensor whose rows may lie `ld` elements apart: contiguous, or a two-dimensional view that says so."""
+def _rows_ptr(t, cols, ld):
+    """Device address of a row-major tensor whose rows may lie `ld` elements apart (0: `cols`): contiguous, or a two-dimensional view that
+    says so.  A broadcast view, whose rows are one row, is neither."""
     if t is None or isinstance(t, int):
         return t
     if not t.is_contiguous():
-        assert t.is_cuda and t.dim() == 2 and t.stride(1) == 1 and t.stride(0) == ld, "device tensor, rows of unit stride, ld apart"
+        apart = t.is_cuda and t.dim() == 2 and t.stride(1) == 1 and t.stride(0) == (ld or cols)
+        assert apart, "device tensor, rows of unit stride, ld apart"
         return t.data_ptr()
     return _dev_ptr(t)
 
@@ -431,7 +433,7 @@ def _check_rows(where, name, t, rows, cols, ld, dtype):
 def tahq_mx4_quantize(cfg, d_in, d_packed=None, d_packed_t=None, stream=None):
     """[rows, cols] -> packed along rows (d_packed) and / or along columns (d_packed_t), read once."""
     _check_rows("tahq_mx4_quantize", "d_in", d_in, cfg.rows, cfg.cols, cfg.ld, cfg.dtype)
-    rc = (_lib or _load()).tahq_mx4_quantize(C.byref(cfg), _rows_ptr(d_in, cfg.ld), _dev_ptr(d_packed), _nbytes(d_packed),
+    rc = (_lib or _load()).tahq_mx4_quantize(C.byref(cfg), _rows_ptr(d_in, cfg.cols, cfg.ld), _dev_ptr(d_packed), _nbytes(d_packed),
                                              _dev_ptr(d_packed_t), _nbytes(d_packed_t), _stream_handle(stream))
     if rc != 0:
         raise TahqError(rc, "tahq_mx4_quantize")
@@ -439,7 +441,7 @@ def tahq_mx4_quantize(cfg, d_in, d_packed=None, d_packed_t=None, stream=None):
 
 def tahq_mx4_dequantize(cfg, d_packed, d_out, stream=None):
     _check_rows("tahq_mx4_dequantize", "d_out", d_out, cfg.rows, cfg.cols, cfg.ld, cfg.dtype)
-    rc = (_lib or _load()).tahq_mx4_dequantize(C.byref(cfg), _dev_ptr(d_packed), _nbytes(d_packed), _rows_ptr(d_out, cfg.ld),
+    rc = (_lib or _load()).tahq_mx4_dequantize(C.byref(cfg), _dev_ptr(d_packed), _nbytes(d_packed), _rows_ptr(d_out, cfg.cols, cfg.ld),
                                                _stream_handle(stream))
     if rc != 0:
         raise TahqError(rc, "tahq_mx4_dequantize")
@@ -464,7 +466,7 @@ def tahq_mx4_matmul_workspace_size(cfg):
 def tahq_mx4_matmul(cfg, d_a, d_b, d_c, d_workspace=None, stream=None):
     """C[m, n] (+)= A[m, k] B[n, k]^T of packed matrices."""
     _check_rows("tahq_mx4_matmul", "d_c", d_c, cfg.m, cfg.n, cfg.ldc, cfg.out_dtype)
-    rc = (_lib or _load()).tahq_mx4_matmul(C.byref(cfg), _dev_ptr(d_a), _nbytes(d_a), _dev_ptr(d_b), _nbytes(d_b), _rows_ptr(d_c, cfg.ldc),
+    rc = (_lib or _load()).tahq_mx4_matmul(C.byref(cfg), _dev_ptr(d_a), _nbytes(d_a), _dev_ptr(d_b), _nbytes(d_b), _rows_ptr(d_c, cfg.n, cfg.ldc),
                                            _dev_ptr(d_workspace), _nbytes(d_workspace), _stream_handle(stream))
     if rc != 0:
         raise TahqError(rc, "tahq_mx4_matmul")
@@ -478,8 +480,8 @@ def tahq_mx4_linear(x, cfg, d_x, d_b, d_y, d_workspace, stream=None):
     """y[m, n] (+)= quantized(x)[m, k] B[n, k]^T, x in fp32 or bf16."""
     _check_rows("tahq_mx4_linear", "d_x", d_x, x.rows, x.cols, x.ld, x.dtype)
     _check_rows("tahq_mx4_linear", "d_y", d_y, cfg.m, cfg.n, cfg.ldc, cfg.out_dtype)
-    rc = (_lib or _load()).tahq_mx4_linear(C.byref(x), C.byref(cfg), _rows_ptr(d_x, x.ld), _dev_ptr(d_b), _nbytes(d_b),
-                                           _rows_ptr(d_y, cfg.ldc), _dev_ptr(d_workspace), _nbytes(d_workspace), _stream_handle(stream))
+    rc = (_lib or _load()).tahq_mx4_linear(C.byref(x), C.byref(cfg), _rows_ptr(d_x, x.cols, x.ld), _dev_ptr(d_b), _nbytes(d_b),
+                                           _rows_ptr(d_y, cfg.n, cfg.ldc), _dev_ptr(d_workspace), _nbytes(d_workspace), _stream_handle(stream))
     if rc != 0:
         raise TahqError(rc, "tahq_mx4_linear")
 

@@ -1,0 +1,52 @@
+"""What the binding and its classes hand to the library, on the CPU: tensors stand in for device memory, and calls that would enqueue
+work are written down instead."""
+import pytest
+import torch
+
+import paper_2506_01352_amd as tahq
+from paper_2506_01352_amd import binding
+
+
+class Recorder:
+    """The library, with calls that take a stream recorded: (name, arguments)."""
+
+    def __init__(self, lib):
+        self.lib, self.calls = lib, []
+
+    def __getattr__(self, name):
+        if name.endswith(("_default", "_size", "_string")):
+            return getattr(self.lib, name)
+
+        def call(*arguments):
+            self.calls.append((name, arguments))
+            return 0
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    recorder = Recorder(binding._load())
+    monkeypatch.setattr(binding, "_lib", recorder)
+    monkeypatch.setattr(binding, "_load", lambda: recorder)
+    monkeypatch.setattr(binding, "_stream_handle", lambda stream: stream)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+    return recorder
+
+
+@pytest.mark.parametrize("ld", (0, 64))
+def test_a_row_that_stands_for_many_is_no_matrix(library, ld):
+    """A broadcast view has the rows' shape and none of their memory, whether the configuration names its row stride or leaves it at 0 = cols."""
+    wide = torch.zeros(1, 64, dtype=torch.bfloat16).expand(40, 64)
+    out = torch.zeros(40, 64, dtype=torch.bfloat16)
+    packed, ws = (torch.zeros(1 << 16, dtype=torch.uint8) for _ in range(2))
+    cfg, product = tahq.make_mx4_config(40, 64, tahq.BF16, ld), tahq.make_mx4_matmul_config(40, 64, 64, tahq.BF16, ld)
+    for call in (lambda: tahq.tahq_mx4_quantize(cfg, wide, packed), lambda: tahq.tahq_mx4_dequantize(cfg, packed, wide),
+                 lambda: tahq.tahq_mx4_matmul(product, packed, packed, wide, ws),
+                 lambda: tahq.tahq_mx4_linear(cfg, product, wide, packed, out, ws),
+                 lambda: tahq.tahq_mx4_linear(cfg, product, out, packed, wide, ws)):
+        with pytest.raises((AssertionError, ValueError)):
+            call()
+    assert not library.calls
+    tahq.tahq_mx4_quantize(cfg, out, packed)
+    tahq.tahq_mx4_quantize(tahq.make_mx4_config(40, 32, tahq.BF16, 64), out[:, :32], packed)
+    assert [name for name, _ in library.calls] == ["tahq_mx4_quantize"] * 2
