@@ -68,7 +68,7 @@ def run(batch=2, seq=512, hidden=1600, features=1600, seed=7):
     grads = post.backward(grad_out, None, b, w_post, gate, None, None, post.stats)
 
     # ---- one token at inference: both halves, h in mx4
-    one = tahq.BlockNorm(tahq.make_norm_config(1, hidden, tahq.BF16, 1, EPS, RESIDUAL_SCALE, 0, 1, tahq.MX4_COVER), mx4=True)
+    one = tahq.BlockNorm(tahq.make_norm_config(1, hidden, tahq.BF16, 1, EPS, RESIDUAL_SCALE, 0, 1, tahq.MX4_COVER), mx4=True, training=False)
     single = tahq.Mx4Linear(weight, 1, transform=1, scale_rule=tahq.MX4_COVER)
     _, h1 = one.forward(r[:1], b[:1], w_post, gate[:1], w_pre)
     y1 = single.product(h1)

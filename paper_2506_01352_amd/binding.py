@@ -673,9 +673,11 @@ def tahq_norm_backward(cfg, d_grad_residual_out, d_grad_h, d_block, d_w_post, d_
 
 
 class BlockNorm:
-    """Buffers of one configuration's norms.  mx4: h leaves as a packed matrix; otherwise in the configuration's dtype."""
+    """Buffers of one configuration's norms.  mx4: h leaves as a packed matrix; otherwise in the configuration's dtype.  training: with the
+    buffers of the backward pass.  All are made, and gradients that are added to cleared, on torch's current stream: a call on another
+    stream comes after that stream has waited for it."""
 
-    def __init__(self, cfg, mx4=False, device="cuda:0"):
+    def __init__(self, cfg, mx4=False, device="cuda:0", training=True):
         import torch
         need = tahq_norm_workspace_size(cfg)
         if need == 0:
@@ -685,7 +687,12 @@ class BlockNorm:
         self.residual_out = torch.empty(shape, dtype=kind, device=device)
         self.h = _bytes_on(device, tahq_mx4_packed_size(*shape)) if mx4 else torch.empty(shape, dtype=kind, device=device)
         self.stats = torch.empty(2, cfg.rows, dtype=torch.float32, device=device)
-        self._need, self._device, self.workspace = need, device, None
+        self.training = training
+        if training:
+            self.workspace = _bytes_on(device, need)
+            self.grad_residual, self.grad_block = (torch.empty(shape, dtype=kind, device=device) for _ in range(2))
+            self.grad_w_post, self.grad_w_pre = (torch.zeros(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
+            self.grad_gate = torch.zeros(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
         self._kind, self._sizes = kind, (cfg.rows * cfg.cols, cfg.cols, _gate_groups(cfg) * cfg.cols)
         h = self.h.data_ptr()
         out, stats, self._cfg = self.residual_out.data_ptr(), self.stats.data_ptr(), C.byref(cfg)
@@ -708,13 +715,8 @@ class BlockNorm:
 
     def backward(self, grad_residual_out, grad_h, block, w_post, gate, residual_out, w_pre, stats, stream=None):
         """Gradients of residual, block, w_post, gate and w_pre by name; None for what there is not."""
-        import torch
-        if self.workspace is None:
-            cfg, device = self.cfg, self._device
-            self.workspace = _bytes_on(device, self._need)
-            self.grad_residual, self.grad_block = (torch.empty_like(self.residual_out) for _ in range(2))
-            self.grad_w_post, self.grad_w_pre = (torch.zeros(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
-            self.grad_gate = torch.zeros(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
+        if not self.training:
+            raise ValueError("BlockNorm.backward: the norm was not made with training=True")
         # in the order of the call's arguments
         got = {"grad_residual": self.grad_residual, "grad_block": None, "grad_w_post": None, "grad_gate": None, "grad_w_pre": None}
         if block is not None:
@@ -729,7 +731,7 @@ class BlockNorm:
         rc = _lib.tahq_norm_backward(
             self._cfg, at("grad_residual_out", grad_residual_out, n), at("grad_h", grad_h, n), at("block", block, n),
             at("w_post", w_post, cols), at("gate", gate, gates), at("residual_out", residual_out, n), at("w_pre", w_pre, cols),
-            at("stats", stats, 2 * self.cfg.rows, torch.float32), *(None if t is None else t.data_ptr() for t in got.values()),
+            at("stats", stats, 2 * self.cfg.rows, self.stats.dtype), *(None if t is None else t.data_ptr() for t in got.values()),
             self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))
         if rc != 0:
             raise TahqError(rc, "tahq_norm_backward")

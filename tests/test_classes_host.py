@@ -50,3 +50,37 @@ def test_a_row_that_stands_for_many_is_no_matrix(library, ld):
     tahq.tahq_mx4_quantize(cfg, out, packed)
     tahq.tahq_mx4_quantize(tahq.make_mx4_config(40, 32, tahq.BF16, 64), out[:, :32], packed)
     assert [name for name, _ in library.calls] == ["tahq_mx4_quantize"] * 2
+
+
+def _norm(mx4=False, accumulate=0, **more):
+    return tahq.BlockNorm(tahq.make_norm_config(6, 64, tahq.BF16, 2, accumulate=accumulate), mx4, device="cpu", **more)
+
+
+def _norm_inputs():
+    t = {n: torch.zeros(6, 64, dtype=torch.bfloat16) for n in ("grad_residual_out", "grad_h", "block", "residual_out")}
+    t.update({n: torch.zeros(64, dtype=torch.bfloat16) for n in ("w_post", "w_pre")})
+    return {**t, "gate": torch.zeros(3, 64, dtype=torch.bfloat16), "stats": torch.zeros(2, 6)}
+
+
+@pytest.mark.parametrize("accumulate", (0, 1))
+def test_gradients_of_norms_start_at_zero_before_any_call(library, monkeypatch, accumulate):
+    """The buffers are made and cleared on torch's current stream, which a call's own stream does not wait for: not within the call."""
+    norm = _norm(accumulate=accumulate)
+    inputs = _norm_inputs()
+
+    def none(*a, **k):
+        raise AssertionError("memory is allocated or filled within the call")
+
+    with monkeypatch.context() as m:
+        for name in ("empty", "zeros", "empty_like", "zeros_like", "full"):
+            m.setattr(torch, name, none)
+        got = norm.backward(**inputs, stream=77)
+    assert [(name, a[-1]) for name, a in library.calls] == [("tahq_norm_backward", 77)]
+    assert all((got[n] == 0).all() and got[n].dtype is torch.float32 for n in ("grad_w_post", "grad_w_pre", "grad_gate"))
+
+
+def test_norms_without_a_backward_pass_keep_no_buffers_for_it(library):
+    norm = _norm(training=False)
+    with pytest.raises(ValueError, match="training"):
+        norm.backward(**_norm_inputs())
+    assert not library.calls and not hasattr(norm, "grad_block")

@@ -1,0 +1,39 @@
+"""The classes' state: streams, what is kept from the forward pass for the backward one, refusals (GPU)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_01352_amd as tahq
+from oracle import norm64
+
+pytestmark = pytest.mark.gpu
+
+UNIT = 2.0 ** -24           # half a unit in the last place of an fp32 number
+
+
+def _np(v):
+    return v.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("accumulate", (0, 1))
+def test_norms_on_a_stream_of_their_own_from_the_first_call_on(accumulate):
+    """Forward and twice backward on a side stream; within 128 roundings of the terms' magnitudes, and one for every row of a sum."""
+    rows, cols, gate_rows, eps, alpha = 3000, 1600, 700, 1e-6, 0.8125
+    g = torch.Generator().manual_seed(6)
+    t = {n: torch.randn(rows, cols, generator=g) for n in ("residual", "block", "grad_out", "grad_h")}
+    t.update(w_post=1 + 0.2 * torch.randn(cols, generator=g), w_pre=1 + 0.2 * torch.randn(cols, generator=g), gate=torch.randn(5, cols, generator=g))
+    d = {n: v.cuda() for n, v in t.items()}
+    norm = tahq.BlockNorm(tahq.make_norm_config(rows, cols, tahq.F32, gate_rows, eps, alpha, accumulate))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    out, _ = norm.forward(d["residual"], d["block"], d["w_post"], d["gate"], d["w_pre"], stream=side)
+    for _ in range(2):
+        got = norm.backward(d["grad_out"], d["grad_h"], d["block"], d["w_post"], d["gate"], out, d["w_pre"], norm.stats, stream=side)
+    side.synchronize()
+    n = {k: v.double().numpy() for k, v in t.items()}
+    want = norm64.backward(n["grad_out"], n["grad_h"], n["block"], n["w_post"], n["gate"], _np(out), n["w_pre"], *_np(norm.stats), gate_rows, alpha)
+    for name in ("grad_residual", "grad_block", "grad_w_post", "grad_gate", "grad_w_pre"):
+        sums = name not in ("grad_residual", "grad_block")
+        times = 1 + accumulate if sums else 1
+        off = (128 + (rows if sums else 0)) * UNIT * times * want[name + "_size"] + 1e-38
+        assert (np.abs(_np(got[name]) - times * want[name]) <= off).all(), name
