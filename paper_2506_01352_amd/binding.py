@@ -564,7 +564,8 @@ class Mx4Linear:
             need = max([need] + [tahq_mx4_matmul_workspace_size(c) for c in (self._forward, self._dx, self._dw)])
         self.workspace = _bytes_on(device, need)
         self._kind = weight.dtype
-        self._kept = {k: getattr(self, k) for k in ("dy", "dy_t", "weight_t", "x_t", "workspace")} if training else {}
+        self._kept = {k: getattr(self, k) for k in ("dy", "dy_t", "weight_t", "workspace")} if training else {}
+        self._forward_x_t = None                  # what the last forward pass was of, along its tokens
         self._linear = (C.byref(self._x), C.byref(self._forward))
         self._own = (self.weight.data_ptr(), self.weight.numel(), self.y.data_ptr(), self.workspace.data_ptr(), self.workspace.numel())
         self.update(weight)
@@ -581,20 +582,27 @@ class Mx4Linear:
             if rc != 0:
                 raise TahqError(rc, "tahq_mx4_linear")
             return self.y
+        self._forward_x_t = None
         tahq_mx4_quantize(self._x, x, self.x, self.x_t, stream)
-        return self.product(self.x, stream)
+        return self.product(self.x, stream, self.x_t)
 
-    def product(self, x_packed, stream=None):
-        """y of an x that is packed already, e.g. by BlockNorm."""
+    def product(self, x_packed, stream=None, x_packed_t=None):
+        """y of an x that is packed already, e.g. by BlockNorm.  The backward pass reads the same x packed along its tokens: x_packed_t, which
+        stays the caller's; without it there is no backward pass of this y."""
+        self._forward_x_t = None
         tahq_mx4_matmul(self._forward, x_packed, self.weight, self.y, self.workspace, stream)
+        self._forward_x_t = x_packed_t
         return self.y
 
     def backward(self, grad_y, stream=None):
         """(gradient of x, gradient of W); the latter is added to with accumulate = 1."""
         if not self.training:
             raise ValueError("Mx4Linear.backward: the layer was not made with training=True")
+        if self._forward_x_t is None:
+            raise ValueError("Mx4Linear.backward: there is no x along its tokens: no forward pass, or a product without x_packed_t")
         d_dy = _input_of("Mx4Linear.backward", "grad_y", grad_y, self._dy.rows * self._dy.cols, self._kind)
-        at, size = {k: t.data_ptr() for k, t in self._kept.items()}, {k: t.numel() for k, t in self._kept.items()}
+        kept = {"x_t": self._forward_x_t, **self._kept}
+        at, size = {k: _dev_ptr(t) for k, t in kept.items()}, {k: _nbytes(t) for k, t in kept.items()}
         handle = _stream_handle(stream)
         for name, call in (
                 ("tahq_mx4_quantize", (C.byref(self._dy), d_dy, at["dy"], size["dy"], at["dy_t"], size["dy_t"])),

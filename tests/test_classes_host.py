@@ -84,3 +84,38 @@ def test_norms_without_a_backward_pass_keep_no_buffers_for_it(library):
     with pytest.raises(ValueError, match="training"):
         norm.backward(**_norm_inputs())
     assert not library.calls and not hasattr(norm, "grad_block")
+
+
+def _layer(tokens=40, n=96, k=64, dtype=torch.bfloat16, **more):
+    return tahq.Mx4Linear(torch.zeros(n, k, dtype=dtype), tokens, **more)
+
+
+def _x_of_weight_gradient(library):
+    """Address of the matrix that the last product, the weight's gradient, took for x."""
+    name, a = library.calls[-1]
+    assert name == "tahq_mx4_matmul"
+    return a[3]
+
+
+def test_the_weights_gradient_is_of_the_x_that_the_layer_was_last_given(library):
+    layer = _layer(training=True)
+    x, dy = torch.zeros(40, 64, dtype=torch.bfloat16), torch.zeros(40, 96, dtype=torch.bfloat16)
+    h, h_t = (torch.zeros(tahq.tahq_mx4_packed_size(*s), dtype=torch.uint8) for s in ((40, 64), (64, 40)))
+    before = len(library.calls)
+    with pytest.raises(ValueError, match="no x"):
+        layer.backward(dy)                                           # nothing went forward
+    layer.forward(x)
+    for _ in range(2):
+        layer.backward(dy)
+        assert _x_of_weight_gradient(library) == layer.x_t.data_ptr()
+    layer.product(h)                                                 # of this x the layer has nothing along tokens
+    enqueued = len(library.calls)
+    with pytest.raises(ValueError, match="no x"):
+        layer.backward(dy)
+    assert len(library.calls) == enqueued > before
+    layer.product(h, x_packed_t=h_t)
+    layer.backward(dy)
+    assert _x_of_weight_gradient(library) == h_t.data_ptr()
+    layer.forward(x)
+    layer.backward(dy)
+    assert _x_of_weight_gradient(library) == layer.x_t.data_ptr()

@@ -37,3 +37,18 @@ def test_norms_on_a_stream_of_their_own_from_the_first_call_on(accumulate):
         times = 1 + accumulate if sums else 1
         off = (128 + (rows if sums else 0)) * UNIT * times * want[name + "_size"] + 1e-38
         assert (np.abs(_np(got[name]) - times * want[name]) <= off).all(), name
+
+
+def test_training_through_an_h_that_is_packed_already():
+    """x given along channels and along tokens: the same bits as of a forward pass that packs it, whatever x came before."""
+    tokens, n, k = 200, 300, 1600
+    w, x, other, dy = (torch.randn(*s, device="cuda").to(torch.bfloat16) for s in ((n, k), (tokens, k), (tokens, k), (tokens, n)))
+    layer = tahq.Mx4Linear(w, tokens, transform=1, scale_rule=tahq.MX4_COVER, training=True)
+    y = layer.forward(x).clone()
+    dx, dw = (t.clone() for t in layer.backward(dy))
+    packed = tahq.Mx4Tensor(tahq.make_mx4_config(tokens, k, tahq.BF16, 0, 1, tahq.MX4_COVER), transposed=True)
+    packed.quantize(x)
+    layer.forward(other)
+    assert torch.equal(layer.product(packed.packed, x_packed_t=packed.packed_t), y)
+    got = layer.backward(dy)
+    assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
