@@ -540,6 +540,8 @@ class Mx4Linear:
 
     def __init__(self, weight, tokens, transform=0, scale_rule=MX4_FLOOR, training=False, accumulate=0):
         import torch
+        if weight.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"Mx4Linear: the weight is a tensor of {weight.dtype}, float32 or bfloat16 is needed")
         n, k = weight.shape
         device, dtype = weight.device, F32 if weight.dtype == torch.float32 else BF16
         self.training = training
@@ -572,12 +574,13 @@ class Mx4Linear:
 
     def update(self, weight, stream=None):
         """Pack W, e.g. after an optimizer's step."""
+        _input_of("Mx4Linear.update", "weight", weight, self._w.rows * self._w.cols, self._kind)
         tahq_mx4_quantize(self._w, weight, self.weight, self.weight_t, stream)
 
     def forward(self, x, stream=None):
         """y; in training x is kept along its tokens for the weight's gradient."""
+        d_x = _input_of("Mx4Linear.forward", "x", x, self._x.rows * self._x.cols, self._kind)
         if not self.training:
-            d_x = _input_of("Mx4Linear.forward", "x", x, self._x.rows * self._x.cols, self._kind)
             rc = _lib.tahq_mx4_linear(*self._linear, d_x, *self._own, _stream_handle(stream))
             if rc != 0:
                 raise TahqError(rc, "tahq_mx4_linear")

@@ -119,3 +119,20 @@ def test_the_weights_gradient_is_of_the_x_that_the_layer_was_last_given(library)
     layer.forward(x)
     layer.backward(dy)
     assert _x_of_weight_gradient(library) == layer.x_t.data_ptr()
+
+
+@pytest.mark.parametrize("dtype", (torch.float16, torch.float64, torch.int16, torch.uint8))
+def test_layers_take_no_types_but_fp32_and_bf16(library, dtype):
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        tahq.Mx4Linear(torch.zeros(96, 64, dtype=dtype), 40)
+    for training in (False, True):
+        layer = _layer(training=training)
+        enqueued = len(library.calls)
+        with pytest.raises(ValueError, match="bfloat16"):
+            layer.update(torch.zeros(96, 64, dtype=dtype))
+        with pytest.raises(ValueError, match="bfloat16"):
+            layer.forward(torch.zeros(40, 64, dtype=dtype))
+        assert len(library.calls) == enqueued
+    layer.forward(torch.zeros(40, 64, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="bfloat16"):
+        layer.backward(torch.zeros(40, 96, dtype=dtype))
