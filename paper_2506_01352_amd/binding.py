@@ -496,12 +496,14 @@ def _torch_dtype(dtype):
     return torch.float32 if dtype == F32 else torch.bfloat16
 
 
-def _input_of(where, name, t, elements, dtype):
-    """Device address of a class's input: a contiguous device tensor of `dtype` with `elements` elements at least.  What a call on a few tokens
-    takes is mostly what it costs the host, so the classes look at an input once and keep their own buffers' addresses at hand."""
-    if t.dtype is not dtype or t.numel() < elements or not t.is_contiguous() or not t.is_cuda:
+def _input_of(where, name, t, rows, cols, dtype):
+    """Device address of a class's input: a contiguous device tensor of `dtype`, [.., cols] with `rows` rows in all, or flat.  What a call on a
+    few tokens takes is mostly what it costs the host, so the classes look at an input once and keep their own buffers' addresses at hand;
+    a single row is the same in any shape."""
+    fits = t.dtype is dtype and t.numel() == rows * cols and t.is_contiguous() and t.is_cuda
+    if not fits or (rows > 1 and t.shape[-1] != cols and t.dim() > 1):
         raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype} on {t.device}"
-                         f"{'' if t.is_contiguous() else ', not contiguous'}: {elements} contiguous elements of {dtype} on the GPU are needed")
+                         f"{'' if t.is_contiguous() else ', not contiguous'}: [{rows}, {cols}] contiguous elements of {dtype} on the GPU are needed")
     return t.data_ptr()
 
 
@@ -574,12 +576,12 @@ class Mx4Linear:
 
     def update(self, weight, stream=None):
         """Pack W, e.g. after an optimizer's step."""
-        _input_of("Mx4Linear.update", "weight", weight, self._w.rows * self._w.cols, self._kind)
+        _input_of("Mx4Linear.update", "weight", weight, self._w.rows, self._w.cols, self._kind)
         tahq_mx4_quantize(self._w, weight, self.weight, self.weight_t, stream)
 
     def forward(self, x, stream=None):
         """y; in training x is kept along its tokens for the weight's gradient."""
-        d_x = _input_of("Mx4Linear.forward", "x", x, self._x.rows * self._x.cols, self._kind)
+        d_x = _input_of("Mx4Linear.forward", "x", x, self._x.rows, self._x.cols, self._kind)
         if not self.training:
             rc = _lib.tahq_mx4_linear(*self._linear, d_x, *self._own, _stream_handle(stream))
             if rc != 0:
@@ -603,7 +605,7 @@ class Mx4Linear:
             raise ValueError("Mx4Linear.backward: the layer was not made with training=True")
         if self._forward_x_t is None:
             raise ValueError("Mx4Linear.backward: there is no x along its tokens: no forward pass, or a product without x_packed_t")
-        d_dy = _input_of("Mx4Linear.backward", "grad_y", grad_y, self._dy.rows * self._dy.cols, self._kind)
+        d_dy = _input_of("Mx4Linear.backward", "grad_y", grad_y, self._dy.rows, self._dy.cols, self._kind)
         kept = {"x_t": self._forward_x_t, **self._kept}
         at, size = {k: _dev_ptr(t) for k, t in kept.items()}, {k: _nbytes(t) for k, t in kept.items()}
         handle = _stream_handle(stream)
@@ -704,7 +706,7 @@ class BlockNorm:
             self.grad_residual, self.grad_block = (torch.empty(shape, dtype=kind, device=device) for _ in range(2))
             self.grad_w_post, self.grad_w_pre = (torch.zeros(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
             self.grad_gate = torch.zeros(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
-        self._kind, self._sizes = kind, (cfg.rows * cfg.cols, cfg.cols, _gate_groups(cfg) * cfg.cols)
+        self._kind, self._sizes = kind, (cfg.rows, cfg.cols, _gate_groups(cfg))
         h = self.h.data_ptr()
         out, stats, self._cfg = self.residual_out.data_ptr(), self.stats.data_ptr(), C.byref(cfg)
         self._own = (out, None if mx4 else h, h if mx4 else None, self.h.numel() if mx4 else 0, stats)
@@ -712,13 +714,13 @@ class BlockNorm:
 
     def forward(self, residual, block, w_post, gate, w_pre, stream=None):
         """(r', h); block, w_post and gate may be None, or w_pre."""
-        where, kind, (n, cols, gates) = "BlockNorm.forward", self._kind, self._sizes
+        where, kind, (rows, cols, groups) = "BlockNorm.forward", self._kind, self._sizes
         rc = _lib.tahq_norm_forward(
-            self._cfg, _input_of(where, "residual", residual, n, kind),
-            None if block is None else _input_of(where, "block", block, n, kind),
-            None if w_post is None else _input_of(where, "w_post", w_post, cols, kind),
-            None if gate is None else _input_of(where, "gate", gate, gates, kind),
-            None if w_pre is None else _input_of(where, "w_pre", w_pre, cols, kind),
+            self._cfg, _input_of(where, "residual", residual, rows, cols, kind),
+            None if block is None else _input_of(where, "block", block, rows, cols, kind),
+            None if w_post is None else _input_of(where, "w_post", w_post, 1, cols, kind),
+            None if gate is None else _input_of(where, "gate", gate, groups, cols, kind),
+            None if w_pre is None else _input_of(where, "w_pre", w_pre, 1, cols, kind),
             *(self._own if w_pre is not None else self._own_post), _stream_handle(stream))
         if rc != 0:
             raise TahqError(rc, "tahq_norm_forward")
@@ -734,15 +736,15 @@ class BlockNorm:
             got.update(grad_block=self.grad_block, grad_w_post=self.grad_w_post, grad_gate=self.grad_gate)
         if grad_h is not None:
             got["grad_w_pre"] = self.grad_w_pre
-        where, kind, (n, cols, gates) = "BlockNorm.backward", self._kind, self._sizes
+        where, kind, (rows, cols, groups) = "BlockNorm.backward", self._kind, self._sizes
 
-        def at(name, t, elements, dtype=kind):
-            return None if t is None else _input_of(where, name, t, elements, dtype)
+        def at(name, t, count=rows, width=cols, dtype=kind):
+            return None if t is None else _input_of(where, name, t, count, width, dtype)
 
         rc = _lib.tahq_norm_backward(
-            self._cfg, at("grad_residual_out", grad_residual_out, n), at("grad_h", grad_h, n), at("block", block, n),
-            at("w_post", w_post, cols), at("gate", gate, gates), at("residual_out", residual_out, n), at("w_pre", w_pre, cols),
-            at("stats", stats, 2 * self.cfg.rows, self.stats.dtype), *(None if t is None else t.data_ptr() for t in got.values()),
+            self._cfg, at("grad_residual_out", grad_residual_out), at("grad_h", grad_h), at("block", block), at("w_post", w_post, 1),
+            at("gate", gate, groups), at("residual_out", residual_out), at("w_pre", w_pre, 1),
+            at("stats", stats, 2, rows, self.stats.dtype), *(None if t is None else t.data_ptr() for t in got.values()),
             self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))
         if rc != 0:
             raise TahqError(rc, "tahq_norm_backward")

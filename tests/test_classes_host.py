@@ -136,3 +136,36 @@ def test_layers_take_no_types_but_fp32_and_bf16(library, dtype):
     layer.forward(torch.zeros(40, 64, dtype=torch.bfloat16))
     with pytest.raises(ValueError, match="bfloat16"):
         layer.backward(torch.zeros(40, 96, dtype=dtype))
+
+
+@pytest.mark.parametrize("shape", [(41, 64), (80, 64), (39, 64), (64, 40), (20, 128), (40, 32), (2, 40, 64), (41 * 64,), (0, 64)])
+def test_layers_take_as_many_tokens_as_they_were_made_for(library, shape):
+    bad = torch.zeros(shape, dtype=torch.bfloat16)
+    for training in (False, True):
+        layer = _layer(training=training)
+        enqueued = len(library.calls)
+        with pytest.raises(ValueError, match="x is a"):
+            layer.forward(bad)
+        with pytest.raises(ValueError, match="weight is a"):
+            layer.update(bad)
+        assert len(library.calls) == enqueued
+        layer.forward(torch.zeros(2, 20, 64, dtype=torch.bfloat16))          # tokens in two dimensions, or one row of them
+        layer.forward(torch.zeros(40 * 64, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="grad_y is a"):
+        layer.backward(bad)
+    layer.backward(torch.zeros(4, 10, 96, dtype=torch.bfloat16))
+
+
+def test_norms_take_tensors_of_their_shape(library):
+    norm, t = _norm(), _norm_inputs()
+    forward = {**{n: t[n] for n in ("block", "w_post", "gate", "w_pre")}, "residual": t["residual_out"]}
+    norm.forward(**forward)
+    norm.backward(**t)
+    assert [name for name, _ in library.calls] == ["tahq_norm_forward", "tahq_norm_backward"]
+    for call, inputs in ((norm.forward, forward), (norm.backward, t)):
+        for name, good in inputs.items():
+            for shape in ({6: [(7, 64), (12, 64), (64, 6), (5, 64)], 3: [(6, 64), (2, 64), (64, 3)], 64: [(65,), (64, 2), (6, 64)],
+                           2: [(2, 7), (3, 6), (6, 2)]}[good.shape[0]]):
+                with pytest.raises(ValueError, match=f" {name} is a"):
+                    call(**{**inputs, name: torch.zeros(shape, dtype=good.dtype)})
+    assert len(library.calls) == 2
