@@ -491,6 +491,20 @@ def _bytes_on(device, size):
     return torch.empty(max(size, 16), dtype=torch.uint8, device=device)
 
 
+def _packed_on(device, rows, cols, transform):
+    """A buffer for a packed matrix, which carries what its bytes do not tell: rows, columns and whether blocks are rotated."""
+    t = _bytes_on(device, tahq_mx4_packed_size(rows, cols))
+    t.mx4_form = (rows, cols, transform)
+    return t
+
+
+def _check_packed(where, name, t, form, size):
+    """A packed matrix that a class is given: bytes enough, and of the form that the buffer carries, if it does."""
+    if t.element_size() != 1 or t.numel() < size or not t.is_contiguous() or getattr(t, "mx4_form", form) != form:
+        raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype}{', packed as ' + str(t.mx4_form) if hasattr(t, 'mx4_form') else ''}: "
+                         f"{size} bytes of a packed matrix of (rows, cols, transform) = {form} are needed")
+
+
 def _torch_dtype(dtype):
     import torch
     return torch.float32 if dtype == F32 else torch.bfloat16
@@ -515,8 +529,8 @@ class Mx4Tensor:
         if tahq_mx4_packed_size(cfg.rows, cfg.cols) == 0:
             raise TahqError(2, "tahq_mx4_packed_size")
         self.cfg = cfg
-        self.packed = _bytes_on(device, tahq_mx4_packed_size(cfg.rows, cfg.cols))
-        self.packed_t = _bytes_on(device, tahq_mx4_packed_size(cfg.cols, cfg.rows)) if transposed else None
+        self.packed = _packed_on(device, cfg.rows, cfg.cols, cfg.transform)
+        self.packed_t = _packed_on(device, cfg.cols, cfg.rows, cfg.transform) if transposed else None
         self._values = make_mx4_config(cfg.rows, cfg.cols, cfg.dtype, 0, cfg.transform, cfg.scale_rule)
         self._values_t = make_mx4_config(cfg.cols, cfg.rows, cfg.dtype, 0, cfg.transform, cfg.scale_rule)
         kind = _torch_dtype(cfg.dtype)
@@ -561,13 +575,14 @@ class Mx4Linear:
         self.weight_t = self.x_t = None
         if training:
             self.weight_t = _bytes_on(device, tahq_mx4_packed_size(k, n))
-            self.x, self.x_t = _bytes_on(device, tahq_mx4_packed_size(tokens, k)), _bytes_on(device, tahq_mx4_packed_size(k, tokens))
+            self.x, self.x_t = _packed_on(device, tokens, k, transform), _packed_on(device, k, tokens, transform)
             self.dy, self.dy_t = _bytes_on(device, tahq_mx4_packed_size(tokens, n)), _bytes_on(device, tahq_mx4_packed_size(n, tokens))
             self.grad_x = torch.empty(tokens, k, dtype=weight.dtype, device=device)
             self.grad_w = torch.zeros(n, k, dtype=torch.float32, device=device)
             need = max([need] + [tahq_mx4_matmul_workspace_size(c) for c in (self._forward, self._dx, self._dw)])
         self.workspace = _bytes_on(device, need)
         self._kind = weight.dtype
+        self._x_form, self._x_t_form = (((r, c, transform), tahq_mx4_packed_size(r, c)) for r, c in ((tokens, k), (k, tokens)))
         self._kept = {k: getattr(self, k) for k in ("dy", "dy_t", "weight_t", "workspace")} if training else {}
         self._forward_x_t = None                  # what the last forward pass was of, along its tokens
         self._linear = (C.byref(self._x), C.byref(self._forward))
@@ -594,6 +609,9 @@ class Mx4Linear:
     def product(self, x_packed, stream=None, x_packed_t=None):
         """y of an x that is packed already, e.g. by BlockNorm.  The backward pass reads the same x packed along its tokens: x_packed_t, which
         stays the caller's; without it there is no backward pass of this y."""
+        _check_packed("Mx4Linear.product", "x_packed", x_packed, *self._x_form)
+        if x_packed_t is not None:
+            _check_packed("Mx4Linear.product", "x_packed_t", x_packed_t, *self._x_t_form)
         self._forward_x_t = None
         tahq_mx4_matmul(self._forward, x_packed, self.weight, self.y, self.workspace, stream)
         self._forward_x_t = x_packed_t
@@ -698,7 +716,7 @@ class BlockNorm:
         self.cfg, self.mx4, kind = cfg, mx4, _torch_dtype(cfg.dtype)
         shape = (cfg.rows, cfg.cols)
         self.residual_out = torch.empty(shape, dtype=kind, device=device)
-        self.h = _bytes_on(device, tahq_mx4_packed_size(*shape)) if mx4 else torch.empty(shape, dtype=kind, device=device)
+        self.h = _packed_on(device, *shape, cfg.transform) if mx4 else torch.empty(shape, dtype=kind, device=device)
         self.stats = torch.empty(2, cfg.rows, dtype=torch.float32, device=device)
         self.training = training
         if training:

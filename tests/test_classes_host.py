@@ -169,3 +169,37 @@ def test_norms_take_tensors_of_their_shape(library):
                 with pytest.raises(ValueError, match=f" {name} is a"):
                     call(**{**inputs, name: torch.zeros(shape, dtype=good.dtype)})
     assert len(library.calls) == 2
+
+
+def test_products_of_packed_matrices_that_do_not_fit_the_layer_are_refused(library):
+    """What the classes pack carries its rows, columns and rotation; other bytes are taken as they are, other types are not."""
+    layer = _layer(transform=1, training=True)
+    size = tahq.tahq_mx4_packed_size(40, 64)
+
+    def packed(rows, cols, transform):
+        t = tahq.Mx4Tensor(tahq.make_mx4_config(rows, cols, tahq.BF16, 0, transform), transposed=True, device="cpu")
+        return t.packed, t.packed_t
+
+    def h(rows, cols, transform):
+        cfg = tahq.make_norm_config(rows, cols, tahq.BF16, transform=transform)
+        norm = tahq.BlockNorm(cfg, mx4=True, device="cpu")
+        assert norm.h.numel() == tahq.tahq_mx4_packed_size(rows, cols)
+        return norm.h
+
+    x, x_t = packed(40, 64, 1)
+    enqueued = len(library.calls)
+    for bad in (packed(40, 64, 0)[0], packed(33, 64, 1)[0], packed(64, 40, 1)[0], packed(40, 63, 1)[0], x_t, h(40, 64, 0), h(64, 64, 1)):
+        with pytest.raises(ValueError, match="x_packed is"):
+            layer.product(bad)
+    for bad in (packed(40, 64, 0)[1], packed(40, 33, 1)[1], x):
+        with pytest.raises(ValueError, match="x_packed_t is"):
+            layer.product(x, x_packed_t=bad)
+    for bad in (torch.zeros(40, 64, dtype=torch.bfloat16), torch.zeros(40, 64), torch.zeros(size - 1, dtype=torch.uint8),
+                torch.zeros(2 * size, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="x_packed is"):
+            layer.product(bad)
+        with pytest.raises(ValueError, match="x_packed_t is"):
+            layer.product(x, x_packed_t=bad)
+    assert len(library.calls) == enqueued
+    for good, good_t in ((x, x_t), (h(40, 64, 1), None), (torch.zeros(size, dtype=torch.uint8), torch.zeros(size + 64, dtype=torch.uint8))):
+        layer.product(good, x_packed_t=good_t)
