@@ -505,6 +505,11 @@ def _check_packed(where, name, t, form, size):
                          f"{size} bytes of a packed matrix of (rows, cols, transform) = {form} are needed")
 
 
+def _check_slot(where, slot, in_flight):
+    if not 0 <= slot < in_flight:
+        raise ValueError(f"{where}: slot {slot} of {in_flight} micro-batches in flight")
+
+
 def _torch_dtype(dtype):
     import torch
     return torch.float32 if dtype == F32 else torch.bfloat16
@@ -552,12 +557,16 @@ class Mx4Tensor:
 
 class Mx4Linear:
     """A linear layer y = x W^T in mx4 for a fixed number of tokens: W packed once, buffers for x, y and, for training, for the
-    backward pass.  `weight`: [n, k], fp32 or bf16, which is also the dtype of x, y and their gradients; grad_w is fp32."""
+    backward pass.  `weight`: [n, k], fp32 or bf16, which is also the dtype of x, y and their gradients; grad_w is fp32.
+    in_flight: micro-batches that go forward before the first of them comes back.  Each has a slot: its own y, and in training its own x
+    along its tokens, until the slot's next forward pass.  The other buffers (gradients among them) are the next call's: calls of one layer follow
+    each other, on one stream or ordered by the caller."""
 
-    def __init__(self, weight, tokens, transform=0, scale_rule=MX4_FLOOR, training=False, accumulate=0):
+    def __init__(self, weight, tokens, transform=0, scale_rule=MX4_FLOOR, training=False, accumulate=0, in_flight=1):
         import torch
         if weight.dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"Mx4Linear: the weight is a tensor of {weight.dtype}, float32 or bfloat16 is needed")
+        _check_slot("Mx4Linear", 0, in_flight)
         n, k = weight.shape
         device, dtype = weight.device, F32 if weight.dtype == torch.float32 else BF16
         self.training = training
@@ -570,12 +579,16 @@ class Mx4Linear:
         if not tahq_mx4_linear_workspace_size(self._x, self._forward):
             raise TahqError(2, "tahq_mx4_linear_workspace_size")
         self.weight = _bytes_on(device, tahq_mx4_packed_size(n, k))
-        self.y = torch.empty(tokens, n, dtype=weight.dtype, device=device)
+        self._in_flight = in_flight
+        self._ys = [torch.empty(tokens, n, dtype=weight.dtype, device=device) for _ in range(in_flight)]
+        self.y = self._ys[0]
         need = tahq_mx4_linear_workspace_size(self._x, self._forward)
         self.weight_t = self.x_t = None
         if training:
             self.weight_t = _bytes_on(device, tahq_mx4_packed_size(k, n))
-            self.x, self.x_t = _packed_on(device, tokens, k, transform), _packed_on(device, k, tokens, transform)
+            self.x = _packed_on(device, tokens, k, transform)
+            self._x_ts = [_packed_on(device, k, tokens, transform) for _ in range(in_flight)]
+            self.x_t = self._x_ts[0]
             self.dy, self.dy_t = _bytes_on(device, tahq_mx4_packed_size(tokens, n)), _bytes_on(device, tahq_mx4_packed_size(n, tokens))
             self.grad_x = torch.empty(tokens, k, dtype=weight.dtype, device=device)
             self.grad_w = torch.zeros(n, k, dtype=torch.float32, device=device)
@@ -584,9 +597,10 @@ class Mx4Linear:
         self._kind = weight.dtype
         self._x_form, self._x_t_form = (((r, c, transform), tahq_mx4_packed_size(r, c)) for r, c in ((tokens, k), (k, tokens)))
         self._kept = {k: getattr(self, k) for k in ("dy", "dy_t", "weight_t", "workspace")} if training else {}
-        self._forward_x_t = None                  # what the last forward pass was of, along its tokens
+        self._forward_x_t = [None] * in_flight    # what a slot's last forward pass was of, along its tokens
         self._linear = (C.byref(self._x), C.byref(self._forward))
-        self._own = (self.weight.data_ptr(), self.weight.numel(), self.y.data_ptr(), self.workspace.data_ptr(), self.workspace.numel())
+        self._own = [(self.weight.data_ptr(), self.weight.numel(), y.data_ptr(), self.workspace.data_ptr(), self.workspace.numel())
+                     for y in self._ys]
         self.update(weight)
 
     def update(self, weight, stream=None):
@@ -594,37 +608,44 @@ class Mx4Linear:
         _input_of("Mx4Linear.update", "weight", weight, self._w.rows, self._w.cols, self._kind)
         tahq_mx4_quantize(self._w, weight, self.weight, self.weight_t, stream)
 
-    def forward(self, x, stream=None):
+    def forward(self, x, stream=None, slot=0):
         """y; in training x is kept along its tokens for the weight's gradient."""
         d_x = _input_of("Mx4Linear.forward", "x", x, self._x.rows, self._x.cols, self._kind)
+        if slot:
+            _check_slot("Mx4Linear.forward", slot, self._in_flight)
         if not self.training:
-            rc = _lib.tahq_mx4_linear(*self._linear, d_x, *self._own, _stream_handle(stream))
+            rc = _lib.tahq_mx4_linear(*self._linear, d_x, *self._own[slot], _stream_handle(stream))
             if rc != 0:
                 raise TahqError(rc, "tahq_mx4_linear")
-            return self.y
-        self._forward_x_t = None
-        tahq_mx4_quantize(self._x, x, self.x, self.x_t, stream)
-        return self.product(self.x, stream, self.x_t)
+            return self._ys[slot]
+        self._forward_x_t[slot] = None
+        tahq_mx4_quantize(self._x, x, self.x, self._x_ts[slot], stream)
+        return self.product(self.x, stream, self._x_ts[slot], slot)
 
-    def product(self, x_packed, stream=None, x_packed_t=None):
+    def product(self, x_packed, stream=None, x_packed_t=None, slot=0):
         """y of an x that is packed already, e.g. by BlockNorm.  The backward pass reads the same x packed along its tokens: x_packed_t, which
         stays the caller's; without it there is no backward pass of this y."""
         _check_packed("Mx4Linear.product", "x_packed", x_packed, *self._x_form)
         if x_packed_t is not None:
             _check_packed("Mx4Linear.product", "x_packed_t", x_packed_t, *self._x_t_form)
-        self._forward_x_t = None
-        tahq_mx4_matmul(self._forward, x_packed, self.weight, self.y, self.workspace, stream)
-        self._forward_x_t = x_packed_t
-        return self.y
+        if slot:
+            _check_slot("Mx4Linear.product", slot, self._in_flight)
+        self._forward_x_t[slot] = None
+        tahq_mx4_matmul(self._forward, x_packed, self.weight, self._ys[slot], self.workspace, stream)
+        self._forward_x_t[slot] = x_packed_t
+        return self._ys[slot]
 
-    def backward(self, grad_y, stream=None):
-        """(gradient of x, gradient of W); the latter is added to with accumulate = 1."""
+    def backward(self, grad_y, stream=None, slot=0):
+        """(gradient of x, gradient of W) of the slot's last forward pass; the latter is added to with accumulate = 1."""
         if not self.training:
             raise ValueError("Mx4Linear.backward: the layer was not made with training=True")
-        if self._forward_x_t is None:
+        if slot:
+            _check_slot("Mx4Linear.backward", slot, self._in_flight)
+        x_t = self._forward_x_t[slot]
+        if x_t is None:
             raise ValueError("Mx4Linear.backward: there is no x along its tokens: no forward pass, or a product without x_packed_t")
         d_dy = _input_of("Mx4Linear.backward", "grad_y", grad_y, self._dy.rows, self._dy.cols, self._kind)
-        kept = {"x_t": self._forward_x_t, **self._kept}
+        kept = {"x_t": x_t, **self._kept}
         at, size = {k: _dev_ptr(t) for k, t in kept.items()}, {k: _nbytes(t) for k, t in kept.items()}
         handle = _stream_handle(stream)
         for name, call in (
@@ -706,32 +727,47 @@ def tahq_norm_backward(cfg, d_grad_residual_out, d_grad_h, d_block, d_w_post, d_
 class BlockNorm:
     """Buffers of one configuration's norms.  mx4: h leaves as a packed matrix; otherwise in the configuration's dtype.  training: with the
     buffers of the backward pass.  All are made, and gradients that are added to cleared, on torch's current stream: a call on another
-    stream comes after that stream has waited for it."""
+    stream comes after that stream has waited for it.
+    in_flight: micro-batches that go forward before the first of them comes back.  Each has a slot: its own r', h and statistics, until the
+    slot's next forward pass; backward is given a slot's r' and stats_of(slot).  Gradients are the next backward call's."""
 
-    def __init__(self, cfg, mx4=False, device="cuda:0", training=True):
+    def __init__(self, cfg, mx4=False, device="cuda:0", training=True, in_flight=1):
         import torch
         need = tahq_norm_workspace_size(cfg)
         if need == 0:
             raise TahqError(2, "tahq_norm_workspace_size")
         self.cfg, self.mx4, kind = cfg, mx4, _torch_dtype(cfg.dtype)
         shape = (cfg.rows, cfg.cols)
-        self.residual_out = torch.empty(shape, dtype=kind, device=device)
-        self.h = _packed_on(device, *shape, cfg.transform) if mx4 else torch.empty(shape, dtype=kind, device=device)
-        self.stats = torch.empty(2, cfg.rows, dtype=torch.float32, device=device)
+        _check_slot("BlockNorm", 0, in_flight)
+
+        def plain():
+            return torch.empty(shape, dtype=kind, device=device)
+
+        # (r', h, statistics) of each slot, and where a call finds them
+        self._slots = [(plain(), _packed_on(device, *shape, cfg.transform) if mx4 else plain(),
+                        torch.empty(2, cfg.rows, dtype=torch.float32, device=device)) for _ in range(in_flight)]
+        self.residual_out, self.h, self.stats = self._slots[0]
         self.training = training
         if training:
             self.workspace = _bytes_on(device, need)
-            self.grad_residual, self.grad_block = (torch.empty(shape, dtype=kind, device=device) for _ in range(2))
+            self.grad_residual, self.grad_block = (plain() for _ in range(2))
             self.grad_w_post, self.grad_w_pre = (torch.zeros(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
             self.grad_gate = torch.zeros(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
         self._kind, self._sizes = kind, (cfg.rows, cfg.cols, _gate_groups(cfg))
-        h = self.h.data_ptr()
-        out, stats, self._cfg = self.residual_out.data_ptr(), self.stats.data_ptr(), C.byref(cfg)
-        self._own = (out, None if mx4 else h, h if mx4 else None, self.h.numel() if mx4 else 0, stats)
-        self._own_post = (out, None, None, 0, stats)
+        self._cfg, self._own, self._own_post = C.byref(cfg), [], []
+        for out, h, stats in self._slots:
+            own = out.data_ptr(), h.data_ptr(), stats.data_ptr()
+            self._own.append((own[0], None, own[1], h.numel(), own[2]) if mx4 else (own[0], own[1], None, 0, own[2]))
+            self._own_post.append((own[0], None, None, 0, own[2]))
 
-    def forward(self, residual, block, w_post, gate, w_pre, stream=None):
+    def stats_of(self, slot):
+        _check_slot("BlockNorm.stats_of", slot, len(self._slots))
+        return self._slots[slot][2]
+
+    def forward(self, residual, block, w_post, gate, w_pre, stream=None, slot=0):
         """(r', h); block, w_post and gate may be None, or w_pre."""
+        if slot:
+            _check_slot("BlockNorm.forward", slot, len(self._slots))
         where, kind, (rows, cols, groups) = "BlockNorm.forward", self._kind, self._sizes
         rc = _lib.tahq_norm_forward(
             self._cfg, _input_of(where, "residual", residual, rows, cols, kind),
@@ -739,10 +775,11 @@ class BlockNorm:
             None if w_post is None else _input_of(where, "w_post", w_post, 1, cols, kind),
             None if gate is None else _input_of(where, "gate", gate, groups, cols, kind),
             None if w_pre is None else _input_of(where, "w_pre", w_pre, 1, cols, kind),
-            *(self._own if w_pre is not None else self._own_post), _stream_handle(stream))
+            *(self._own if w_pre is not None else self._own_post)[slot], _stream_handle(stream))
         if rc != 0:
             raise TahqError(rc, "tahq_norm_forward")
-        return self.residual_out, None if w_pre is None else self.h
+        out, h, _ = self._slots[slot]
+        return out, None if w_pre is None else h
 
     def backward(self, grad_residual_out, grad_h, block, w_post, gate, residual_out, w_pre, stats, stream=None):
         """Gradients of residual, block, w_post, gate and w_pre by name; None for what there is not."""

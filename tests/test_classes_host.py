@@ -203,3 +203,31 @@ def test_products_of_packed_matrices_that_do_not_fit_the_layer_are_refused(libra
     assert len(library.calls) == enqueued
     for good, good_t in ((x, x_t), (h(40, 64, 1), None), (torch.zeros(size, dtype=torch.uint8), torch.zeros(size + 64, dtype=torch.uint8))):
         layer.product(good, x_packed_t=good_t)
+
+
+def test_micro_batches_in_flight_keep_what_their_backward_pass_needs(library):
+    """Two forward passes in front of the first backward one, as a pipeline has them: each in a slot of its own."""
+    layer = _layer(training=True, in_flight=3)
+    x, dy = torch.zeros(40, 64, dtype=torch.bfloat16), torch.zeros(40, 96, dtype=torch.bfloat16)
+    assert len({layer.forward(x, slot=i).data_ptr() for i in range(2)}) == 2
+    with pytest.raises(ValueError, match="no x"):
+        layer.backward(dy, slot=2)
+    of = []
+    for i in range(2):
+        layer.backward(dy, slot=i)
+        of.append(_x_of_weight_gradient(library))
+    assert len(set(of)) == 2 and of[0] == layer.x_t.data_ptr()
+    assert [a[4] for name, a in library.calls if name == "tahq_mx4_quantize" and a[2] == layer.x.data_ptr()] == of
+
+    norm = _norm(in_flight=2)
+    t = _norm_inputs()
+    inputs = (t["residual_out"], t["block"], t["w_post"], t["gate"], t["w_pre"])
+    first, second = norm.forward(*inputs), norm.forward(*inputs, slot=1)
+    assert len({v.data_ptr() for v in (*first, *second)}) == 4 and norm.stats_of(0) is norm.stats
+    assert norm.stats_of(1).data_ptr() != norm.stats.data_ptr() and norm.stats_of(1).shape == norm.stats.shape
+    written = [a for name, a in library.calls if name == "tahq_norm_forward"][-1]
+    assert written[6] == second[0].data_ptr() and written[7] == second[1].data_ptr() and written[10] == norm.stats_of(1).data_ptr()
+    for call in (lambda: layer.forward(x, slot=3), lambda: layer.backward(dy, slot=3), lambda: norm.forward(*inputs, slot=2),
+                 lambda: norm.stats_of(2), lambda: layer.forward(x, slot=-1), lambda: norm.forward(*inputs, slot=-1), lambda: _layer(in_flight=0)):
+        with pytest.raises((ValueError, IndexError)):
+            call()

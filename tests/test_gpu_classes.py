@@ -52,3 +52,33 @@ def test_training_through_an_h_that_is_packed_already():
     assert torch.equal(layer.product(packed.packed, x_packed_t=packed.packed_t), y)
     got = layer.backward(dy)
     assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
+
+
+def test_two_micro_batches_in_flight_give_what_they_give_one_after_the_other():
+    rows, cols, n = 100, 512, 320
+    g = torch.Generator(device="cuda").manual_seed(9)
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)      # noqa: E731
+    w, w_post, w_pre, gate = make(n, cols), make(cols), make(cols), make(1, cols)
+    batches = [{"residual": make(rows, cols), "block": make(rows, cols), "dy": make(rows, n), "dr": make(rows, cols)} for _ in range(2)]
+    cfg = tahq.make_norm_config(rows, cols, tahq.BF16, rows)
+
+    def forward(norm, layer, b, slot):
+        out, h = norm.forward(b["residual"], b["block"], w_post, gate, w_pre, slot=slot)
+        return out, layer.forward(h, slot=slot)
+
+    def backward(norm, layer, b, out, slot):
+        dh, dw = layer.backward(b["dy"], slot=slot)
+        got = norm.backward(b["dr"], dh, b["block"], w_post, gate, out, w_pre, norm.stats_of(slot))
+        return [t.clone() for t in (dw, *got.values())]
+
+    one, one_layer = tahq.BlockNorm(cfg), tahq.Mx4Linear(w, rows, training=True)
+    want, ys = [], []
+    for b in batches:
+        out, y = forward(one, one_layer, b, 0)
+        ys.append(y.clone())
+        want.append(backward(one, one_layer, b, out, 0))
+    both, both_layer = tahq.BlockNorm(cfg, in_flight=2), tahq.Mx4Linear(w, rows, training=True, in_flight=2)
+    kept = [forward(both, both_layer, b, i) for i, b in enumerate(batches)]
+    for i, b in enumerate(batches):
+        assert torch.equal(kept[i][1], ys[i])
+        assert all(torch.equal(a, c) for a, c in zip(backward(both, both_layer, b, kept[i][0], i), want[i]))
