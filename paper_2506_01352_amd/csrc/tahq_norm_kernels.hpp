@@ -169,6 +169,9 @@ void k_norm_forward(const void *residual, const void *block, const void *w_post,
             for (int i = 0; i < 8; ++i) x[i] = x[i] * rstd_r * pre[i];
             if (h && there && mine) keep<BF16, EIGHTS>(row_of<BF16>(h, row, C), c, C, x);
             if (h_mx4) {
+                // what fills up the packed matrix: zeros, also where the statistics or the weight's sign would make NaN or -0 of them
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) x[i] = there && (EIGHTS ? mine : c + i < C) ? x[i] : 0.0f;
                 uint32_t e;
                 const uint32_t codes = rotate ? quantize_quad<true>(x, cover, e) : quantize_quad<false>(x, cover, e);
                 const uint32_t blk = c / 32;
