@@ -24,7 +24,9 @@
  *   Rows from `rows` to 32*RB, and columns behind `cols`, are zeros with s = 0.
  *
  * Conventions as in tahq.h: d_* are device pointers, 16-byte aligned, no overlap between inputs and outputs; the caller owns every buffer;
- * nothing is allocated, kept or synchronized; argument errors come back before anything is enqueued.
+ * nothing is allocated, kept or synchronized; argument errors come back before anything is enqueued.  TAHQ_ERR_UNSUPPORTED: matrices
+ * of 2^24 tiles of 32 x 256 and more (2^29 rows of up to 256 columns), products of up to 16 rows with n from about 2^27 on, and of 2^24
+ * tiles of C of at most 256 x 256 and more: a launch has fewer than 2^32 lanes.
  */
 #ifndef TAHQ_MX4_H
 #define TAHQ_MX4_H

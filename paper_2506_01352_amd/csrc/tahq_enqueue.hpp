@@ -12,6 +12,9 @@ namespace tahq {
 
 inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
+// The runtime counts a launch's lanes along a dimension in 32 bits
+inline bool launchable(uint64_t workgroups, uint32_t lanes) { return workgroups * lanes < (uint64_t)1 << 32; }
+
 // Kernel launches of one call: each launch returns its own status (the thread's sticky "last error", which may
 // belong to the caller's earlier work, is neither read nor cleared), and after a failure nothing more is enqueued.
 struct Enqueue {

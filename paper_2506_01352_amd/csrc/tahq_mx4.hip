@@ -28,7 +28,6 @@ tahq_status check(const tahq_mx4_matmul_config *c)
     return TAHQ_OK;
 }
 
-constexpr uint64_t kMaxGrid = 0x7fffffffu;
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 uint32_t cover_of(const tahq_mx4_config *c) { return c->scale_rule == TAHQ_MX4_COVER ? kCover : 0u; }
 uint64_t ld_of(const tahq_mx4_config *c) { return c->ld ? c->ld : c->cols; }
@@ -44,20 +43,28 @@ void launch_quantize(const tahq_mx4_config *c, const void *d_in, uint8_t *p, uin
     else run(k_mx4_quantize<BF16, false, true, ROTATE>);
 }
 
-tahq_status enqueue_quantize(const tahq_mx4_config *c, const void *d_in, void *d_packed, void *d_packed_t, Enqueue *q)
+struct QuantGrid {
+    uint64_t tiles_x, tiles_y;
+    bool fits() const { return launchable(tiles_x * tiles_y, kQuantThreads); }
+};
+QuantGrid quant_grid(const tahq_mx4_config *c, bool transposed)
 {
     // along columns the last four units of 64 rows are filled up: their scale bytes are written, too
-    const uint64_t tiles_y = d_packed_t ? ceil_div(c->rows, 256) * (256 / kQuantRows) : ceil_div(c->rows, kQuantRows);
-    const uint64_t tiles_x = ceil_div(c->cols, kQuantCols);
-    if (tiles_x * tiles_y > kMaxGrid) return TAHQ_ERR_UNSUPPORTED;
+    return {ceil_div(c->cols, kQuantCols), transposed ? ceil_div(c->rows, 256) * (256 / kQuantRows) : ceil_div(c->rows, kQuantRows)};
+}
+
+tahq_status enqueue_quantize(const tahq_mx4_config *c, const void *d_in, void *d_packed, void *d_packed_t, Enqueue *q)
+{
+    const QuantGrid tiles = quant_grid(c, d_packed_t != nullptr);
+    if (!tiles.fits()) return TAHQ_ERR_UNSUPPORTED;
     uint8_t *p = static_cast<uint8_t *>(d_packed), *pt = static_cast<uint8_t *>(d_packed_t);
-    const uint32_t grid = (uint32_t)(tiles_x * tiles_y);
+    const uint32_t grid = (uint32_t)(tiles.tiles_x * tiles.tiles_y), tiles_x = (uint32_t)tiles.tiles_x;
     if (c->dtype == TAHQ_BF16) {
-        if (c->transform) launch_quantize<true, true>(c, d_in, p, pt, grid, (uint32_t)tiles_x, q);
-        else launch_quantize<true, false>(c, d_in, p, pt, grid, (uint32_t)tiles_x, q);
+        if (c->transform) launch_quantize<true, true>(c, d_in, p, pt, grid, tiles_x, q);
+        else launch_quantize<true, false>(c, d_in, p, pt, grid, tiles_x, q);
     } else {
-        if (c->transform) launch_quantize<false, true>(c, d_in, p, pt, grid, (uint32_t)tiles_x, q);
-        else launch_quantize<false, false>(c, d_in, p, pt, grid, (uint32_t)tiles_x, q);
+        if (c->transform) launch_quantize<false, true>(c, d_in, p, pt, grid, tiles_x, q);
+        else launch_quantize<false, false>(c, d_in, p, pt, grid, tiles_x, q);
     }
     return q->result();
 }
@@ -130,6 +137,13 @@ uint64_t product_workspace(const tahq_mx4_matmul_config *c)
     return p.parts > 1 ? (uint64_t)p.parts * c->m * c->n * 4 : 0;
 }
 
+bool product_fits(const tahq_mx4_matmul_config *c)
+{
+    const ProductPlan p = plan_product(c);
+    if (p.kind < 0) return launchable(ceil_div(c->n, c->m <= 16 ? 16 : 32), 64 * kFewWaves);
+    return launchable(tiles_of(kTiles[p.kind], c), p.kind == 5 ? 512 : 256);
+}
+
 uint64_t ldc_of(const tahq_mx4_matmul_config *c) { return c->ldc ? c->ldc : c->n; }
 
 template <int WM, int WN, int MF, int NF, int NB, int KS, int PER_CU>
@@ -170,7 +184,7 @@ tahq_status enqueue_product(const tahq_mx4_matmul_config *c, const void *d_a, co
 {
     const ProductPlan p = plan_product(c);
     const uint8_t *a = static_cast<const uint8_t *>(d_a), *b = static_cast<const uint8_t *>(d_b);
-    if (p.kind >= 0 && tiles_of(kTiles[p.kind], c) > kMaxGrid) return TAHQ_ERR_UNSUPPORTED;
+    if (!product_fits(c)) return TAHQ_ERR_UNSUPPORTED;
     switch (p.kind) {
     case 0: launch_tiles<2, 2, 4, 4, 4, 1, 1>(c, p, a, b, d_c, d_workspace, q); break;
     case 1: launch_tiles<2, 2, 4, 2, 3, 1, 2>(c, p, a, b, d_c, d_workspace, q); break;
@@ -245,12 +259,12 @@ tahq_status tahq_mx4_dequantize(const tahq_mx4_config *cfg, const void *d_packed
     if (!d_packed || !d_out) return TAHQ_ERR_NULL;
     if (packed_bytes < tahq_mx4_packed_size(cfg->rows, cfg->cols)) return TAHQ_ERR_BUFFER_TOO_SMALL;
     if (misaligned(d_packed) || misaligned(d_out)) return TAHQ_ERR_MISALIGNED;
-    const uint64_t tiles_x = ceil_div(cfg->cols, kQuantCols), tiles = tiles_x * ceil_div(cfg->rows, 32);
-    if (tiles > kMaxGrid) return TAHQ_ERR_UNSUPPORTED;
+    const QuantGrid tiles = quant_grid(cfg, false);
+    if (!tiles.fits()) return TAHQ_ERR_UNSUPPORTED;
     Enqueue q{(hipStream_t)stream};
     auto run = [&](auto kernel) {
-        q(kernel, dim3((uint32_t)tiles), dim3(kQuantThreads), static_cast<const uint8_t *>(d_packed), d_out, cfg->rows, cfg->cols,
-          ld_of(cfg), (uint32_t)tiles_x);
+        q(kernel, dim3((uint32_t)(tiles.tiles_x * tiles.tiles_y)), dim3(kQuantThreads), static_cast<const uint8_t *>(d_packed), d_out, cfg->rows,
+          cfg->cols, ld_of(cfg), (uint32_t)tiles.tiles_x);
     };
     if (cfg->dtype == TAHQ_BF16) {
         if (cfg->transform) run(k_mx4_dequantize<true, true>);
@@ -299,6 +313,7 @@ tahq_status tahq_mx4_linear(const tahq_mx4_config *x, const tahq_mx4_matmul_conf
     if (b_bytes < tahq_mx4_packed_size(cfg->n, cfg->k)) return TAHQ_ERR_BUFFER_TOO_SMALL;
     if (workspace_capacity < need) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
     if (misaligned(d_x) || misaligned(d_b) || misaligned(d_y) || misaligned(d_workspace)) return TAHQ_ERR_MISALIGNED;
+    if (!product_fits(cfg)) return TAHQ_ERR_UNSUPPORTED;
     Enqueue q{(hipStream_t)stream};
     if (quantizes_itself(cfg)) return enqueue_few(x, cfg, d_x, static_cast<const uint8_t *>(d_b), d_y, &q);
     uint8_t *packed = static_cast<uint8_t *>(d_workspace);
