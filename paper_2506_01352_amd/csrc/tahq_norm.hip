@@ -51,11 +51,12 @@ void with_kind(const tahq_norm_config *c, bool post, bool pre, Run run)
 
 // Forward: rows that a workgroup takes one after another.  Two where there are many (8192 x 4096, one row: 45 us, two: 42.7, eight: 47); eight where a
 // workgroup of more than twelve wavefronts has a compute unit to itself and only the next row on its way keeps memory busy (2048 x 8192: one
-// 36, two 31, eight 28); one where there are few.
+// 36, two 31, eight 28); one where there are few.  From 2^27 rows on (of few channels) as many more as a launch's 2^32 lanes ask for.
 uint32_t forward_rows(const tahq_norm_config *c, uint32_t rows)
 {
-    if (waves_of(c) > 12) return rows >= 2048 ? 8 : 1;
-    return rows >= 4096 ? 2 : 1;
+    uint32_t each = waves_of(c) > 12 ? (rows >= 2048 ? 8 : 1) : rows >= 4096 ? 2 : 1;
+    while (!launchable((rows - 1) / each + 1, 64 * waves_of(c))) each *= 2;
+    return each;
 }
 
 // Backward: the workgroups that share the rows.  A compute unit holds sixteen wavefronts of up to 128 registers, so `most` workgroups at once; more than one
@@ -134,12 +135,12 @@ tahq_status tahq_norm_forward(const tahq_norm_config *cfg, const void *d_residua
     const NormShape s = shape_of(cfg);
     const uint32_t cover = cfg->scale_rule == TAHQ_MX4_COVER ? kCover : 0u;
     const uint32_t total = d_h_mx4 ? 32 * ((cfg->rows + 31) / 32) : cfg->rows;
-    const uint32_t rows_each = forward_rows(cfg, total);
-    const dim3 grid((total + rows_each - 1) / rows_each);
+    const uint32_t rows_each = forward_rows(cfg, total), together = rows_each <= 32 ? 256 / rows_each : 1;
+    const dim3 grid((total - 1) / rows_each + 1);
     Enqueue q{(hipStream_t)stream};
     with_kind(cfg, d_block, d_w_pre, [&](auto bf16, auto eights, auto post, auto pre) {
         q(k_norm_forward<bf16, eights, post, pre>, grid, dim3(64 * waves_of(cfg)), d_residual, d_block, d_w_post, d_block ? d_gate : nullptr, d_w_pre, d_residual_out, d_h,
-          static_cast<uint8_t *>(d_h_mx4), d_stats, s, cover, cfg->transform, rows_each, 256 / rows_each);
+          static_cast<uint8_t *>(d_h_mx4), d_stats, s, cover, cfg->transform, rows_each, together);
     });
     return q.result();
 }

@@ -115,7 +115,8 @@ void k_norm_forward(const void *residual, const void *block, const void *w_post,
     const Mx4Layout L(s.rows, C);
     const uint32_t end = h_mx4 ? 32 * L.rb : s.rows;       // rows behind the last one fill up the packed matrix with zeros
     // The workgroups of 256 rows in another order, so that a unit's rows, whose codes lie side by side in a line, are on one XCD and merge in its
-    // L2: 8192 x 4096 bf16 to mx4 57 -> 52 us, to h and mx4 58 -> 51.  `together`, workgroups for 256 rows, is a power of two.
+    // L2: 8192 x 4096 bf16 to mx4 57 -> 52 us, to h and mx4 58 -> 51.  `together`, workgroups for 256 rows, is a power of two;
+    // 1: their own order.
     uint32_t place = blockIdx.x;
     const uint32_t in = place & (together - 1);
     if (h_mx4 && place - in + together <= gridDim.x) place += in % 8 * (together / 8) + in / 8 - in;
