@@ -419,10 +419,19 @@ def _rows_ptr(t, cols, ld):
     return _dev_ptr(t)
 
 
+def _check_not_half(where, name, t, dtype):
+    """float16 is no bf16, though its elements have the size that _check_tensor asks for (integers and bytes are taken for bf16's bits)."""
+    if dtype == BF16 and t is not None and not isinstance(t, int) and t.element_size() == 2:
+        import torch
+        if t.dtype is torch.float16:
+            raise ValueError(f"{where}: {name} is a tensor of {t.dtype}, the configuration says torch.bfloat16")
+
+
 def _check_rows(where, name, t, rows, cols, ld, dtype):
     """_check_tensor for a tensor of rows that lie `ld` elements apart; a view is checked by its own shape."""
     if t is None or isinstance(t, int):
         return
+    _check_not_half(where, name, t, dtype)
     if t.is_contiguous():
         _check_tensor(where, name, t, _strided_elements(rows, cols, ld), dtype)
     elif dtype in _ESIZE and (t.element_size() != _ESIZE[dtype] or t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols):
@@ -683,6 +692,8 @@ def _gate_groups(cfg):
 
 
 def _check_norm(where, cfg, tensors, weights, gate):
+    for name, t in (*tensors.items(), *weights.items(), ("d_gate", gate)):
+        _check_not_half(where, name, t, cfg.dtype)
     for name, t in tensors.items():
         _check_tensor(where, name, t, cfg.rows * cfg.cols, cfg.dtype)
     for name, t in weights.items():

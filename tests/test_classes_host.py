@@ -231,3 +231,36 @@ def test_micro_batches_in_flight_keep_what_their_backward_pass_needs(library):
                  lambda: norm.stats_of(2), lambda: layer.forward(x, slot=-1), lambda: norm.forward(*inputs, slot=-1), lambda: _layer(in_flight=0)):
         with pytest.raises((ValueError, IndexError)):
             call()
+
+
+def test_tensors_of_another_floating_point_type_of_the_same_size_are_refused(library):
+    """16 bits of another type than bf16 mean something else; integers of 16 bits are taken for bf16's bits, as the codec takes them."""
+    half, bits, bf = (torch.zeros(40, 64, dtype=d) for d in (torch.float16, torch.int16, torch.bfloat16))
+    packed, ws = (torch.zeros(1 << 16, dtype=torch.uint8) for _ in range(2))
+    row, row_bf = torch.zeros(64, dtype=torch.float16), torch.zeros(64, dtype=torch.bfloat16)
+    cfg, product = tahq.make_mx4_config(40, 64, tahq.BF16), tahq.make_mx4_matmul_config(40, 64, 64, tahq.BF16)
+    norm = tahq.make_norm_config(40, 64, tahq.BF16)
+    strided = torch.zeros(40, 128, dtype=torch.float16)[:, :64]
+    stats, column, out = torch.zeros(2, 40), torch.zeros(64), torch.zeros_like(bf)
+    backward = (stats, out, out, column, None, column, ws)
+    for call in (lambda: tahq.tahq_mx4_quantize(cfg, half, packed), lambda: tahq.tahq_mx4_dequantize(cfg, packed, half),
+                 lambda: tahq.tahq_mx4_quantize(tahq.make_mx4_config(40, 64, tahq.BF16, 128), strided, packed),
+                 lambda: tahq.tahq_mx4_matmul(product, packed, packed, half, ws),
+                 lambda: tahq.tahq_mx4_linear(cfg, product, half, packed, bf, ws),
+                 lambda: tahq.tahq_mx4_linear(cfg, product, bf, packed, half, ws),
+                 lambda: tahq.Mx4Tensor(cfg, device="cpu").quantize(half),
+                 lambda: tahq.tahq_norm_forward(norm, half, None, None, None, row_bf, out, out),
+                 lambda: tahq.tahq_norm_forward(norm, bf, None, None, None, row, out, out),
+                 lambda: tahq.tahq_norm_forward(norm, bf, None, None, None, row_bf, out, half),
+                 lambda: tahq.tahq_norm_backward(norm, half, bf, bf, row_bf, None, bf, row_bf, *backward),
+                 lambda: tahq.tahq_norm_backward(norm, bf, bf, bf, row_bf, None, bf, row, *backward)):
+        with pytest.raises(ValueError, match="float16"):
+            call()
+    gate = tahq.make_norm_config(40, 64, tahq.BF16, 40)
+    with pytest.raises(ValueError, match="float16"):
+        tahq.tahq_norm_forward(gate, bf, bf, row_bf, row, row_bf, out, out)
+    assert not library.calls
+    tahq.tahq_mx4_quantize(cfg, bits, packed)
+    tahq.tahq_norm_forward(norm, bits, None, None, None, row_bf, out, out)
+    tahq.tahq_norm_backward(norm, bf, bits, bf, row_bf, None, bf, row_bf, *backward)
+    assert len(library.calls) == 3
