@@ -552,6 +552,13 @@ class Mx4Tensor:
         self.out_t = torch.empty(cfg.cols, cfg.rows, dtype=kind, device=device) if transposed else None
 
     def quantize(self, d_in, stream=None):
+        """Packs a [rows, cols] tensor, one with its rows in several dimensions, or the whole buffer that they lie in, ld elements apart; flat
+        buffers and bytes are taken as they are."""
+        cfg = self.cfg
+        if not isinstance(d_in, int) and d_in.dim() > 1 and d_in.element_size() > 1:
+            cols = d_in.shape[-1]
+            if cols not in (cfg.cols, cfg.ld) or d_in.numel() != cfg.rows * cols:
+                raise ValueError(f"Mx4Tensor.quantize: d_in is a {tuple(d_in.shape)} tensor, the configuration says [{cfg.rows}, {cfg.cols}]")
         tahq_mx4_quantize(self.cfg, d_in, self.packed, self.packed_t, stream)
         return (self.packed,) if self.packed_t is None else (self.packed, self.packed_t)
 

@@ -264,3 +264,20 @@ def test_tensors_of_another_floating_point_type_of_the_same_size_are_refused(lib
     tahq.tahq_norm_forward(norm, bits, None, None, None, row_bf, out, out)
     tahq.tahq_norm_backward(norm, bf, bits, bf, row_bf, None, bf, row_bf, *backward)
     assert len(library.calls) == 3
+
+
+@pytest.mark.parametrize("shape", [(41, 64), (64, 40), (39, 64), (40, 128)])
+def test_packed_tensors_take_tensors_of_their_shape(library, shape):
+    tensor = tahq.Mx4Tensor(tahq.make_mx4_config(40, 64, tahq.BF16), device="cpu")
+    with pytest.raises(ValueError, match="d_in"):
+        tensor.quantize(torch.zeros(shape, dtype=torch.bfloat16))
+    assert not library.calls
+    for good in (torch.zeros(2, 20, 64, dtype=torch.bfloat16), torch.zeros(40 * 64, dtype=torch.int16), torch.zeros(40 * 64 * 2, dtype=torch.uint8),
+                 torch.zeros(41 * 64, dtype=torch.bfloat16)):
+        tensor.quantize(good)
+    apart = tahq.Mx4Tensor(tahq.make_mx4_config(40, 64, tahq.BF16, 80), device="cpu")
+    apart.quantize(torch.zeros(40, 80, dtype=torch.bfloat16)[:, :64])
+    apart.quantize(torch.zeros(40, 80, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="d_in"):
+        apart.quantize(torch.zeros(50, 80, dtype=torch.bfloat16)[:, :64])
+    assert len(library.calls) == 6
