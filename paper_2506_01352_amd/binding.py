@@ -419,12 +419,17 @@ def _rows_ptr(t, cols, ld):
     return _dev_ptr(t)
 
 
+_half = None
+
+
 def _check_not_half(where, name, t, dtype):
     """float16 is no bf16, though its elements have the size that _check_tensor asks for (integers and bytes are taken for bf16's bits)."""
-    if dtype == BF16 and t is not None and not isinstance(t, int) and t.element_size() == 2:
+    global _half
+    if _half is None:
         import torch
-        if t.dtype is torch.float16:
-            raise ValueError(f"{where}: {name} is a tensor of {t.dtype}, the configuration says torch.bfloat16")
+        _half = torch.float16
+    if dtype == BF16 and getattr(t, "dtype", None) is _half:
+        raise ValueError(f"{where}: {name} is a tensor of {t.dtype}, the configuration says torch.bfloat16")
 
 
 def _check_rows(where, name, t, rows, cols, ld, dtype):
@@ -508,7 +513,12 @@ def _packed_on(device, rows, cols, transform):
 
 
 def _check_packed(where, name, t, form, size):
-    """A packed matrix that a class is given: bytes enough, and of the form that the buffer carries, if it does."""
+    """A packed matrix that a class is given: of the form that the buffer carries, if it does, and bytes enough."""
+    if getattr(t, "mx4_form", None) != form or t.numel() < size:
+        _check_bytes(where, name, t, form, size)
+
+
+def _check_bytes(where, name, t, form, size):
     if t.element_size() != 1 or t.numel() < size or not t.is_contiguous() or getattr(t, "mx4_form", form) != form:
         raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype}{', packed as ' + str(t.mx4_form) if hasattr(t, 'mx4_form') else ''}: "
                          f"{size} bytes of a packed matrix of (rows, cols, transform) = {form} are needed")
@@ -524,12 +534,16 @@ def _torch_dtype(dtype):
     return torch.float32 if dtype == F32 else torch.bfloat16
 
 
+def _holds(t, rows, cols):
+    return t.numel() == rows * cols and (t.dim() < 2 or t.shape[-1] == cols)
+
+
 def _input_of(where, name, t, rows, cols, dtype):
     """Device address of a class's input: a contiguous device tensor of `dtype`, [.., cols] with `rows` rows in all, or flat.  What a call on a
     few tokens takes is mostly what it costs the host, so the classes look at an input once and keep their own buffers' addresses at hand;
     a single row is the same in any shape."""
-    fits = t.dtype is dtype and t.numel() == rows * cols and t.is_contiguous() and t.is_cuda
-    if not fits or (rows > 1 and t.shape[-1] != cols and t.dim() > 1):
+    if (t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda
+            or (t.numel() != cols if rows == 1 else t.shape != (rows, cols) and not _holds(t, rows, cols))):
         raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype} on {t.device}"
                          f"{'' if t.is_contiguous() else ', not contiguous'}: [{rows}, {cols}] contiguous elements of {dtype} on the GPU are needed")
     return t.data_ptr()
@@ -555,7 +569,7 @@ class Mx4Tensor:
         """Packs a [rows, cols] tensor, one with its rows in several dimensions, or the whole buffer that they lie in, ld elements apart; flat
         buffers and bytes are taken as they are."""
         cfg = self.cfg
-        if not isinstance(d_in, int) and d_in.dim() > 1 and d_in.element_size() > 1:
+        if not isinstance(d_in, int) and d_in.shape != self.out.shape and d_in.dim() > 1 and d_in.element_size() > 1:
             cols = d_in.shape[-1]
             if cols not in (cfg.cols, cfg.ld) or d_in.numel() != cfg.rows * cols:
                 raise ValueError(f"Mx4Tensor.quantize: d_in is a {tuple(d_in.shape)} tensor, the configuration says [{cfg.rows}, {cfg.cols}]")
@@ -576,7 +590,7 @@ class Mx4Linear:
     backward pass.  `weight`: [n, k], fp32 or bf16, which is also the dtype of x, y and their gradients; grad_w is fp32.
     in_flight: micro-batches that go forward before the first of them comes back.  Each has a slot: its own y, and in training its own x
     along its tokens, until the slot's next forward pass.  The other buffers (gradients among them) are the next call's: calls of one layer follow
-    each other, on one stream or ordered by the caller."""
+    each other, on one stream or ordered by the caller, as they do the constructor's packing of W on torch's current stream."""
 
     def __init__(self, weight, tokens, transform=0, scale_rule=MX4_FLOOR, training=False, accumulate=0, in_flight=1):
         import torch
@@ -612,11 +626,15 @@ class Mx4Linear:
         self.workspace = _bytes_on(device, need)
         self._kind = weight.dtype
         self._x_form, self._x_t_form = (((r, c, transform), tahq_mx4_packed_size(r, c)) for r, c in ((tokens, k), (k, tokens)))
-        self._kept = {k: getattr(self, k) for k in ("dy", "dy_t", "weight_t", "workspace")} if training else {}
         self._forward_x_t = [None] * in_flight    # what a slot's last forward pass was of, along its tokens
         self._linear = (C.byref(self._x), C.byref(self._forward))
         self._own = [(self.weight.data_ptr(), self.weight.numel(), y.data_ptr(), self.workspace.data_ptr(), self.workspace.numel())
                      for y in self._ys]
+        if training:
+            self._dy_by_ref, self._dx_by_ref, self._dw_by_ref = C.byref(self._dy), C.byref(self._dx), C.byref(self._dw)
+            self._own_backward = (*((t.data_ptr(), t.numel()) for t in (self.dy, self.dy_t, self.weight_t, self.workspace)),
+                                  self.grad_x.data_ptr(), self.grad_w.data_ptr())
+            self._own_x = [(self.x.data_ptr(), self.x.numel(), x_t.data_ptr(), x_t.numel()) for x_t in self._x_ts]
         self.update(weight)
 
     def update(self, weight, stream=None):
@@ -635,8 +653,11 @@ class Mx4Linear:
                 raise TahqError(rc, "tahq_mx4_linear")
             return self._ys[slot]
         self._forward_x_t[slot] = None
-        tahq_mx4_quantize(self._x, x, self.x, self._x_ts[slot], stream)
-        return self.product(self.x, stream, self._x_ts[slot], slot)
+        handle = _stream_handle(stream)
+        rc = _lib.tahq_mx4_quantize(self._linear[0], d_x, *self._own_x[slot], handle)
+        if rc != 0:
+            raise TahqError(rc, "tahq_mx4_quantize")
+        return self._multiply(self._own_x[0][:2], self._x_ts[slot], handle, slot)
 
     def product(self, x_packed, stream=None, x_packed_t=None, slot=0):
         """y of an x that is packed already, e.g. by BlockNorm.  The backward pass reads the same x packed along its tokens: x_packed_t, which
@@ -646,8 +667,14 @@ class Mx4Linear:
             _check_packed("Mx4Linear.product", "x_packed_t", x_packed_t, *self._x_t_form)
         if slot:
             _check_slot("Mx4Linear.product", slot, self._in_flight)
+        return self._multiply((_dev_ptr(x_packed), x_packed.numel()), x_packed_t, _stream_handle(stream), slot)
+
+    def _multiply(self, x_packed, x_packed_t, handle, slot):
         self._forward_x_t[slot] = None
-        tahq_mx4_matmul(self._forward, x_packed, self.weight, self._ys[slot], self.workspace, stream)
+        weight, weight_size, *y_and_workspace = self._own[slot]
+        rc = _lib.tahq_mx4_matmul(self._linear[1], *x_packed, weight, weight_size, *y_and_workspace, handle)
+        if rc != 0:
+            raise TahqError(rc, "tahq_mx4_matmul")
         self._forward_x_t[slot] = x_packed_t
         return self._ys[slot]
 
@@ -661,15 +688,12 @@ class Mx4Linear:
         if x_t is None:
             raise ValueError("Mx4Linear.backward: there is no x along its tokens: no forward pass, or a product without x_packed_t")
         d_dy = _input_of("Mx4Linear.backward", "grad_y", grad_y, self._dy.rows, self._dy.cols, self._kind)
-        kept = {"x_t": x_t, **self._kept}
-        at, size = {k: _dev_ptr(t) for k, t in kept.items()}, {k: _nbytes(t) for k, t in kept.items()}
+        dy, dy_t, weight_t, workspace, grad_x, grad_w = self._own_backward
         handle = _stream_handle(stream)
         for name, call in (
-                ("tahq_mx4_quantize", (C.byref(self._dy), d_dy, at["dy"], size["dy"], at["dy_t"], size["dy_t"])),
-                ("tahq_mx4_matmul", (C.byref(self._dx), at["dy"], size["dy"], at["weight_t"], size["weight_t"], self.grad_x.data_ptr(),
-                                     at["workspace"], size["workspace"])),
-                ("tahq_mx4_matmul", (C.byref(self._dw), at["dy_t"], size["dy_t"], at["x_t"], size["x_t"], self.grad_w.data_ptr(),
-                                     at["workspace"], size["workspace"]))):
+                ("tahq_mx4_quantize", (self._dy_by_ref, d_dy, *dy, *dy_t)),
+                ("tahq_mx4_matmul", (self._dx_by_ref, *dy, *weight_t, grad_x, *workspace)),
+                ("tahq_mx4_matmul", (self._dw_by_ref, *dy_t, _dev_ptr(x_t), x_t.numel(), grad_w, *workspace))):
             rc = getattr(_lib, name)(*call, handle)
             if rc != 0:
                 raise TahqError(rc, name)
@@ -764,6 +788,7 @@ class BlockNorm:
         # (r', h, statistics) of each slot, and where a call finds them
         self._slots = [(plain(), _packed_on(device, *shape, cfg.transform) if mx4 else plain(),
                         torch.empty(2, cfg.rows, dtype=torch.float32, device=device)) for _ in range(in_flight)]
+        self._results = [(out, h) for out, h, _ in self._slots]
         self.residual_out, self.h, self.stats = self._slots[0]
         self.training = training
         if training:
@@ -796,8 +821,7 @@ class BlockNorm:
             *(self._own if w_pre is not None else self._own_post)[slot], _stream_handle(stream))
         if rc != 0:
             raise TahqError(rc, "tahq_norm_forward")
-        out, h, _ = self._slots[slot]
-        return out, None if w_pre is None else h
+        return self._results[slot] if w_pre is not None else (self._slots[slot][0], None)
 
     def backward(self, grad_residual_out, grad_h, block, w_post, gate, residual_out, w_pre, stats, stream=None):
         """Gradients of residual, block, w_post, gate and w_pre by name; None for what there is not."""
