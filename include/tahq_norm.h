@@ -7,7 +7,8 @@
  *   post half   r' = residual_scale * r + g . (b / RMS(b)) . w_post      b: the block's output, r: the residual stream
  *   pre half    h  = (r' / RMS(r')) . w_pre                              h: the next block's input
  *
- * All of it in fp32 from one read of r and b; r' is rounded when it is stored, h is computed from the unrounded r'.  A
+ * All of it in fp32 from one read of r and b; r' is rounded when it is stored, h is computed from the unrounded r'.  A row whose
+ * mean square is beyond fp32 (values from about 1e19 on) has 1/RMS 0.  A
  * boundary may lie between the halves: without b the post half is r' = residual_scale * r, without w_pre there is no h.
  * h is stored in the tensors' dtype, as a packed mx4 matrix (tahq_mx4.h, blocks along channels, quantized from fp32), or both.
  *

@@ -65,9 +65,9 @@ struct Eight {
     }
 };
 // Rows need no alignment beyond their elements': a 16-byte access may start anywhere.  EIGHTS: rows of whole eights.
-// Elements c .. c + 7 of a row of C, of which the first is there; zeros behind the row's end.  `more`: seven elements behind it can be read, too, as they
-// can in all rows but the last: a row's end then takes no more loads than the rest of it (norms of 16384 x 2047 bf16, which wait for a row's
-// last wavefront: backward 172 -> 118 us, forward 112 -> 84).
+// Elements c .. c + 7 of a row of C, of which the first is there; zeros behind the row's end.  `more`: seven elements behind it can be
+// read, too, as they can in all rows but the last: a row's end then takes no more loads than the rest of it (norms of 16384 x 2047 bf16,
+// which wait for a row's last wavefront: backward 172 -> 118 us, forward 112 -> 84).
 template <bool BF16, bool EIGHTS>
 __device__ __forceinline__ Eight<BF16> fetch(const void *row, uint32_t c, uint32_t C, bool more)
 {

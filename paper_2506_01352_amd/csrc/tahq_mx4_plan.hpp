@@ -12,11 +12,12 @@ inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 // tiles and a long k several runs of it, whose sums are added afterwards.
 constexpr uint32_t kFewRows = 32, kFewQuantRows = 8;
 
-// Time of a product on 256 compute units, in us, with tiles of tm x tn of which `per_cu` are on a compute unit at once: `start` for each that one takes after
-// another, `each` byte of results, and for 256 columns `alone` while a unit has one tile and not all units have one, `loaded` for each tile of a
-// unit's once they have.  (All units at work slow down: 256 x 256 tiles 1.37 -> 1.77 us; the clock gives way.)  Fitted to 253 shapes from
-// 33 x 512 x 512 to 8192^3, both types of C: what it chooses takes 0.4 % longer on average than the best of the six.  The last kind has two teams
-// to a tile: 64 x 8192 x 8192 11.4 -> 9.6 us, 512 x 2048 x 8192 11.1 -> 10.1; two teams for larger tiles and four for these gained nothing more.
+// Time of a product on 256 compute units, in us, with tiles of tm x tn of which `per_cu` are on a compute unit at once: `start` for
+// each that one takes after another, `each` byte of results, and for 256 columns `alone` while a unit has one tile and not all units
+// have one, `loaded` for each tile of a unit's once they have.  (All units at work slow down: 256 x 256 tiles 1.37 -> 1.77 us; the
+// clock gives way.)  Fitted to 166 shapes from 33 x 512 x 512 to 8192^3, of a part of them both types of C: what it chooses takes 0.4 %
+// longer on average than the best of the six.  The last kind has two teams to a tile: 64 x 8192 x 8192 11.4 -> 9.6 us, 512 x 2048 x
+// 8192 11.1 -> 10.1; two teams for larger tiles and four for these gained nothing more.
 struct TileKind {
     uint32_t tm, tn, per_cu;
     float start, alone, loaded;

@@ -101,8 +101,10 @@ __device__ __forceinline__ void store16(void *c, uint64_t at, uint32_t valid, ui
 //   KS: teams of WM * WN wavefronts that share the tile's columns, each with stages of its own, where there are too few tiles for two to a compute
 // unit: one wavefront to a vector unit waits more than it multiplies.
 //   OUT: 0 fp32, 1 bf16, 2 fp32 parts of a sum over k in gridDim.y runs of `run` groups of 256 columns.
-//   Measured, 256 x 256 tiles: 8192 x 8192 x 8192 252 to 278 us, 4.2 PFLOP/s of the 8.7 that the instruction alone reaches; 407 k cycles, in 262 k of
-// which the matrix cores work.  The clock gives way to power: matrices of zeros reach 6.4 PFLOP/s.
+//   Measured, 256 x 256 tiles: 8192 x 8192 x 8192 257 to 295 us, 4.2 PFLOP/s of the 8.7 that the instruction alone reaches.  Two things are
+// lost.  Of 445 k cycles the matrix cores work in 262 k; the others go to starts and ends of four rounds of tiles, about 10 us a round, with nothing
+// beside them on a compute unit, and to waits between stages.  And the clock gives way to power: matrices of zeros take as many cycles, but 186
+// to 192 us, at 2.35 GHz instead of 1.72.
 // Small products wait: 2048 x 1600 x 1600 8.0 us (1.3 PFLOP/s), launch, first loads and last stores being about 4 of them.
 template <int WM, int WN, int MF, int NF, int NB, int KS, int PER_CU, int OUT>
 __global__ __launch_bounds__(64 * WM * WN * KS, PER_CU * KS)
@@ -364,11 +366,13 @@ __device__ __forceinline__ float4v mfma16(const uint4 &b, const uint4 &a, const 
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb, va, c, 4, 4, BYTE, (int)sb, BYTE, (int)sa);
 }
 
-// Up to 16 * MT rows of A: what counts is how fast B streams in.  A workgroup takes 16 * NT rows of B (half a unit, or whole ones); its wavefronts share the
-// columns by groups of 256, ask for several groups before they use the first, and add their sums in LDS.  Bound by memory: 5 x 8192 x 8192 7.7 us,
-// 4.6 TB/s; one token of 1600 x 1600, with its quantization, 2.9 us, a launch's time and one round trip to memory.
-//   QUANT 0: A is packed.  1, 2: A is a tensor of bf16, fp32 with up to 2 * PAIRS <= 16 rows, of which every wavefront quantizes its own
-// columns, 32 lanes to a row of a group, and turns them into operands through LDS that no other wavefront uses.
+// Up to 16 * MT rows of A: what counts is how fast B streams in.  A workgroup takes 16 * NT rows of B (half a unit, or whole ones); its
+// wavefronts share the columns by groups of 256, ask for several groups before they use the first, and add their sums in LDS.  Bound by
+// memory: 5 x 8192 x 8192 10.8 us out of HBM (after a copy of 1 GiB), 3.3 TB/s, of which a launch's start is 2; 7.8 where the last
+// cache still holds the matrix, 4.6 TB/s.  One token of 1600 x 1600, with its quantization, 5.0 and 2.9 us, a launch's time and one
+// round trip to memory.
+//   QUANT 0: A is packed.  1, 2: A is a tensor of bf16, fp32 with up to 2 * PAIRS <= 16 rows, of which every wavefront quantizes its
+// own columns, 32 lanes to a row of a group, and turns them into operands through LDS that no other wavefront uses.
 constexpr int kFewWaves = 8, kFewAhead = 4;
 
 struct FewInput {

@@ -1,8 +1,9 @@
 // Quantization to mx4 along rows, along columns or both from one read, and back.
 //
 // Both are bound by memory: an element takes 2 or 4 bytes to read, 17/32 of a byte to write per orientation, and about ten vector
-// instructions.  bf16 32768 x 8192, tensors of which no cache holds a part: both ways 162 us, back 128, i.e. 5.1 and 5.3 TB/s, as a large copy.  Where a
-// compute unit has one workgroup or two, latency: 2048 x 2047 fp32 with the transform 6.3 and 6.9 us, of which a launch takes 2.
+// instructions.  bf16 32768 x 8192, tensors of which no cache holds a part: both ways 162 us, back 128, i.e. 5.1 and 5.3 TB/s, as a large copy; fp32
+// 16384 x 8192, rotated or not, both ways 125 to 147, back 140.  Where a compute unit has one workgroup or two, latency: 2048 x 2047 fp32 with the
+// transform 6.4 and 6.8 us, of which a launch takes 2; 8.4 and 7.3 out of HBM.
 #pragma once
 #include "tahq_mx4_common.hpp"
 

@@ -49,9 +49,10 @@ void with_kind(const tahq_norm_config *c, bool post, bool pre, Run run)
     else eights ? with_halves<false, true>(post, pre, run) : with_halves<false, false>(post, pre, run);
 }
 
-// Forward: rows that a workgroup takes one after another.  Two where there are many (8192 x 4096, one row: 45 us, two: 42.7, eight: 47); eight where a
-// workgroup of more than twelve wavefronts has a compute unit to itself and only the next row on its way keeps memory busy (2048 x 8192: one
-// 36, two 31, eight 28); one where there are few.  From 2^27 rows on (of few channels) as many more as a launch's 2^32 lanes ask for.
+// Forward: rows that a workgroup takes one after another.  Two where there are many (8192 x 4096, one row: 45 us, two: 42.7, eight:
+// 47); eight where a workgroup of more than twelve wavefronts has a compute unit to itself and only the next row on its way keeps
+// memory busy (2048 x 8192: one 36, two 31, eight 28); one where there are few.  From 2^27 rows on (of few channels) as many more as a
+// launch's 2^32 lanes ask for.
 uint32_t forward_rows(const tahq_norm_config *c, uint32_t rows)
 {
     uint32_t each = waves_of(c) > 12 ? (rows >= 2048 ? 8 : 1) : rows >= 4096 ? 2 : 1;
@@ -59,11 +60,12 @@ uint32_t forward_rows(const tahq_norm_config *c, uint32_t rows)
     return each;
 }
 
-// Backward: the workgroups that share the rows.  A compute unit holds sixteen wavefronts of up to 128 registers, so `most` workgroups at once; more than one
-// round of workgroups of unlike length costs more than it gives (rows side by side: 32768 x 5120, ten wavefronts: 256 workgroups 455 us, 409 534, 512
-// 458; 32768 x 1024, two: 512 152, 1024 111, 2048 101).  What counts below that, in rows of a compute unit: the rows of the unit with most of them, a third of a
-// workgroup's rows, which nobody hides, and a row for every 256 workgroups, whose column sums are added afterwards.  Both kernels, fp32 with one row of
-// a gate, by a workgroup's rows: 777 x 1600 one 20.7 us, four 15.3; 4096 x 1600 four 35.6, eight 31.2, sixteen 33.3; 2331 x 1600 five 22.3, ten 23.7.
+// Backward: the workgroups that share the rows.  A compute unit holds sixteen wavefronts of up to 128 registers, so `most` workgroups
+// at once; more than one round of workgroups of unlike length costs more than it gives (rows side by side: 32768 x 5120, ten
+// wavefronts: 256 workgroups 455 us, 409 534, 512 458; 32768 x 1024, two: 512 152, 1024 111, 2048 101).  What counts below that, in
+// rows of a compute unit: the rows of the unit with most of them, a third of a workgroup's rows, which nobody hides, and a row for
+// every 256 workgroups, whose column sums are added afterwards.  Both kernels, fp32 with one row of a gate, by a workgroup's rows: 777
+// x 1600 one 20.7 us, four 15.3; 4096 x 1600 four 35.6, eight 31.2, sixteen 33.3; 2331 x 1600 five 22.3, ten 23.7.
 struct BackwardPlan {
     uint32_t rows_each, workgroups;
     uint64_t workspace;

@@ -1,10 +1,11 @@
 // The norms before and after a block with its gate and residual scale (include/tahq_norm.h), forward and backward.
 //
 // Bound by memory: four tensors forward (three and 17/32 of a byte an element where h leaves in mx4), six backward, each once.  A
-// workgroup takes a row at a time, eight channels to a lane and no more wavefronts than that needs, so that both of its row sums come from
-// registers; the next row is on its way meanwhile.
-//   Measured, bf16: forward 8192 x 4096 to mx4 with a gate 50 us (219 MB, 4.4 TB/s), one row of 4096 2.9 us, a launch's time; backward 32768 x 5120 385 us
-// (2.0 GB, 5.2 TB/s, as a large copy) and its column sums 10.
+// workgroup takes a row at a time, eight channels to a lane and no more wavefronts than that needs, so that both of its row sums come
+// from registers; the next row is on its way meanwhile.
+//   Measured, bf16: forward 8192 x 4096 to mx4 with a gate 50 us (219 MB, 4.4 TB/s), one row of 4096 2.9 us, a launch's time (5.0 out
+// of HBM); backward 32768 x 5120 386 to 398 us (2.0 GB, 5.1 TB/s, as a large copy) and its column sums 10.  Halves alone, 32768 x 5120:
+// forward post 188, pre 178 (1.0 GB), backward post 252 (1.3 GB), pre without a gradient of r' 214 (1.0 GB).
 #pragma once
 #include "tahq_mx4_common.hpp"
 
@@ -93,13 +94,10 @@ __device__ __forceinline__ void settle(float (&v)[8])
 }
 
 // Forward, elements are rounded operation by operation, in the formulas' order: h is then what unfused operations give, and its codes are, too,
-// but in rows whose sum comes out differently in the last place.  Of 2000 x 4096 fp32 elements 72 % have the same bits; with fused multiply-adds
-// 49 %, and no less time, as memory is waited for.
-__device__ __forceinline__ float rstd_of(float sum, float inv_c, float eps)
-{
-#pragma clang fp contract(off)
-    return rsqrtf(sum * inv_c + eps);
-}
+// but in rows whose sum comes out differently in the last place.  Of 2000 x 4096 fp32 elements 72 % have the same bits; with explicit fused
+// multiply-adds and 1 / sqrt 49 %, and no less time, as memory is waited for.  Against 64 bits both err alike: the rounding that a fused
+// multiply-add saves is given up for equal bits.
+__device__ __forceinline__ float rstd_of(float sum, float inv_c, float eps) { return rsqrtf(sum * inv_c + eps); }
 
 // POST, PRE: whether the halves are there
 template <bool BF16, bool EIGHTS, bool POST, bool PRE>
@@ -153,7 +151,6 @@ void k_norm_forward(const void *residual, const void *block, const void *w_post,
             for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(b[i], b[i], sum);
             rstd_b = rstd_of(group_sum(sum, s.waves, places, turn), inv_c, s.eps);
             if (there) {
-#pragma clang fp contract(off)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = x[i] + b[i] * rstd_b * post[i] * k[i];
             }
