@@ -794,8 +794,9 @@ class BlockNorm:
         if training:
             self.workspace = _bytes_on(device, need)
             self.grad_residual, self.grad_block = (plain() for _ in range(2))
-            self.grad_w_post, self.grad_w_pre = (torch.zeros(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
-            self.grad_gate = torch.zeros(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
+            sums = torch.zeros if cfg.accumulate else torch.empty
+            self.grad_w_post, self.grad_w_pre = (sums(cfg.cols, dtype=torch.float32, device=device) for _ in range(2))
+            self.grad_gate = sums(_gate_groups(cfg), cfg.cols, dtype=torch.float32, device=device) if cfg.gate_rows else None
         self._kind, self._sizes = kind, (cfg.rows, cfg.cols, _gate_groups(cfg))
         self._cfg, self._own, self._own_post = C.byref(cfg), [], []
         for out, h, stats in self._slots:
