@@ -3,7 +3,8 @@
 The work is done by hand-written HIP kernels in libtahq.so behind a C ABI
 (include/tahq.h; include/tahq_naive.h for the backward-pass fixed-point compressor;
 include/tahq_mx4.h and include/tahq_norm.h for what a stage runs next to the codec: microscaled 4-bit
-matrices and their products, and the norms around a block).  This package is argument marshalling only: it hands device
+matrices and their products, the norms around a block, include/tahq_heads.h, include/tahq_dropout.h and include/tahq_loss.h
+for the rest of a training stage: norms and rotation of heads, dropout, the loss over a vocabulary).  This package is argument marshalling only: it hands device
 pointers of torch tensors and the current HIP stream to the library.  There is
 no CPU or PyTorch fallback: if the library is missing, importing the binding's
 functions raises.
@@ -24,4 +25,10 @@ from .binding import (  # noqa: F401
     tahq_mx4_linear_workspace_size, tahq_mx4_linear, Mx4Tensor, Mx4Linear,
     NORM_MAX_COLS, tahq_norm_config, make_norm_config, tahq_norm_config_default, tahq_norm_workspace_size,
     tahq_norm_forward, tahq_norm_backward, BlockNorm,
+    tahq_dropout_config, make_dropout_config, tahq_dropout_config_default, tahq_dropout_forward, tahq_dropout_backward, Dropout,
+    HEADS_HALVES, HEADS_PAIRS, HEADS_MAX, ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_STRETCHED, ROTARY_PARTS,
+    tahq_heads_config, make_heads_config, tahq_heads_config_default, tahq_rotary_config, make_rotary_config, tahq_rotary_config_default,
+    tahq_rotary_frequencies, tahq_heads_forward, tahq_heads_workspace_size, tahq_heads_backward, HeadRotary,
+    LOSS_NONE, LOSS_SUM, LOSS_MEAN, LOSS_MAX_COLS, tahq_loss_config, make_loss_config, tahq_loss_config_default,
+    tahq_loss_forward_workspace_size, tahq_loss_backward_workspace_size, tahq_loss_forward, tahq_loss_backward, LinearLoss,
 )

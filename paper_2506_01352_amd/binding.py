@@ -48,6 +48,26 @@ class tahq_norm_config(C.Structure):
     ]
 
 
+class tahq_dropout_config(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("elements", C.c_uint64), ("seed", C.c_uint64), ("offset", C.c_uint64),
+                ("p", C.c_float)]
+
+
+class tahq_heads_config(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "tokens", "q_heads", "k_heads", "head", "rotated", "layout", "dtype", "norm",
+                                          "accumulate", "ldq", "ldk", "ldq_out", "ldk_out")] + [("eps", C.c_float), ("magnitude", C.c_float)]
+
+
+class tahq_rotary_config(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "rotated", "scaling", "original")] + [
+        (n, C.c_double) for n in ("base", "factor", "low", "high")]
+
+
+class tahq_loss_config(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("struct_size", "rows", "cols", "vocab", "dtype", "weight_dtype", "reduction", "accumulate")] + [
+        ("ignore", C.c_int64)]
+
+
 _lib = None
 
 
@@ -112,6 +132,7 @@ def _load():
     L.tahq_naive_decode.restype = C.c_int
     L.tahq_naive_decode.argtypes = [PN, C.c_void_p, C.c_size_t, C.c_void_p, C.c_uint32, C.c_void_p]
     V, Z, PX, PM, PB = C.c_void_p, C.c_size_t, C.POINTER(tahq_mx4_config), C.POINTER(tahq_mx4_matmul_config), C.POINTER(tahq_norm_config)
+    PD, PH, PR, PL = (C.POINTER(c) for c in (tahq_dropout_config, tahq_heads_config, tahq_rotary_config, tahq_loss_config))
     for name, result, arguments in (
             ("tahq_mx4_config_default", None, [PX]),
             ("tahq_mx4_packed_size", Z, [C.c_uint32, C.c_uint32]),
@@ -125,7 +146,21 @@ def _load():
             ("tahq_norm_config_default", None, [PB]),
             ("tahq_norm_forward", C.c_int, [PB, V, V, V, V, V, V, V, V, Z, V, V]),
             ("tahq_norm_workspace_size", Z, [PB]),
-            ("tahq_norm_backward", C.c_int, [PB] + [V] * 14 + [Z, V])):
+            ("tahq_norm_backward", C.c_int, [PB] + [V] * 14 + [Z, V]),
+            ("tahq_dropout_config_default", None, [PD]),
+            ("tahq_dropout_forward", C.c_int, [PD] + [V] * 5),
+            ("tahq_dropout_backward", C.c_int, [PD] + [V] * 4),
+            ("tahq_heads_config_default", None, [PH]),
+            ("tahq_rotary_config_default", None, [PR]),
+            ("tahq_rotary_frequencies", C.c_int, [PR, V]),
+            ("tahq_heads_forward", C.c_int, [PH] + [V] * 9),
+            ("tahq_heads_workspace_size", Z, [PH]),
+            ("tahq_heads_backward", C.c_int, [PH] + [V] * 13 + [Z, V]),
+            ("tahq_loss_config_default", None, [PL]),
+            ("tahq_loss_forward_workspace_size", Z, [PL]),
+            ("tahq_loss_backward_workspace_size", Z, [PL]),
+            ("tahq_loss_forward", C.c_int, [PL] + [V] * 7 + [Z, V]),
+            ("tahq_loss_backward", C.c_int, [PL] + [V] * 8 + [Z, V])):
         f = getattr(L, name)
         f.restype, f.argtypes = result, arguments
     _lib = L
@@ -847,3 +882,472 @@ class BlockNorm:
         if rc != 0:
             raise TahqError(rc, "tahq_norm_backward")
         return got
+
+
+# ---- what the operators below share
+
+def _placed(where, name, t, dtype, device):
+    """A class's tensor is of the type that its configuration says and on the class's device, which is the current one: kernels are enqueued on a
+    stream of the current device."""
+    import torch
+    if t.dtype is not dtype or t.device != device or torch.cuda.current_device() != device.index:
+        raise ValueError(f"{where}: {name} is a tensor of {t.dtype} on {t.device}, {dtype} on {device} is needed, and that to be the current device "
+                         f"(cuda:{torch.cuda.current_device()})")
+
+
+def _whole(where, name, t, elements, dtype, device):
+    """Device address of a contiguous tensor of so many elements, in any shape."""
+    _placed(where, name, t, dtype, device)
+    if t.numel() != elements or not t.is_contiguous():
+        raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor{'' if t.is_contiguous() else ', not contiguous'}: {elements} contiguous elements are needed")
+    return t.data_ptr()
+
+
+def _matrix(where, name, t, rows, cols, dtype, device):
+    """Device address of a contiguous [.., cols] tensor with `rows` rows in all, or a flat one."""
+    at = _whole(where, name, t, rows * cols, dtype, device)
+    if t.dim() > 1 and t.shape[-1] != cols:
+        raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor, [{rows}, {cols}] is needed")
+    return at
+
+
+def _device_of(device):
+    import torch
+    device = torch.device(device)
+    return torch.device(device.type, torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
+
+
+# ---- dropout (include/tahq_dropout.h)
+
+def tahq_dropout_config_default():
+    cfg = tahq_dropout_config()
+    _load().tahq_dropout_config_default(C.byref(cfg))
+    return cfg
+
+
+def make_dropout_config(elements, dtype, p, seed=0, offset=0):
+    cfg = tahq_dropout_config_default()
+    cfg.elements, cfg.dtype, cfg.p, cfg.seed, cfg.offset = elements, dtype, p, seed, offset
+    return cfg
+
+
+def _check_offset(where, t):
+    if t is not None and not isinstance(t, int) and (t.element_size() != 8 or t.numel() < 1):
+        raise ValueError(f"{where}: d_offset is a {tuple(t.shape)} tensor of {t.dtype}, a 64-bit number is needed")
+
+
+def tahq_dropout_forward(cfg, d_x, d_residual, d_out, d_offset=None, stream=None):
+    """out = residual + dropped(x); d_residual may be None."""
+    for name, t in (("d_x", d_x), ("d_residual", d_residual), ("d_out", d_out)):
+        _check_not_half("tahq_dropout_forward", name, t, cfg.dtype)
+        _check_tensor("tahq_dropout_forward", name, t, cfg.elements, cfg.dtype)
+    _check_offset("tahq_dropout_forward", d_offset)
+    rc = (_lib or _load()).tahq_dropout_forward(C.byref(cfg), _dev_ptr(d_x), _dev_ptr(d_residual), _dev_ptr(d_out), _dev_ptr(d_offset), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_dropout_forward")
+
+
+def tahq_dropout_backward(cfg, d_grad_out, d_grad_x, d_offset=None, stream=None):
+    for name, t in (("d_grad_out", d_grad_out), ("d_grad_x", d_grad_x)):
+        _check_not_half("tahq_dropout_backward", name, t, cfg.dtype)
+        _check_tensor("tahq_dropout_backward", name, t, cfg.elements, cfg.dtype)
+    _check_offset("tahq_dropout_backward", d_offset)
+    rc = (_lib or _load()).tahq_dropout_backward(C.byref(cfg), _dev_ptr(d_grad_out), _dev_ptr(d_grad_x), _dev_ptr(d_offset), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, "tahq_dropout_backward")
+
+
+class Dropout:
+    """Dropout of one tensor of the stage, with or without the residual that it is added to.  Every forward pass takes the next offset, from
+    cfg.offset on, unless it is given one; a slot's backward pass takes that of the slot's last forward pass.
+    in_flight: micro-batches that go forward before the first of them comes back; each has a slot with an output of its own.  The gradient is the next
+    backward call's.
+    graph_offset: a tensor of one int64 on the device that is added to the offset when a kernel runs: a program that captures passes into a graph
+    changes it between replays (between a forward pass and its backward pass not)."""
+
+    def __init__(self, cfg, device="cuda:0", in_flight=1, graph_offset=None):
+        import torch
+        _check_slot("Dropout", 0, in_flight)
+        self.cfg, self.device, self._kind = cfg, _device_of(device), _torch_dtype(cfg.dtype)
+        self._graph = None if graph_offset is None else _whole("Dropout", "graph_offset", graph_offset, 1, torch.int64, self.device)
+        self.graph_offset = graph_offset
+        self._outs = [torch.empty(cfg.elements, dtype=self._kind, device=device) for _ in range(in_flight)]
+        self._grad = torch.empty(cfg.elements, dtype=self._kind, device=device)
+        self._next, self._offsets = cfg.offset, [None] * in_flight
+        self._views = {}
+
+    def _call(self, where, offset, *arguments):
+        cfg = self.cfg
+        call = tahq_dropout_config(cfg.struct_size, cfg.dtype, cfg.elements, cfg.seed, offset % (1 << 64), cfg.p)
+        rc = getattr(_lib or _load(), where)(C.byref(call), *arguments)
+        if rc != 0:
+            raise TahqError(rc, where)
+
+    def _shaped(self, t, like):
+        """A buffer in the shape of what it is made from: the same view as long as shapes do not change."""
+        key = (t.data_ptr(), like.shape)
+        view = self._views.get(key)
+        if view is None:
+            if len(self._views) > 64:
+                self._views.clear()
+            view = self._views[key] = t.view(like.shape)
+        return view
+
+    def forward(self, x, residual=None, stream=None, slot=0, offset=None):
+        _check_slot("Dropout.forward", slot, len(self._outs))
+        d_x = _whole("Dropout.forward", "x", x, self.cfg.elements, self._kind, self.device)
+        d_residual = None if residual is None else _whole("Dropout.forward", "residual", residual, self.cfg.elements, self._kind, self.device)
+        used = self._next if offset is None else offset
+        self._offsets[slot] = None
+        out = self._outs[slot]
+        self._call("tahq_dropout_forward", used, d_x, d_residual, out.data_ptr(), self._graph, _stream_handle(stream))
+        if offset is None:
+            self._next += 1
+        self._offsets[slot] = used
+        return self._shaped(out, x)
+
+    def backward(self, grad_out, stream=None, slot=0, offset=None):
+        """Gradient of x; the residual's is grad_out."""
+        _check_slot("Dropout.backward", slot, len(self._outs))
+        used = self._offsets[slot] if offset is None else offset
+        if used is None:
+            raise ValueError("Dropout.backward: the slot has had no forward pass, and no offset is given")
+        d_grad = _whole("Dropout.backward", "grad_out", grad_out, self.cfg.elements, self._kind, self.device)
+        self._call("tahq_dropout_backward", used, d_grad, self._grad.data_ptr(), self._graph, _stream_handle(stream))
+        return self._shaped(self._grad, grad_out)
+
+
+# ---- norms and rotation of heads (include/tahq_heads.h)
+
+HEADS_HALVES, HEADS_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_STRETCHED, ROTARY_PARTS = 0, 1, 2, 3
+HEADS_MAX = 512
+
+
+def tahq_heads_config_default():
+    cfg = tahq_heads_config()
+    _load().tahq_heads_config_default(C.byref(cfg))
+    return cfg
+
+
+def make_heads_config(tokens, q_heads, k_heads, head, rotated, dtype, layout=HEADS_HALVES, norm=1, eps=1e-6, magnitude=1.0, accumulate=0,
+                      ldq=0, ldk=0, ldq_out=0, ldk_out=0):
+    cfg = tahq_heads_config_default()
+    cfg.tokens, cfg.q_heads, cfg.k_heads, cfg.head, cfg.rotated, cfg.dtype = tokens, q_heads, k_heads, head, rotated, dtype
+    cfg.layout, cfg.norm, cfg.eps, cfg.magnitude, cfg.accumulate = layout, norm, eps, magnitude, accumulate
+    cfg.ldq, cfg.ldk, cfg.ldq_out, cfg.ldk_out = ldq, ldk, ldq_out, ldk_out
+    return cfg
+
+
+def tahq_rotary_config_default():
+    cfg = tahq_rotary_config()
+    _load().tahq_rotary_config_default(C.byref(cfg))
+    return cfg
+
+
+def make_rotary_config(rotated, base=10000.0, scaling=ROTARY_PLAIN, factor=1.0, original=4096, low=1.0, high=32.0):
+    cfg = tahq_rotary_config_default()
+    cfg.rotated, cfg.base, cfg.scaling, cfg.factor, cfg.original, cfg.low, cfg.high = rotated, base, scaling, factor, original, low, high
+    return cfg
+
+
+def tahq_rotary_frequencies(cfg):
+    """Turns per position in units of 2^-64, one int for each pair."""
+    out = (C.c_uint64 * max(cfg.rotated // 2, 1))()
+    rc = _load().tahq_rotary_frequencies(C.byref(cfg), out)
+    if rc != 0:
+        raise TahqError(rc, "tahq_rotary_frequencies")
+    return list(out)
+
+
+def _heads_ptr(where, name, t, tokens, heads, head, ld, dtype):
+    """Device address of [tokens, heads, head] (or [tokens, heads * head]) elements whose tokens lie `ld` apart (0: heads * head): a contiguous tensor
+    of at least as many, or a view with these strides."""
+    if t is None or isinstance(t, int):
+        return t
+    ld = ld or heads * head
+    _check_not_half(where, name, t, dtype)
+    if t.is_contiguous() and (t.dim() < 2 or t.shape[0] != tokens or ld == heads * head):
+        _check_tensor(where, name, t, (tokens - 1) * ld + heads * head if tokens else 0, dtype)
+        return _dev_ptr(t)
+    shape, strides = ((tokens, heads, head), (ld, head, 1)) if t.dim() == 3 else ((tokens, heads * head), (ld, 1))
+    fits = t.is_cuda and tuple(t.shape) == shape and all(n == 1 or a == b for n, a, b in zip(shape, t.stride(), strides))
+    if not fits or t.element_size() != _ESIZE.get(dtype, t.element_size()):
+        raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype} with strides {tuple(t.stride())}, the configuration says "
+                         f"{shape} with {strides}")
+    return t.data_ptr()
+
+
+def _heads_tables(where, cfg, tensors):
+    for name, t, elements, size in tensors:
+        if t is None or isinstance(t, int):
+            continue
+        if t.element_size() != size or t.numel() < elements:
+            raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype}, {elements} elements of {size} bytes are needed")
+    return [_dev_ptr(t) for _, t, _, _ in tensors]
+
+
+def tahq_heads_forward(cfg, d_q, d_k, d_w_q, d_w_k, d_positions, d_frequencies, d_q_out, d_k_out, stream=None):
+    where, size = "tahq_heads_forward", _ESIZE.get(cfg.dtype, 1)
+    for name, t in (("d_w_q", d_w_q), ("d_w_k", d_w_k)):
+        _check_not_half(where, name, t, cfg.dtype)
+    tables = _heads_tables(where, cfg, (("d_w_q", d_w_q, cfg.head, size), ("d_w_k", d_w_k, cfg.head, size), ("d_positions", d_positions, cfg.tokens, 8),
+                                        ("d_frequencies", d_frequencies, cfg.rotated // 2, 8)))
+    rc = (_lib or _load()).tahq_heads_forward(
+        C.byref(cfg), _heads_ptr(where, "d_q", d_q, cfg.tokens, cfg.q_heads, cfg.head, cfg.ldq, cfg.dtype),
+        _heads_ptr(where, "d_k", d_k, cfg.tokens, cfg.k_heads, cfg.head, cfg.ldk, cfg.dtype), *tables,
+        _heads_ptr(where, "d_q_out", d_q_out, cfg.tokens, cfg.q_heads, cfg.head, cfg.ldq_out, cfg.dtype),
+        _heads_ptr(where, "d_k_out", d_k_out, cfg.tokens, cfg.k_heads, cfg.head, cfg.ldk_out, cfg.dtype), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, where)
+
+
+def tahq_heads_workspace_size(cfg):
+    return int(_load().tahq_heads_workspace_size(C.byref(cfg)))
+
+
+def tahq_heads_backward(cfg, d_grad_q_out, d_grad_k_out, d_q, d_k, d_w_q, d_w_k, d_positions, d_frequencies, d_grad_q, d_grad_k, d_grad_w_q,
+                        d_grad_w_k, d_workspace, stream=None):
+    where, size = "tahq_heads_backward", _ESIZE.get(cfg.dtype, 1)
+    for name, t in (("d_w_q", d_w_q), ("d_w_k", d_w_k)):
+        _check_not_half(where, name, t, cfg.dtype)
+    tables = _heads_tables(where, cfg, (("d_w_q", d_w_q, cfg.head, size), ("d_w_k", d_w_k, cfg.head, size), ("d_positions", d_positions, cfg.tokens, 8),
+                                        ("d_frequencies", d_frequencies, cfg.rotated // 2, 8)))
+    sums = _heads_tables(where, cfg, (("d_grad_w_q", d_grad_w_q, cfg.head, 4), ("d_grad_w_k", d_grad_w_k, cfg.head, 4)))
+
+    def queries(name, t, ld):
+        return _heads_ptr(where, name, t, cfg.tokens, cfg.q_heads, cfg.head, ld, cfg.dtype)
+
+    def keys(name, t, ld):
+        return _heads_ptr(where, name, t, cfg.tokens, cfg.k_heads, cfg.head, ld, cfg.dtype)
+
+    rc = (_lib or _load()).tahq_heads_backward(
+        C.byref(cfg), queries("d_grad_q_out", d_grad_q_out, cfg.ldq_out), keys("d_grad_k_out", d_grad_k_out, cfg.ldk_out), queries("d_q", d_q, cfg.ldq),
+        keys("d_k", d_k, cfg.ldk), *tables, queries("d_grad_q", d_grad_q, cfg.ldq), keys("d_grad_k", d_grad_k, cfg.ldk), *sums, _dev_ptr(d_workspace),
+        _nbytes(d_workspace), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, where)
+
+
+class HeadRotary:
+    """Norm and rotation of a stage's queries and keys.  cfg: of make_heads_config; rotary: of make_rotary_config, whose frequencies are put into
+    device memory once (None if nothing is rotated).  Tensors are [tokens, heads, head], or [tokens, heads * head], with the configuration's strides; keys
+    are None where there are none, weights where there are no norms.
+    in_flight: micro-batches that go forward before the first of them comes back; each has a slot with outputs of its own.  The norms' weights'
+    gradients, and the gradients of queries and keys where the call is given no place for them, are the next backward call's."""
+
+    def __init__(self, cfg, rotary=None, device="cuda:0", training=True, in_flight=1):
+        import torch
+        _check_slot("HeadRotary", 0, in_flight)
+        if (rotary.rotated if rotary is not None else 0) != cfg.rotated:
+            raise ValueError(f"HeadRotary: {rotary.rotated if rotary is not None else 0} rotated channels in the frequencies' configuration, {cfg.rotated} in the heads'")
+        self.cfg, self.device, self._kind, self.training = cfg, _device_of(device), _torch_dtype(cfg.dtype), training
+        self.frequencies = None
+        if rotary is not None:
+            signed = [f - (1 << 64) if f >> 63 else f for f in tahq_rotary_frequencies(rotary)]
+            self.frequencies = torch.tensor(signed, dtype=torch.int64).to(device)
+        if training and cfg.norm and not tahq_heads_workspace_size(cfg):
+            raise TahqError(2, "tahq_heads_workspace_size")
+
+        def buffer(heads, ld):
+            """[tokens, heads, head] with tokens ld apart"""
+            wide = torch.empty(cfg.tokens, ld or heads * cfg.head, dtype=self._kind, device=device)
+            return wide[:, :heads * cfg.head].unflatten(1, (heads, cfg.head)) if heads else None
+
+        self._outs = [(buffer(cfg.q_heads, cfg.ldq_out), buffer(cfg.k_heads, cfg.ldk_out)) for _ in range(in_flight)]
+        self.q, self.k = self._outs[0]
+        self._own = [tuple(None if t is None else t.data_ptr() for t in out) for out in self._outs]
+        self._cfg = C.byref(cfg)
+        if training:
+            # rows of a packed projection are the caller's to give
+            self._grads = (buffer(cfg.q_heads, cfg.ldq), buffer(cfg.k_heads, cfg.ldk)) if not cfg.ldq and not cfg.ldk else None
+            self.workspace = _bytes_on(device, tahq_heads_workspace_size(cfg))
+            sums = torch.zeros if cfg.accumulate else torch.empty
+            self.grad_w_q = sums(cfg.head, dtype=torch.float32, device=device) if cfg.norm else None
+            self.grad_w_k = sums(cfg.head, dtype=torch.float32, device=device) if cfg.norm and cfg.k_heads else None
+
+    def _queries(self, where, name, t, heads, ld):
+        if t is None:
+            return None
+        _placed(where, name, t, self._kind, self.device)
+        cfg = self.cfg
+        if tuple(t.shape) not in ((cfg.tokens, heads, cfg.head), (cfg.tokens, heads * cfg.head)):
+            raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor, [{cfg.tokens}, {heads}, {cfg.head}] is needed")
+        return _heads_ptr(where, name, t, cfg.tokens, heads, cfg.head, ld, cfg.dtype)
+
+    def _tables(self, where, w_q, w_k, positions):
+        import torch
+        cfg = self.cfg
+        weights = [None if w is None else _whole(where, name, w, cfg.head, self._kind, self.device) for name, w in (("w_q", w_q), ("w_k", w_k))]
+        return (*weights, None if positions is None else _whole(where, "positions", positions, cfg.tokens, torch.int64, self.device),
+                None if self.frequencies is None else self.frequencies.data_ptr())
+
+    def forward(self, q, k, w_q, w_k, positions, stream=None, slot=0, out=None):
+        """(q, k) normed and rotated: the slot's, or `out`, which may be q and k themselves if strides are the same."""
+        where, cfg = "HeadRotary.forward", self.cfg
+        _check_slot(where, slot, len(self._outs))
+        to = self._own[slot] if out is None else (self._queries(where, "out[0]", out[0], cfg.q_heads, cfg.ldq_out),
+                                                  self._queries(where, "out[1]", out[1], cfg.k_heads, cfg.ldk_out))
+        rc = (_lib or _load()).tahq_heads_forward(self._cfg, self._queries(where, "q", q, cfg.q_heads, cfg.ldq), self._queries(where, "k", k, cfg.k_heads, cfg.ldk),
+                                                  *self._tables(where, w_q, w_k, positions), *to, _stream_handle(stream))
+        if rc != 0:
+            raise TahqError(rc, "tahq_heads_forward")
+        return self._outs[slot] if out is None else out
+
+    def backward(self, grad_q, grad_k, q, k, w_q, w_k, positions, stream=None, out=None):
+        """Gradients of q, k, w_q and w_k by name, None for what there is not, from those of the outputs.  q, k, w_q, w_k and positions are the forward
+        pass's (without norms q and k may be None); `out`: where the gradients of q and k go, with the strides of q and k."""
+        where, cfg = "HeadRotary.backward", self.cfg
+        if not self.training:
+            raise ValueError("HeadRotary.backward: the class was not made with training=True")
+        to = self._grads if out is None else out
+        if to is None:
+            raise ValueError("HeadRotary.backward: the configuration's q and k have strides of their own: give the gradients' places, out=(grad_q, grad_k)")
+        if not cfg.norm:
+            q = k = w_q = w_k = None
+        rc = (_lib or _load()).tahq_heads_backward(
+            self._cfg, self._queries(where, "grad_q", grad_q, cfg.q_heads, cfg.ldq_out), self._queries(where, "grad_k", grad_k, cfg.k_heads, cfg.ldk_out),
+            self._queries(where, "q", q, cfg.q_heads, cfg.ldq), self._queries(where, "k", k, cfg.k_heads, cfg.ldk),
+            *self._tables(where, w_q, w_k, positions), self._queries(where, "out[0]", to[0], cfg.q_heads, cfg.ldq),
+            self._queries(where, "out[1]", to[1], cfg.k_heads, cfg.ldk), *(None if t is None else t.data_ptr() for t in (self.grad_w_q, self.grad_w_k)),
+            self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))
+        if rc != 0:
+            raise TahqError(rc, "tahq_heads_backward")
+        return {"grad_q": to[0], "grad_k": to[1], "grad_w_q": self.grad_w_q, "grad_w_k": self.grad_w_k}
+
+
+# ---- loss over a vocabulary (include/tahq_loss.h)
+
+LOSS_NONE, LOSS_SUM, LOSS_MEAN = 0, 1, 2
+LOSS_MAX_COLS = 65536
+
+
+def tahq_loss_config_default():
+    cfg = tahq_loss_config()
+    _load().tahq_loss_config_default(C.byref(cfg))
+    return cfg
+
+
+def make_loss_config(rows, cols, vocab, dtype, weight_dtype=None, reduction=LOSS_MEAN, ignore=-100, accumulate=0):
+    """weight_dtype: of the weight's gradient, the tensors' own if None."""
+    cfg = tahq_loss_config_default()
+    cfg.rows, cfg.cols, cfg.vocab, cfg.dtype, cfg.weight_dtype = rows, cols, vocab, dtype, dtype if weight_dtype is None else weight_dtype
+    cfg.reduction, cfg.ignore, cfg.accumulate = reduction, ignore, accumulate
+    return cfg
+
+
+def tahq_loss_forward_workspace_size(cfg):
+    return int(_load().tahq_loss_forward_workspace_size(C.byref(cfg)))
+
+
+def tahq_loss_backward_workspace_size(cfg):
+    return int(_load().tahq_loss_backward_workspace_size(C.byref(cfg)))
+
+
+def _check_loss(where, cfg, tensors, targets, floats):
+    for name, t, elements, dtype in tensors:
+        _check_not_half(where, name, t, dtype)
+        _check_tensor(where, name, t, elements, dtype)
+    if targets is not None and not isinstance(targets, int) and (targets.element_size() != 8 or targets.numel() < cfg.rows):
+        raise ValueError(f"{where}: d_target is a {tuple(targets.shape)} tensor of {targets.dtype}, {cfg.rows} int64 are needed")
+    for name, t, elements in floats:
+        _check_tensor(where, name, t, elements, F32)
+
+
+def tahq_loss_forward(cfg, d_x, d_weight, d_target, d_losses, d_lse, d_total, d_workspace, stream=None):
+    where = "tahq_loss_forward"
+    _check_loss(where, cfg, (("d_x", d_x, cfg.rows * cfg.cols, cfg.dtype), ("d_weight", d_weight, cfg.vocab * cfg.cols, cfg.dtype)), d_target,
+                (("d_losses", d_losses, cfg.rows), ("d_lse", d_lse, cfg.rows), ("d_total", d_total, 2)))
+    rc = (_lib or _load()).tahq_loss_forward(C.byref(cfg), *(_dev_ptr(t) for t in (d_x, d_weight, d_target, d_losses, d_lse, d_total, d_workspace)),
+                                             _nbytes(d_workspace), _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, where)
+
+
+def tahq_loss_backward(cfg, d_x, d_weight, d_target, d_lse, d_grad_loss, d_grad_x, d_grad_weight, d_workspace, stream=None):
+    where = "tahq_loss_backward"
+    _check_loss(where, cfg, (("d_x", d_x, cfg.rows * cfg.cols, cfg.dtype), ("d_weight", d_weight, cfg.vocab * cfg.cols, cfg.dtype),
+                             ("d_grad_x", d_grad_x, cfg.rows * cfg.cols, cfg.dtype),
+                             ("d_grad_weight", d_grad_weight, cfg.vocab * cfg.cols, cfg.weight_dtype)), d_target,
+                (("d_lse", d_lse, cfg.rows), ("d_grad_loss", d_grad_loss, cfg.rows if cfg.reduction == LOSS_NONE else 1)))
+    rc = (_lib or _load()).tahq_loss_backward(
+        C.byref(cfg), *(_dev_ptr(t) for t in (d_x, d_weight, d_target, d_lse, d_grad_loss, d_grad_x, d_grad_weight, d_workspace)), _nbytes(d_workspace),
+        _stream_handle(stream))
+    if rc != 0:
+        raise TahqError(rc, where)
+
+
+class LinearLoss:
+    """The loss of hidden states [rows, cols] against a vocabulary's weight [vocab, cols], and its gradients, on buffers of its own.  All are made, and
+    a gradient that is added to cleared, on torch's current stream: a call on another stream comes after that stream has waited for it.
+    training: with the buffers of the backward pass; frozen: of the hidden states' gradient alone.
+    in_flight: micro-batches that go forward before the first of them comes back; each has a slot with losses and statistics of its own.  Gradients and
+    workspace are the next call's: calls of one object follow each other."""
+
+    def __init__(self, cfg, device="cuda:0", training=True, frozen=False, in_flight=1):
+        import torch
+        _check_slot("LinearLoss", 0, in_flight)
+        need = tahq_loss_forward_workspace_size(cfg)
+        if need == 0:
+            raise TahqError(2, "tahq_loss_forward_workspace_size")
+        self.cfg, self.device, self._kind, self.training = cfg, _device_of(device), _torch_dtype(cfg.dtype), training
+
+        def floats(n):
+            return torch.empty(n, dtype=torch.float32, device=device)
+
+        # (losses, log-sum-exps, reduced loss and number of tokens) of each slot
+        self._slots = [(floats(cfg.rows), floats(cfg.rows), floats(2)) for _ in range(in_flight)]
+        self._results = [slot[0] if cfg.reduction == LOSS_NONE else slot[2][:1] for slot in self._slots]
+        self.losses, self.lse, self.total = self._slots[0]
+        self._own = [tuple(t.data_ptr() for t in slot) for slot in self._slots]
+        self._done = [False] * in_flight
+        self.grad_x = self.grad_weight = None
+        if training:
+            need = max(need, tahq_loss_backward_workspace_size(cfg))
+            self.grad_x = torch.empty(cfg.rows, cfg.cols, dtype=self._kind, device=device)
+            if not frozen:
+                sums = torch.zeros if cfg.accumulate else torch.empty
+                self.grad_weight = sums(cfg.vocab, cfg.cols, dtype=_torch_dtype(cfg.weight_dtype), device=device)
+        self.workspace = _bytes_on(device, need)
+        self._cfg = C.byref(cfg)
+
+    def of(self, slot):
+        """(losses, log-sum-exps, [reduced loss, number of tokens that count]) of a slot's last forward pass."""
+        _check_slot("LinearLoss.of", slot, len(self._slots))
+        return self._slots[slot]
+
+    def _inputs(self, where, x, weight, target):
+        import torch
+        cfg = self.cfg
+        return (_matrix(where, "x", x, cfg.rows, cfg.cols, self._kind, self.device), _matrix(where, "weight", weight, cfg.vocab, cfg.cols, self._kind, self.device),
+                _whole(where, "target", target, cfg.rows, torch.int64, self.device))
+
+    def forward(self, x, weight, target, stream=None, slot=0):
+        """The reduced loss, a tensor of one element; with LOSS_NONE every token's."""
+        _check_slot("LinearLoss.forward", slot, len(self._slots))
+        inputs = self._inputs("LinearLoss.forward", x, weight, target)
+        self._done[slot] = False
+        rc = (_lib or _load()).tahq_loss_forward(self._cfg, *inputs, *self._own[slot], self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))
+        if rc != 0:
+            raise TahqError(rc, "tahq_loss_forward")
+        self._done[slot] = True
+        return self._results[slot]
+
+    def backward(self, x, weight, target, grad_loss=None, stream=None, slot=0):
+        """(gradient of x, gradient of the weight or None) of the slot's last forward pass, which was of the same x, weight and target.  grad_loss:
+        float, that of the reduced loss (of every token with LOSS_NONE); None: ones."""
+        _check_slot("LinearLoss.backward", slot, len(self._slots))
+        if not self.training:
+            raise ValueError("LinearLoss.backward: the loss was not made with training=True")
+        if not self._done[slot]:
+            raise ValueError("LinearLoss.backward: the slot has had no forward pass")
+        import torch
+        where, cfg = "LinearLoss.backward", self.cfg
+        inputs = self._inputs(where, x, weight, target)
+        d_grad = None if grad_loss is None else _whole(where, "grad_loss", grad_loss, cfg.rows if cfg.reduction == LOSS_NONE else 1, torch.float32, self.device)
+        rc = (_lib or _load()).tahq_loss_backward(
+            self._cfg, *inputs, self._own[slot][1], d_grad, self.grad_x.data_ptr(), None if self.grad_weight is None else self.grad_weight.data_ptr(),
+            self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))
+        if rc != 0:
+            raise TahqError(rc, "tahq_loss_backward")
+        return self.grad_x, self.grad_weight

@@ -1,0 +1,335 @@
+// Heads of queries and keys, normed and rotated (include/tahq_heads.h), forward and backward.
+//
+// Bound by memory: forward two tensors, backward three, each once.  A wavefront takes a token at a time and several of its heads side by side, a
+// group of `lanes` lanes to a head.  A lane holds both channels of each of its pairs, so that rotations stay within it, and the same channels of
+// every head, so that it works out its angles once for a token.
+#pragma once
+#include "tahq_heads.h"
+#include "tahq_lanes.hpp"
+#include "tahq_mx4_common.hpp"
+
+namespace tahq {
+
+struct HeadShape {
+    uint32_t tokens, heads[2], head, rotated, lanes, splits;    // heads: of queries, of keys; splits: wavefronts that share a token's heads
+    uint64_t ld[2], ld_out[2];
+    float eps, magnitude;
+};
+struct HeadTensors {                         // queries', keys'
+    const void *of[2];
+};
+struct HeadOutputs {
+    void *of[2];
+};
+constexpr uint32_t kHeadWaves = 4;           // of a workgroup
+
+// cos and sin of a fraction of a turn in units of 2^-32.  The nearest quarter turn is taken off, exactly; what is left, up to pi/4, goes into
+// the sums' first terms: the next ones are below 2^-28 of the result.
+__device__ __forceinline__ void cos_sin(uint32_t turn, float &c, float &s)
+{
+    const uint32_t quarter = (turn + 0x20000000u) >> 30;
+    const float t = (float)(int)(turn - (quarter << 30)) * 1.4629180792671596e-09f;       // 2 pi / 2^32
+    const float x = t * t;
+    const float sine = __builtin_fmaf(t * x, __builtin_fmaf(x, __builtin_fmaf(x, __builtin_fmaf(x, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f), t);
+    const float cosine = __builtin_fmaf(x, __builtin_fmaf(x, __builtin_fmaf(x, __builtin_fmaf(x, __builtin_fmaf(x, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.0f);
+    const bool swapped = quarter & 1;
+    c = swapped ? sine : cosine;
+    s = swapped ? cosine : sine;
+    c = (quarter + 1) & 2 ? -c : c;
+    s = quarter & 2 ? -s : s;
+}
+
+// The channels that a lane holds of every head: E pairs.  WIDE: two chunks of 16 bytes, at channels `at[0]` and `at[1]`; otherwise pair by pair,
+// whatever the sizes and strides.
+template <bool BF16, bool WIDE, bool PAIRS>
+struct HeadLane {
+    static constexpr int E = WIDE && BF16 ? 8 : 4;
+    uint32_t u, at[2];
+    bool there[2];
+    __device__ __forceinline__ HeadLane(const HeadShape &s) : u(threadIdx.x % s.lanes), at{0, 0}, there{false, false}
+    {
+        if constexpr (WIDE) {
+            const uint32_t turned = PAIRS ? 0 : s.rotated / (2 * E);         // lanes of which both chunks are turned, against each other
+            at[0] = u < turned ? u * E : (PAIRS ? 0 : s.rotated) + 2 * (u - turned) * E;
+            at[1] = u < turned ? s.rotated / 2 + u * E : at[0] + E;
+            there[0] = at[0] < s.head;
+            there[1] = at[1] < s.head;
+        }
+    }
+    // number of pair i among the pairs of a head; of WIDE halves, where it is turned
+    __device__ __forceinline__ uint32_t pair(const HeadShape &s, int i) const
+    {
+        if constexpr (!WIDE) return u + s.lanes * i;
+        else if constexpr (PAIRS) return at[i / (E / 2)] / 2 + i % (E / 2);
+        else return u * E + i;
+    }
+    __device__ __forceinline__ bool turned(const HeadShape &s, int i) const { return 2 * pair(s, i) < s.rotated; }
+    // channel of pair i's first (0) or second (1) number; may be behind the head's end
+    __device__ __forceinline__ uint32_t channel(const HeadShape &s, int i, int which) const
+    {
+        if constexpr (WIDE) {
+            if constexpr (PAIRS) return at[i / (E / 2)] + 2 * (i % (E / 2)) + which;
+            else return at[which] + i;
+        } else {
+            const uint32_t p = pair(s, i);
+            if (PAIRS || 2 * p >= s.rotated) return 2 * p + which;           // behind the rotated channels neighbours are together, too
+            return p + which * (s.rotated / 2);
+        }
+    }
+    // A head's channels as they lie in memory, and as numbers: pair i is a[i], b[i]; zeros for what there is not
+    struct Raw {
+        uint4 q[2];
+        float x[WIDE ? 1 : 2 * E];
+    };
+    __device__ __forceinline__ Raw load(const HeadShape &s, const void *base, uint64_t from, bool mine) const
+    {
+        Raw r = {};
+        if constexpr (WIDE) {
+            const uint8_t *p = static_cast<const uint8_t *>(base) + from * (16 / E);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (mine && there[k]) r.q[k] = *reinterpret_cast<const uint4 *>(p + at[k] * (16 / E));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * E; ++i) {
+                const uint32_t c = channel(s, i / 2, i % 2);
+                if (mine && c < s.head) r.x[i] = load1<BF16>(base, from + c);
+            }
+        }
+        return r;
+    }
+    __device__ __forceinline__ void unpack(const Raw &r, float (&a)[E], float (&b)[E]) const
+    {
+        if constexpr (WIDE) {
+            float x[2][E];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t w[4] = {r.q[k].x, r.q[k].y, r.q[k].z, r.q[k].w};
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[k][i] = __uint_as_float(!BF16 ? w[i % 4] : i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                a[i] = PAIRS ? x[i / (E / 2)][2 * (i % (E / 2))] : x[0][i];
+                b[i] = PAIRS ? x[i / (E / 2)][2 * (i % (E / 2)) + 1] : x[1][i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                a[i] = r.x[2 * i];
+                b[i] = r.x[2 * i + 1];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(const HeadShape &s, void *base, uint64_t from, bool mine, const float (&a)[E], const float (&b)[E]) const
+    {
+        if constexpr (WIDE) {
+            float x[2][E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if constexpr (PAIRS) {
+                    x[i / (E / 2)][2 * (i % (E / 2))] = a[i];
+                    x[i / (E / 2)][2 * (i % (E / 2)) + 1] = b[i];
+                } else {
+                    x[0][i] = a[i];
+                    x[1][i] = b[i];
+                }
+            }
+            uint8_t *p = static_cast<uint8_t *>(base) + from * (16 / E);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = BF16 ? two_bf16(x[k][2 * i % E], x[k][(2 * i + 1) % E]) : __float_as_uint(x[k][i]);
+                if (mine && there[k]) *reinterpret_cast<uint4 *>(p + at[k] * (16 / E)) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * E; ++i) {
+                const uint32_t c = channel(s, i / 2, i % 2);
+                if (mine && c < s.head) store1<BF16>(base, from + c, i % 2 ? b[i / 2] : a[i / 2]);
+            }
+        }
+    }
+    __device__ __forceinline__ void angles(const HeadShape &s, const int64_t *positions, const uint64_t *frequencies, uint32_t token, float (&c)[E], float (&n)[E]) const
+    {
+        const uint64_t position = s.rotated ? (uint64_t)positions[token] : 0;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            c[i] = 1.0f;
+            n[i] = 0.0f;
+            if (turned(s, i)) {
+                cos_sin((uint32_t)((position * frequencies[pair(s, i)] + 0x80000000u) >> 32), c[i], n[i]);
+                c[i] *= s.magnitude;
+                n[i] *= s.magnitude;
+            }
+        }
+    }
+};
+
+// Sum over the lanes of a head, a power of two of them, the same in each
+__device__ __forceinline__ float head_sum(float v, uint32_t lanes)
+{
+    if (lanes > 1) v = add_permuted<0xb1>(v);
+    if (lanes > 2) v = add_permuted<0x4e>(v);
+    if (lanes > 4) v = add_permuted<0x141>(v);
+    if (lanes > 8) v = add_permuted<0x140>(v);
+    if (lanes > 16) v += __shfl_xor(v, 16);
+    if (lanes > 32) v += __shfl_xor(v, 32);
+    return v;
+}
+
+template <bool BF16, bool WIDE, bool PAIRS, bool NORM>
+__global__ __launch_bounds__(64 * kHeadWaves)
+void k_heads_forward(HeadTensors in, HeadTensors weights, const int64_t *positions, const uint64_t *frequencies, HeadOutputs out, HeadShape s)
+{
+    using Lane = HeadLane<BF16, WIDE, PAIRS>;
+    constexpr int E = Lane::E;
+    const Lane lane(s);
+    const uint32_t each = 64 / s.lanes, mine = threadIdx.x % 64 / s.lanes;
+    const uint32_t groups_q = (s.heads[0] + each - 1) / each, groups = groups_q + (s.heads[1] + each - 1) / each;
+    const uint64_t waves = (uint64_t)gridDim.x * kHeadWaves;
+    const float inv = 1.0f / (float)s.head;
+    for (uint64_t id = (uint64_t)blockIdx.x * kHeadWaves + uniform(threadIdx.x / 64); id < (uint64_t)s.tokens * s.splits; id += waves) {
+        const uint32_t token = (uint32_t)(id / s.splits);
+        float c[E], n[E];
+        lane.angles(s, positions, frequencies, token, c, n);
+        for (uint32_t g = (uint32_t)(id % s.splits); g < groups; g += s.splits) {
+            const int which = g < groups_q ? 0 : 1;
+            const uint32_t h = (which ? g - groups_q : g) * each + mine;
+            const bool valid = h < s.heads[which];
+            float a[E], b[E];
+            lane.unpack(lane.load(s, in.of[which], token * s.ld[which] + (uint64_t)h * s.head, valid), a, b);
+            if constexpr (NORM) {
+                float wa[E], wb[E], sum = 0.0f;
+                lane.unpack(lane.load(s, weights.of[which], 0, true), wa, wb);
+#pragma unroll
+                for (int i = 0; i < E; ++i) sum = __builtin_fmaf(b[i], b[i], __builtin_fmaf(a[i], a[i], sum));
+                const float rstd = rsqrtf(head_sum(sum, s.lanes) * inv + s.eps);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    a[i] = a[i] * rstd * wa[i];
+                    b[i] = b[i] * rstd * wb[i];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float x = a[i], y = b[i];
+                a[i] = x * c[i] - y * n[i];
+                b[i] = x * n[i] + y * c[i];
+            }
+            lane.store(s, out.of[which], token * s.ld_out[which] + (uint64_t)h * s.head, valid, a, b);
+        }
+    }
+}
+
+// With u the gradient of the normed head, turned back and times w: dx = rstd (u - n mean(u n)), n = x rstd; w's gradient is the sum of the turned
+// gradient times n over tokens and heads: in a lane's registers, then over the wavefront and the workgroup, which leaves its part in the workspace,
+// [workgroup][query or key][head].
+template <bool BF16, bool WIDE, bool PAIRS, bool NORM>
+__global__ __launch_bounds__(64 * kHeadWaves)
+void k_heads_backward(HeadTensors grads, HeadTensors in, HeadTensors weights, const int64_t *positions, const uint64_t *frequencies, HeadOutputs out, float *parts, HeadShape s)
+{
+    using Lane = HeadLane<BF16, WIDE, PAIRS>;
+    constexpr int E = Lane::E;
+    __shared__ float sums[NORM ? kHeadWaves : 1][2][NORM ? TAHQ_HEADS_MAX : 1];
+    const Lane lane(s);
+    const uint32_t each = 64 / s.lanes, mine = threadIdx.x % 64 / s.lanes, wave = uniform(threadIdx.x / 64);
+    const uint32_t groups_q = (s.heads[0] + each - 1) / each, groups = groups_q + (s.heads[1] + each - 1) / each;
+    const uint64_t waves = (uint64_t)gridDim.x * kHeadWaves;
+    const float inv = 1.0f / (float)s.head;
+    float da[2][E] = {}, db[2][E] = {};
+    for (uint64_t id = (uint64_t)blockIdx.x * kHeadWaves + wave; id < (uint64_t)s.tokens * s.splits; id += waves) {
+        const uint32_t token = (uint32_t)(id / s.splits);
+        float c[E], n[E];
+        lane.angles(s, positions, frequencies, token, c, n);
+        auto one = [&](auto which_tensor, uint32_t g) {
+            constexpr int which = decltype(which_tensor)::value;
+            const uint32_t h = g * each + mine;
+            const bool valid = h < s.heads[which];
+            float a[E], b[E];
+            lane.unpack(lane.load(s, grads.of[which], token * s.ld_out[which] + (uint64_t)h * s.head, valid), a, b);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float x = a[i], y = b[i];
+                a[i] = x * c[i] + y * n[i];
+                b[i] = y * c[i] - x * n[i];
+            }
+            if constexpr (NORM) {
+                float xa[E], xb[E], wa[E], wb[E], square = 0.0f, dot = 0.0f;
+                lane.unpack(lane.load(s, in.of[which], token * s.ld[which] + (uint64_t)h * s.head, valid), xa, xb);
+                lane.unpack(lane.load(s, weights.of[which], 0, true), wa, wb);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    square = __builtin_fmaf(xb[i], xb[i], __builtin_fmaf(xa[i], xa[i], square));
+                }
+                const float rstd = rsqrtf(head_sum(square, s.lanes) * inv + s.eps);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    xa[i] *= rstd;
+                    xb[i] *= rstd;
+                    da[which][i] = __builtin_fmaf(a[i], xa[i], da[which][i]);
+                    db[which][i] = __builtin_fmaf(b[i], xb[i], db[which][i]);
+                    a[i] *= wa[i];
+                    b[i] *= wb[i];
+                    dot = __builtin_fmaf(b[i], xb[i], __builtin_fmaf(a[i], xa[i], dot));
+                }
+                const float mean = head_sum(dot, s.lanes) * inv;
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    a[i] = rstd * __builtin_fmaf(-xa[i], mean, a[i]);
+                    b[i] = rstd * __builtin_fmaf(-xb[i], mean, b[i]);
+                }
+            }
+            lane.store(s, out.of[which], token * s.ld[which] + (uint64_t)h * s.head, valid, a, b);
+        };
+        uint32_t g = (uint32_t)(id % s.splits);
+        for (; g < groups_q; g += s.splits) one(std::integral_constant<int, 0>{}, g);
+        for (; g < groups; g += s.splits) one(std::integral_constant<int, 1>{}, g - groups_q);
+    }
+    if constexpr (NORM) {
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                float a = da[which][i], b = db[which][i];
+                for (uint32_t step = s.lanes; step < 64; step *= 2) {
+                    a += __shfl_xor(a, (int)step);
+                    b += __shfl_xor(b, (int)step);
+                }
+                if (mine == 0) {
+                    const uint32_t ca = lane.channel(s, i, 0), cb = lane.channel(s, i, 1);
+                    if (ca < s.head) sums[wave][which][ca] = a;
+                    if (cb < s.head) sums[wave][which][cb] = b;
+                }
+            }
+        __syncthreads();
+        for (uint32_t at = threadIdx.x; at < 2 * s.head; at += 64 * kHeadWaves) {
+            const uint32_t which = at / s.head, channel = at % s.head;
+            float sum = sums[0][which][channel];
+            for (uint32_t w = 1; w < kHeadWaves; ++w) sum += sums[w][which][channel];
+            parts[(uint64_t)blockIdx.x * 2 * s.head + at] = sum;
+        }
+    }
+}
+
+// The workgroups' parts, added in a fixed order: 16 channels of 64 runs of workgroups to a block.  blockIdx.y: queries', keys'.
+__global__ __launch_bounds__(1024)
+void k_heads_reduce(const float *parts, float *grad_w_q, float *grad_w_k, uint32_t head, uint32_t workgroups, uint32_t accumulate)
+{
+    __shared__ float sums[1024];
+    const uint32_t c = blockIdx.x * 16 + threadIdx.x % 16, run = threadIdx.x / 16, each = (workgroups + 63) / 64;
+    float sum = 0.0f;
+    if (c < head)
+        for (uint32_t i = run * each; i < min((run + 1) * each, workgroups); ++i) sum += parts[((uint64_t)i * 2 + blockIdx.y) * head + c];
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    for (uint32_t half = 512; half >= 16; half /= 2) {
+        if (threadIdx.x < half) sums[threadIdx.x] += sums[threadIdx.x + half];
+        __syncthreads();
+    }
+    float *to = blockIdx.y ? grad_w_k : grad_w_q;
+    if (run == 0 && c < head) to[c] = accumulate ? to[c] + sums[threadIdx.x] : sums[threadIdx.x];
+}
+
+}  // namespace tahq

@@ -1,0 +1,184 @@
+// Entry points of the loss over a vocabulary (include/tahq_loss.h): validation, plan, launches.
+#include "tahq_enqueue.hpp"
+#include "tahq_loss.h"
+#include "tahq_loss_kernels.hpp"
+#include "tahq_loss_plan.hpp"
+
+using namespace tahq;
+
+namespace {
+
+static_assert(kLossSpan == kLossScan, "the plan's and the kernels'");
+
+tahq_status check(const tahq_loss_config *c)
+{
+    if (!c) return TAHQ_ERR_NULL;
+    if (c->struct_size != sizeof *c) return TAHQ_ERR_INVALID_ARG;
+    if (c->rows == 0 || c->rows >= 0x80000000u || c->vocab == 0 || c->vocab >= 0x80000000u || c->cols == 0) return TAHQ_ERR_INVALID_ARG;
+    if (c->dtype > TAHQ_BF16 || c->weight_dtype > TAHQ_BF16 || c->reduction > TAHQ_LOSS_MEAN || c->accumulate > 1) return TAHQ_ERR_INVALID_ARG;
+    if (c->cols > TAHQ_LOSS_MAX_COLS) return TAHQ_ERR_UNSUPPORTED;
+    const LossPlan p = plan_loss(c);
+    if (!launchable(loss_tiles(p.forward_kind, c->rows, p.forward_piece), 256) || !launchable(loss_tiles(p.grads_kind, c->rows, p.backward_piece), 256) ||
+        !launchable(loss_tiles(p.x_kind, c->rows, c->cols), 256) || !launchable(loss_tiles(kLossMiddle, p.backward_piece, c->cols), 256) ||
+        !launchable(loss_ceil(c->rows, kGatherRows), 256))
+        return TAHQ_ERR_UNSUPPORTED;
+    return TAHQ_OK;
+}
+
+struct Call {
+    const tahq_loss_config *cfg;
+    LossPlan p;
+    uint8_t *ws;
+    Enqueue q;
+    LossTokens tokens;
+
+    Call(const tahq_loss_config *c, void *workspace, tahq_stream stream)
+        : cfg(c), p(plan_loss(c)), ws(static_cast<uint8_t *>(workspace)), q{(hipStream_t)stream}, tokens{at<uint32_t>(p.rows), at<uint32_t>(p.targets), at<uint32_t>(0)} {}
+    template <typename T>
+    T *at(uint64_t place) const { return reinterpret_cast<T *>(ws + place); }
+
+    void gather(const void *d_x, const int64_t *d_target, float *zero, float *zero_also, void *grad_x)
+    {
+        uint32_t *counts = p.spans > 1 ? at<uint32_t>(p.counts) : nullptr;
+        if (counts) q(k_loss_count, dim3(p.spans), dim3(256), d_target, cfg->ignore, cfg->rows, counts);
+        q(p.bf16 ? k_loss_gather<true> : k_loss_gather<false>, dim3((uint32_t)loss_ceil(cfg->rows, kGatherRows)), dim3(256), d_x, d_target, counts, cfg->rows, cfg->cols,
+          cfg->vocab, cfg->ignore, at<void>(p.x), p.ldx, tokens, zero, zero_also, grad_x);
+    }
+    // rows first .. first + rows - 1 of the weight as the tiles take them
+    const uint8_t *weight(const void *d_weight, uint32_t first, uint32_t rows, uint64_t copy)
+    {
+        const uint8_t *from = static_cast<const uint8_t *>(d_weight) + (uint64_t)first * cfg->cols * p.es;
+        if (!p.pad) return from;
+        const uint64_t groups = loss_ceil((uint64_t)rows * (p.ldx / 8), 256);
+        q(p.bf16 ? k_loss_pad<true> : k_loss_pad<false>, dim3((uint32_t)(groups < 65536 ? groups : 65536)), dim3(256), from, at<void>(copy), rows, cfg->cols, p.ldx);
+        return at<uint8_t>(copy);
+    }
+    template <int MODE>
+    void logits(int kind, const LogitArgs &g)
+    {
+        const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[kind].tm) * g.tiles_n)), block(256);
+        if (kind == kLossLarge) q(k_loss_logits<true, 2, 2, 4, 4, 1, MODE>, grid, block, g);
+        else if (kind == kLossMiddle) p.bf16 ? q(k_loss_logits<true, 2, 2, 2, 2, 2, MODE>, grid, block, g) : q(k_loss_logits<false, 2, 2, 2, 2, 2, MODE>, grid, block, g);
+        else p.bf16 ? q(k_loss_logits<true, 1, 4, 1, 1, 3, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 4, 1, 1, 3, MODE>, grid, block, g);
+    }
+    LogitArgs logit_args(const uint8_t *w, uint32_t first, uint32_t rows, int kind) const
+    {
+        LogitArgs g = {};
+        g.x = at<uint8_t>(p.x);
+        g.weight = w;
+        g.ldx = g.ldw = (uint64_t)p.ldx * p.es;
+        g.tokens = tokens;
+        g.stages = p.ldx / p.whole;
+        g.first = first;
+        g.vocab = first + rows;
+        g.tiles_n = (uint32_t)loss_ceil(rows, kLossTiles[kind].tn);
+        g.padded = p.padded;
+        return g;
+    }
+    void grad_x(const GradXArgs &g)
+    {
+        const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[p.x_kind].tm) * g.tiles_n), (uint32_t)loss_ceil(g.stages, g.run)), block(256);
+        if (p.x_kind == kLossLarge) q(k_loss_grad_x<true, 2, 2, 4, 4, 1>, grid, block, g);
+        else if (p.x_kind == kLossMiddle) p.bf16 ? q(k_loss_grad_x<true, 2, 2, 2, 2, 2>, grid, block, g) : q(k_loss_grad_x<false, 2, 2, 2, 2, 2>, grid, block, g);
+        else p.bf16 ? q(k_loss_grad_x<true, 1, 4, 1, 1, 3>, grid, block, g) : q(k_loss_grad_x<false, 1, 4, 1, 1, 3>, grid, block, g);
+    }
+    void grad_w(GradWArgs g)
+    {
+        const int kind = p.bf16 && loss_tiles(kLossLarge, g.rows, g.cols) >= 256 ? kLossLarge : kLossMiddle;
+        g.tiles_m = (uint32_t)loss_ceil(g.rows, kLossTiles[kind].tm);
+        g.tiles_n = (uint32_t)loss_ceil(g.cols, kLossTiles[kind].tn);
+        const dim3 grid(g.tiles_m * g.tiles_n), block(256);
+        if (kind == kLossLarge) q(k_loss_grad_w<true, 2, 2, 4, 4, 1>, grid, block, g);
+        else p.bf16 ? q(k_loss_grad_w<true, 2, 2, 2, 2, 2>, grid, block, g) : q(k_loss_grad_w<false, 2, 2, 2, 2, 2>, grid, block, g);
+    }
+};
+
+}  // namespace
+
+extern "C" {
+
+void tahq_loss_config_default(tahq_loss_config *cfg)
+{
+    if (!cfg) return;
+    *cfg = tahq_loss_config{};
+    cfg->struct_size = (uint32_t)sizeof *cfg;
+    cfg->dtype = cfg->weight_dtype = TAHQ_BF16;
+    cfg->reduction = TAHQ_LOSS_MEAN;
+    cfg->ignore = -100;
+}
+
+size_t tahq_loss_forward_workspace_size(const tahq_loss_config *cfg) { return check(cfg) == TAHQ_OK ? (size_t)plan_loss(cfg).forward_total : 0; }
+size_t tahq_loss_backward_workspace_size(const tahq_loss_config *cfg) { return check(cfg) == TAHQ_OK ? (size_t)plan_loss(cfg).backward_total : 0; }
+
+tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, const void *d_weight, const int64_t *d_target, float *d_losses,
+                              float *d_lse, float *d_total, void *d_workspace, size_t workspace_capacity, tahq_stream stream)
+{
+    const tahq_status rc = check(cfg);
+    if (rc != TAHQ_OK) return rc;
+    for (const void *p : {d_x, d_weight, (const void *)d_target, (const void *)d_losses, (const void *)d_lse, (const void *)d_total, (const void *)d_workspace})
+        if (!p) return TAHQ_ERR_NULL;
+    Call call(cfg, d_workspace, stream);
+    const LossPlan &p = call.p;
+    if (workspace_capacity < p.forward_total) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
+    for (const void *x : {d_x, d_weight, (const void *)d_losses, (const void *)d_lse, (const void *)d_total, (const void *)d_workspace})
+        if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
+    if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target) return TAHQ_ERR_MISALIGNED;
+    call.gather(d_x, d_target, d_losses, d_lse, nullptr);
+    for (uint32_t first = 0; first < cfg->vocab; first += p.forward_piece) {
+        const uint32_t rows = cfg->vocab - first < p.forward_piece ? cfg->vocab - first : p.forward_piece;
+        LogitArgs g = call.logit_args(call.weight(d_weight, first, rows, p.forward_weight), first, rows, p.forward_kind);
+        g.parts = call.at<float2>(p.stats);
+        g.at_target = call.at<float>(p.at_target);
+        call.logits<kStats>(p.forward_kind, g);
+        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, 32)), dim3(256), g.parts, g.tiles_n * kLossTiles[p.forward_kind].along, p.padded, call.tokens, g.at_target,
+               call.at<float2>(p.running), first != 0, first + rows == cfg->vocab, d_losses, d_lse);
+    }
+    call.q(k_loss_total, dim3(1), dim3(1024), d_losses, cfg->rows, call.tokens, cfg->reduction == TAHQ_LOSS_MEAN, d_total);
+    return call.q.result();
+}
+
+tahq_status tahq_loss_backward(const tahq_loss_config *cfg, const void *d_x, const void *d_weight, const int64_t *d_target, const float *d_lse,
+                               const float *d_grad_loss, void *d_grad_x, void *d_grad_weight, void *d_workspace, size_t workspace_capacity,
+                               tahq_stream stream)
+{
+    const tahq_status rc = check(cfg);
+    if (rc != TAHQ_OK) return rc;
+    if (!d_grad_x && !d_grad_weight) return TAHQ_ERR_NULL;
+    for (const void *p : {d_x, d_weight, (const void *)d_target, (const void *)d_lse, (const void *)d_workspace})
+        if (!p) return TAHQ_ERR_NULL;
+    Call call(cfg, d_workspace, stream);
+    const LossPlan &p = call.p;
+    if (workspace_capacity < p.backward_total) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
+    for (const void *x : {d_x, d_weight, (const void *)d_lse, (const void *)d_grad_x, (const void *)d_grad_weight, (const void *)d_workspace})
+        if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
+    if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target || reinterpret_cast<uintptr_t>(d_grad_loss) % sizeof *d_grad_loss) return TAHQ_ERR_MISALIGNED;
+    const bool each = cfg->reduction == TAHQ_LOSS_NONE;
+    const uint32_t mean = cfg->reduction == TAHQ_LOSS_MEAN;
+    const float *whole = each ? nullptr : d_grad_loss;
+    call.gather(d_x, d_target, nullptr, nullptr, d_grad_x);
+    for (uint32_t first = 0; first < cfg->vocab; first += p.backward_piece) {
+        const uint32_t rows = cfg->vocab - first < p.backward_piece ? cfg->vocab - first : p.backward_piece;
+        const uint8_t *w = call.weight(d_weight, first, rows, p.backward_weight);
+        LogitArgs g = call.logit_args(w, first, rows, p.grads_kind);
+        g.lse = d_lse;
+        g.grad_loss = each ? d_grad_loss : nullptr;
+        g.grads = call.at<uint8_t>(p.grads);
+        g.ldg = p.ldg;
+        call.logits<kGrads>(p.grads_kind, g);
+        const uint64_t ldw = (uint64_t)p.ldx * p.es;
+        if (d_grad_x)
+            call.grad_x({g.grads, w, p.ldg, ldw, call.tokens, rows, cfg->cols, (uint32_t)loss_ceil(rows, p.whole), p.x_run,
+                         (uint32_t)loss_ceil(cfg->cols, kLossTiles[p.x_kind].tn), p.padded, first != 0, call.at<float>(p.sums)});
+        if (d_grad_weight)
+            call.grad_w({g.grads, g.x, p.ldg, g.ldx, call.tokens, rows, cfg->cols, 0, 0, whole, mean, cfg->weight_dtype == TAHQ_BF16, cfg->accumulate,
+                         static_cast<uint8_t *>(d_grad_weight) + (uint64_t)first * cfg->cols * (cfg->weight_dtype == TAHQ_BF16 ? 2 : 4)});
+    }
+    if (d_grad_x) {
+        const uint64_t groups = loss_ceil(cfg->rows, 4);
+        call.q(p.bf16 ? k_loss_scatter<true> : k_loss_scatter<false>, dim3((uint32_t)(groups < 65536 ? groups : 65536)), dim3(256), call.at<float>(p.sums), p.x_parts, p.padded,
+               call.tokens, cfg->cols, whole, mean, d_grad_x);
+    }
+    return call.q.result();
+}
+
+}  // extern "C"

@@ -3,11 +3,11 @@
 #include <type_traits>
 
 #include "tahq_mx4_common.hpp"
+#include "tahq_tiles.hpp"
 
 namespace tahq {
 
 typedef int int8v __attribute__((ext_vector_type(8)));
-typedef float float16v __attribute__((ext_vector_type(16)));
 
 // One instruction: 32 rows of each operand, 64 columns.  A lane holds row lane % 32 of both operands, columns 32 * (lane / 32) on,
 // and of D column lane % 32 (second operand's row), rows 8 * (i / 4) + 4 * (lane / 32) + i % 4 (first operand's).  B goes first, so that a lane's
@@ -18,76 +18,6 @@ __device__ __forceinline__ float16v mfma(const uint4 &b, const uint4 &a, const f
     const int8v vb = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
     const int8v va = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vb, va, c, 4, 4, BYTE, (int)sb, BYTE, (int)sa);
-}
-
-// Four neighbours of a row of C: row m, columns n .. n + 3
-template <bool BF16>
-__device__ __forceinline__ void store4(void *c, uint64_t ldc, uint32_t m, uint32_t n, uint32_t N, float (&v)[4], bool accumulate)
-{
-    const uint64_t at = (uint64_t)m * ldc + n;
-    const bool whole = n + 4 <= N;
-    if (accumulate) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (whole || n + i < N) v[i] += load1<BF16>(c, at + i);
-    }
-    if (whole) {
-        if constexpr (BF16) {
-            const uint32_t w[2] = {two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
-            __builtin_memcpy(static_cast<uint16_t *>(c) + at, w, 8);
-        } else {
-            __builtin_memcpy(static_cast<float *>(c) + at, v, 16);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < N) store1<BF16>(c, at + i, v[i]);
-    }
-}
-
-// ---------------------------------------------------------------- tiles through LDS
-
-// Workgroups go around the eight dies, each with a cache of its own: a die gets neighbouring tiles, in strips of eight rows of tiles.
-__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn)
-{
-    const uint32_t total = tiles_m * tiles_n, die = id % 8, extra = total % 8;
-    id = die * (total / 8) + min(die, extra) + id / 8;
-    const uint32_t strip = id / (8 * tiles_n), at = id % (8 * tiles_n), height = min(tiles_m - strip * 8, 8u);
-    tm = strip * 8 + at % height;
-    tn = at / height;
-}
-
-// s_waitcnt's operand: at most `vm` loads and `lgkm` LDS accesses outstanding (no exports are)
-constexpr int waitcnt(int vm, int lgkm) { return (vm & 15) | 7 << 4 | lgkm << 8 | (vm >> 4) << 14; }
-
-// what was read is used here: the reads are not moved behind this place
-__device__ __forceinline__ void pin(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
-
-typedef const __attribute__((address_space(1))) void *GlobalPtr;
-typedef __attribute__((address_space(3))) void *LdsPtr;
-
-// Eight bf16 or four fp32 neighbours of a row of C, of which `valid` are there; fp32 may be added to what is there
-template <bool BF16>
-__device__ __forceinline__ void store16(void *c, uint64_t at, uint32_t valid, uint4 x, bool accumulate)
-{
-    constexpr uint32_t COUNT = BF16 ? 8 : 4;
-    uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    if constexpr (!BF16) {
-        if (accumulate)
-#pragma unroll
-            for (uint32_t i = 0; i < 4; ++i)
-                if (i < valid) w[i] = __float_as_uint(__uint_as_float(w[i]) + static_cast<const float *>(c)[at + i]);
-    }
-    if (valid >= COUNT) {
-        __builtin_memcpy(static_cast<uint8_t *>(c) + at * (16 / COUNT), w, 16);
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < COUNT; ++i)
-            if (i < valid) {
-                if constexpr (BF16) static_cast<uint16_t *>(c)[at + i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
-                else static_cast<uint32_t *>(c)[at + i] = w[i];
-            }
-    }
 }
 
 // A workgroup's tile is WM * MF units of A's rows by WN * NF of B's; its WM * WN wavefronts take MF x NF units each.  A stage is 128

@@ -7,6 +7,7 @@
 // of HBM); backward 32768 x 5120 386 to 398 us (2.0 GB, 5.1 TB/s, as a large copy) and its column sums 10.  Halves alone, 32768 x 5120:
 // forward post 188, pre 178 (1.0 GB), backward post 252 (1.3 GB), pre without a gradient of r' 214 (1.0 GB).
 #pragma once
+#include "tahq_lanes.hpp"
 #include "tahq_mx4_common.hpp"
 
 namespace tahq {
@@ -45,22 +46,6 @@ __device__ __forceinline__ void stay_packed(Eight<BF16> &e)
     if constexpr (BF16) asm volatile("" : "+v"(e.q[0].x), "+v"(e.q[0].y), "+v"(e.q[0].z), "+v"(e.q[0].w));
 }
 
-// Sum over a wavefront, the same in every lane: pairs, quads, eights and sixteens by permutations within rows of sixteen lanes, then the four rows.
-template <int CTRL>
-__device__ __forceinline__ float add_permuted(float v)
-{
-    return v + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float wave_sum(float v)
-{
-    v = add_permuted<0xb1>(v);                             // lane ^ 1
-    v = add_permuted<0x4e>(v);                             // lane ^ 2
-    v = add_permuted<0x141>(v);                            // mirrored in eight: the other quad
-    v = add_permuted<0x140>(v);                            // mirrored in sixteen: the other eight
-    const int w = (int)__float_as_uint(v);
-    auto row = [&](int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane(w, lane)); };
-    return (row(0) + row(16)) + (row(32) + row(48));
-}
 // Sum over a workgroup of `waves` wavefronts, the same in every lane; places of wavefronts that there are not hold zeros.  `turn` alternates
 // between two places, so that one barrier per sum is enough: nobody writes a place again before all have passed the barrier of the sum in between.
 struct Places {
