@@ -39,7 +39,8 @@ typedef struct {
     int64_t ignore;           /* target of tokens that do not count                                      */
 } tahq_loss_config;
 
-#define TAHQ_LOSS_MAX_COLS 65536u   /* more give TAHQ_ERR_UNSUPPORTED */
+#define TAHQ_LOSS_MAX_COLS 65536u       /* more give TAHQ_ERR_UNSUPPORTED */
+#define TAHQ_LOSS_MAX_ROWS 8388608u     /* more tokens, and launches of 2^32 lanes and more, too */
 
 void tahq_loss_config_default(tahq_loss_config *cfg);   /* bf16 both, mean, no accumulation, ignore -100, dimensions 0 */
 

@@ -16,7 +16,7 @@ tahq_status check(const tahq_loss_config *c)
     if (c->struct_size != sizeof *c) return TAHQ_ERR_INVALID_ARG;
     if (c->rows == 0 || c->rows >= 0x80000000u || c->vocab == 0 || c->vocab >= 0x80000000u || c->cols == 0) return TAHQ_ERR_INVALID_ARG;
     if (c->dtype > TAHQ_BF16 || c->weight_dtype > TAHQ_BF16 || c->reduction > TAHQ_LOSS_MEAN || c->accumulate > 1) return TAHQ_ERR_INVALID_ARG;
-    if (c->cols > TAHQ_LOSS_MAX_COLS) return TAHQ_ERR_UNSUPPORTED;
+    if (c->cols > TAHQ_LOSS_MAX_COLS || c->rows > TAHQ_LOSS_MAX_ROWS) return TAHQ_ERR_UNSUPPORTED;
     const LossPlan p = plan_loss(c);
     if (!launchable(loss_tiles(p.forward_kind, c->rows, p.forward_piece), 256) || !launchable(loss_tiles(p.grads_kind, c->rows, p.backward_piece), 256) ||
         !launchable(loss_tiles(p.x_kind, c->rows, c->cols), 256) || !launchable(loss_tiles(kLossMiddle, p.backward_piece, c->cols), 256) ||
@@ -42,31 +42,37 @@ struct Call {
         uint32_t *counts = p.spans > 1 ? at<uint32_t>(p.counts) : nullptr;
         if (counts) q(k_loss_count, dim3(p.spans), dim3(256), d_target, cfg->ignore, cfg->rows, counts);
         q(p.bf16 ? k_loss_gather<true> : k_loss_gather<false>, dim3((uint32_t)loss_ceil(cfg->rows, kGatherRows)), dim3(256), d_x, d_target, counts, cfg->rows, cfg->cols,
-          cfg->vocab, cfg->ignore, at<void>(p.x), p.ldx, tokens, zero, zero_also, grad_x);
+          cfg->vocab, cfg->ignore, at<uint8_t>(p.x), p.ldx / p.whole, p.padded, tokens, zero, zero_also, grad_x);
     }
-    // rows first .. first + rows - 1 of the weight as the tiles take them
-    const uint8_t *weight(const void *d_weight, uint32_t first, uint32_t rows, uint64_t copy)
+    // rows first .. first + rows - 1 of the weight as the tiles take them, and bytes from row to row or from block to block
+    std::pair<const uint8_t *, uint64_t> weight(const void *d_weight, uint32_t first, uint32_t rows, uint64_t copy)
     {
         const uint8_t *from = static_cast<const uint8_t *>(d_weight) + (uint64_t)first * cfg->cols * p.es;
-        if (!p.pad) return from;
-        const uint64_t groups = loss_ceil((uint64_t)rows * (p.ldx / 8), 256);
-        q(p.bf16 ? k_loss_pad<true> : k_loss_pad<false>, dim3((uint32_t)(groups < 65536 ? groups : 65536)), dim3(256), from, at<void>(copy), rows, cfg->cols, p.ldx);
-        return at<uint8_t>(copy);
+        if (!p.pad) return {from, (uint64_t)cfg->cols * p.es};
+        const uint32_t padded = (uint32_t)loss_ceil(rows, p.whole) * p.whole;
+        q(p.bf16 ? k_loss_blocks<true> : k_loss_blocks<false>, dim3((uint32_t)loss_ceil(padded, 16)), dim3(256), from, at<uint8_t>(copy), rows, cfg->cols, padded);
+        return {at<uint8_t>(copy), (uint64_t)padded * 64};
+    }
+    template <int MODE, Lies LIES>
+    void logits_of(int kind, const LogitArgs &g)
+    {
+        const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[kind].tm) * g.tiles_n)), block(256);
+        if (kind == kLossLarge) q(k_loss_logits<true, 2, 2, 4, 4, 1, LIES, MODE>, grid, block, g);
+        else if (kind == kLossMiddle) p.bf16 ? q(k_loss_logits<true, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g);
+        else p.bf16 ? q(k_loss_logits<true, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g);
     }
     template <int MODE>
     void logits(int kind, const LogitArgs &g)
     {
-        const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[kind].tm) * g.tiles_n)), block(256);
-        if (kind == kLossLarge) q(k_loss_logits<true, 2, 2, 4, 4, 1, MODE>, grid, block, g);
-        else if (kind == kLossMiddle) p.bf16 ? q(k_loss_logits<true, 2, 2, 2, 2, 2, MODE>, grid, block, g) : q(k_loss_logits<false, 2, 2, 2, 2, 2, MODE>, grid, block, g);
-        else p.bf16 ? q(k_loss_logits<true, 1, 4, 1, 1, 3, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 4, 1, 1, 3, MODE>, grid, block, g);
+        if (p.pad) logits_of<MODE, kBlocks>(kind, g);
+        else logits_of<MODE, kRows>(kind, g);
     }
-    LogitArgs logit_args(const uint8_t *w, uint32_t first, uint32_t rows, int kind) const
+    LogitArgs logit_args(std::pair<const uint8_t *, uint64_t> w, uint32_t first, uint32_t rows, int kind) const
     {
         LogitArgs g = {};
         g.x = at<uint8_t>(p.x);
-        g.weight = w;
-        g.ldx = g.ldw = (uint64_t)p.ldx * p.es;
+        g.weight = w.first;
+        g.ldw = w.second;
         g.tokens = tokens;
         g.stages = p.ldx / p.whole;
         g.first = first;
@@ -75,12 +81,18 @@ struct Call {
         g.padded = p.padded;
         return g;
     }
-    void grad_x(const GradXArgs &g)
+    template <Lies LIES>
+    void grad_x_of(const GradXArgs &g)
     {
         const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[p.x_kind].tm) * g.tiles_n), (uint32_t)loss_ceil(g.stages, g.run)), block(256);
-        if (p.x_kind == kLossLarge) q(k_loss_grad_x<true, 2, 2, 4, 4, 1>, grid, block, g);
-        else if (p.x_kind == kLossMiddle) p.bf16 ? q(k_loss_grad_x<true, 2, 2, 2, 2, 2>, grid, block, g) : q(k_loss_grad_x<false, 2, 2, 2, 2, 2>, grid, block, g);
-        else p.bf16 ? q(k_loss_grad_x<true, 1, 4, 1, 1, 3>, grid, block, g) : q(k_loss_grad_x<false, 1, 4, 1, 1, 3>, grid, block, g);
+        if (p.x_kind == kLossLarge) q(k_loss_grad_x<true, 2, 2, 4, 4, 1, LIES>, grid, block, g);
+        else if (p.x_kind == kLossMiddle) p.bf16 ? q(k_loss_grad_x<true, 2, 2, 2, 2, 2, LIES>, grid, block, g) : q(k_loss_grad_x<false, 2, 2, 2, 2, 2, LIES>, grid, block, g);
+        else p.bf16 ? q(k_loss_grad_x<true, 1, 4, 1, 1, 3, LIES>, grid, block, g) : q(k_loss_grad_x<false, 1, 4, 1, 1, 3, LIES>, grid, block, g);
+    }
+    void grad_x(const GradXArgs &g)
+    {
+        if (p.pad) grad_x_of<kBlocksTurned>(g);
+        else grad_x_of<kTurned>(g);
     }
     void grad_w(GradWArgs g)
     {
@@ -124,16 +136,18 @@ tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, cons
         if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
     if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target) return TAHQ_ERR_MISALIGNED;
     call.gather(d_x, d_target, d_losses, d_lse, nullptr);
+    // tokens of a workgroup that joins statistics: fewer where there would be few workgroups
+    uint32_t width = 32;
+    while (width > 1 && cfg->rows < 256 * width) width /= 2;
     for (uint32_t first = 0; first < cfg->vocab; first += p.forward_piece) {
         const uint32_t rows = cfg->vocab - first < p.forward_piece ? cfg->vocab - first : p.forward_piece;
         LogitArgs g = call.logit_args(call.weight(d_weight, first, rows, p.forward_weight), first, rows, p.forward_kind);
         g.parts = call.at<float2>(p.stats);
         g.at_target = call.at<float>(p.at_target);
         call.logits<kStats>(p.forward_kind, g);
-        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, 32)), dim3(256), g.parts, g.tiles_n * kLossTiles[p.forward_kind].along, p.padded, call.tokens, g.at_target,
-               call.at<float2>(p.running), first != 0, first + rows == cfg->vocab, d_losses, d_lse);
+        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, width)), dim3(256), g.parts, g.tiles_n * kLossTiles[p.forward_kind].along, p.padded, call.tokens, g.at_target,
+               call.at<float2>(p.running), first != 0, first + rows == cfg->vocab, width, d_losses, d_lse, cfg->rows, cfg->reduction == TAHQ_LOSS_MEAN, d_total);
     }
-    call.q(k_loss_total, dim3(1), dim3(1024), d_losses, cfg->rows, call.tokens, cfg->reduction == TAHQ_LOSS_MEAN, d_total);
     return call.q.result();
 }
 
@@ -158,25 +172,24 @@ tahq_status tahq_loss_backward(const tahq_loss_config *cfg, const void *d_x, con
     call.gather(d_x, d_target, nullptr, nullptr, d_grad_x);
     for (uint32_t first = 0; first < cfg->vocab; first += p.backward_piece) {
         const uint32_t rows = cfg->vocab - first < p.backward_piece ? cfg->vocab - first : p.backward_piece;
-        const uint8_t *w = call.weight(d_weight, first, rows, p.backward_weight);
+        const auto w = call.weight(d_weight, first, rows, p.backward_weight);
         LogitArgs g = call.logit_args(w, first, rows, p.grads_kind);
         g.lse = d_lse;
         g.grad_loss = each ? d_grad_loss : nullptr;
         g.grads = call.at<uint8_t>(p.grads);
-        g.ldg = p.ldg;
         call.logits<kGrads>(p.grads_kind, g);
-        const uint64_t ldw = (uint64_t)p.ldx * p.es;
         if (d_grad_x)
-            call.grad_x({g.grads, w, p.ldg, ldw, call.tokens, rows, cfg->cols, (uint32_t)loss_ceil(rows, p.whole), p.x_run,
-                         (uint32_t)loss_ceil(cfg->cols, kLossTiles[p.x_kind].tn), p.padded, first != 0, call.at<float>(p.sums)});
+            call.grad_x({g.grads, w.first, w.second, call.tokens, rows, cfg->cols, (uint32_t)loss_ceil(rows, p.whole), p.x_run,
+                         (uint32_t)loss_ceil(cfg->cols, kLossTiles[p.x_kind].tn), p.padded, first != 0, p.x_tiles, call.at<float4>(p.sums)});
         if (d_grad_weight)
-            call.grad_w({g.grads, g.x, p.ldg, g.ldx, call.tokens, rows, cfg->cols, 0, 0, whole, mean, cfg->weight_dtype == TAHQ_BF16, cfg->accumulate,
+            call.grad_w({g.grads, g.x, call.tokens, rows, cfg->cols, 0, 0, p.padded, whole, mean, cfg->weight_dtype == TAHQ_BF16, cfg->accumulate,
                          static_cast<uint8_t *>(d_grad_weight) + (uint64_t)first * cfg->cols * (cfg->weight_dtype == TAHQ_BF16 ? 2 : 4)});
     }
     if (d_grad_x) {
-        const uint64_t groups = loss_ceil(cfg->rows, 4);
-        call.q(p.bf16 ? k_loss_scatter<true> : k_loss_scatter<false>, dim3((uint32_t)(groups < 65536 ? groups : 65536)), dim3(256), call.at<float>(p.sums), p.x_parts, p.padded,
-               call.tokens, cfg->cols, whole, mean, d_grad_x);
+        const LossTile &t = kLossTiles[p.x_kind];
+        const uint32_t eights = (uint32_t)loss_ceil(cfg->rows, 8), columns = (uint32_t)loss_ceil(cfg->cols, 128);
+        call.q(p.bf16 ? k_loss_scatter<true> : k_loss_scatter<false>, dim3(eights, columns < 8 ? columns : 8), dim3(256), call.at<float4>(p.sums), p.x_parts, p.x_tiles,
+               (uint32_t)loss_ceil(cfg->cols, t.tn), SumsLayout{t.tm, t.tn, t.wm, t.wn}, call.tokens, cfg->cols, whole, mean, d_grad_x);
     }
     return call.q.result();
 }

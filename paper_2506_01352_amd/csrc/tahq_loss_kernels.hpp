@@ -16,7 +16,7 @@ constexpr uint32_t kBadTarget = 0xffffffffu;
 
 // What the workspace holds of the tokens that count, in their order: row numbers, targets, and how many there are
 struct LossTokens {
-    uint32_t *rows, *targets, *count;
+    uint32_t *rows, *targets, *count;        // count[1]: k_loss_join's own
 };
 
 // ---------------------------------------------------------------- tokens that count
@@ -45,12 +45,12 @@ void k_loss_count(const int64_t *target, int64_t ignore, uint32_t rows, uint32_t
 
 constexpr uint32_t kGatherRows = 16;
 
-// Sixteen tokens to a workgroup, four to a wavefront.  counts: of the spans of kLossScan tokens, NULL if there is one.  zero, zero_also: float
+// Sixteen tokens to a workgroup, four to a wavefront.  gathered: blocks of 64 bytes of every row, `padded` rows each, `blocks` of them.  counts: of the spans of kLossScan tokens, NULL if there is one.  zero, zero_also: float
 // results of tokens that do not count (NULL: none); grad_x: their gradients.
 template <bool BF16>
 __global__ __launch_bounds__(256)
 void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts, uint32_t rows, uint32_t cols, uint32_t vocab, int64_t ignore,
-                   void *gathered, uint32_t ld, LossTokens tokens, float *zero, float *zero_also, void *grad_x)
+                   uint8_t *gathered, uint32_t blocks, uint32_t padded, LossTokens tokens, float *zero, float *zero_also, void *grad_x)
 {
     constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16>;
     __shared__ uint32_t places[4];
@@ -66,11 +66,10 @@ void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts,
     const uint32_t counted = (uint32_t)__ballot(t != ignore) & ((1u << kGatherRows) - 1);
     auto copy = [&](uint32_t from, uint32_t to, bool there) {
         const uint8_t *src = static_cast<const uint8_t *>(x) + (uint64_t)from * cols * ES;
-        uint8_t *dst = static_cast<uint8_t *>(gathered) + (uint64_t)to * ld * ES;
-        for (uint32_t c = lane * 8; c < ld; c += 512) {
+        for (uint32_t c = lane * 8; c < blocks * WHOLE; c += 512) {
             Eight<BF16> e = {};
             if (there && c < cols) e = fetch<BF16, false>(src, c, cols, false);
-            __builtin_memcpy(__builtin_assume_aligned(dst + c * ES, 16), e.q, sizeof e.q);
+            __builtin_memcpy(__builtin_assume_aligned(gathered + ((uint64_t)(c / WHOLE) * padded + to) * 64 + c % WHOLE * ES, 16), e.q, sizeof e.q);
         }
     };
     for (uint32_t i = wave * 4; i < wave * 4 + 4; ++i) {
@@ -98,23 +97,27 @@ void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts,
         // rows behind the last token up to a whole stage are zeros: they are summed over
         const uint32_t total = before + __popc(counted), end = (max(total, 1u) + WHOLE - 1) / WHOLE * WHOLE;
         for (uint32_t r = total + wave; r < end; r += 4) copy(0, r, false);
-        if (threadIdx.x == 0) *tokens.count = total;
+        if (threadIdx.x == 0) {
+            tokens.count[0] = total;
+            tokens.count[1] = 0;                             // workgroups that have joined their statistics
+        }
     }
 }
 
-// A piece of the weight with rows of whole stages, for odd numbers of channels
+// A piece of the weight in blocks, for numbers of channels that are not whole stages; rows up to whole stages, and channels, are filled up with zeros.
+// Sixteen rows to a workgroup, so that it writes runs of 1 KB.
 template <bool BF16>
 __global__ __launch_bounds__(256)
-void k_loss_pad(const void *weight, void *padded, uint64_t rows, uint32_t cols, uint32_t ld)
+void k_loss_blocks(const void *weight, uint8_t *blocks, uint32_t rows, uint32_t cols, uint32_t padded)
 {
-    constexpr uint32_t ES = BF16 ? 2 : 4;
-    const uint64_t per_row = ld / 8;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += (uint64_t)gridDim.x * 256) {
-        const uint64_t row = i / per_row;
-        const uint32_t c = (uint32_t)(i % per_row) * 8;
+    constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16>, RUNS = WHOLE / 8;
+    const uint32_t row = blockIdx.x * 16 + threadIdx.x / RUNS % 16;
+    if (row >= padded) return;
+    for (uint32_t c = (threadIdx.x / (16 * RUNS)) * WHOLE + threadIdx.x % RUNS * 8; c < (cols + WHOLE - 1) / WHOLE * WHOLE; c += 256 / (16 * RUNS) * WHOLE) {
         Eight<BF16> e = {};
-        if (c < cols) e = fetch<BF16, false>(static_cast<const uint8_t *>(weight) + row * cols * ES, c, cols, more_behind((uint32_t)min(row, (uint64_t)0xffffffff), (uint32_t)rows, cols));
-        __builtin_memcpy(__builtin_assume_aligned(static_cast<uint8_t *>(padded) + (row * ld + c) * ES, 16), e.q, sizeof e.q);
+        if (row < rows && c < cols)
+            e = fetch<BF16, false>(static_cast<const uint8_t *>(weight) + (uint64_t)row * cols * ES, c, cols, more_behind(row, rows, cols));
+        __builtin_memcpy(__builtin_assume_aligned(blocks + ((uint64_t)(c / WHOLE) * padded + row) * 64 + c % WHOLE * ES, 16), e.q, sizeof e.q);
     }
 }
 
@@ -122,7 +125,7 @@ void k_loss_pad(const void *weight, void *padded, uint64_t rows, uint32_t cols, 
 
 struct LogitArgs {
     const uint8_t *x, *weight;               // gathered hidden states, the piece's first row
-    uint64_t ldx, ldw;                       // bytes
+    uint64_t ldw;                            // bytes from row to row, or from block to block
     LossTokens tokens;
     uint32_t stages, first, vocab;           // of columns; the piece's first row of the vocabulary, and rows of the vocabulary up to the piece's end
     uint32_t tiles_n;
@@ -130,26 +133,25 @@ struct LogitArgs {
     float *at_target;                        // logits of the targets
     uint32_t part, padded;                   // number of the piece's first part
     const float *lse, *grad_loss;            // backward; grad_loss: of every token, or NULL
-    uint8_t *grads;                          // p - [v = t] of the piece, rows of ldg bytes
-    uint64_t ldg;
+    uint8_t *grads;                          // p - [v = t] of the piece, in blocks
 };
 
 enum { kStats = 0, kGrads = 1 };
 
-template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU, int MODE>
+// LIES: how the weight does
+template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES, int MODE>
 __global__ __launch_bounds__(256, PER_CU)
 void k_loss_logits(LogitArgs g)
 {
-    using T = TileKind_<BF16, WM, WN, MF, NF>;
-    __shared__ __attribute__((aligned(1024))) uint8_t s0[T::STAGE], s1[T::STAGE], s2[T::STAGE], s3[T::STAGE];
-    uint8_t *const stages[4] = {s0, s1, s2, s3};
+    using T = TileKind<BF16, WM, WN, MF, NF>;
+    const Stages stages = stages_of<T, LIES>();
     const uint32_t count = *g.tokens.count, tiles_m = (max(count, 1u) + T::UM * 32 - 1) / (T::UM * 32);
     if (blockIdx.x >= (uint64_t)tiles_m * g.tiles_n) return;
     uint32_t tm, tn;
     tile_of(blockIdx.x, tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
-    const Operand a = {g.x, g.ldx, max(count, 1u), 0}, b = {g.weight, g.ldw, g.vocab - g.first, 0};
-    multiply_tile<T, BF16, false, false, false>(a, b, tm, tn, 0, g.stages, stages, r);
+    const Operand a = {g.x, (uint64_t)g.padded * 64, g.padded, 0}, b = {g.weight, g.ldw, g.vocab - g.first, 0};
+    multiply_tile<T, BF16, kBlocks, LIES>(a, b, tm, tn, 0, g.stages, stages, r);
     const uint32_t lane = threadIdx.x % 64, half = lane / 32, wave = uniform(threadIdx.x / 64);
     const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = g.first + tn * T::UN * 32 + r.n0;         // n0: in the vocabulary
     auto column = [&](int j, int k) { return n0 + 32 * j + 8 * (k / 4) + 4 * half + k % 4; };
@@ -157,21 +159,24 @@ void k_loss_logits(LogitArgs g)
     if constexpr (MODE == kStats) {
 #pragma unroll
         for (int i = 0; i < MF; ++i) {
-            const uint32_t m = m0 + 32 * i + lane % 32, target = m < count ? g.tokens.targets[m] : kBadTarget;
-            float top = -INFINITY;
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t m = m0 + 32 * i + lane % 32;
+            asm volatile("" : "+v"(m));
+            const uint32_t target = m < count ? g.tokens.targets[m] : kBadTarget;
+            float l[NF][16], top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < NF; ++j)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    if (column(j, k) >= g.vocab) r.acc[i][j][k] = -INFINITY;
-                    top = fmaxf(top, r.acc[i][j][k]);
+                    l[j][k] = column(j, k) < g.vocab ? r.acc[i][j][k] : -INFINITY;
+                    top = fmaxf(top, l[j][k]);
                 }
             if (target - n0 < (uint32_t)NF * 32) {
 #pragma unroll
                 for (int j = 0; j < NF; ++j)
 #pragma unroll
                     for (int k = 0; k < 16; ++k)
-                        if (column(j, k) == target) g.at_target[m] = r.acc[i][j][k];
+                        if (column(j, k) == target) g.at_target[m] = l[j][k];
             }
             top = fmaxf(top, __shfl_xor(top, 32));
             const float shift = top == -INFINITY ? 0.0f : top;               // a part without a logit above -infinity: its sum is 0
@@ -179,7 +184,7 @@ void k_loss_logits(LogitArgs g)
 #pragma unroll
             for (int j = 0; j < NF; ++j)
 #pragma unroll
-                for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f((r.acc[i][j][k] - shift) * kLog2e);
+                for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f((l[j][k] - shift) * kLog2e);
             sum += __shfl_xor(sum, 32);
             if (half == 0 && m < count) g.parts[(uint64_t)(g.part + tn * WN + wave % WN) * g.padded + m] = make_float2(top, sum);
         }
@@ -198,19 +203,40 @@ void k_loss_logits(LogitArgs g)
             factor[i] = there && g.grad_loss ? g.grad_loss[row] : 1.0f;
             if (there && target[i] == kBadTarget) factor[i] = NAN;
         }
-        store_tile<T>(r, stages, [&](int i, int j, int k) {
-            const uint32_t m = m0 + 32 * i + lane % 32, v = column(j, k);
-            const float p = __builtin_amdgcn_exp2f((r.acc[i][j][k] - lse[i]) * kLog2e);
-            return m < count && v < g.vocab ? (v == target[i] ? p - 1.0f : p) * factor[i] : 0.0f;
-        }, [&](uint32_t m, uint32_t n, const float (&x)[4]) {
-            m += tm * T::UM * 32;
-            const uint64_t at = (uint64_t)(tn * T::UN * 32 + n) * T::ES;
-            if (m < end && at < g.ldg) {
-                uint8_t *to = g.grads + m * g.ldg + at;
-                if constexpr (BF16) *reinterpret_cast<uint2 *>(to) = make_uint2(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]));
-                else *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const uint32_t m = m0 + 32 * i + lane % 32;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                float d[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const uint32_t v = column(j, k);
+                    const float p = __builtin_amdgcn_exp2f((r.acc[i][j][k] - lse[i]) * kLog2e);
+                    d[k] = m < count && v < g.vocab ? (v == target[i] ? p - 1.0f : p) * factor[i] : 0.0f;
+                }
+                // of the vocabulary's last block all columns: zeros behind its end
+                const uint32_t n = n0 - g.first + 32 * j;                    // in the piece
+                if constexpr (BF16) {
+                    uint8_t *to = g.grads + ((uint64_t)(n / 32) * g.padded + m) * 64 + half * 16;
+                    const uint4 w0 = eight_of(four_bf16(d, 0), four_bf16(d, 4)), w1 = eight_of(four_bf16(d, 8), four_bf16(d, 12));
+                    if (m < end && g.first + n < g.vocab) {
+                        *reinterpret_cast<uint4 *>(to) = w0;
+                        *reinterpret_cast<uint4 *>(to + 32) = w1;
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        uint8_t *to = g.grads + ((uint64_t)(n / 16 + b) * g.padded + m) * 64 + half * 16;
+                        if (m < end && g.first + n + 16 * b < g.vocab) {
+                            *reinterpret_cast<float4 *>(to) = make_float4(d[8 * b], d[8 * b + 1], d[8 * b + 2], d[8 * b + 3]);
+                            *reinterpret_cast<float4 *>(to + 32) = make_float4(d[8 * b + 4], d[8 * b + 5], d[8 * b + 6], d[8 * b + 7]);
+                        }
+                    }
+                }
             }
-        });
+        }
     }
 }
 
@@ -221,67 +247,106 @@ __device__ __forceinline__ float loss_scale(const float *grad_loss, uint32_t mea
     return mean ? g / (float)max(count, 1u) : g;
 }
 
-// Sums over the vocabulary's piece: [part][tokens][cols], part blockIdx.y of the piece's stages, `run` each; `add` to what earlier pieces left
+// Sums over the vocabulary's piece, part blockIdx.y of its stages, `run` each; `add`: to what earlier pieces left.  They stay in the order that the
+// lanes have them in, [part][tile][wavefront][i][j][group of four][lane] of four numbers: 1 KB in a row.
 struct GradXArgs {
     const uint8_t *grads, *weight;
-    uint64_t ldg, ldw;
+    uint64_t ldw;
     LossTokens tokens;
     uint32_t rows, cols, stages, run, tiles_n, padded, add;
-    float *sums;
+    uint64_t tiles;                          // of a part
+    float4 *sums;
 };
-template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU>
+template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES>
 __global__ __launch_bounds__(256, PER_CU)
 void k_loss_grad_x(GradXArgs g)
 {
-    using T = TileKind_<BF16, WM, WN, MF, NF>;
-    __shared__ __attribute__((aligned(1024))) uint8_t s0[T::STAGE], s1[T::STAGE], s2[T::STAGE], s3[T::STAGE];
-    uint8_t *const stages[4] = {s0, s1, s2, s3};
+    using T = TileKind<BF16, WM, WN, MF, NF>;
+    const Stages stages = stages_of<T, LIES>();
     const uint32_t count = *g.tokens.count, tiles_m = (count + T::UM * 32 - 1) / (T::UM * 32);
     if (blockIdx.x >= (uint64_t)tiles_m * g.tiles_n) return;
     uint32_t tm, tn;
     tile_of(blockIdx.x, tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
-    const Operand a = {g.grads, g.ldg, count, 0}, b = {g.weight, g.ldw, g.cols, g.rows};
+    const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, 0}, b = {g.weight, g.ldw, g.rows, (g.cols + T::COLS - 1) / T::COLS};
     const uint32_t from = blockIdx.y * g.run;
-    multiply_tile<T, BF16, false, true, true>(a, b, tm, tn, from, min(g.run, g.stages - from), stages, r);
-    float *to = g.sums + (uint64_t)blockIdx.y * g.padded * g.cols;
-    store_tile<T>(r, stages, [&](int i, int j, int k) { return r.acc[i][j][k]; }, [&](uint32_t m, uint32_t n, const float (&x)[4]) {
-        m += tm * T::UM * 32;
-        n += tn * T::UN * 32;
-        if (m < count && n < g.cols)
-            store16<false>(to, (uint64_t)m * g.cols + n, g.cols - n, make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])), g.add != 0);
-    });
+    multiply_tile<T, BF16, kBlocks, LIES>(a, b, tm, tn, from, min(g.run, g.stages - from), stages, r);
+    uint32_t lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));                           // not an address to keep in registers all along
+    float4 *to = g.sums + (((uint64_t)blockIdx.y * g.tiles + (uint64_t)tm * g.tiles_n + tn) * 4 + uniform(threadIdx.x / 64)) * (MF * NF * 256) + lane;
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" : "+v"(to));                     // one by one: addresses of all of them would not fit the registers
+            float4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = g.add ? to[((i * NF + j) * 4 + k) * 64] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float16v &v = r.acc[i][j];
+                to[((i * NF + j) * 4 + k) * 64] = make_float4(x[k].x + v[4 * k], x[k].y + v[4 * k + 1], x[k].z + v[4 * k + 2], x[k].w + v[4 * k + 3]);
+            }
+        }
 }
 
-// The hidden states' gradient from its sums, to the tokens' own rows
+// Up to four neighbours
+template <bool BF16>
+__device__ __forceinline__ void store_four(void *to, uint64_t at, uint32_t valid, const float (&v)[4])
+{
+    if (valid >= 4) {
+        if constexpr (BF16) {
+            const uint2 w = four_bf16(v, 0);
+            __builtin_memcpy(static_cast<uint16_t *>(to) + at, &w, 8);
+        } else {
+            __builtin_memcpy(static_cast<float *>(to) + at, v, 16);
+        }
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (i < valid) store1<BF16>(to, at + i, v[i]);
+    }
+}
+
+// The hidden states' gradient from its sums, to the tokens' own rows.  How the sums lie: tiles of tm x tn, wavefronts of wm x wn in them.  A wavefront takes
+// eight tokens, whose numbers lie side by side, and 32 columns at a time.
+struct SumsLayout {
+    uint32_t tm, tn, wm, wn;
+};
 template <bool BF16>
 __global__ __launch_bounds__(256)
-void k_loss_scatter(const float *sums, uint32_t parts, uint32_t padded, LossTokens tokens, uint32_t cols, const float *grad_loss, uint32_t mean, void *grad_x)
+void k_loss_scatter(const float4 *sums, uint32_t parts, uint64_t tiles, uint32_t tiles_n, SumsLayout s, LossTokens tokens, uint32_t cols, const float *grad_loss, uint32_t mean,
+                    void *grad_x)
 {
-    constexpr uint32_t ES = BF16 ? 2 : 4;
-    const uint32_t lane = threadIdx.x % 64, count = *tokens.count;
+    const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), count = *tokens.count, r = blockIdx.x * 8 + lane % 8;
+    if (blockIdx.x * 8 >= count) return;
     const float scale = loss_scale(grad_loss, mean, count);
-    for (uint32_t r = blockIdx.x * 4 + uniform(threadIdx.x / 64); r < count; r += gridDim.x * 4) {
-        uint8_t *to = static_cast<uint8_t *>(grad_x) + (uint64_t)tokens.rows[r] * cols * ES;
-        for (uint32_t c = lane * 8; c < cols; c += 512) {
-            float v[8] = {};
+    const bool there = r < count;
+    const uint64_t row = there ? (uint64_t)tokens.rows[r] * cols : 0;
+    const uint32_t m = r % s.tm, units = s.wn / 32, piece = s.wm * s.wn / 4;              // piece: of a wavefront, in fours
+    for (uint32_t c = blockIdx.y * 128 + wave * 32 + lane / 8 * 4; c < cols; c += gridDim.y * 128) {
+        const uint32_t n = c % s.tn, w = m / s.wm * (s.tn / s.wn) + n / s.wn, unit = m % s.wm / 32 * units + n % s.wn / 32;
+        const float4 *from = sums + ((uint64_t)(r / s.tm) * tiles_n + c / s.tn) * 4 * piece + w * piece + (unit * 4 + n % 32 / 8) * 64 + n % 8 / 4 * 32 + m % 32;
+        float v[4] = {};
+        if (there)
             for (uint32_t p = 0; p < parts; ++p) {
-                const Eight<false> e = fetch<false, false>(sums + ((uint64_t)p * padded + r) * cols, c, cols, false);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += e[i];
+                const float4 x = from[p * tiles * 4 * piece];
+                v[0] += x.x;
+                v[1] += x.y;
+                v[2] += x.z;
+                v[3] += x.w;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= scale;
-            keep<BF16, false>(to, c, cols, v);
-        }
+        for (int i = 0; i < 4; ++i) v[i] *= scale;
+        if (there) store_four<BF16>(grad_x, row + c, cols - c, v);
     }
 }
 
 struct GradWArgs {
     const uint8_t *grads, *x;
-    uint64_t ldg, ldx;
     LossTokens tokens;
-    uint32_t rows, cols, tiles_m, tiles_n;   // rows of the piece
+    uint32_t rows, cols, tiles_m, tiles_n, padded;           // rows of the piece
     const float *grad_loss;                  // of the reduced loss, or NULL
     uint32_t mean, out_bf16, accumulate;
     void *out;                               // the gradient's first row of the piece
@@ -290,75 +355,84 @@ template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU>
 __global__ __launch_bounds__(256, PER_CU)
 void k_loss_grad_w(GradWArgs g)
 {
-    using T = TileKind_<BF16, WM, WN, MF, NF>;
-    __shared__ __attribute__((aligned(1024))) uint8_t s0[T::STAGE], s1[T::STAGE], s2[T::STAGE], s3[T::STAGE];
-    uint8_t *const stages[4] = {s0, s1, s2, s3};
+    using T = TileKind<BF16, WM, WN, MF, NF>;
+    const Stages stages = stages_of<T, kBlocksTurned>();
     const uint32_t count = *g.tokens.count, depth = (max(count, 1u) + T::COLS - 1) / T::COLS;
     uint32_t tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
-    const Operand a = {g.grads, g.ldg, g.rows, 0}, b = {g.x, g.ldx, g.cols, 0};
-    multiply_tile<T, BF16, true, true, false>(a, b, tm, tn, 0, depth, stages, r);
+    const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, (g.rows + T::COLS - 1) / T::COLS}, b = {g.x, (uint64_t)g.padded * 64, g.padded, (g.cols + T::COLS - 1) / T::COLS};
+    multiply_tile<T, BF16, kBlocksTurned, kBlocksTurned>(a, b, tm, tn, 0, depth, stages, r);
     const float scale = loss_scale(g.grad_loss, g.mean, count);
-    store_tile<T>(r, stages, [&](int i, int j, int k) { return r.acc[i][j][k] * scale; }, [&](uint32_t m, uint32_t n, const float (&x)[4]) {
-        m += tm * T::UM * 32;
-        n += tn * T::UN * 32;
-        if (m >= g.rows || n >= g.cols) return;
-        float y[4] = {x[0], x[1], x[2], x[3]};
-        if (g.out_bf16) store4<true>(g.out, g.cols, m, n, g.cols, y, g.accumulate != 0);
-        else store4<false>(g.out, g.cols, m, n, g.cols, y, g.accumulate != 0);
-    });
+    const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = tn * T::UN * 32 + r.n0;
+    if (g.out_bf16) store_rows<true, T>(r, m0, n0, g.rows, g.cols, scale, g.out, g.accumulate != 0);
+    else store_rows<false, T>(r, m0, n0, g.rows, g.cols, scale, g.out, g.accumulate != 0);
 }
 
 // ---------------------------------------------------------------- joining
 
-// 32 tokens to a workgroup, the parts in eight runs.  `later`: with what earlier pieces of the vocabulary left in `running`; `last`: there is no
-// piece after this one.
+// The parts of some tokens' statistics, and at the end of the vocabulary (`last`) lse and losses; `later`: with what earlier pieces left in `running`.
+// A workgroup of 256 takes `width` tokens, a power of two up to 32, and the parts in 256 / width runs, four at a time.  The last workgroup that is
+// done adds up the losses of all tokens, in their order.
 __global__ __launch_bounds__(256)
 void k_loss_join(const float2 *from, uint32_t parts, uint32_t padded, LossTokens tokens, const float *at_target, float2 *running, uint32_t later,
-                 uint32_t last, float *losses, float *lse)
+                 uint32_t last, uint32_t width, float *losses, float *lse, uint32_t rows, uint32_t mean, float *total)
 {
-    __shared__ float2 places[8][32];
-    const uint32_t lane = threadIdx.x % 32, run = threadIdx.x / 32, count = *tokens.count, r = blockIdx.x * 32 + lane;
-    if (blockIdx.x * 32 >= count) return;
+    __shared__ float2 places[256];
+    __shared__ uint32_t done;
+    const uint32_t lane = threadIdx.x % width, run = threadIdx.x / width, runs = 256 / width, count = *tokens.count, r = blockIdx.x * width + lane;
     auto joined = [](float2 a, float2 b) {
         const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
         return make_float2(top, a.y * __expf(a.x - shift) + b.y * __expf(b.x - shift));
     };
     float2 v = make_float2(-INFINITY, 0.0f);
     if (r < count)
-        for (uint32_t p = run; p < parts; p += 8) v = joined(v, from[(uint64_t)p * padded + r]);
-    places[run][lane] = v;
-    __syncthreads();
-    if (run == 0 && r < count) {
-        for (int i = 1; i < 8; ++i) v = joined(v, places[i][lane]);
-        if (later) v = joined(running[r], v);
-        if (!last) {
-            running[r] = v;
-            return;
+        for (uint32_t p = run; p < parts; p += 4 * runs) {
+            // behind the last part the first of the four again, which then does not count
+            const float2 *const at = from + (uint64_t)p * padded + r;
+            const uint64_t step = (uint64_t)runs * padded;
+            float2 w0 = *at, w1 = at[p + runs < parts ? step : 0], w2 = at[p + 2 * runs < parts ? 2 * step : 0], w3 = at[p + 3 * runs < parts ? 3 * step : 0];
+            if (p + runs >= parts) w1.x = -INFINITY, w1.y = 0.0f;
+            if (p + 2 * runs >= parts) w2.x = -INFINITY, w2.y = 0.0f;
+            if (p + 3 * runs >= parts) w3.x = -INFINITY, w3.y = 0.0f;
+            v = joined(v, joined(joined(w0, w1), joined(w2, w3)));
         }
-        const float all = v.x + logf(v.y);
-        const uint32_t row = tokens.rows[r];
-        lse[row] = all;
-        losses[row] = tokens.targets[r] == kBadTarget ? NAN : all - at_target[r];
+    places[threadIdx.x] = v;
+    __syncthreads();
+    for (uint32_t half = 128; half >= width; half /= 2) {
+        if (threadIdx.x < half) places[threadIdx.x] = joined(places[threadIdx.x], places[threadIdx.x + half]);
+        __syncthreads();
     }
-}
-
-// The reduced loss and the number of tokens that count
-__global__ __launch_bounds__(1024)
-void k_loss_total(const float *losses, uint32_t rows, LossTokens tokens, uint32_t mean, float *total)
-{
-    __shared__ float sums[1024];
+    if (run == 0 && r < count) {
+        v = places[lane];
+        if (later) v = joined(running[r], v);
+        if (last) {
+            const float all = v.x + logf(v.y);
+            const uint32_t row = tokens.rows[r];
+            lse[row] = all;
+            losses[row] = tokens.targets[r] == kBadTarget ? NAN : all - at_target[r];
+        } else {
+            running[r] = v;
+        }
+    }
+    if (!last) return;
+    // losses are visible to whoever sees this workgroup counted
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) done = atomicAdd(tokens.count + 1, 1u);
+    __syncthreads();
+    if (done != gridDim.x - 1) return;
+    __threadfence();
     float sum = 0.0f;
-    for (uint64_t i = threadIdx.x; i < rows; i += 1024) sum += losses[i];
+    for (uint32_t i = threadIdx.x; i < rows; i += 256) sum += __hip_atomic_load(losses + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float *const sums = reinterpret_cast<float *>(places);
     sums[threadIdx.x] = sum;
     __syncthreads();
-    for (uint32_t half = 512; half; half /= 2) {
+    for (uint32_t half = 128; half; half /= 2) {
         if (threadIdx.x < half) sums[threadIdx.x] += sums[threadIdx.x + half];
         __syncthreads();
     }
     if (threadIdx.x == 0) {
-        const uint32_t count = *tokens.count;
         total[0] = mean ? sums[0] / (float)max(count, 1u) : sums[0];
         total[1] = (float)count;
     }

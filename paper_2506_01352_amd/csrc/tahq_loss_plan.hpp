@@ -9,11 +9,11 @@ namespace tahq {
 constexpr uint32_t kLossSpan = 4096;         // tokens that are counted together
 constexpr uint64_t kLossBudget = 256u << 20; // bytes of a piece, where the hidden states have no more
 
-// Tiles: 256 x 256, 128 x 128, 32 x 128; wavefronts side by side along the second
+// Tiles, and what a wavefront has of one; `along`: wavefronts side by side along the second
 struct LossTile {
-    uint32_t tm, tn, along;
+    uint32_t tm, tn, wm, wn, along;
 };
-constexpr LossTile kLossTiles[] = {{256, 256, 2}, {128, 128, 2}, {32, 128, 4}};
+constexpr LossTile kLossTiles[] = {{256, 256, 128, 128, 2}, {128, 128, 64, 64, 2}, {32, 128, 32, 32, 4}};
 enum { kLossLarge = 0, kLossMiddle = 1, kLossFew = 2 };
 
 inline uint64_t loss_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
@@ -27,7 +27,7 @@ inline int loss_kind(bool bf16, uint64_t m, uint64_t n)
 }
 
 struct LossPlan {
-    bool bf16, pad;                          // pad: rows of the weight are copied to rows of whole stages
+    bool bf16, pad;                          // pad: the weight is copied into blocks of whole stages
     uint32_t es, whole, ldx, padded;         // bytes of an element; columns of a stage; elements of a gathered row; tokens up to whole stages
     uint32_t spans;                          // of kLossSpan tokens
     uint32_t forward_piece, backward_piece;  // rows of the vocabulary
@@ -35,8 +35,7 @@ struct LossPlan {
     uint32_t parts, x_parts, x_run;          // of a forward piece's statistics; of the sums for the hidden states' gradient, stages of a part
     // places in the workspace
     uint64_t rows, targets, counts, x, at_target, running, stats, forward_weight, forward_total;
-    uint64_t grads, sums, backward_weight, backward_total;
-    uint64_t ldg;                            // bytes
+    uint64_t x_tiles, grads, sums, backward_weight, backward_total;
 };
 
 inline LossPlan plan_loss(const tahq_loss_config *c)
@@ -82,16 +81,16 @@ inline LossPlan plan_loss(const tahq_loss_config *c)
     p.backward_piece = piece((uint64_t)p.padded * p.es);
     if (p.pad && piece((uint64_t)p.ldx * p.es) < p.backward_piece) p.backward_piece = piece((uint64_t)p.ldx * p.es);
     const uint64_t widest = p.backward_piece < c->vocab ? p.backward_piece : c->vocab;
-    p.ldg = loss_ceil(widest * p.es, 64) * 64;
     p.grads_kind = loss_kind(p.bf16, c->rows, widest);
     p.x_kind = loss_kind(p.bf16, c->rows, c->cols);
     // few tiles: several of them share the sums over the vocabulary, sixteen stages and more for each
-    const uint64_t tiles = loss_tiles(p.x_kind, c->rows, c->cols), stages = loss_ceil(widest, p.whole), want = loss_ceil(p.x_kind == kLossLarge ? 256 : 512, tiles);
-    const uint64_t most = stages / 16 ? stages / 16 : 1, parts = want < most ? want : most;
+    const uint64_t tiles = loss_tiles(p.x_kind, c->rows, c->cols), stages = loss_ceil(widest, p.whole), at_once = p.x_kind == kLossLarge ? 256 : 512;
+    const uint64_t most = stages / 16 ? stages / 16 : 1, want = at_once / tiles ? at_once / tiles : 1, parts = want < most ? want : most;
     p.x_run = (uint32_t)loss_ceil(stages, parts);
     p.x_parts = (uint32_t)loss_ceil(stages, p.x_run);
-    p.grads = place((uint64_t)p.padded * p.ldg);
-    p.sums = place((uint64_t)p.x_parts * p.padded * c->cols * 4);
+    p.grads = place((uint64_t)p.padded * loss_ceil(widest, p.whole) * 64);
+    p.x_tiles = tiles;
+    p.sums = place(p.x_parts * tiles * kLossTiles[p.x_kind].tm * kLossTiles[p.x_kind].tn * 4);
     p.backward_weight = place(p.pad ? (uint64_t)p.backward_piece * p.ldx * p.es : 0);
     p.backward_total = at;
     return p;
