@@ -19,7 +19,7 @@ tahq_status check(const tahq_loss_config *c)
     if (c->cols > TAHQ_LOSS_MAX_COLS || c->rows > TAHQ_LOSS_MAX_ROWS) return TAHQ_ERR_UNSUPPORTED;
     const LossPlan p = plan_loss(c);
     if (!launchable(loss_tiles(p.forward_kind, c->rows, p.forward_piece), 256) || !launchable(loss_tiles(p.grads_kind, c->rows, p.backward_piece), 256) ||
-        !launchable(loss_tiles(p.x_kind, c->rows, c->cols), 256) || !launchable(loss_tiles(kLossMiddle, p.backward_piece, c->cols), 256) ||
+        !launchable(p.x_groups, 256) || !launchable(loss_tiles(kLossMiddle, p.backward_piece, c->cols), 256) ||
         !launchable(loss_ceil(c->rows, kGatherRows), 256))
         return TAHQ_ERR_UNSUPPORTED;
     return TAHQ_OK;
@@ -40,7 +40,7 @@ struct Call {
     void gather(const void *d_x, const int64_t *d_target, float *zero, float *zero_also, void *grad_x)
     {
         uint32_t *counts = p.spans > 1 ? at<uint32_t>(p.counts) : nullptr;
-        if (counts) q(k_loss_count, dim3(p.spans), dim3(256), d_target, cfg->ignore, cfg->rows, counts);
+        if (counts) q(k_loss_count, dim3(p.spans), dim3(1024), d_target, cfg->ignore, cfg->rows, counts);
         q(p.bf16 ? k_loss_gather<true> : k_loss_gather<false>, dim3((uint32_t)loss_ceil(cfg->rows, kGatherRows)), dim3(256), d_x, d_target, counts, cfg->rows, cfg->cols,
           cfg->vocab, cfg->ignore, at<uint8_t>(p.x), p.ldx / p.whole, p.padded, tokens, zero, zero_also, grad_x);
     }
@@ -84,7 +84,7 @@ struct Call {
     template <Lies LIES>
     void grad_x_of(const GradXArgs &g)
     {
-        const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[p.x_kind].tm) * g.tiles_n), (uint32_t)loss_ceil(g.stages, g.run)), block(256);
+        const dim3 grid((uint32_t)p.x_groups), block(256);
         if (p.x_kind == kLossLarge) q(k_loss_grad_x<true, 2, 2, 4, 4, 1, LIES>, grid, block, g);
         else if (p.x_kind == kLossMiddle) p.bf16 ? q(k_loss_grad_x<true, 2, 2, 2, 2, 2, LIES>, grid, block, g) : q(k_loss_grad_x<false, 2, 2, 2, 2, 2, LIES>, grid, block, g);
         else p.bf16 ? q(k_loss_grad_x<true, 1, 4, 1, 1, 3, LIES>, grid, block, g) : q(k_loss_grad_x<false, 1, 4, 1, 1, 3, LIES>, grid, block, g);
@@ -136,18 +136,21 @@ tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, cons
         if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
     if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target) return TAHQ_ERR_MISALIGNED;
     call.gather(d_x, d_target, d_losses, d_lse, nullptr);
-    // tokens of a workgroup that joins statistics: fewer where there would be few workgroups
+    // tokens of a workgroup that joins statistics: up to 32 in one, then a workgroup to every compute unit and more
     uint32_t width = 32;
-    while (width > 1 && cfg->rows < 256 * width) width /= 2;
+    while (width > 1 && (cfg->rows <= 32 ? cfg->rows <= width / 2 : cfg->rows < 256 * width)) width /= 2;
+    const bool alone = cfg->rows <= width;
     for (uint32_t first = 0; first < cfg->vocab; first += p.forward_piece) {
         const uint32_t rows = cfg->vocab - first < p.forward_piece ? cfg->vocab - first : p.forward_piece;
         LogitArgs g = call.logit_args(call.weight(d_weight, first, rows, p.forward_weight), first, rows, p.forward_kind);
         g.parts = call.at<float2>(p.stats);
         g.at_target = call.at<float>(p.at_target);
         call.logits<kStats>(p.forward_kind, g);
-        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, width)), dim3(256), g.parts, g.tiles_n * kLossTiles[p.forward_kind].along, p.padded, call.tokens, g.at_target,
-               call.at<float2>(p.running), first != 0, first + rows == cfg->vocab, width, d_losses, d_lse, cfg->rows, cfg->reduction == TAHQ_LOSS_MEAN, d_total);
+        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, width)), dim3(kJoinLanes), g.parts, g.tiles_n * kLossTiles[p.forward_kind].along, p.padded, call.tokens, g.at_target,
+               call.at<float2>(p.running), first != 0, first + rows == cfg->vocab, width, d_losses, d_lse, cfg->reduction == TAHQ_LOSS_MEAN,
+               alone && first + rows == cfg->vocab ? d_total : nullptr);
     }
+    if (!alone) call.q(k_loss_total, dim3(1), dim3(kJoinLanes), d_losses, cfg->rows, call.tokens, cfg->reduction == TAHQ_LOSS_MEAN, d_total);
     return call.q.result();
 }
 
@@ -179,8 +182,8 @@ tahq_status tahq_loss_backward(const tahq_loss_config *cfg, const void *d_x, con
         g.grads = call.at<uint8_t>(p.grads);
         call.logits<kGrads>(p.grads_kind, g);
         if (d_grad_x)
-            call.grad_x({g.grads, w.first, w.second, call.tokens, rows, cfg->cols, (uint32_t)loss_ceil(rows, p.whole), p.x_run,
-                         (uint32_t)loss_ceil(cfg->cols, kLossTiles[p.x_kind].tn), p.padded, first != 0, p.x_tiles, call.at<float4>(p.sums)});
+            call.grad_x({g.grads, w.first, w.second, call.tokens, rows, cfg->cols, (uint32_t)loss_ceil(rows, p.whole), p.x_slots,
+                         (uint32_t)loss_ceil(cfg->cols, kLossTiles[p.x_kind].tn), p.padded, first != 0, call.at<float4>(p.sums)});
         if (d_grad_weight)
             call.grad_w({g.grads, g.x, call.tokens, rows, cfg->cols, 0, 0, p.padded, whole, mean, cfg->weight_dtype == TAHQ_BF16, cfg->accumulate,
                          static_cast<uint8_t *>(d_grad_weight) + (uint64_t)first * cfg->cols * (cfg->weight_dtype == TAHQ_BF16 ? 2 : 4)});
@@ -188,7 +191,7 @@ tahq_status tahq_loss_backward(const tahq_loss_config *cfg, const void *d_x, con
     if (d_grad_x) {
         const LossTile &t = kLossTiles[p.x_kind];
         const uint32_t eights = (uint32_t)loss_ceil(cfg->rows, 8), columns = (uint32_t)loss_ceil(cfg->cols, 128);
-        call.q(p.bf16 ? k_loss_scatter<true> : k_loss_scatter<false>, dim3(eights, columns < 8 ? columns : 8), dim3(256), call.at<float4>(p.sums), p.x_parts, p.x_tiles,
+        call.q(p.bf16 ? k_loss_scatter<true> : k_loss_scatter<false>, dim3(eights, columns < 8 ? columns : 8), dim3(256), call.at<float4>(p.sums), p.x_stages, p.x_slots,
                (uint32_t)loss_ceil(cfg->cols, t.tn), SumsLayout{t.tm, t.tn, t.wm, t.wn}, call.tokens, cfg->cols, whole, mean, d_grad_x);
     }
     return call.q.result();

@@ -16,91 +16,107 @@ constexpr uint32_t kBadTarget = 0xffffffffu;
 
 // What the workspace holds of the tokens that count, in their order: row numbers, targets, and how many there are
 struct LossTokens {
-    uint32_t *rows, *targets, *count;        // count[1]: k_loss_join's own
+    uint32_t *rows, *targets, *count;
 };
 
 // ---------------------------------------------------------------- tokens that count
 
-__device__ __forceinline__ uint32_t group_count(uint32_t v, uint32_t (&places)[4])
+template <int WAVES>
+__device__ __forceinline__ uint32_t group_count(uint32_t v, uint32_t (&places)[WAVES])
 {
     for (int step = 1; step < 64; step *= 2) v += __shfl_xor(v, step);
-    __syncthreads();
     if (threadIdx.x % 64 == 0) places[threadIdx.x / 64] = v;
     __syncthreads();
-    return places[0] + places[1] + places[2] + places[3];
+    v = places[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) v += places[i];
+    return v;
 }
 
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(1024)
 void k_loss_count(const int64_t *target, int64_t ignore, uint32_t rows, uint32_t *counts)
 {
-    __shared__ uint32_t places[4];
+    __shared__ uint32_t places[16];
     uint32_t n = 0;
-    for (uint32_t i = threadIdx.x; i < kLossScan; i += 256) {
-        const uint64_t row = (uint64_t)blockIdx.x * kLossScan + i;
-        n += row < rows && target[row] != ignore;
+#pragma unroll
+    for (uint32_t i = 0; i < kLossScan / 1024; ++i) {
+        const uint32_t row = min(blockIdx.x * kLossScan + i * 1024 + threadIdx.x, rows - 1);
+        n += target[row] != ignore && row == blockIdx.x * kLossScan + i * 1024 + threadIdx.x;
     }
     n = group_count(n, places);
     if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
-constexpr uint32_t kGatherRows = 16;
+constexpr uint32_t kGatherRows = 4;          // of a workgroup, one to a wavefront
 
-// Sixteen tokens to a workgroup, four to a wavefront.  gathered: blocks of 64 bytes of every row, `padded` rows each, `blocks` of them.  counts: of the spans of kLossScan tokens, NULL if there is one.  zero, zero_also: float
-// results of tokens that do not count (NULL: none); grad_x: their gradients.
+// gathered: blocks of 64 bytes of every row, `padded` rows each, `blocks` of them.  counts: of the spans of kLossScan tokens, NULL if there is one.
+// zero, zero_also: float results of tokens that do not count (NULL: none); grad_x: their gradients.
 template <bool BF16>
 __global__ __launch_bounds__(256)
 void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts, uint32_t rows, uint32_t cols, uint32_t vocab, int64_t ignore,
                    uint8_t *gathered, uint32_t blocks, uint32_t padded, LossTokens tokens, float *zero, float *zero_also, void *grad_x)
 {
-    constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16>;
+    constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16>, AHEAD = 4;
     __shared__ uint32_t places[4];
-    const uint32_t first = blockIdx.x * kGatherRows, span = first / kLossScan;
-    uint32_t before = 0;
-    for (uint32_t i = threadIdx.x; i < span; i += 256) before += counts[i];
-    for (uint32_t i = span * kLossScan + threadIdx.x; i < first; i += 256) before += target[i] != ignore;
-    before = group_count(before, places);
-    const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64);
-    // all sixteen tokens, the same in every wavefront
-    const uint32_t row = first + lane % kGatherRows;
-    const int64_t t = row < rows ? target[row] : ignore;
-    const uint32_t counted = (uint32_t)__ballot(t != ignore) & ((1u << kGatherRows) - 1);
-    auto copy = [&](uint32_t from, uint32_t to, bool there) {
-        const uint8_t *src = static_cast<const uint8_t *>(x) + (uint64_t)from * cols * ES;
-        for (uint32_t c = lane * 8; c < blocks * WHOLE; c += 512) {
-            Eight<BF16> e = {};
-            if (there && c < cols) e = fetch<BF16, false>(src, c, cols, false);
-            __builtin_memcpy(__builtin_assume_aligned(gathered + ((uint64_t)(c / WHOLE) * padded + to) * 64 + c % WHOLE * ES, 16), e.q, sizeof e.q);
+    const uint32_t first = blockIdx.x * kGatherRows, span = first / kLossScan, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), row = first + wave;
+    // the row is on its way while its place is counted
+    Eight<BF16> e[AHEAD];
+    auto ask = [&](uint32_t c0) {
+        const uint8_t *src = static_cast<const uint8_t *>(x) + (uint64_t)row * cols * ES;
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k) {
+            const uint32_t c = c0 + k * 512 + lane * 8;
+            e[k] = Eight<BF16>{};
+            if (row < rows && c < cols) e[k] = fetch<BF16, false>(src, c, cols, more_behind(row, rows, cols));
         }
     };
-    for (uint32_t i = wave * 4; i < wave * 4 + 4; ++i) {
-        if (first + i >= rows) break;
-        const uint32_t rank = before + __popc(counted & ((1u << i) - 1));
-        if (counted >> i & 1) {
-            copy(first + i, rank, true);
+    auto put = [&](uint32_t c0, uint32_t to) {
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k) {
+            const uint32_t c = c0 + k * 512 + lane * 8;
+            if (c < blocks * WHOLE) __builtin_memcpy(__builtin_assume_aligned(gathered + ((uint64_t)(c / WHOLE) * padded + to) * 64 + c % WHOLE * ES, 16), e[k].q, sizeof e[k].q);
+        }
+    };
+    ask(0);
+    const uint32_t any = first + lane % kGatherRows;         // the workgroup's tokens, the same in every wavefront
+    const int64_t t = any < rows ? target[any] : ignore;
+    uint32_t before = 0;
+    for (uint32_t i = threadIdx.x; i < span; i += 256) before += counts[i];
+#pragma unroll 4
+    for (uint32_t i = span * kLossScan + threadIdx.x; i < first; i += 256) before += target[i] != ignore;
+    before = group_count(before, places);
+    const uint32_t counted = (uint32_t)__ballot(t != ignore) & ((1u << kGatherRows) - 1);
+    if (row < rows) {
+        const uint32_t rank = before + __popc(counted & ((1u << wave) - 1));
+        if (counted >> wave & 1) {
+            put(0, rank);
+            for (uint32_t c0 = AHEAD * 512; c0 < blocks * WHOLE; c0 += AHEAD * 512) {
+                ask(c0);
+                put(c0, rank);
+            }
+            if (lane == wave) {
+                tokens.rows[rank] = row;
+                tokens.targets[rank] = t >= 0 && t < (int64_t)vocab ? (uint32_t)t : kBadTarget;
+            }
         } else {
             if (lane == 0) {
-                if (zero) zero[first + i] = 0.0f;
-                if (zero_also) zero_also[first + i] = 0.0f;
+                if (zero) zero[row] = 0.0f;
+                if (zero_also) zero_also[row] = 0.0f;
             }
             if (grad_x) {
                 const float zeros[8] = {};
-                for (uint32_t c = lane * 8; c < cols; c += 512) keep<BF16, false>(static_cast<uint8_t *>(grad_x) + (uint64_t)(first + i) * cols * ES, c, cols, zeros);
+                for (uint32_t c = lane * 8; c < cols; c += 512) keep<BF16, false>(static_cast<uint8_t *>(grad_x) + (uint64_t)row * cols * ES, c, cols, zeros);
             }
         }
-    }
-    if (wave == 0 && lane < kGatherRows && (counted >> lane & 1)) {
-        const uint32_t rank = before + __popc(counted & ((1u << lane) - 1));
-        tokens.rows[rank] = row;
-        tokens.targets[rank] = t >= 0 && t < (int64_t)vocab ? (uint32_t)t : kBadTarget;
     }
     if (blockIdx.x == gridDim.x - 1) {
         // rows behind the last token up to a whole stage are zeros: they are summed over
         const uint32_t total = before + __popc(counted), end = (max(total, 1u) + WHOLE - 1) / WHOLE * WHOLE;
-        for (uint32_t r = total + wave; r < end; r += 4) copy(0, r, false);
-        if (threadIdx.x == 0) {
-            tokens.count[0] = total;
-            tokens.count[1] = 0;                             // workgroups that have joined their statistics
-        }
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k) e[k] = Eight<BF16>{};
+        for (uint32_t r = total + wave; r < end; r += 4)
+            for (uint32_t c0 = 0; c0 < blocks * WHOLE; c0 += AHEAD * 512) put(c0, r);
+        if (threadIdx.x == 0) *tokens.count = total;
     }
 }
 
@@ -247,14 +263,24 @@ __device__ __forceinline__ float loss_scale(const float *grad_loss, uint32_t mea
     return mean ? g / (float)max(count, 1u) : g;
 }
 
-// Sums over the vocabulary's piece, part blockIdx.y of its stages, `run` each; `add`: to what earlier pieces left.  They stay in the order that the
-// lanes have them in, [part][tile][wavefront][i][j][group of four][lane] of four numbers: 1 KB in a row.
+// How sums over a piece's `stages` are shared: `parts` of `run` stages, so many that `slots` workgroups, what the device holds at once, have one each of
+// the tiles of the tokens that count; sixteen stages and more to a part.  Later pieces have as many parts as the first or, with fewer stages, fewer.
+struct Shares {
+    uint32_t tiles, parts, run;
+    __device__ __forceinline__ Shares(uint32_t tiles_, uint32_t stages, uint32_t slots) : tiles(tiles_)
+    {
+        const uint32_t most = max(stages / 16, 1u), want = min(max(slots / max(tiles, 1u), 1u), most);
+        run = (stages + want - 1) / want;
+        parts = (stages + run - 1) / run;
+    }
+};
+// Sums over the vocabulary's piece, in parts; `add`: to what earlier pieces left.  They stay in the order that the lanes have them in, [part][tile]
+// [wavefront][i][j][group of four][lane] of four numbers: 1 KB in a row.
 struct GradXArgs {
     const uint8_t *grads, *weight;
     uint64_t ldw;
     LossTokens tokens;
-    uint32_t rows, cols, stages, run, tiles_n, padded, add;
-    uint64_t tiles;                          // of a part
+    uint32_t rows, cols, stages, slots, tiles_n, padded, add;
     float4 *sums;
 };
 template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES>
@@ -264,16 +290,18 @@ void k_loss_grad_x(GradXArgs g)
     using T = TileKind<BF16, WM, WN, MF, NF>;
     const Stages stages = stages_of<T, LIES>();
     const uint32_t count = *g.tokens.count, tiles_m = (count + T::UM * 32 - 1) / (T::UM * 32);
-    if (blockIdx.x >= (uint64_t)tiles_m * g.tiles_n) return;
+    const Shares shares(tiles_m * g.tiles_n, g.stages, g.slots);
+    const uint32_t part = shares.tiles ? blockIdx.x / shares.tiles : shares.parts;
+    if (part >= shares.parts) return;
     uint32_t tm, tn;
-    tile_of(blockIdx.x, tiles_m, g.tiles_n, tm, tn);
+    tile_of(blockIdx.x % shares.tiles, tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
     const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, 0}, b = {g.weight, g.ldw, g.rows, (g.cols + T::COLS - 1) / T::COLS};
-    const uint32_t from = blockIdx.y * g.run;
-    multiply_tile<T, BF16, kBlocks, LIES>(a, b, tm, tn, from, min(g.run, g.stages - from), stages, r);
+    const uint32_t from = part * shares.run;
+    multiply_tile<T, BF16, kBlocks, LIES>(a, b, tm, tn, from, min(shares.run, g.stages - from), stages, r);
     uint32_t lane = threadIdx.x % 64;
     asm volatile("" : "+v"(lane));                           // not an address to keep in registers all along
-    float4 *to = g.sums + (((uint64_t)blockIdx.y * g.tiles + (uint64_t)tm * g.tiles_n + tn) * 4 + uniform(threadIdx.x / 64)) * (MF * NF * 256) + lane;
+    float4 *to = g.sums + (((uint64_t)part * shares.tiles + (uint64_t)tm * g.tiles_n + tn) * 4 + uniform(threadIdx.x / 64)) * (MF * NF * 256) + lane;
 #pragma unroll
     for (int i = 0; i < MF; ++i)
 #pragma unroll
@@ -314,13 +342,15 @@ __device__ __forceinline__ void store_four(void *to, uint64_t at, uint32_t valid
 struct SumsLayout {
     uint32_t tm, tn, wm, wn;
 };
+// stages: of the first piece
 template <bool BF16>
 __global__ __launch_bounds__(256)
-void k_loss_scatter(const float4 *sums, uint32_t parts, uint64_t tiles, uint32_t tiles_n, SumsLayout s, LossTokens tokens, uint32_t cols, const float *grad_loss, uint32_t mean,
+void k_loss_scatter(const float4 *sums, uint32_t stages, uint32_t slots, uint32_t tiles_n, SumsLayout s, LossTokens tokens, uint32_t cols, const float *grad_loss, uint32_t mean,
                     void *grad_x)
 {
     const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), count = *tokens.count, r = blockIdx.x * 8 + lane % 8;
     if (blockIdx.x * 8 >= count) return;
+    const Shares shares((count + s.tm - 1) / s.tm * tiles_n, stages, slots);
     const float scale = loss_scale(grad_loss, mean, count);
     const bool there = r < count;
     const uint64_t row = there ? (uint64_t)tokens.rows[r] * cols : 0;
@@ -330,8 +360,8 @@ void k_loss_scatter(const float4 *sums, uint32_t parts, uint64_t tiles, uint32_t
         const float4 *from = sums + ((uint64_t)(r / s.tm) * tiles_n + c / s.tn) * 4 * piece + w * piece + (unit * 4 + n % 32 / 8) * 64 + n % 8 / 4 * 32 + m % 32;
         float v[4] = {};
         if (there)
-            for (uint32_t p = 0; p < parts; ++p) {
-                const float4 x = from[p * tiles * 4 * piece];
+            for (uint32_t p = 0; p < shares.parts; ++p) {
+                const float4 x = from[(uint64_t)p * shares.tiles * 4 * piece];
                 v[0] += x.x;
                 v[1] += x.y;
                 v[2] += x.z;
@@ -372,19 +402,32 @@ void k_loss_grad_w(GradWArgs g)
 // ---------------------------------------------------------------- joining
 
 // The parts of some tokens' statistics, and at the end of the vocabulary (`last`) lse and losses; `later`: with what earlier pieces left in `running`.
-// A workgroup of 256 takes `width` tokens, a power of two up to 32, and the parts in 256 / width runs, four at a time.  The last workgroup that is
-// done adds up the losses of all tokens, in their order.
-__global__ __launch_bounds__(256)
-void k_loss_join(const float2 *from, uint32_t parts, uint32_t padded, LossTokens tokens, const float *at_target, float2 *running, uint32_t later,
-                 uint32_t last, uint32_t width, float *losses, float *lse, uint32_t rows, uint32_t mean, float *total)
+// A workgroup takes `width` tokens, a power of two up to 32, and the parts in kJoinLanes / width runs, four at a time.
+constexpr uint32_t kJoinLanes = 1024;
+
+__device__ __forceinline__ float2 joined(float2 a, float2 b)
 {
-    __shared__ float2 places[256];
-    __shared__ uint32_t done;
-    const uint32_t lane = threadIdx.x % width, run = threadIdx.x / width, runs = 256 / width, count = *tokens.count, r = blockIdx.x * width + lane;
-    auto joined = [](float2 a, float2 b) {
-        const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
-        return make_float2(top, a.y * __expf(a.x - shift) + b.y * __expf(b.x - shift));
-    };
+    const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, a.y * __expf(a.x - shift) + b.y * __expf(b.x - shift));
+}
+// Sum over a workgroup of kJoinLanes, in the first lane
+__device__ __forceinline__ float lanes_sum(float v, float *sums)
+{
+    sums[threadIdx.x] = v;
+    __syncthreads();
+    for (uint32_t half = kJoinLanes / 2; half; half /= 2) {
+        if (threadIdx.x < half) sums[threadIdx.x] += sums[threadIdx.x + half];
+        __syncthreads();
+    }
+    return sums[0];
+}
+
+__global__ __launch_bounds__(kJoinLanes)
+void k_loss_join(const float2 *from, uint32_t parts, uint32_t padded, LossTokens tokens, const float *at_target, float2 *running, uint32_t later,
+                 uint32_t last, uint32_t width, float *losses, float *lse, uint32_t mean, float *total)
+{
+    __shared__ float2 places[kJoinLanes];
+    const uint32_t lane = threadIdx.x % width, run = threadIdx.x / width, runs = kJoinLanes / width, count = *tokens.count, r = blockIdx.x * width + lane;
     float2 v = make_float2(-INFINITY, 0.0f);
     if (r < count)
         for (uint32_t p = run; p < parts; p += 4 * runs) {
@@ -399,41 +442,50 @@ void k_loss_join(const float2 *from, uint32_t parts, uint32_t padded, LossTokens
         }
     places[threadIdx.x] = v;
     __syncthreads();
-    for (uint32_t half = 128; half >= width; half /= 2) {
+    for (uint32_t half = kJoinLanes / 2; half >= width; half /= 2) {
         if (threadIdx.x < half) places[threadIdx.x] = joined(places[threadIdx.x], places[threadIdx.x + half]);
         __syncthreads();
     }
+    float loss = 0.0f;
     if (run == 0 && r < count) {
         v = places[lane];
         if (later) v = joined(running[r], v);
         if (last) {
             const float all = v.x + logf(v.y);
             const uint32_t row = tokens.rows[r];
+            loss = tokens.targets[r] == kBadTarget ? NAN : all - at_target[r];
             lse[row] = all;
-            losses[row] = tokens.targets[r] == kBadTarget ? NAN : all - at_target[r];
+            losses[row] = loss;
         } else {
             running[r] = v;
         }
     }
-    if (!last) return;
-    // losses are visible to whoever sees this workgroup counted
-    __threadfence();
+    if (!total) return;
+    // the only workgroup: the reduced loss, too
     __syncthreads();
-    if (threadIdx.x == 0) done = atomicAdd(tokens.count + 1, 1u);
-    __syncthreads();
-    if (done != gridDim.x - 1) return;
-    __threadfence();
-    float sum = 0.0f;
-    for (uint32_t i = threadIdx.x; i < rows; i += 256) sum += __hip_atomic_load(losses + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    float *const sums = reinterpret_cast<float *>(places);
-    sums[threadIdx.x] = sum;
-    __syncthreads();
-    for (uint32_t half = 128; half; half /= 2) {
-        if (threadIdx.x < half) sums[threadIdx.x] += sums[threadIdx.x + half];
-        __syncthreads();
-    }
+    const float sum = lanes_sum(loss, reinterpret_cast<float *>(places));
     if (threadIdx.x == 0) {
-        total[0] = mean ? sums[0] / (float)max(count, 1u) : sums[0];
+        total[0] = mean ? sum / (float)max(count, 1u) : sum;
+        total[1] = (float)count;
+    }
+}
+
+// The reduced loss and the number of tokens that count
+__global__ __launch_bounds__(kJoinLanes)
+void k_loss_total(const float *losses, uint32_t rows, LossTokens tokens, uint32_t mean, float *total)
+{
+    __shared__ float sums[kJoinLanes];
+    float sum = 0.0f;
+    for (uint32_t i = threadIdx.x; i < rows; i += 8 * kJoinLanes) {
+        float v[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) v[k] = i + k * kJoinLanes < rows ? losses[i + k * kJoinLanes] : 0.0f;
+        sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    }
+    sum = lanes_sum(sum, sums);
+    if (threadIdx.x == 0) {
+        const uint32_t count = *tokens.count;
+        total[0] = mean ? sum / (float)max(count, 1u) : sum;
         total[1] = (float)count;
     }
 }

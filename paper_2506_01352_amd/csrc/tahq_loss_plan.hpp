@@ -32,10 +32,11 @@ struct LossPlan {
     uint32_t spans;                          // of kLossSpan tokens
     uint32_t forward_piece, backward_piece;  // rows of the vocabulary
     int forward_kind, grads_kind, x_kind;
-    uint32_t parts, x_parts, x_run;          // of a forward piece's statistics; of the sums for the hidden states' gradient, stages of a part
+    uint32_t parts, x_stages, x_slots;       // of a forward piece's statistics; of the sums for the hidden states' gradient: stages of the first piece, Shares
+    uint64_t x_groups;                       // workgroups for them
     // places in the workspace
     uint64_t rows, targets, counts, x, at_target, running, stats, forward_weight, forward_total;
-    uint64_t x_tiles, grads, sums, backward_weight, backward_total;
+    uint64_t grads, sums, backward_weight, backward_total;
 };
 
 inline LossPlan plan_loss(const tahq_loss_config *c)
@@ -82,15 +83,16 @@ inline LossPlan plan_loss(const tahq_loss_config *c)
     if (p.pad && piece((uint64_t)p.ldx * p.es) < p.backward_piece) p.backward_piece = piece((uint64_t)p.ldx * p.es);
     const uint64_t widest = p.backward_piece < c->vocab ? p.backward_piece : c->vocab;
     p.grads_kind = loss_kind(p.bf16, c->rows, widest);
-    p.x_kind = loss_kind(p.bf16, c->rows, c->cols);
-    // few tiles: several of them share the sums over the vocabulary, sixteen stages and more for each
-    const uint64_t tiles = loss_tiles(p.x_kind, c->rows, c->cols), stages = loss_ceil(widest, p.whole), at_once = p.x_kind == kLossLarge ? 256 : 512;
-    const uint64_t most = stages / 16 ? stages / 16 : 1, want = at_once / tiles ? at_once / tiles : 1, parts = want < most ? want : most;
-    p.x_run = (uint32_t)loss_ceil(stages, parts);
-    p.x_parts = (uint32_t)loss_ceil(stages, p.x_run);
+    // Few tiles: several workgroups share the sums of one over the vocabulary (Shares), as many as the device holds at once.  Then large tiles are as good
+    // where there are few, but for what hangs over the edges (2048 x 1600, of which 1448 tokens count, x 50257: 356 us in 128 x 128, LARGE).
+    const uint64_t stages = loss_ceil(widest, p.whole), large = loss_tiles(kLossLarge, c->rows, c->cols), middle = loss_tiles(kLossMiddle, c->rows, c->cols);
+    p.x_kind = c->rows <= 32 ? kLossFew : p.bf16 && 3 * large <= middle && large * stages >= 256 * 16 ? kLossLarge : kLossMiddle;
+    p.x_stages = (uint32_t)stages;
+    p.x_slots = p.x_kind == kLossLarge ? 256 : 512;
+    const uint64_t tiles = loss_tiles(p.x_kind, c->rows, c->cols);
+    p.x_groups = tiles > p.x_slots ? tiles : p.x_slots;
     p.grads = place((uint64_t)p.padded * loss_ceil(widest, p.whole) * 64);
-    p.x_tiles = tiles;
-    p.sums = place(p.x_parts * tiles * kLossTiles[p.x_kind].tm * kLossTiles[p.x_kind].tn * 4);
+    p.sums = place(p.x_groups * kLossTiles[p.x_kind].tm * kLossTiles[p.x_kind].tn * 4);
     p.backward_weight = place(p.pad ? (uint64_t)p.backward_piece * p.ldx * p.es : 0);
     p.backward_total = at;
     return p;
