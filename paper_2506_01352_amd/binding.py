@@ -886,13 +886,19 @@ class BlockNorm:
 
 # ---- what the operators below share
 
+_current_device = None
+
+
 def _placed(where, name, t, dtype, device):
     """A class's tensor is of the type that its configuration says and on the class's device, which is the current one: kernels are enqueued on a
     stream of the current device."""
-    import torch
-    if t.dtype is not dtype or t.device != device or torch.cuda.current_device() != device.index:
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if t.dtype is not dtype or t.get_device() != device.index or _current_device() != device.index:
         raise ValueError(f"{where}: {name} is a tensor of {t.dtype} on {t.device}, {dtype} on {device} is needed, and that to be the current device "
-                         f"(cuda:{torch.cuda.current_device()})")
+                         f"(cuda:{_current_device()})")
 
 
 def _whole(where, name, t, elements, dtype, device):
@@ -974,12 +980,14 @@ class Dropout:
         self._outs = [torch.empty(cfg.elements, dtype=self._kind, device=device) for _ in range(in_flight)]
         self._grad = torch.empty(cfg.elements, dtype=self._kind, device=device)
         self._next, self._offsets = cfg.offset, [None] * in_flight
+        _load()
+        self._config = tahq_dropout_config.from_buffer_copy(cfg)             # a call's own: the offset changes
+        self._by_ref = C.byref(self._config)
         self._views = {}
 
     def _call(self, where, offset, *arguments):
-        cfg = self.cfg
-        call = tahq_dropout_config(cfg.struct_size, cfg.dtype, cfg.elements, cfg.seed, offset % (1 << 64), cfg.p)
-        rc = getattr(_lib or _load(), where)(C.byref(call), *arguments)
+        self._config.offset = offset % (1 << 64)
+        rc = getattr(_lib, where)(self._by_ref, *arguments)
         if rc != 0:
             raise TahqError(rc, where)
 
@@ -994,7 +1002,8 @@ class Dropout:
         return view
 
     def forward(self, x, residual=None, stream=None, slot=0, offset=None):
-        _check_slot("Dropout.forward", slot, len(self._outs))
+        if slot:
+            _check_slot("Dropout.forward", slot, len(self._outs))
         d_x = _whole("Dropout.forward", "x", x, self.cfg.elements, self._kind, self.device)
         d_residual = None if residual is None else _whole("Dropout.forward", "residual", residual, self.cfg.elements, self._kind, self.device)
         used = self._next if offset is None else offset
@@ -1008,7 +1017,8 @@ class Dropout:
 
     def backward(self, grad_out, stream=None, slot=0, offset=None):
         """Gradient of x; the residual's is grad_out."""
-        _check_slot("Dropout.backward", slot, len(self._outs))
+        if slot:
+            _check_slot("Dropout.backward", slot, len(self._outs))
         used = self._offsets[slot] if offset is None else offset
         if used is None:
             raise ValueError("Dropout.backward: the slot has had no forward pass, and no offset is given")
@@ -1142,6 +1152,7 @@ class HeadRotary:
         if (rotary.rotated if rotary is not None else 0) != cfg.rotated:
             raise ValueError(f"HeadRotary: {rotary.rotated if rotary is not None else 0} rotated channels in the frequencies' configuration, {cfg.rotated} in the heads'")
         self.cfg, self.device, self._kind, self.training = cfg, _device_of(device), _torch_dtype(cfg.dtype), training
+        self._int64 = torch.int64
         self.frequencies = None
         if rotary is not None:
             signed = [f - (1 << 64) if f >> 63 else f for f in tahq_rotary_frequencies(rotary)]
@@ -1158,6 +1169,8 @@ class HeadRotary:
         self.q, self.k = self._outs[0]
         self._own = [tuple(None if t is None else t.data_ptr() for t in out) for out in self._outs]
         self._cfg = C.byref(cfg)
+        self._known = set()          # shapes and strides that were found to be right
+        self._d_frequencies = None if self.frequencies is None else self.frequencies.data_ptr()
         if training:
             # rows of a packed projection are the caller's to give
             self._grads = (buffer(cfg.q_heads, cfg.ldq), buffer(cfg.k_heads, cfg.ldk)) if not cfg.ldq and not cfg.ldk else None
@@ -1170,22 +1183,26 @@ class HeadRotary:
         if t is None:
             return None
         _placed(where, name, t, self._kind, self.device)
+        form = (heads, ld, t.shape, t.stride())
+        if form in self._known:
+            return t.data_ptr()
         cfg = self.cfg
         if tuple(t.shape) not in ((cfg.tokens, heads, cfg.head), (cfg.tokens, heads * cfg.head)):
             raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor, [{cfg.tokens}, {heads}, {cfg.head}] is needed")
-        return _heads_ptr(where, name, t, cfg.tokens, heads, cfg.head, ld, cfg.dtype)
+        at = _heads_ptr(where, name, t, cfg.tokens, heads, cfg.head, ld, cfg.dtype)
+        self._known.add(form)
+        return at
 
     def _tables(self, where, w_q, w_k, positions):
-        import torch
-        cfg = self.cfg
-        weights = [None if w is None else _whole(where, name, w, cfg.head, self._kind, self.device) for name, w in (("w_q", w_q), ("w_k", w_k))]
-        return (*weights, None if positions is None else _whole(where, "positions", positions, cfg.tokens, torch.int64, self.device),
-                None if self.frequencies is None else self.frequencies.data_ptr())
+        head, kind, device = self.cfg.head, self._kind, self.device
+        return (None if w_q is None else _whole(where, "w_q", w_q, head, kind, device), None if w_k is None else _whole(where, "w_k", w_k, head, kind, device),
+                None if positions is None else _whole(where, "positions", positions, self.cfg.tokens, self._int64, device), self._d_frequencies)
 
     def forward(self, q, k, w_q, w_k, positions, stream=None, slot=0, out=None):
         """(q, k) normed and rotated: the slot's, or `out`, which may be q and k themselves if strides are the same."""
         where, cfg = "HeadRotary.forward", self.cfg
-        _check_slot(where, slot, len(self._outs))
+        if slot:
+            _check_slot(where, slot, len(self._outs))
         to = self._own[slot] if out is None else (self._queries(where, "out[0]", out[0], cfg.q_heads, cfg.ldq_out),
                                                   self._queries(where, "out[1]", out[1], cfg.k_heads, cfg.ldk_out))
         rc = (_lib or _load()).tahq_heads_forward(self._cfg, self._queries(where, "q", q, cfg.q_heads, cfg.ldq), self._queries(where, "k", k, cfg.k_heads, cfg.ldk),
@@ -1324,7 +1341,8 @@ class LinearLoss:
 
     def forward(self, x, weight, target, stream=None, slot=0):
         """The reduced loss, a tensor of one element; with LOSS_NONE every token's."""
-        _check_slot("LinearLoss.forward", slot, len(self._slots))
+        if slot:
+            _check_slot("LinearLoss.forward", slot, len(self._slots))
         inputs = self._inputs("LinearLoss.forward", x, weight, target)
         self._done[slot] = False
         rc = (_lib or _load()).tahq_loss_forward(self._cfg, *inputs, *self._own[slot], self.workspace.data_ptr(), self.workspace.numel(), _stream_handle(stream))

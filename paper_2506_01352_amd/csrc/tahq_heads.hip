@@ -68,19 +68,42 @@ uint32_t lanes_of(const tahq_heads_config *c, bool wide)
     return lanes;
 }
 
-// Wavefronts that share a token's heads: all that they make where tokens alone would leave vector units idle
-uint32_t splits_of(const HeadShape &s)
+// Where tokens alone would leave vector units idle, each of a token's groups of heads has a wavefront of its own.
+constexpr uint32_t kSplitBelow = 4096;
+
+// groups of queries' (0) and of keys' heads (1) that a wavefront takes side by side
+uint32_t groups_of(const HeadShape &s, int which)
 {
-    const uint32_t each = 64 / s.lanes, groups = (s.heads[0] + each - 1) / each + (s.heads[1] + each - 1) / each;
-    return s.tokens >= 4096 ? 1 : groups;
+    const uint32_t each = 64 / s.lanes;
+    return (s.heads[which] + each - 1) / each;
+}
+// workgroups that give every wavefront one token, or one group
+uint32_t workgroups_of(const HeadShape &s, uint32_t groups)
+{
+    const uint64_t all = ((uint64_t)s.tokens * (s.split ? groups : 1) + kHeadWaves - 1) / kHeadWaves;
+    return (uint32_t)(all < (1u << 23) ? all : 1u << 23);
 }
 
-constexpr uint32_t kBackwardGroups = 1024;          // workgroups that leave a part of the weights' gradients, at most
-
-uint32_t forward_groups(const HeadShape &s)
+// Workgroups of the backward pass, queries' and keys'.  With norms each leaves a part of a weight's gradient, so there are no more than are at work at
+// once: three to a compute unit of bf16 in chunks of 16 bytes, which has up to 144 registers (32768 x 48 x 128: 768 workgroups 250 us, 1024 311, and with 128
+// registers, some of them in memory, 367), five of the others with up to 105 (fp32 2331 x 25 x 80: 768 17.6 us, 1280 16.1).
+// They are shared as the work is, a token's angles counting as a group.
+constexpr uint32_t kBackwardMost = 1280;
+struct BackwardGroups {
+    uint32_t queries, keys;
+};
+BackwardGroups backward_groups(const tahq_heads_config *c, const HeadShape &s, bool by_chunks)
 {
-    const uint64_t all = ((uint64_t)s.tokens * s.splits + kHeadWaves - 1) / kHeadWaves;
-    return (uint32_t)(all < (1u << 23) ? all : 1u << 23);
+    const uint32_t at_once = by_chunks && c->dtype == TAHQ_BF16 ? 768 : kBackwardMost;
+    const uint32_t gq = groups_of(s, 0), gk = groups_of(s, 1);
+    BackwardGroups g = {workgroups_of(s, gq), gk ? workgroups_of(s, gk) : 0};
+    if (!c->norm || g.queries + g.keys <= at_once) return g;
+    const uint32_t angles = s.split ? 0 : 1, all = gq + gk + 2 * angles;
+    const uint32_t keys = gk ? (at_once * (gk + angles) + all / 2) / all : 0;
+    const uint32_t least = keys < 1 && gk ? 1 : keys, most = least < at_once ? least : at_once - 1;
+    if (g.keys > most) g.keys = most;
+    if (g.queries > at_once - g.keys) g.queries = at_once - g.keys;
+    return g;
 }
 
 // what a configuration's kernel is compiled for
@@ -193,10 +216,10 @@ tahq_status tahq_heads_forward(const tahq_heads_config *cfg, const void *d_q, co
     HeadShape s = shape_of(cfg);
     const bool by_chunks = wide(cfg, s, {d_q, d_k, d_q_out, d_k_out});
     s.lanes = lanes_of(cfg, by_chunks);
-    s.splits = splits_of(s);
+    s.split = cfg->tokens < kSplitBelow;
     Enqueue q{(hipStream_t)stream};
     with_kind(cfg, by_chunks, [&](auto bf16, auto w, auto pairs, auto normed) {
-        q(k_heads_forward<bf16, w, pairs, normed>, dim3(forward_groups(s)), dim3(64 * kHeadWaves), HeadTensors{{d_q, d_k}}, HeadTensors{{d_w_q, d_w_k}}, d_positions,
+        q(k_heads_forward<bf16, w, pairs, normed>, dim3(workgroups_of(s, groups_of(s, 0) + groups_of(s, 1))), dim3(64 * kHeadWaves), HeadTensors{{d_q, d_k}}, HeadTensors{{d_w_q, d_w_k}}, d_positions,
           d_frequencies, HeadOutputs{{d_q_out, d_k_out}}, s);
     });
     return q.result();
@@ -204,7 +227,7 @@ tahq_status tahq_heads_forward(const tahq_heads_config *cfg, const void *d_q, co
 
 size_t tahq_heads_workspace_size(const tahq_heads_config *cfg)
 {
-    return check(cfg) == TAHQ_OK && cfg->norm ? (size_t)kBackwardGroups * 2 * cfg->head * sizeof(float) : 0;
+    return check(cfg) == TAHQ_OK && cfg->norm ? (size_t)kBackwardMost * cfg->head * sizeof(float) : 0;
 }
 
 tahq_status tahq_heads_backward(const tahq_heads_config *cfg, const void *d_grad_q_out, const void *d_grad_k_out, const void *d_q,
@@ -226,15 +249,15 @@ tahq_status tahq_heads_backward(const tahq_heads_config *cfg, const void *d_grad
     HeadShape s = shape_of(cfg);
     const bool by_chunks = wide(cfg, s, {d_grad_q_out, d_grad_k_out, d_q, d_k, d_grad_q, d_grad_k});
     s.lanes = lanes_of(cfg, by_chunks);
-    s.splits = splits_of(s);
-    const uint32_t all = forward_groups(s), groups = norm && all > kBackwardGroups ? kBackwardGroups : all;
+    s.split = cfg->tokens < kSplitBelow;
+    const BackwardGroups g = backward_groups(cfg, s, by_chunks);
     float *parts = static_cast<float *>(d_workspace);
     Enqueue q{(hipStream_t)stream};
     with_kind(cfg, by_chunks, [&](auto bf16, auto w, auto pairs, auto normed) {
-        q(k_heads_backward<bf16, w, pairs, normed>, dim3(groups), dim3(64 * kHeadWaves), HeadTensors{{d_grad_q_out, d_grad_k_out}}, HeadTensors{{d_q, d_k}},
-          HeadTensors{{d_w_q, d_w_k}}, d_positions, d_frequencies, HeadOutputs{{d_grad_q, d_grad_k}}, parts, s);
+        q(k_heads_backward<bf16, w, pairs, normed>, dim3(g.queries + g.keys), dim3(64 * kHeadWaves), HeadTensors{{d_grad_q_out, d_grad_k_out}}, HeadTensors{{d_q, d_k}},
+          HeadTensors{{d_w_q, d_w_k}}, d_positions, d_frequencies, HeadOutputs{{d_grad_q, d_grad_k}}, parts, g.queries, s);
     });
-    if (norm) q(k_heads_reduce, dim3((cfg->head + 15) / 16, keys ? 2 : 1), dim3(1024), parts, d_grad_w_q, d_grad_w_k, cfg->head, groups, cfg->accumulate);
+    if (norm) q(k_heads_reduce, dim3((cfg->head + 15) / 16, keys ? 2 : 1), dim3(1024), parts, d_grad_w_q, d_grad_w_k, cfg->head, g.queries, g.queries + g.keys, cfg->accumulate);
     return q.result();
 }
 

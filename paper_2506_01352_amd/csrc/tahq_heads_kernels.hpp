@@ -11,7 +11,7 @@
 namespace tahq {
 
 struct HeadShape {
-    uint32_t tokens, heads[2], head, rotated, lanes, splits;    // heads: of queries, of keys; splits: wavefronts that share a token's heads
+    uint32_t tokens, heads[2], head, rotated, lanes, split;     // heads: of queries, of keys; split: a token's heads go to as many wavefronts as there are for
     uint64_t ld[2], ld_out[2];
     float eps, magnitude;
 };
@@ -154,15 +154,17 @@ struct HeadLane {
     __device__ __forceinline__ void angles(const HeadShape &s, const int64_t *positions, const uint64_t *frequencies, uint32_t token, float (&c)[E], float (&n)[E]) const
     {
         const uint64_t position = s.rotated ? (uint64_t)positions[token] : 0;
+        uint64_t f[E] = {};
+        // WIDE: runs of pairs are turned as a whole or not at all, and are asked for as a whole
+        constexpr int RUN = !WIDE ? 1 : PAIRS ? E / 2 : E;
+#pragma unroll
+        for (int i = 0; i < E; i += RUN)
+            if (turned(s, i)) __builtin_memcpy(f + i, frequencies + pair(s, i), RUN * sizeof *f);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            c[i] = 1.0f;
-            n[i] = 0.0f;
-            if (turned(s, i)) {
-                cos_sin((uint32_t)((position * frequencies[pair(s, i)] + 0x80000000u) >> 32), c[i], n[i]);
-                c[i] *= s.magnitude;
-                n[i] *= s.magnitude;
-            }
+            cos_sin((uint32_t)((position * f[i] + 0x80000000u) >> 32), c[i], n[i]);
+            c[i] = turned(s, i) ? c[i] * s.magnitude : 1.0f;
+            n[i] = turned(s, i) ? n[i] * s.magnitude : 0.0f;
         }
     }
 };
@@ -179,6 +181,40 @@ __device__ __forceinline__ float head_sum(float v, uint32_t lanes)
     return v;
 }
 
+// A wavefront's way through tokens and groups of heads: every splits-th group of a token, then the token that all wavefronts are further.  Forward groups
+// of queries, then of keys; backward (`only`) of one of them.
+struct HeadWay {
+    uint32_t each, groups_q, groups, splits, split, step_split;
+    uint64_t token, step_token;
+    uint32_t group;
+    __device__ __forceinline__ HeadWay(const HeadShape &s, int only, uint32_t waves, uint32_t wave)
+    {
+        each = 64 / s.lanes;
+        const uint32_t groups_k = (s.heads[1] + each - 1) / each;
+        groups_q = (s.heads[0] + each - 1) / each;
+        groups = only < 0 ? groups_q + groups_k : only ? groups_k : groups_q;
+        splits = max(s.split ? groups : 1u, 1u);
+        token = wave / splits;
+        group = split = wave % splits;
+        step_token = waves / splits;
+        step_split = waves % splits;
+    }
+    // to the next group; whether it is another token's
+    __device__ __forceinline__ bool next()
+    {
+        group += splits;
+        if (group < groups) return false;
+        token += step_token;
+        split += step_split;
+        if (split >= splits) {
+            split -= splits;
+            ++token;
+        }
+        group = split;
+        return true;
+    }
+};
+
 template <bool BF16, bool WIDE, bool PAIRS, bool NORM>
 __global__ __launch_bounds__(64 * kHeadWaves)
 void k_heads_forward(HeadTensors in, HeadTensors weights, const int64_t *positions, const uint64_t *frequencies, HeadOutputs out, HeadShape s)
@@ -186,142 +222,148 @@ void k_heads_forward(HeadTensors in, HeadTensors weights, const int64_t *positio
     using Lane = HeadLane<BF16, WIDE, PAIRS>;
     constexpr int E = Lane::E;
     const Lane lane(s);
-    const uint32_t each = 64 / s.lanes, mine = threadIdx.x % 64 / s.lanes;
-    const uint32_t groups_q = (s.heads[0] + each - 1) / each, groups = groups_q + (s.heads[1] + each - 1) / each;
-    const uint64_t waves = (uint64_t)gridDim.x * kHeadWaves;
+    const uint32_t mine = threadIdx.x % 64 / s.lanes;
+    HeadWay way(s, -1, gridDim.x * kHeadWaves, blockIdx.x * kHeadWaves + uniform(threadIdx.x / 64));
     const float inv = 1.0f / (float)s.head;
-    for (uint64_t id = (uint64_t)blockIdx.x * kHeadWaves + uniform(threadIdx.x / 64); id < (uint64_t)s.tokens * s.splits; id += waves) {
-        const uint32_t token = (uint32_t)(id / s.splits);
-        float c[E], n[E];
-        lane.angles(s, positions, frequencies, token, c, n);
-        for (uint32_t g = (uint32_t)(id % s.splits); g < groups; g += s.splits) {
-            const int which = g < groups_q ? 0 : 1;
-            const uint32_t h = (which ? g - groups_q : g) * each + mine;
-            const bool valid = h < s.heads[which];
-            float a[E], b[E];
-            lane.unpack(lane.load(s, in.of[which], token * s.ld[which] + (uint64_t)h * s.head, valid), a, b);
-            if constexpr (NORM) {
-                float wa[E], wb[E], sum = 0.0f;
-                lane.unpack(lane.load(s, weights.of[which], 0, true), wa, wb);
+    float c[E], n[E];
+    bool another = true;
+    while (way.token < s.tokens) {
+        const int which = way.group < way.groups_q ? 0 : 1;
+        const uint32_t h = (which ? way.group - way.groups_q : way.group) * way.each + mine;
+        const bool valid = h < s.heads[which];
+        const typename Lane::Raw raw = lane.load(s, in.of[which], way.token * s.ld[which] + (uint64_t)h * s.head, valid);
+        const uint64_t to = way.token * s.ld_out[which] + (uint64_t)h * s.head;
+        if (another) lane.angles(s, positions, frequencies, (uint32_t)way.token, c, n);
+        another = way.next();
+        float a[E], b[E];
+        lane.unpack(raw, a, b);
+        if constexpr (NORM) {
+            float wa[E], wb[E], sum = 0.0f;
+            lane.unpack(lane.load(s, weights.of[which], 0, true), wa, wb);
 #pragma unroll
-                for (int i = 0; i < E; ++i) sum = __builtin_fmaf(b[i], b[i], __builtin_fmaf(a[i], a[i], sum));
-                const float rstd = rsqrtf(head_sum(sum, s.lanes) * inv + s.eps);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    a[i] = a[i] * rstd * wa[i];
-                    b[i] = b[i] * rstd * wb[i];
-                }
-            }
+            for (int i = 0; i < E; ++i) sum = __builtin_fmaf(b[i], b[i], __builtin_fmaf(a[i], a[i], sum));
+            const float rstd = rsqrtf(head_sum(sum, s.lanes) * inv + s.eps);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float x = a[i], y = b[i];
-                a[i] = x * c[i] - y * n[i];
-                b[i] = x * n[i] + y * c[i];
+                a[i] = a[i] * rstd * wa[i];
+                b[i] = b[i] * rstd * wb[i];
             }
-            lane.store(s, out.of[which], token * s.ld_out[which] + (uint64_t)h * s.head, valid, a, b);
         }
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float x = a[i], y = b[i];
+            a[i] = x * c[i] - y * n[i];
+            b[i] = x * n[i] + y * c[i];
+        }
+        lane.store(s, out.of[which], to, valid, a, b);
     }
 }
 
 // With u the gradient of the normed head, turned back and times w: dx = rstd (u - n mean(u n)), n = x rstd; w's gradient is the sum of the turned
 // gradient times n over tokens and heads: in a lane's registers, then over the wavefront and the workgroup, which leaves its part in the workspace,
-// [workgroup][query or key][head].
+// [workgroup][head].  The first `queries` workgroups take queries, the others keys, as sums for both would take a quarter of the registers; the next
+// group's numbers are on their way while a group is worked on.
 template <bool BF16, bool WIDE, bool PAIRS, bool NORM>
 __global__ __launch_bounds__(64 * kHeadWaves)
-void k_heads_backward(HeadTensors grads, HeadTensors in, HeadTensors weights, const int64_t *positions, const uint64_t *frequencies, HeadOutputs out, float *parts, HeadShape s)
+void k_heads_backward(HeadTensors grads, HeadTensors in, HeadTensors weights, const int64_t *positions, const uint64_t *frequencies, HeadOutputs out, float *parts, uint32_t queries, HeadShape s)
 {
     using Lane = HeadLane<BF16, WIDE, PAIRS>;
     constexpr int E = Lane::E;
-    __shared__ float sums[NORM ? kHeadWaves : 1][2][NORM ? TAHQ_HEADS_MAX : 1];
+    __shared__ float sums[NORM ? kHeadWaves : 1][NORM ? TAHQ_HEADS_MAX : 1];
     const Lane lane(s);
-    const uint32_t each = 64 / s.lanes, mine = threadIdx.x % 64 / s.lanes, wave = uniform(threadIdx.x / 64);
-    const uint32_t groups_q = (s.heads[0] + each - 1) / each, groups = groups_q + (s.heads[1] + each - 1) / each;
-    const uint64_t waves = (uint64_t)gridDim.x * kHeadWaves;
+    const uint32_t mine = threadIdx.x % 64 / s.lanes, wave = uniform(threadIdx.x / 64);
     const float inv = 1.0f / (float)s.head;
-    float da[2][E] = {}, db[2][E] = {};
-    for (uint64_t id = (uint64_t)blockIdx.x * kHeadWaves + wave; id < (uint64_t)s.tokens * s.splits; id += waves) {
-        const uint32_t token = (uint32_t)(id / s.splits);
-        float c[E], n[E];
-        lane.angles(s, positions, frequencies, token, c, n);
-        auto one = [&](auto which_tensor, uint32_t g) {
-            constexpr int which = decltype(which_tensor)::value;
-            const uint32_t h = g * each + mine;
-            const bool valid = h < s.heads[which];
-            float a[E], b[E];
-            lane.unpack(lane.load(s, grads.of[which], token * s.ld_out[which] + (uint64_t)h * s.head, valid), a, b);
+    const int which = blockIdx.x < queries ? 0 : 1;
+    HeadWay way(s, which, (which ? gridDim.x - queries : queries) * kHeadWaves, (which ? blockIdx.x - queries : blockIdx.x) * kHeadWaves + wave);
+    float da[E] = {}, db[E] = {}, c[E], n[E];
+    typename Lane::Raw next_grad = {}, next_x = {};
+    const typename Lane::Raw weight = NORM ? lane.load(s, weights.of[which], 0, true) : typename Lane::Raw{};
+    auto ask = [&] {
+        if (way.token >= s.tokens) return;
+        const uint32_t h = way.group * way.each + mine;
+        next_grad = lane.load(s, grads.of[which], way.token * s.ld_out[which] + (uint64_t)h * s.head, h < s.heads[which]);
+        if constexpr (NORM) next_x = lane.load(s, in.of[which], way.token * s.ld[which] + (uint64_t)h * s.head, h < s.heads[which]);
+    };
+    ask();
+    bool another = true;
+    while (way.token < s.tokens) {
+        const uint32_t h = way.group * way.each + mine;
+        const uint64_t to = way.token * s.ld[which] + (uint64_t)h * s.head;
+        float a[E], b[E], xa[E], xb[E];
+        lane.unpack(next_grad, a, b);
+        if constexpr (NORM) lane.unpack(next_x, xa, xb);
+        if (another) lane.angles(s, positions, frequencies, (uint32_t)way.token, c, n);
+        another = way.next();
+        ask();
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float x = a[i], y = b[i];
+            a[i] = x * c[i] + y * n[i];
+            b[i] = y * c[i] - x * n[i];
+        }
+        if constexpr (NORM) {
+            float wa[E], wb[E], square = 0.0f, dot = 0.0f;
+            lane.unpack(weight, wa, wb);
+#pragma unroll
+            for (int i = 0; i < E; ++i) square = __builtin_fmaf(xb[i], xb[i], __builtin_fmaf(xa[i], xa[i], square));
+            const float rstd = rsqrtf(head_sum(square, s.lanes) * inv + s.eps);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float x = a[i], y = b[i];
-                a[i] = x * c[i] + y * n[i];
-                b[i] = y * c[i] - x * n[i];
+                xa[i] *= rstd;
+                xb[i] *= rstd;
+                da[i] = __builtin_fmaf(a[i], xa[i], da[i]);
+                db[i] = __builtin_fmaf(b[i], xb[i], db[i]);
+                a[i] *= wa[i];
+                b[i] *= wb[i];
+                dot = __builtin_fmaf(b[i], xb[i], __builtin_fmaf(a[i], xa[i], dot));
             }
-            if constexpr (NORM) {
-                float xa[E], xb[E], wa[E], wb[E], square = 0.0f, dot = 0.0f;
-                lane.unpack(lane.load(s, in.of[which], token * s.ld[which] + (uint64_t)h * s.head, valid), xa, xb);
-                lane.unpack(lane.load(s, weights.of[which], 0, true), wa, wb);
+            const float mean = head_sum(dot, s.lanes) * inv;
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    square = __builtin_fmaf(xb[i], xb[i], __builtin_fmaf(xa[i], xa[i], square));
-                }
-                const float rstd = rsqrtf(head_sum(square, s.lanes) * inv + s.eps);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    xa[i] *= rstd;
-                    xb[i] *= rstd;
-                    da[which][i] = __builtin_fmaf(a[i], xa[i], da[which][i]);
-                    db[which][i] = __builtin_fmaf(b[i], xb[i], db[which][i]);
-                    a[i] *= wa[i];
-                    b[i] *= wb[i];
-                    dot = __builtin_fmaf(b[i], xb[i], __builtin_fmaf(a[i], xa[i], dot));
-                }
-                const float mean = head_sum(dot, s.lanes) * inv;
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    a[i] = rstd * __builtin_fmaf(-xa[i], mean, a[i]);
-                    b[i] = rstd * __builtin_fmaf(-xb[i], mean, b[i]);
-                }
+            for (int i = 0; i < E; ++i) {
+                a[i] = rstd * __builtin_fmaf(-xa[i], mean, a[i]);
+                b[i] = rstd * __builtin_fmaf(-xb[i], mean, b[i]);
             }
-            lane.store(s, out.of[which], token * s.ld[which] + (uint64_t)h * s.head, valid, a, b);
-        };
-        uint32_t g = (uint32_t)(id % s.splits);
-        for (; g < groups_q; g += s.splits) one(std::integral_constant<int, 0>{}, g);
-        for (; g < groups; g += s.splits) one(std::integral_constant<int, 1>{}, g - groups_q);
+        }
+        lane.store(s, out.of[which], to, h < s.heads[which], a, b);
     }
     if constexpr (NORM) {
 #pragma unroll
-        for (int which = 0; which < 2; ++which)
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                float a = da[which][i], b = db[which][i];
-                for (uint32_t step = s.lanes; step < 64; step *= 2) {
-                    a += __shfl_xor(a, (int)step);
-                    b += __shfl_xor(b, (int)step);
-                }
-                if (mine == 0) {
-                    const uint32_t ca = lane.channel(s, i, 0), cb = lane.channel(s, i, 1);
-                    if (ca < s.head) sums[wave][which][ca] = a;
-                    if (cb < s.head) sums[wave][which][cb] = b;
-                }
+        for (int i = 0; i < E; ++i) {
+            float a = da[i], b = db[i];
+            for (uint32_t step = s.lanes; step < 64; step *= 2) {
+                a += __shfl_xor(a, (int)step);
+                b += __shfl_xor(b, (int)step);
             }
+            if (mine == 0) {
+                const uint32_t ca = lane.channel(s, i, 0), cb = lane.channel(s, i, 1);
+                if (ca < s.head) sums[wave][ca] = a;
+                if (cb < s.head) sums[wave][cb] = b;
+            }
+        }
         __syncthreads();
-        for (uint32_t at = threadIdx.x; at < 2 * s.head; at += 64 * kHeadWaves) {
-            const uint32_t which = at / s.head, channel = at % s.head;
-            float sum = sums[0][which][channel];
-            for (uint32_t w = 1; w < kHeadWaves; ++w) sum += sums[w][which][channel];
-            parts[(uint64_t)blockIdx.x * 2 * s.head + at] = sum;
+        for (uint32_t at = threadIdx.x; at < s.head; at += 64 * kHeadWaves) {
+            float sum = sums[0][at];
+            for (uint32_t w = 1; w < kHeadWaves; ++w) sum += sums[w][at];
+            parts[(uint64_t)blockIdx.x * s.head + at] = sum;
         }
     }
 }
 
 // The workgroups' parts, added in a fixed order: 16 channels of 64 runs of workgroups to a block.  blockIdx.y: queries', keys'.
 __global__ __launch_bounds__(1024)
-void k_heads_reduce(const float *parts, float *grad_w_q, float *grad_w_k, uint32_t head, uint32_t workgroups, uint32_t accumulate)
+void k_heads_reduce(const float *parts, float *grad_w_q, float *grad_w_k, uint32_t head, uint32_t queries, uint32_t workgroups, uint32_t accumulate)
 {
     __shared__ float sums[1024];
-    const uint32_t c = blockIdx.x * 16 + threadIdx.x % 16, run = threadIdx.x / 16, each = (workgroups + 63) / 64;
+    const uint32_t base = blockIdx.y ? queries : 0, count = blockIdx.y ? workgroups - queries : queries;
+    const uint32_t c = blockIdx.x * 16 + threadIdx.x % 16, run = threadIdx.x / 16, each = (count + 63) / 64;
     float sum = 0.0f;
     if (c < head)
-        for (uint32_t i = run * each; i < min((run + 1) * each, workgroups); ++i) sum += parts[((uint64_t)i * 2 + blockIdx.y) * head + c];
+        for (uint32_t i = run * each, end = min((run + 1) * each, count); i < end; i += 8) {
+            float v[8];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) v[k] = i + k < end ? parts[(uint64_t)(base + i + k) * head + c] : 0.0f;
+            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
     sums[threadIdx.x] = sum;
     __syncthreads();
     for (uint32_t half = 512; half >= 16; half /= 2) {
