@@ -360,12 +360,17 @@ void k_loss_scatter(const float4 *sums, uint32_t stages, uint32_t slots, uint32_
         const float4 *from = sums + ((uint64_t)(r / s.tm) * tiles_n + c / s.tn) * 4 * piece + w * piece + (unit * 4 + n % 32 / 8) * 64 + n % 8 / 4 * 32 + m % 32;
         float v[4] = {};
         if (there)
-            for (uint32_t p = 0; p < shares.parts; ++p) {
-                const float4 x = from[(uint64_t)p * shares.tiles * 4 * piece];
-                v[0] += x.x;
-                v[1] += x.y;
-                v[2] += x.z;
-                v[3] += x.w;
+            for (uint32_t p = 0; p < shares.parts; p += 8) {
+                float4 x[8];
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) x[k] = p + k < shares.parts ? from[(uint64_t)(p + k) * shares.tiles * 4 * piece] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) {
+                    v[0] += x[k].x;
+                    v[1] += x[k].y;
+                    v[2] += x[k].z;
+                    v[3] += x[k].w;
+                }
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] *= scale;
@@ -410,16 +415,18 @@ __device__ __forceinline__ float2 joined(float2 a, float2 b)
     const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
     return make_float2(top, a.y * __expf(a.x - shift) + b.y * __expf(b.x - shift));
 }
-// Sum over a workgroup of kJoinLanes, in the first lane
+// Sum over a workgroup of kJoinLanes, in every lane
 __device__ __forceinline__ float lanes_sum(float v, float *sums)
 {
-    sums[threadIdx.x] = v;
+    v = wave_sum(v);
+    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = v;
     __syncthreads();
-    for (uint32_t half = kJoinLanes / 2; half; half /= 2) {
-        if (threadIdx.x < half) sums[threadIdx.x] += sums[threadIdx.x + half];
-        __syncthreads();
-    }
-    return sums[0];
+    v = sums[threadIdx.x % 16];
+    static_assert(kJoinLanes == 16 * 64, "a row of sixteen lanes adds the wavefronts' sums");
+    v = add_permuted<0xb1>(v);
+    v = add_permuted<0x4e>(v);
+    v = add_permuted<0x141>(v);
+    return add_permuted<0x140>(v);
 }
 
 __global__ __launch_bounds__(kJoinLanes)
@@ -474,7 +481,8 @@ void k_loss_join(const float2 *from, uint32_t parts, uint32_t padded, LossTokens
 __global__ __launch_bounds__(kJoinLanes)
 void k_loss_total(const float *losses, uint32_t rows, LossTokens tokens, uint32_t mean, float *total)
 {
-    __shared__ float sums[kJoinLanes];
+    __shared__ float sums[kJoinLanes / 64];
+    const uint32_t count = *tokens.count;
     float sum = 0.0f;
     for (uint32_t i = threadIdx.x; i < rows; i += 8 * kJoinLanes) {
         float v[8];
@@ -484,7 +492,6 @@ void k_loss_total(const float *losses, uint32_t rows, LossTokens tokens, uint32_
     }
     sum = lanes_sum(sum, sums);
     if (threadIdx.x == 0) {
-        const uint32_t count = *tokens.count;
         total[0] = mean ? sum / (float)max(count, 1u) : sum;
         total[1] = (float)count;
     }
