@@ -902,8 +902,10 @@ def _placed(where, name, t, dtype, device):
 
 
 def _whole(where, name, t, elements, dtype, device):
-    """Device address of a contiguous tensor of so many elements, in any shape."""
-    _placed(where, name, t, dtype, device)
+    """Device address of a contiguous tensor of so many elements, in any shape.  (What calls on small tensors take is mostly what they cost the
+    host: the looks that are usually enough come first.)"""
+    if t.dtype is not dtype or t.get_device() != device.index or _current_device is None or _current_device() != device.index:
+        _placed(where, name, t, dtype, device)
     if t.numel() != elements or not t.is_contiguous():
         raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor{'' if t.is_contiguous() else ', not contiguous'}: {elements} contiguous elements are needed")
     return t.data_ptr()
@@ -915,6 +917,11 @@ def _matrix(where, name, t, rows, cols, dtype, device):
     if t.dim() > 1 and t.shape[-1] != cols:
         raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor, [{rows}, {cols}] is needed")
     return at
+
+
+def _own_copy(cfg):
+    """What a class's buffers were made for, whatever becomes of the configuration that it was given."""
+    return type(cfg).from_buffer_copy(cfg)
 
 
 def _device_of(device):
@@ -967,21 +974,23 @@ class Dropout:
     """Dropout of one tensor of the stage, with or without the residual that it is added to.  Every forward pass takes the next offset, from
     cfg.offset on, unless it is given one; a slot's backward pass takes that of the slot's last forward pass.
     in_flight: micro-batches that go forward before the first of them comes back; each has a slot with an output of its own.  The gradient is the next
-    backward call's.
+    backward call's: calls of one object follow each other, and calls on another stream than that which was torch's current one at construction come after
+    that stream has waited for it.
     graph_offset: a tensor of one int64 on the device that is added to the offset when a kernel runs: a program that captures passes into a graph
     changes it between replays (between a forward pass and its backward pass not)."""
 
     def __init__(self, cfg, device="cuda:0", in_flight=1, graph_offset=None):
         import torch
         _check_slot("Dropout", 0, in_flight)
+        _load()
+        cfg = _own_copy(cfg)
         self.cfg, self.device, self._kind = cfg, _device_of(device), _torch_dtype(cfg.dtype)
         self._graph = None if graph_offset is None else _whole("Dropout", "graph_offset", graph_offset, 1, torch.int64, self.device)
         self.graph_offset = graph_offset
         self._outs = [torch.empty(cfg.elements, dtype=self._kind, device=device) for _ in range(in_flight)]
         self._grad = torch.empty(cfg.elements, dtype=self._kind, device=device)
         self._next, self._offsets = cfg.offset, [None] * in_flight
-        _load()
-        self._config = tahq_dropout_config.from_buffer_copy(cfg)             # a call's own: the offset changes
+        self._config = _own_copy(cfg)        # a call's own: the offset changes
         self._by_ref = C.byref(self._config)
         self._views = {}
 
@@ -1006,6 +1015,8 @@ class Dropout:
             _check_slot("Dropout.forward", slot, len(self._outs))
         d_x = _whole("Dropout.forward", "x", x, self.cfg.elements, self._kind, self.device)
         d_residual = None if residual is None else _whole("Dropout.forward", "residual", residual, self.cfg.elements, self._kind, self.device)
+        if residual is not None and residual.shape != x.shape:
+            raise ValueError(f"Dropout.forward: residual is a {tuple(residual.shape)} tensor, x a {tuple(x.shape)} tensor")
         used = self._next if offset is None else offset
         self._offsets[slot] = None
         out = self._outs[slot]
@@ -1144,11 +1155,13 @@ class HeadRotary:
     device memory once (None if nothing is rotated).  Tensors are [tokens, heads, head], or [tokens, heads * head], with the configuration's strides; keys
     are None where there are none, weights where there are no norms.
     in_flight: micro-batches that go forward before the first of them comes back; each has a slot with outputs of its own.  The norms' weights'
-    gradients, and the gradients of queries and keys where the call is given no place for them, are the next backward call's."""
+    gradients, and the gradients of queries and keys where the call is given no place for them, are the next backward call's: calls of one object
+    follow each other.  All buffers are made on torch's current stream: a call on another stream comes after that stream has waited for it."""
 
     def __init__(self, cfg, rotary=None, device="cuda:0", training=True, in_flight=1):
         import torch
         _check_slot("HeadRotary", 0, in_flight)
+        cfg = _own_copy(cfg)
         if (rotary.rotated if rotary is not None else 0) != cfg.rotated:
             raise ValueError(f"HeadRotary: {rotary.rotated if rotary is not None else 0} rotated channels in the frequencies' configuration, {cfg.rotated} in the heads'")
         self.cfg, self.device, self._kind, self.training = cfg, _device_of(device), _torch_dtype(cfg.dtype), training
@@ -1169,7 +1182,7 @@ class HeadRotary:
         self.q, self.k = self._outs[0]
         self._own = [tuple(None if t is None else t.data_ptr() for t in out) for out in self._outs]
         self._cfg = C.byref(cfg)
-        self._known = set()          # shapes and strides that were found to be right
+        self._known = {}             # of shapes the strides that were found to be right
         self._d_frequencies = None if self.frequencies is None else self.frequencies.data_ptr()
         if training:
             # rows of a packed projection are the caller's to give
@@ -1182,15 +1195,16 @@ class HeadRotary:
     def _queries(self, where, name, t, heads, ld):
         if t is None:
             return None
-        _placed(where, name, t, self._kind, self.device)
-        form = (heads, ld, t.shape, t.stride())
-        if form in self._known:
+        index = self.device.index
+        if t.dtype is not self._kind or t.get_device() != index or _current_device is None or _current_device() != index:
+            _placed(where, name, t, self._kind, self.device)
+        if self._known.get((heads, ld, t.shape)) == t.stride():
             return t.data_ptr()
         cfg = self.cfg
         if tuple(t.shape) not in ((cfg.tokens, heads, cfg.head), (cfg.tokens, heads * cfg.head)):
             raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor, [{cfg.tokens}, {heads}, {cfg.head}] is needed")
         at = _heads_ptr(where, name, t, cfg.tokens, heads, cfg.head, ld, cfg.dtype)
-        self._known.add(form)
+        self._known[heads, ld, t.shape] = t.stride()
         return at
 
     def _tables(self, where, w_q, w_k, positions):
@@ -1304,6 +1318,7 @@ class LinearLoss:
     def __init__(self, cfg, device="cuda:0", training=True, frozen=False, in_flight=1):
         import torch
         _check_slot("LinearLoss", 0, in_flight)
+        cfg = _own_copy(cfg)
         need = tahq_loss_forward_workspace_size(cfg)
         if need == 0:
             raise TahqError(2, "tahq_loss_forward_workspace_size")

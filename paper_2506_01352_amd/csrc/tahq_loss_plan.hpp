@@ -8,6 +8,7 @@ namespace tahq {
 
 constexpr uint32_t kLossSpan = 4096;         // tokens that are counted together
 constexpr uint64_t kLossBudget = 256u << 20; // bytes of a piece, where the hidden states have no more
+constexpr uint64_t kLossMostRows = 1u << 22; // rows of the vocabulary in a piece
 
 // Tiles, and what a wavefront has of one; `along`: wavefronts side by side along the second
 struct LossTile {
@@ -61,9 +62,10 @@ inline LossPlan plan_loss(const tahq_loss_config *c)
     p.x = place((uint64_t)p.padded * p.ldx * p.es);
     const uint64_t common = at, x_bytes = (uint64_t)p.padded * p.ldx * p.es, budget = x_bytes > kLossBudget ? x_bytes : kLossBudget;
     const uint64_t vocab = loss_ceil(c->vocab, 256) * 256;
-    // rows of the vocabulary for which `each` bytes are kept: multiples of 256
+    // rows of the vocabulary for which `each` bytes are kept: multiples of 256, and so few that eight blocks of them are less than 2^32 bytes apart
     auto piece = [&](uint64_t each) {
-        const uint64_t n = budget / each / 256 * 256;
+        uint64_t n = budget / each / 256 * 256;
+        n = n < kLossMostRows ? n : kLossMostRows;
         return (uint32_t)(n < 256 ? 256 : n < vocab ? n : vocab);
     };
     // forward: 8 bytes of statistics of every token and 32 rows of the vocabulary at least; the copy of the weight

@@ -76,6 +76,8 @@ def test_class_counts_and_keeps_offsets():
         assert torch.equal((drop.backward(ones, slot=slot) != 0).flatten().cpu(), torch.from_numpy(dropout.kept(0, x.numel(), 0.5, 21, offset)))
     with pytest.raises(ValueError):
         tahq.Dropout(tahq.make_dropout_config(8, tahq.F32, 0.5)).backward(torch.ones(8, device="cuda"))
+    with pytest.raises(ValueError):
+        drop.forward(x, torch.randn(33, 4, device="cuda"))
     for bad in (x.bfloat16(), x[:, :32], x.cpu(), torch.randn(33, 4, device="cuda").t()):
         with pytest.raises((ValueError, AssertionError)):
             drop.forward(bad)
@@ -99,3 +101,13 @@ def test_graph_replays_take_other_masks():
         torch.cuda.synchronize()
         assert torch.equal(out, eager.forward(x, r, offset=50 + replay * 3)) and torch.equal(grad, eager.backward(r))
         assert _same(out.cpu(), _want(x.cpu(), r.cpu(), 0.25, 1, 50 + replay * 3, "bf16"))
+
+
+def test_class_keeps_its_configuration():
+    """What the caller does to the configuration afterwards changes nothing."""
+    cfg = tahq.make_dropout_config(64, tahq.F32, 0.5, 3)
+    drop = tahq.Dropout(cfg)
+    x = torch.randn(64, device="cuda")
+    want = drop.forward(x, offset=0).clone()
+    cfg.elements, cfg.seed, cfg.p = 1 << 40, 9, 0.0
+    assert torch.equal(drop.forward(x, offset=0), want)

@@ -166,7 +166,7 @@ def test_heads_differences():
 
 # ---------------------------------------------------------------- loss
 
-@pytest.mark.parametrize("field, value, status", [("rows", 0, 2), ("rows", 1 << 31, 2), ("cols", 0, 2), ("cols", 65537, 3), ("vocab", 0, 2), ("vocab", 1 << 31, 2), ("dtype", 2, 2),
+@pytest.mark.parametrize("field, value, status", [("rows", 0, 2), ("rows", 1 << 31, 2), ("cols", 0, 2), ("cols", 65537, 3), ("rows", (1 << 23) + 1, 3), ("vocab", 0, 2), ("vocab", 1 << 31, 2), ("dtype", 2, 2),
                                                   ("weight_dtype", 2, 2), ("reduction", 3, 2), ("accumulate", 2, 2), ("struct_size", 8, 2)])
 def test_loss_refuses_configurations(field, value, status):
     cfg = tahq.make_loss_config(10, 64, 100, tahq.BF16)
