@@ -168,91 +168,106 @@ void k_loss_logits(LogitArgs g)
     TileResult<T> r;
     const Operand a = {g.x, (uint64_t)g.padded * 64, g.padded, 0}, b = {g.weight, g.ldw, g.vocab - g.first, 0};
     multiply_tile<T, BF16, kBlocks, LIES>(a, b, tm, tn, 0, g.stages, stages, r);
-    const uint32_t lane = threadIdx.x % 64, half = lane / 32, wave = uniform(threadIdx.x / 64);
+    uint32_t lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));                           // what follows from it is not kept in registers all along
+    const uint32_t half = lane / 32, wave = uniform(threadIdx.x / 64);
     const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = g.first + tn * T::UN * 32 + r.n0;         // n0: in the vocabulary
     auto column = [&](int j, int k) { return n0 + 32 * j + 8 * (k / 4) + 4 * half + k % 4; };
     constexpr float kLog2e = 1.4426950408889634f;
+    // Exponentials as 2^(l log2(e) - shift log2(e)), one fused multiply-add each: off by the rounding of the second term, |shift| 2^-24 of the result.
+    // Columns behind the vocabulary are asked for in the tiles that have them alone, targets in the 32 tokens that have one here.
     if constexpr (MODE == kStats) {
+        auto stats = [&](auto edge) {
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            __builtin_amdgcn_sched_barrier(0);
-            uint32_t m = m0 + 32 * i + lane % 32;
-            asm volatile("" : "+v"(m));
-            const uint32_t target = m < count ? g.tokens.targets[m] : kBadTarget;
-            float l[NF][16], top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < NF; ++j)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    l[j][k] = column(j, k) < g.vocab ? r.acc[i][j][k] : -INFINITY;
-                    top = fmaxf(top, l[j][k]);
-                }
-            if (target - n0 < (uint32_t)NF * 32) {
+            for (int i = 0; i < MF; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                uint32_t m = m0 + 32 * i + lane % 32;
+                asm volatile("" : "+v"(m));
+                const uint32_t target = m < count ? g.tokens.targets[m] : kBadTarget;
+                float l[NF][16], top = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < NF; ++j)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (column(j, k) == target) g.at_target[m] = l[j][k];
+                    for (int k = 0; k < 16; ++k) {
+                        l[j][k] = !decltype(edge)::value || column(j, k) < g.vocab ? r.acc[i][j][k] : -INFINITY;
+                        top = fmaxf(top, l[j][k]);
+                    }
+                if (target - n0 < (uint32_t)NF * 32) {
+#pragma unroll
+                    for (int j = 0; j < NF; ++j)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (column(j, k) == target) g.at_target[m] = l[j][k];
+                }
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float shift = top == -INFINITY ? 0.0f : -top * kLog2e;         // a part without a logit above -infinity: its sum is 0
+                float sum[4] = {};
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(l[j][k], kLog2e, shift));
+                float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                all += __shfl_xor(all, 32);
+                if (half == 0 && m < count) g.parts[(uint64_t)(g.part + tn * WN + wave % WN) * g.padded + m] = make_float2(top, all);
             }
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float shift = top == -INFINITY ? 0.0f : top;               // a part without a logit above -infinity: its sum is 0
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < NF; ++j)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f((l[j][k] - shift) * kLog2e);
-            sum += __shfl_xor(sum, 32);
-            if (half == 0 && m < count) g.parts[(uint64_t)(g.part + tn * WN + wave % WN) * g.padded + m] = make_float2(top, sum);
-        }
+        };
+        if (n0 + NF * 32 > g.vocab) stats(std::true_type{});
+        else stats(std::false_type{});
     } else {
         constexpr uint32_t WHOLE = kStageCols<BF16>;
         const uint32_t end = (max(count, 1u) + WHOLE - 1) / WHOLE * WHOLE;   // rows that are summed over: zeros behind the last token
-        float lse[MF], factor[MF];
-        uint32_t target[MF];
+        auto gradients = [&](auto edge) {
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const uint32_t m = m0 + 32 * i + lane % 32;
-            const bool there = m < count;
-            const uint32_t row = there ? g.tokens.rows[m] : 0;
-            target[i] = there ? g.tokens.targets[m] : kBadTarget;
-            lse[i] = there ? g.lse[row] : 0.0f;
-            factor[i] = there && g.grad_loss ? g.grad_loss[row] : 1.0f;
-            if (there && target[i] == kBadTarget) factor[i] = NAN;
-        }
+            for (int i = 0; i < MF; ++i) {
+                uint32_t m = m0 + 32 * i + lane % 32;
+                asm volatile("" : "+v"(m));
+                const bool there = m < count;
+                const uint32_t row = there ? g.tokens.rows[m] : 0, target = there ? g.tokens.targets[m] : kBadTarget;
+                // tokens that there are not have logits of 0 and probabilities of 0
+                const float shift = there ? -g.lse[row] * kLog2e : -INFINITY;
+                float factor = there && g.grad_loss ? g.grad_loss[row] : 1.0f;
+                if (there && target == kBadTarget) factor = NAN;
+                const bool here = target - n0 < (uint32_t)NF * 32, any = __ballot(here) != 0;
 #pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            const uint32_t m = m0 + 32 * i + lane % 32;
+                for (int j = 0; j < NF; ++j) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    float d[16];
 #pragma unroll
-            for (int j = 0; j < NF; ++j) {
-                __builtin_amdgcn_sched_barrier(0);
-                float d[16];
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const uint32_t v = column(j, k);
-                    const float p = __builtin_amdgcn_exp2f((r.acc[i][j][k] - lse[i]) * kLog2e);
-                    d[k] = m < count && v < g.vocab ? (v == target[i] ? p - 1.0f : p) * factor[i] : 0.0f;
-                }
-                // of the vocabulary's last block all columns: zeros behind its end
-                const uint32_t n = n0 - g.first + 32 * j;                    // in the piece
-                if constexpr (BF16) {
-                    uint8_t *to = g.grads + ((uint64_t)(n / 32) * g.padded + m) * 64 + half * 16;
-                    const uint4 w0 = eight_of(four_bf16(d, 0), four_bf16(d, 4)), w1 = eight_of(four_bf16(d, 8), four_bf16(d, 12));
-                    if (m < end && g.first + n < g.vocab) {
-                        *reinterpret_cast<uint4 *>(to) = w0;
-                        *reinterpret_cast<uint4 *>(to + 32) = w1;
+                    for (int k = 0; k < 16; ++k) {
+                        d[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(r.acc[i][j][k], kLog2e, shift));
+                        if (decltype(edge)::value && column(j, k) >= g.vocab) d[k] = 0.0f;
                     }
-                } else {
+                    if (any) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        uint8_t *to = g.grads + ((uint64_t)(n / 16 + b) * g.padded + m) * 64 + half * 16;
-                        if (m < end && g.first + n + 16 * b < g.vocab) {
-                            *reinterpret_cast<float4 *>(to) = make_float4(d[8 * b], d[8 * b + 1], d[8 * b + 2], d[8 * b + 3]);
-                            *reinterpret_cast<float4 *>(to + 32) = make_float4(d[8 * b + 4], d[8 * b + 5], d[8 * b + 6], d[8 * b + 7]);
+                        for (int k = 0; k < 16; ++k)
+                            if (column(j, k) == target) d[k] -= 1.0f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) d[k] *= factor;
+                    // of the vocabulary's last block all columns: zeros behind its end
+                    const uint32_t n = n0 - g.first + 32 * j;                // in the piece
+                    if constexpr (BF16) {
+                        uint8_t *to = g.grads + ((uint64_t)(n / 32) * g.padded + m) * 64 + half * 16;
+                        const uint4 w0 = eight_of(four_bf16(d, 0), four_bf16(d, 4)), w1 = eight_of(four_bf16(d, 8), four_bf16(d, 12));
+                        if (m < end && g.first + n < g.vocab) {
+                            *reinterpret_cast<uint4 *>(to) = w0;
+                            *reinterpret_cast<uint4 *>(to + 32) = w1;
+                        }
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            uint8_t *to = g.grads + ((uint64_t)(n / 16 + b) * g.padded + m) * 64 + half * 16;
+                            if (m < end && g.first + n + 16 * b < g.vocab) {
+                                *reinterpret_cast<float4 *>(to) = make_float4(d[8 * b], d[8 * b + 1], d[8 * b + 2], d[8 * b + 3]);
+                                *reinterpret_cast<float4 *>(to + 32) = make_float4(d[8 * b + 4], d[8 * b + 5], d[8 * b + 6], d[8 * b + 7]);
+                            }
                         }
                     }
                 }
             }
-        }
+        };
+        if (n0 + NF * 32 > g.vocab) gradients(std::true_type{});
+        else gradients(std::false_type{});
     }
 }
 
