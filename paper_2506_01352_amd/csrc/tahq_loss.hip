@@ -8,8 +8,6 @@ using namespace tahq;
 
 namespace {
 
-static_assert(kLossSpan == kLossScan, "the plan's and the kernels'");
-
 tahq_status check(const tahq_loss_config *c)
 {
     if (!c) return TAHQ_ERR_NULL;
@@ -17,11 +15,11 @@ tahq_status check(const tahq_loss_config *c)
     if (c->rows == 0 || c->rows >= 0x80000000u || c->vocab == 0 || c->vocab >= 0x80000000u || c->cols == 0) return TAHQ_ERR_INVALID_ARG;
     if (c->dtype > TAHQ_BF16 || c->weight_dtype > TAHQ_BF16 || c->reduction > TAHQ_LOSS_MEAN || c->accumulate > 1) return TAHQ_ERR_INVALID_ARG;
     if (c->cols > TAHQ_LOSS_MAX_COLS || c->rows > TAHQ_LOSS_MAX_ROWS) return TAHQ_ERR_UNSUPPORTED;
-    const LossPlan p = plan_loss(c);
-    if (!launchable(loss_tiles(p.forward_kind, c->rows, p.forward_piece), 256) || !launchable(loss_tiles(p.grads_kind, c->rows, p.backward_piece), 256) ||
-        !launchable(p.x_groups, 256) || !launchable(loss_tiles(kLossMiddle, p.backward_piece, c->cols), 256) ||
-        !launchable(loss_ceil(c->rows, kGatherRows), 256))
-        return TAHQ_ERR_UNSUPPORTED;
+    for (const bool backward : {false, true}) {
+        const LossPlan p = plan_loss(c, backward);
+        if (!launchable(loss_tiles(p.kind, c->rows, p.piece), 256) || !launchable(p.x_groups, 256) || !launchable(loss_tiles(kLossMiddle, p.piece, c->cols), 256))
+            return TAHQ_ERR_UNSUPPORTED;
+    }
     return TAHQ_OK;
 }
 
@@ -32,8 +30,9 @@ struct Call {
     Enqueue q;
     LossTokens tokens;
 
-    Call(const tahq_loss_config *c, void *workspace, tahq_stream stream)
-        : cfg(c), p(plan_loss(c)), ws(static_cast<uint8_t *>(workspace)), q{(hipStream_t)stream}, tokens{at<uint32_t>(p.rows), at<uint32_t>(p.targets), at<uint32_t>(0)} {}
+    Call(const tahq_loss_config *c, bool backward, void *workspace, tahq_stream stream)
+        : cfg(c), p(plan_loss(c, backward)), ws(static_cast<uint8_t *>(workspace)), q{(hipStream_t)stream},
+          tokens{at<uint32_t>(p.rows), at<uint32_t>(p.targets), at<uint32_t>(0)} {}
     template <typename T>
     T *at(uint64_t place) const { return reinterpret_cast<T *>(ws + place); }
 
@@ -41,43 +40,59 @@ struct Call {
     {
         uint32_t *counts = p.spans > 1 ? at<uint32_t>(p.counts) : nullptr;
         if (counts) q(k_loss_count, dim3(p.spans), dim3(1024), d_target, cfg->ignore, cfg->rows, counts);
-        q(p.bf16 ? k_loss_gather<true> : k_loss_gather<false>, dim3((uint32_t)loss_ceil(cfg->rows, kGatherRows)), dim3(256), d_x, d_target, counts, cfg->rows, cfg->cols,
-          cfg->vocab, cfg->ignore, at<uint8_t>(p.x), p.ldx / p.whole, p.padded, tokens, zero, zero_also, grad_x);
+        q(p.bf16 ? k_loss_gather<true, 1> : p.planes ? k_loss_gather<false, 3> : k_loss_gather<false, 1>, dim3((uint32_t)loss_ceil(cfg->rows, kGatherRows)), dim3(256), d_x, d_target,
+          counts, cfg->rows, cfg->cols, cfg->vocab, cfg->ignore, at<uint8_t>(p.x), p.blocks, p.padded, tokens, zero, zero_also, grad_x);
     }
-    // rows first .. first + rows - 1 of the weight as the tiles take them, and bytes from row to row or from block to block
-    std::pair<const uint8_t *, uint64_t> weight(const void *d_weight, uint32_t first, uint32_t rows, uint64_t copy)
+    // Rows of the weight as the tiles take them: the first one's address, bytes from row to row or from block to block, and from plane to plane
+    struct Weight {
+        const uint8_t *from;
+        uint64_t ld, plane;
+    };
+    Weight weight(const void *d_weight, uint32_t first, uint32_t rows)
     {
-        const uint8_t *from = static_cast<const uint8_t *>(d_weight) + (uint64_t)first * cfg->cols * p.es;
-        if (!p.pad) return {from, (uint64_t)cfg->cols * p.es};
+        const uint64_t row = (uint64_t)cfg->cols * (p.bf16 ? 2 : 4);
+        const uint8_t *from = static_cast<const uint8_t *>(d_weight) + first * row;
+        if (!p.copy) return {from, row, 0};
         const uint32_t padded = (uint32_t)loss_ceil(rows, p.whole) * p.whole;
-        q(p.bf16 ? k_loss_blocks<true> : k_loss_blocks<false>, dim3((uint32_t)loss_ceil(padded, 16)), dim3(256), from, at<uint8_t>(copy), rows, cfg->cols, padded);
-        return {at<uint8_t>(copy), (uint64_t)padded * 64};
+        q(p.bf16 ? k_loss_blocks<true, 1> : p.planes ? k_loss_blocks<false, 3> : k_loss_blocks<false, 1>, dim3((uint32_t)loss_ceil(padded, 16)), dim3(256), from, at<uint8_t>(p.weight),
+          rows, cfg->cols, padded);
+        return {at<uint8_t>(p.weight), (uint64_t)padded * 64, (uint64_t)padded * 64 * p.blocks};
     }
     template <int MODE, Lies LIES>
-    void logits_of(int kind, const LogitArgs &g)
+    void logits_of(const LogitArgs &g)
     {
-        const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[kind].tm) * g.tiles_n)), block(256);
-        if (kind == kLossLarge) q(k_loss_logits<true, 2, 2, 4, 4, 1, LIES, MODE>, grid, block, g);
-        else if (kind == kLossMiddle) p.bf16 ? q(k_loss_logits<true, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g);
-        else p.bf16 ? q(k_loss_logits<true, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g);
+        const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[p.kind].tm) * g.tiles_n)), block(256);
+        if (p.kind == kLossLarge) q(k_loss_logits<true, 1, 2, 2, 4, 4, 1, LIES, MODE>, grid, block, g);
+        else if (p.kind == kLossMiddle) p.bf16 ? q(k_loss_logits<true, 1, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g);
+        else p.bf16 ? q(k_loss_logits<true, 1, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g);
     }
     template <int MODE>
-    void logits(int kind, const LogitArgs &g)
+    void logits(const LogitArgs &g)
     {
-        if (p.pad) logits_of<MODE, kBlocks>(kind, g);
-        else logits_of<MODE, kRows>(kind, g);
+        if (p.planes) {
+            const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[p.kind].tm) * g.tiles_n)), block(256);
+            if (p.kind == kLossLarge) q(k_loss_logits<true, 3, 2, 2, 4, 4, 1, kBlocks, MODE>, grid, block, g);
+            else q(k_loss_logits<true, 3, 2, 2, 2, 2, 2, kBlocks, MODE>, grid, block, g);
+        } else if (p.copy) {
+            logits_of<MODE, kBlocks>(g);
+        } else {
+            logits_of<MODE, kRows>(g);
+        }
     }
-    LogitArgs logit_args(std::pair<const uint8_t *, uint64_t> w, uint32_t first, uint32_t rows, int kind) const
+    LogitArgs logit_args(const Weight &w, uint32_t first, uint32_t rows) const
     {
         LogitArgs g = {};
         g.x = at<uint8_t>(p.x);
-        g.weight = w.first;
-        g.ldw = w.second;
+        g.weight = w.from;
+        g.ldw = w.ld;
+        g.x_plane = p.x_plane;
+        g.w_plane = w.plane;
+        g.g_plane = p.g_plane;
         g.tokens = tokens;
-        g.stages = p.ldx / p.whole;
+        g.stages = p.blocks;
         g.first = first;
         g.vocab = first + rows;
-        g.tiles_n = (uint32_t)loss_ceil(rows, kLossTiles[kind].tn);
+        g.tiles_n = (uint32_t)loss_ceil(rows, kLossTiles[p.kind].tn);
         g.padded = p.padded;
         return g;
     }
@@ -85,23 +100,26 @@ struct Call {
     void grad_x_of(const GradXArgs &g)
     {
         const dim3 grid((uint32_t)p.x_groups), block(256);
-        if (p.x_kind == kLossLarge) q(k_loss_grad_x<true, 2, 2, 4, 4, 1, LIES>, grid, block, g);
-        else if (p.x_kind == kLossMiddle) p.bf16 ? q(k_loss_grad_x<true, 2, 2, 2, 2, 2, LIES>, grid, block, g) : q(k_loss_grad_x<false, 2, 2, 2, 2, 2, LIES>, grid, block, g);
-        else p.bf16 ? q(k_loss_grad_x<true, 1, 4, 1, 1, 3, LIES>, grid, block, g) : q(k_loss_grad_x<false, 1, 4, 1, 1, 3, LIES>, grid, block, g);
+        if (p.x_kind == kLossLarge) q(k_loss_grad_x<true, 1, 2, 2, 4, 4, 1, LIES>, grid, block, g);
+        else if (p.x_kind == kLossMiddle) p.bf16 ? q(k_loss_grad_x<true, 1, 2, 2, 2, 2, 2, LIES>, grid, block, g) : q(k_loss_grad_x<false, 1, 2, 2, 2, 2, 2, LIES>, grid, block, g);
+        else p.bf16 ? q(k_loss_grad_x<true, 1, 1, 4, 1, 1, 3, LIES>, grid, block, g) : q(k_loss_grad_x<false, 1, 1, 4, 1, 1, 3, LIES>, grid, block, g);
     }
     void grad_x(const GradXArgs &g)
     {
-        if (p.pad) grad_x_of<kBlocksTurned>(g);
+        const dim3 grid((uint32_t)p.x_groups), block(256);
+        if (p.planes) p.x_kind == kLossLarge ? q(k_loss_grad_x<true, 3, 2, 2, 4, 4, 1, kBlocksTurned>, grid, block, g) : q(k_loss_grad_x<true, 3, 2, 2, 2, 2, 2, kBlocksTurned>, grid, block, g);
+        else if (p.copy) grad_x_of<kBlocksTurned>(g);
         else grad_x_of<kTurned>(g);
     }
     void grad_w(GradWArgs g)
     {
-        const int kind = p.bf16 && loss_tiles(kLossLarge, g.rows, g.cols) >= 256 ? kLossLarge : kLossMiddle;
+        const int kind = p.es == 2 && loss_tiles(kLossLarge, g.rows, g.cols) >= 256 ? kLossLarge : kLossMiddle;
         g.tiles_m = (uint32_t)loss_ceil(g.rows, kLossTiles[kind].tm);
         g.tiles_n = (uint32_t)loss_ceil(g.cols, kLossTiles[kind].tn);
         const dim3 grid(g.tiles_m * g.tiles_n), block(256);
-        if (kind == kLossLarge) q(k_loss_grad_w<true, 2, 2, 4, 4, 1>, grid, block, g);
-        else p.bf16 ? q(k_loss_grad_w<true, 2, 2, 2, 2, 2>, grid, block, g) : q(k_loss_grad_w<false, 2, 2, 2, 2, 2>, grid, block, g);
+        if (p.planes) kind == kLossLarge ? q(k_loss_grad_w<true, 3, 2, 2, 4, 4, 1>, grid, block, g) : q(k_loss_grad_w<true, 3, 2, 2, 2, 2, 2>, grid, block, g);
+        else if (kind == kLossLarge) q(k_loss_grad_w<true, 1, 2, 2, 4, 4, 1>, grid, block, g);
+        else p.bf16 ? q(k_loss_grad_w<true, 1, 2, 2, 2, 2, 2>, grid, block, g) : q(k_loss_grad_w<false, 1, 2, 2, 2, 2, 2>, grid, block, g);
     }
 };
 
@@ -119,8 +137,8 @@ void tahq_loss_config_default(tahq_loss_config *cfg)
     cfg->ignore = -100;
 }
 
-size_t tahq_loss_forward_workspace_size(const tahq_loss_config *cfg) { return check(cfg) == TAHQ_OK ? (size_t)plan_loss(cfg).forward_total : 0; }
-size_t tahq_loss_backward_workspace_size(const tahq_loss_config *cfg) { return check(cfg) == TAHQ_OK ? (size_t)plan_loss(cfg).backward_total : 0; }
+size_t tahq_loss_forward_workspace_size(const tahq_loss_config *cfg) { return check(cfg) == TAHQ_OK ? (size_t)plan_loss(cfg, false).total : 0; }
+size_t tahq_loss_backward_workspace_size(const tahq_loss_config *cfg) { return check(cfg) == TAHQ_OK ? (size_t)plan_loss(cfg, true).total : 0; }
 
 tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, const void *d_weight, const int64_t *d_target, float *d_losses,
                               float *d_lse, float *d_total, void *d_workspace, size_t workspace_capacity, tahq_stream stream)
@@ -129,9 +147,9 @@ tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, cons
     if (rc != TAHQ_OK) return rc;
     for (const void *p : {d_x, d_weight, (const void *)d_target, (const void *)d_losses, (const void *)d_lse, (const void *)d_total, (const void *)d_workspace})
         if (!p) return TAHQ_ERR_NULL;
-    Call call(cfg, d_workspace, stream);
+    Call call(cfg, false, d_workspace, stream);
     const LossPlan &p = call.p;
-    if (workspace_capacity < p.forward_total) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_capacity < p.total) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
     for (const void *x : {d_x, d_weight, (const void *)d_losses, (const void *)d_lse, (const void *)d_total, (const void *)d_workspace})
         if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
     if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target) return TAHQ_ERR_MISALIGNED;
@@ -140,13 +158,13 @@ tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, cons
     uint32_t width = 32;
     while (width > 1 && (cfg->rows <= 32 ? cfg->rows <= width / 2 : cfg->rows < 256 * width)) width /= 2;
     const bool alone = cfg->rows <= width;
-    for (uint32_t first = 0; first < cfg->vocab; first += p.forward_piece) {
-        const uint32_t rows = cfg->vocab - first < p.forward_piece ? cfg->vocab - first : p.forward_piece;
-        LogitArgs g = call.logit_args(call.weight(d_weight, first, rows, p.forward_weight), first, rows, p.forward_kind);
+    for (uint32_t first = 0; first < cfg->vocab; first += p.piece) {
+        const uint32_t rows = cfg->vocab - first < p.piece ? cfg->vocab - first : p.piece;
+        LogitArgs g = call.logit_args(call.weight(d_weight, first, rows), first, rows);
         g.parts = call.at<float2>(p.stats);
         g.at_target = call.at<float>(p.at_target);
-        call.logits<kStats>(p.forward_kind, g);
-        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, width)), dim3(kJoinLanes), g.parts, g.tiles_n * kLossTiles[p.forward_kind].along, p.padded, call.tokens, g.at_target,
+        call.logits<kStats>(g);
+        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, width)), dim3(kJoinLanes), g.parts, g.tiles_n * kLossTiles[p.kind].along, p.padded, call.tokens, g.at_target,
                call.at<float2>(p.running), first != 0, first + rows == cfg->vocab, width, d_losses, d_lse, cfg->reduction == TAHQ_LOSS_MEAN,
                alone && first + rows == cfg->vocab ? d_total : nullptr);
     }
@@ -163,9 +181,9 @@ tahq_status tahq_loss_backward(const tahq_loss_config *cfg, const void *d_x, con
     if (!d_grad_x && !d_grad_weight) return TAHQ_ERR_NULL;
     for (const void *p : {d_x, d_weight, (const void *)d_target, (const void *)d_lse, (const void *)d_workspace})
         if (!p) return TAHQ_ERR_NULL;
-    Call call(cfg, d_workspace, stream);
+    Call call(cfg, true, d_workspace, stream);
     const LossPlan &p = call.p;
-    if (workspace_capacity < p.backward_total) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_capacity < p.total) return TAHQ_ERR_WORKSPACE_TOO_SMALL;
     for (const void *x : {d_x, d_weight, (const void *)d_lse, (const void *)d_grad_x, (const void *)d_grad_weight, (const void *)d_workspace})
         if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
     if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target || reinterpret_cast<uintptr_t>(d_grad_loss) % sizeof *d_grad_loss) return TAHQ_ERR_MISALIGNED;
@@ -173,19 +191,19 @@ tahq_status tahq_loss_backward(const tahq_loss_config *cfg, const void *d_x, con
     const uint32_t mean = cfg->reduction == TAHQ_LOSS_MEAN;
     const float *whole = each ? nullptr : d_grad_loss;
     call.gather(d_x, d_target, nullptr, nullptr, d_grad_x);
-    for (uint32_t first = 0; first < cfg->vocab; first += p.backward_piece) {
-        const uint32_t rows = cfg->vocab - first < p.backward_piece ? cfg->vocab - first : p.backward_piece;
-        const auto w = call.weight(d_weight, first, rows, p.backward_weight);
-        LogitArgs g = call.logit_args(w, first, rows, p.grads_kind);
+    for (uint32_t first = 0; first < cfg->vocab; first += p.piece) {
+        const uint32_t rows = cfg->vocab - first < p.piece ? cfg->vocab - first : p.piece;
+        const Call::Weight w = call.weight(d_weight, first, rows);
+        LogitArgs g = call.logit_args(w, first, rows);
         g.lse = d_lse;
         g.grad_loss = each ? d_grad_loss : nullptr;
         g.grads = call.at<uint8_t>(p.grads);
-        call.logits<kGrads>(p.grads_kind, g);
+        call.logits<kGrads>(g);
         if (d_grad_x)
-            call.grad_x({g.grads, w.first, w.second, call.tokens, rows, cfg->cols, (uint32_t)loss_ceil(rows, p.whole), p.x_slots,
+            call.grad_x({g.grads, w.from, w.ld, p.g_plane, w.plane, call.tokens, rows, cfg->cols, (uint32_t)loss_ceil(rows, p.whole), p.x_stages, p.x_slots,
                          (uint32_t)loss_ceil(cfg->cols, kLossTiles[p.x_kind].tn), p.padded, first != 0, call.at<float4>(p.sums)});
         if (d_grad_weight)
-            call.grad_w({g.grads, g.x, call.tokens, rows, cfg->cols, 0, 0, p.padded, whole, mean, cfg->weight_dtype == TAHQ_BF16, cfg->accumulate,
+            call.grad_w({g.grads, g.x, p.g_plane, p.x_plane, call.tokens, rows, cfg->cols, 0, 0, p.padded, whole, mean, cfg->weight_dtype == TAHQ_BF16, cfg->accumulate,
                          static_cast<uint8_t *>(d_grad_weight) + (uint64_t)first * cfg->cols * (cfg->weight_dtype == TAHQ_BF16 ? 2 : 4)});
     }
     if (d_grad_x) {

@@ -7,11 +7,11 @@
 #pragma once
 #include "tahq_lanes.hpp"
 #include "tahq_loss.h"
+#include "tahq_loss_plan.hpp"
 #include "tahq_loss_tiles.hpp"
 
 namespace tahq {
 
-constexpr uint32_t kLossScan = 4096;         // tokens whose number of those that count is known in front of the gather
 constexpr uint32_t kBadTarget = 0xffffffffu;
 
 // What the workspace holds of the tokens that count, in their order: row numbers, targets, and how many there are
@@ -39,26 +39,42 @@ void k_loss_count(const int64_t *target, int64_t ignore, uint32_t rows, uint32_t
     __shared__ uint32_t places[16];
     uint32_t n = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kLossScan / 1024; ++i) {
-        const uint32_t row = min(blockIdx.x * kLossScan + i * 1024 + threadIdx.x, rows - 1);
-        n += target[row] != ignore && row == blockIdx.x * kLossScan + i * 1024 + threadIdx.x;
+    for (uint32_t i = 0; i < kLossSpan / 1024; ++i) {
+        const uint32_t row = min(blockIdx.x * kLossSpan + i * 1024 + threadIdx.x, rows - 1);
+        n += target[row] != ignore && row == blockIdx.x * kLossSpan + i * 1024 + threadIdx.x;
     }
     n = group_count(n, places);
     if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
+// Eight elements to their place in blocks, or in three planes of them
+template <bool BF16, int PLANES>
+__device__ __forceinline__ void put_eight(const Eight<BF16> &e, uint8_t *base, uint64_t plane, uint64_t at)
+{
+    if constexpr (PLANES == 3) {
+        float x[8];
+        unpack(e, x);
+        uint4 p[3];
+        split_planes(x, p);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4 *>(base + i * plane + at) = p[i];
+    } else {
+        __builtin_memcpy(__builtin_assume_aligned(base + at, 16), e.q, sizeof e.q);
+    }
+}
+
 constexpr uint32_t kGatherRows = 4;          // of a workgroup, one to a wavefront
 
-// gathered: blocks of 64 bytes of every row, `padded` rows each, `blocks` of them.  counts: of the spans of kLossScan tokens, NULL if there is one.
+// gathered: blocks of 64 bytes of every row, `padded` rows each, `blocks` of them, of fp32 in planes of bf16 three times.  counts: of the spans of kLossSpan tokens, NULL if there is one.
 // zero, zero_also: float results of tokens that do not count (NULL: none); grad_x: their gradients.
-template <bool BF16>
+template <bool BF16, int PLANES>
 __global__ __launch_bounds__(256)
 void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts, uint32_t rows, uint32_t cols, uint32_t vocab, int64_t ignore,
                    uint8_t *gathered, uint32_t blocks, uint32_t padded, LossTokens tokens, float *zero, float *zero_also, void *grad_x)
 {
-    constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16>, AHEAD = 4;
+    constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16 || PLANES == 3>, AHEAD = 4;
     __shared__ uint32_t places[4];
-    const uint32_t first = blockIdx.x * kGatherRows, span = first / kLossScan, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), row = first + wave;
+    const uint32_t first = blockIdx.x * kGatherRows, span = first / kLossSpan, lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), row = first + wave;
     // the row is on its way while its place is counted
     Eight<BF16> e[AHEAD];
     auto ask = [&](uint32_t c0) {
@@ -74,7 +90,7 @@ void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts,
 #pragma unroll
         for (uint32_t k = 0; k < AHEAD; ++k) {
             const uint32_t c = c0 + k * 512 + lane * 8;
-            if (c < blocks * WHOLE) __builtin_memcpy(__builtin_assume_aligned(gathered + ((uint64_t)(c / WHOLE) * padded + to) * 64 + c % WHOLE * ES, 16), e[k].q, sizeof e[k].q);
+            if (c < blocks * WHOLE) put_eight<BF16, PLANES>(e[k], gathered, (uint64_t)blocks * padded * 64, ((uint64_t)(c / WHOLE) * padded + to) * 64 + c % WHOLE * (64 / WHOLE));
         }
     };
     ask(0);
@@ -83,7 +99,7 @@ void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts,
     uint32_t before = 0;
     for (uint32_t i = threadIdx.x; i < span; i += 256) before += counts[i];
 #pragma unroll 4
-    for (uint32_t i = span * kLossScan + threadIdx.x; i < first; i += 256) before += target[i] != ignore;
+    for (uint32_t i = span * kLossSpan + threadIdx.x; i < first; i += 256) before += target[i] != ignore;
     before = group_count(before, places);
     const uint32_t counted = (uint32_t)__ballot(t != ignore) & ((1u << kGatherRows) - 1);
     if (row < rows) {
@@ -120,20 +136,20 @@ void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts,
     }
 }
 
-// A piece of the weight in blocks, for numbers of channels that are not whole stages; rows up to whole stages, and channels, are filled up with zeros.
-// Sixteen rows to a workgroup, so that it writes runs of 1 KB.
-template <bool BF16>
+// A piece of the weight in blocks, for numbers of channels that are not whole stages, and of fp32 in planes; rows up to whole stages, and channels, are filled up
+// with zeros.  Sixteen rows to a workgroup, so that it writes runs of 1 KB.
+template <bool BF16, int PLANES>
 __global__ __launch_bounds__(256)
 void k_loss_blocks(const void *weight, uint8_t *blocks, uint32_t rows, uint32_t cols, uint32_t padded)
 {
-    constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16>, RUNS = WHOLE / 8;
-    const uint32_t row = blockIdx.x * 16 + threadIdx.x / RUNS % 16;
+    constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16 || PLANES == 3>, RUNS = WHOLE / 8;
+    const uint32_t row = blockIdx.x * 16 + threadIdx.x / RUNS % 16, count = (cols + WHOLE - 1) / WHOLE;
     if (row >= padded) return;
-    for (uint32_t c = (threadIdx.x / (16 * RUNS)) * WHOLE + threadIdx.x % RUNS * 8; c < (cols + WHOLE - 1) / WHOLE * WHOLE; c += 256 / (16 * RUNS) * WHOLE) {
+    for (uint32_t c = (threadIdx.x / (16 * RUNS)) * WHOLE + threadIdx.x % RUNS * 8; c < count * WHOLE; c += 256 / (16 * RUNS) * WHOLE) {
         Eight<BF16> e = {};
         if (row < rows && c < cols)
             e = fetch<BF16, false>(static_cast<const uint8_t *>(weight) + (uint64_t)row * cols * ES, c, cols, more_behind(row, rows, cols));
-        __builtin_memcpy(__builtin_assume_aligned(blocks + ((uint64_t)(c / WHOLE) * padded + row) * 64 + c % WHOLE * ES, 16), e.q, sizeof e.q);
+        put_eight<BF16, PLANES>(e, blocks, (uint64_t)count * padded * 64, ((uint64_t)(c / WHOLE) * padded + row) * 64 + c % WHOLE * (64 / WHOLE));
     }
 }
 
@@ -142,6 +158,7 @@ void k_loss_blocks(const void *weight, uint8_t *blocks, uint32_t rows, uint32_t 
 struct LogitArgs {
     const uint8_t *x, *weight;               // gathered hidden states, the piece's first row
     uint64_t ldw;                            // bytes from row to row, or from block to block
+    uint64_t x_plane, w_plane, g_plane;      // bytes from plane to plane
     LossTokens tokens;
     uint32_t stages, first, vocab;           // of columns; the piece's first row of the vocabulary, and rows of the vocabulary up to the piece's end
     uint32_t tiles_n;
@@ -155,7 +172,7 @@ struct LogitArgs {
 enum { kStats = 0, kGrads = 1 };
 
 // LIES: how the weight does
-template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES, int MODE>
+template <bool BF16, int PLANES, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES, int MODE>
 __global__ __launch_bounds__(256, PER_CU)
 void k_loss_logits(LogitArgs g)
 {
@@ -166,8 +183,8 @@ void k_loss_logits(LogitArgs g)
     uint32_t tm, tn;
     tile_of(blockIdx.x, tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
-    const Operand a = {g.x, (uint64_t)g.padded * 64, g.padded, 0}, b = {g.weight, g.ldw, g.vocab - g.first, 0};
-    multiply_tile<T, BF16, kBlocks, LIES>(a, b, tm, tn, 0, g.stages, stages, r);
+    const Operand a = {g.x, (uint64_t)g.padded * 64, g.padded, 0, g.x_plane}, b = {g.weight, g.ldw, g.vocab - g.first, 0, g.w_plane};
+    multiply_tile<T, BF16, PLANES, kBlocks, LIES>(a, b, tm, tn, 0, g.stages, stages, r);
     uint32_t lane = threadIdx.x % 64;
     asm volatile("" : "+v"(lane));                           // what follows from it is not kept in registers all along
     const uint32_t half = lane / 32, wave = uniform(threadIdx.x / 64);
@@ -248,10 +265,23 @@ void k_loss_logits(LogitArgs g)
                     const uint32_t n = n0 - g.first + 32 * j;                // in the piece
                     if constexpr (BF16) {
                         uint8_t *to = g.grads + ((uint64_t)(n / 32) * g.padded + m) * 64 + half * 16;
-                        const uint4 w0 = eight_of(four_bf16(d, 0), four_bf16(d, 4)), w1 = eight_of(four_bf16(d, 8), four_bf16(d, 12));
-                        if (m < end && g.first + n < g.vocab) {
-                            *reinterpret_cast<uint4 *>(to) = w0;
-                            *reinterpret_cast<uint4 *>(to + 32) = w1;
+#pragma unroll
+                        for (int plane = 0; plane < PLANES; ++plane) {
+                            uint2 w[4];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) w[q] = four_bf16(d, 4 * q);
+                            if (plane + 1 < PLANES) {                        // what is left for the next one
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) {
+                                    const uint32_t two = k % 4 < 2 ? w[k / 4].x : w[k / 4].y;
+                                    d[k] -= __uint_as_float(k % 2 ? two & 0xffff0000u : two << 16);
+                                }
+                            }
+                            const uint4 w0 = eight_of(w[0], w[1]), w1 = eight_of(w[2], w[3]);
+                            if (m < end && g.first + n < g.vocab) {
+                                *reinterpret_cast<uint4 *>(to + plane * g.g_plane) = w0;
+                                *reinterpret_cast<uint4 *>(to + plane * g.g_plane + 32) = w1;
+                            }
                         }
                     } else {
 #pragma unroll
@@ -278,42 +308,31 @@ __device__ __forceinline__ float loss_scale(const float *grad_loss, uint32_t mea
     return mean ? g / (float)max(count, 1u) : g;
 }
 
-// How sums over a piece's `stages` are shared: `parts` of `run` stages, so many that `slots` workgroups, what the device holds at once, have one each of
-// the tiles of the tokens that count; sixteen stages and more to a part.  Later pieces have as many parts as the first or, with fewer stages, fewer.
-struct Shares {
-    uint32_t tiles, parts, run;
-    __device__ __forceinline__ Shares(uint32_t tiles_, uint32_t stages, uint32_t slots) : tiles(tiles_)
-    {
-        const uint32_t most = max(stages / 16, 1u), want = min(max(slots / max(tiles, 1u), 1u), most);
-        run = (stages + want - 1) / want;
-        parts = (stages + run - 1) / run;
-    }
-};
 // Sums over the vocabulary's piece, in parts; `add`: to what earlier pieces left.  They stay in the order that the lanes have them in, [part][tile]
 // [wavefront][i][j][group of four][lane] of four numbers: 1 KB in a row.
 struct GradXArgs {
     const uint8_t *grads, *weight;
-    uint64_t ldw;
+    uint64_t ldw, g_plane, w_plane;
     LossTokens tokens;
-    uint32_t rows, cols, stages, slots, tiles_n, padded, add;
+    uint32_t rows, cols, stages, first_stages, slots, tiles_n, padded, add;
     float4 *sums;
 };
-template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES>
+template <bool BF16, int PLANES, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES>
 __global__ __launch_bounds__(256, PER_CU)
 void k_loss_grad_x(GradXArgs g)
 {
     using T = TileKind<BF16, WM, WN, MF, NF>;
     const Stages stages = stages_of<T, LIES>();
     const uint32_t count = *g.tokens.count, tiles_m = (count + T::UM * 32 - 1) / (T::UM * 32);
-    const Shares shares(tiles_m * g.tiles_n, g.stages, g.slots);
+    const Shares shares(tiles_m * g.tiles_n, g.first_stages, g.stages, g.slots);
     const uint32_t part = shares.tiles ? blockIdx.x / shares.tiles : shares.parts;
     if (part >= shares.parts) return;
     uint32_t tm, tn;
     tile_of(blockIdx.x % shares.tiles, tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
-    const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, 0}, b = {g.weight, g.ldw, g.rows, (g.cols + T::COLS - 1) / T::COLS};
+    const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, 0, g.g_plane}, b = {g.weight, g.ldw, g.rows, (g.cols + T::COLS - 1) / T::COLS, g.w_plane};
     const uint32_t from = part * shares.run;
-    multiply_tile<T, BF16, kBlocks, LIES>(a, b, tm, tn, from, min(shares.run, g.stages - from), stages, r);
+    multiply_tile<T, BF16, PLANES, kBlocks, LIES>(a, b, tm, tn, from, min(shares.run, g.stages - from), stages, r);
     uint32_t lane = threadIdx.x % 64;
     asm volatile("" : "+v"(lane));                           // not an address to keep in registers all along
     float4 *to = g.sums + (((uint64_t)part * shares.tiles + (uint64_t)tm * g.tiles_n + tn) * 4 + uniform(threadIdx.x / 64)) * (MF * NF * 256) + lane;
@@ -365,7 +384,7 @@ void k_loss_scatter(const float4 *sums, uint32_t stages, uint32_t slots, uint32_
 {
     const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), count = *tokens.count, r = blockIdx.x * 8 + lane % 8;
     if (blockIdx.x * 8 >= count) return;
-    const Shares shares((count + s.tm - 1) / s.tm * tiles_n, stages, slots);
+    const Shares shares((count + s.tm - 1) / s.tm * tiles_n, stages, stages, slots);
     const float scale = loss_scale(grad_loss, mean, count);
     const bool there = r < count;
     const uint64_t row = there ? (uint64_t)tokens.rows[r] * cols : 0;
@@ -395,13 +414,14 @@ void k_loss_scatter(const float4 *sums, uint32_t stages, uint32_t slots, uint32_
 
 struct GradWArgs {
     const uint8_t *grads, *x;
+    uint64_t g_plane, x_plane;
     LossTokens tokens;
     uint32_t rows, cols, tiles_m, tiles_n, padded;           // rows of the piece
     const float *grad_loss;                  // of the reduced loss, or NULL
     uint32_t mean, out_bf16, accumulate;
     void *out;                               // the gradient's first row of the piece
 };
-template <bool BF16, int WM, int WN, int MF, int NF, int PER_CU>
+template <bool BF16, int PLANES, int WM, int WN, int MF, int NF, int PER_CU>
 __global__ __launch_bounds__(256, PER_CU)
 void k_loss_grad_w(GradWArgs g)
 {
@@ -411,8 +431,9 @@ void k_loss_grad_w(GradWArgs g)
     uint32_t tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
-    const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, (g.rows + T::COLS - 1) / T::COLS}, b = {g.x, (uint64_t)g.padded * 64, g.padded, (g.cols + T::COLS - 1) / T::COLS};
-    multiply_tile<T, BF16, kBlocksTurned, kBlocksTurned>(a, b, tm, tn, 0, depth, stages, r);
+    const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, (g.rows + T::COLS - 1) / T::COLS, g.g_plane},
+                  b = {g.x, (uint64_t)g.padded * 64, g.padded, (g.cols + T::COLS - 1) / T::COLS, g.x_plane};
+    multiply_tile<T, BF16, PLANES, kBlocksTurned, kBlocksTurned>(a, b, tm, tn, 0, depth, stages, r);
     const float scale = loss_scale(g.grad_loss, g.mean, count);
     const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = tn * T::UN * 32 + r.n0;
     if (g.out_bf16) store_rows<true, T>(r, m0, n0, g.rows, g.cols, scale, g.out, g.accumulate != 0);

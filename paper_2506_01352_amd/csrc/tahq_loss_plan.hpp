@@ -1,14 +1,26 @@
-// How a loss over a vocabulary is cut, from its sizes alone: host code.
+// How a loss over a vocabulary is cut, from its sizes alone: host code, but for Shares.
 #pragma once
 #include <stdint.h>
 
 #include "tahq_loss.h"
+
+#ifdef __HIP__
+#define TAHQ_LOSS_BOTH __host__ __device__
+#else
+#define TAHQ_LOSS_BOTH
+#endif
 
 namespace tahq {
 
 constexpr uint32_t kLossSpan = 4096;         // tokens that are counted together
 constexpr uint64_t kLossBudget = 256u << 20; // bytes of a piece, where the hidden states have no more
 constexpr uint64_t kLossMostRows = 1u << 22; // rows of the vocabulary in a piece
+
+// fp32 is multiplied as such (v_mfma_f32_32x32x2_f32, 110 to 135 TFLOP/s here), or as three bf16 whose sum it is, six products of bf16 for one (at the tiles; 155
+// to 200 TFLOP/s of fp32), for which the weight is copied into planes first.  So many tokens pay for that, 2048 x 32000: forward with rows of no whole stages, which
+// are copied in any case (2047: 100 tokens 273 us and as such 274, 130 324 and 382); forward (260 413 and 386, 400 487 and 501, 1000 738 and 986); backward, where three
+// products share a copy (200 1018 and 1004 with the forward pass, 260 1342 and 1454, 1000 2808 and 3890).
+constexpr uint32_t kPlanesPadded = 112, kPlanesForward = 384, kPlanesBackward = 224;
 
 // Tiles, and what a wavefront has of one; `along`: wavefronts side by side along the second
 struct LossTile {
@@ -20,36 +32,57 @@ enum { kLossLarge = 0, kLossMiddle = 1, kLossFew = 2 };
 inline uint64_t loss_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 inline uint64_t loss_tiles(int kind, uint64_t m, uint64_t n) { return loss_ceil(m, kLossTiles[kind].tm) * loss_ceil(n, kLossTiles[kind].tn); }
 
-// The kind of tile of a product [m, n]
-inline int loss_kind(bool bf16, uint64_t m, uint64_t n)
+// The kind of tile of a product [m, n]; `large`: there are large ones (of bf16)
+inline int loss_kind(bool large, uint64_t m, uint64_t n)
 {
     if (m <= 32) return kLossFew;
-    return bf16 && loss_tiles(kLossLarge, m, n) >= 256 ? kLossLarge : kLossMiddle;
+    return large && loss_tiles(kLossLarge, m, n) >= 256 ? kLossLarge : kLossMiddle;
 }
 
-struct LossPlan {
-    bool bf16, pad;                          // pad: the weight is copied into blocks of whole stages
-    uint32_t es, whole, ldx, padded;         // bytes of an element; columns of a stage; elements of a gathered row; tokens up to whole stages
-    uint32_t spans;                          // of kLossSpan tokens
-    uint32_t forward_piece, backward_piece;  // rows of the vocabulary
-    int forward_kind, grads_kind, x_kind;
-    uint32_t parts, x_stages, x_slots;       // of a forward piece's statistics; of the sums for the hidden states' gradient: stages of the first piece, Shares
-    uint64_t x_groups;                       // workgroups for them
-    // places in the workspace
-    uint64_t rows, targets, counts, x, at_target, running, stats, forward_weight, forward_total;
-    uint64_t grads, sums, backward_weight, backward_total;
+// How sums over a piece's `stages` are shared: `parts` of `run` stages, so many that `slots` workgroups, what the device holds at once, have one each of
+// the tiles of the tokens that count; sixteen stages and more to a part of the first piece.  Later pieces, which are no longer, are added to the first
+// one's parts, to no more of them than there are.
+struct Shares {
+    uint32_t tiles, parts, run;
+    TAHQ_LOSS_BOTH Shares(uint32_t tiles_, uint32_t first_stages, uint32_t stages, uint32_t slots) : tiles(tiles_)
+    {
+        const uint32_t fit = slots / (tiles ? tiles : 1), most = first_stages / 16;
+        const uint32_t want = fit < most ? (fit ? fit : 1) : (most ? most : 1);
+        const uint32_t each = (first_stages + want - 1) / want, first = (first_stages + each - 1) / each;
+        run = (stages + first - 1) / first;
+        parts = (stages + run - 1) / run;
+    }
 };
 
-inline LossPlan plan_loss(const tahq_loss_config *c)
+// The plan of one direction.
+struct LossPlan {
+    bool bf16, planes;                       // the tensors' type; fp32 as three planes of bf16
+    bool copy;                               // the weight is copied into blocks of whole stages
+    uint32_t es, whole, blocks, padded;      // bytes of an element in a tile; columns of a stage; stages of a row of x; tokens up to whole stages
+    uint32_t spans;                          // of kLossSpan tokens
+    uint32_t piece;                          // rows of the vocabulary
+    int kind, x_kind;                        // tiles of logits, of the hidden states' gradient
+    uint32_t parts;                          // of a forward piece's statistics
+    uint32_t x_stages, x_slots;              // sums for the hidden states' gradient: stages of the first piece, Shares
+    uint64_t x_groups;                       // workgroups for them
+    uint64_t x_plane, g_plane;               // bytes of a plane
+    // places in the workspace
+    uint64_t rows, targets, counts, x, at_target, running, stats, grads, sums, weight, total;
+};
+
+inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
 {
     LossPlan p = {};
     p.bf16 = c->dtype == TAHQ_BF16;
-    p.es = p.bf16 ? 2 : 4;
+    const bool odd = c->cols % (p.bf16 ? 32 : 16) != 0;
+    p.planes = !p.bf16 && c->rows >= (odd ? kPlanesPadded : backward ? kPlanesBackward : kPlanesForward);
+    p.copy = odd || p.planes;
+    p.es = p.bf16 || p.planes ? 2 : 4;
     p.whole = 64 / p.es;
-    p.ldx = (uint32_t)loss_ceil(c->cols, p.whole) * p.whole;
-    p.pad = p.ldx != c->cols;
+    p.blocks = (uint32_t)loss_ceil(c->cols, p.whole);
     p.padded = (uint32_t)loss_ceil(c->rows, p.whole) * p.whole;
     p.spans = (uint32_t)loss_ceil(c->rows, kLossSpan);
+    const uint32_t n = p.planes ? 3 : 1;
     uint64_t at = 256;
     auto place = [&](uint64_t bytes) {
         const uint64_t here = at;
@@ -59,44 +92,65 @@ inline LossPlan plan_loss(const tahq_loss_config *c)
     p.rows = place((uint64_t)p.padded * 4);
     p.targets = place((uint64_t)p.padded * 4);
     p.counts = place((uint64_t)p.spans * 4);
-    p.x = place((uint64_t)p.padded * p.ldx * p.es);
-    const uint64_t common = at, x_bytes = (uint64_t)p.padded * p.ldx * p.es, budget = x_bytes > kLossBudget ? x_bytes : kLossBudget;
+    p.x_plane = (uint64_t)p.padded * p.blocks * 64;
+    p.x = place(n * p.x_plane);
+    const uint64_t x_bytes = n * p.x_plane, least = p.planes ? 2 * kLossBudget : kLossBudget, budget = x_bytes > least ? x_bytes : least;
     const uint64_t vocab = loss_ceil(c->vocab, 256) * 256;
     // rows of the vocabulary for which `each` bytes are kept: multiples of 256, and so few that eight blocks of them are less than 2^32 bytes apart
     auto piece = [&](uint64_t each) {
-        uint64_t n = budget / each / 256 * 256;
-        n = n < kLossMostRows ? n : kLossMostRows;
-        return (uint32_t)(n < 256 ? 256 : n < vocab ? n : vocab);
+        uint64_t rows = budget / each / 256 * 256;
+        rows = rows < kLossMostRows ? rows : kLossMostRows;
+        return (uint32_t)(rows < 256 ? 256 : rows < vocab ? rows : vocab);
     };
-    // forward: 8 bytes of statistics of every token and 32 rows of the vocabulary at least; the copy of the weight
-    p.forward_kind = loss_kind(p.bf16, c->rows, c->vocab);
-    const LossTile &f = kLossTiles[p.forward_kind];
-    p.forward_piece = piece((uint64_t)p.padded * 8 * f.along / f.tn + 1);
-    if (p.pad && piece((uint64_t)p.ldx * p.es) < p.forward_piece) p.forward_piece = piece((uint64_t)p.ldx * p.es);
-    p.parts = p.forward_piece / f.tn * f.along;
-    p.at_target = place((uint64_t)p.padded * 4);
-    p.running = place((uint64_t)p.padded * 8);
-    p.stats = place((uint64_t)p.parts * p.padded * 8);
-    p.forward_weight = place(p.pad ? (uint64_t)p.forward_piece * p.ldx * p.es : 0);
-    p.forward_total = at;
-    // backward
-    at = common;
-    p.backward_piece = piece((uint64_t)p.padded * p.es);
-    if (p.pad && piece((uint64_t)p.ldx * p.es) < p.backward_piece) p.backward_piece = piece((uint64_t)p.ldx * p.es);
-    const uint64_t widest = p.backward_piece < c->vocab ? p.backward_piece : c->vocab;
-    p.grads_kind = loss_kind(p.bf16, c->rows, widest);
-    // Few tiles: several workgroups share the sums of one over the vocabulary (Shares), as many as the device holds at once.  Then large tiles are as good
-    // where there are few, but for what hangs over the edges (2048 x 1600, of which 1448 tokens count, x 50257: 365 us in tiles of 128 x 128, 245 in 256 x 256).
-    const uint64_t stages = loss_ceil(widest, p.whole), large = loss_tiles(kLossLarge, c->rows, c->cols), middle = loss_tiles(kLossMiddle, c->rows, c->cols);
-    p.x_kind = c->rows <= 32 ? kLossFew : p.bf16 && 3 * large <= middle && large * stages >= 256 * 16 ? kLossLarge : kLossMiddle;
-    p.x_stages = (uint32_t)stages;
-    p.x_slots = p.x_kind == kLossLarge ? 256 : 512;
-    const uint64_t tiles = loss_tiles(p.x_kind, c->rows, c->cols);
-    p.x_groups = tiles > p.x_slots ? tiles : p.x_slots;
-    p.grads = place((uint64_t)p.padded * loss_ceil(widest, p.whole) * 64);
-    p.sums = place(p.x_groups * kLossTiles[p.x_kind].tm * kLossTiles[p.x_kind].tn * 4);
-    p.backward_weight = place(p.pad ? (uint64_t)p.backward_piece * p.ldx * p.es : 0);
-    p.backward_total = at;
+    // Pieces of at most `most` rows, so long that their tiles make whole rounds of the compute units where that is possible: launches take a round for every 256
+    // tiles, begun or not, of as many stages as `logits` and `weights` say and a start as long as twenty more.  (Tiles of 256 x 256; fp32 4319 x 1024 x 50257, pieces of
+    // 20480 rows, 320 tiles of the weight's gradient: 9.99 ms, chosen so 9.87.)
+    const uint64_t factor = p.planes ? 6 : 1, tiles_m = loss_tiles(kLossLarge, c->rows, 1), tiles_c = loss_tiles(kLossLarge, c->cols, 1);
+    auto even = [&](uint32_t most, uint64_t logits, uint64_t weights) {
+        if (p.es != 2 || c->rows <= 32 || most >= vocab) return most;
+        auto cost = [&](uint64_t t) {
+            return t ? loss_ceil(tiles_m * t, 256) * (logits + 20) + (weights ? loss_ceil(t * tiles_c, 256) * (weights + 20) : 0) + 30 : 0;
+        };
+        uint64_t best = most / 256, least_cost = ~0ull;
+        for (uint64_t t = most / 256, end = t > 64 ? t - 64 : 0; t > end; --t) {
+            const uint64_t all = vocab / 256, here = all / t * cost(t) + cost(all % t);
+            if (here < least_cost) {
+                least_cost = here;
+                best = t;
+            }
+        }
+        return (uint32_t)(best * 256);
+    };
+    const uint32_t copied = p.copy ? piece((uint64_t)n * p.blocks * 64) : ~0u;
+    if (!backward) {
+        // 8 bytes of statistics of every token and 32 rows of the vocabulary at least
+        p.kind = loss_kind(p.es == 2, c->rows, c->vocab);
+        const LossTile &t = kLossTiles[p.kind];
+        p.piece = piece((uint64_t)p.padded * 8 * t.along / t.tn + 1);
+        if (copied < p.piece) p.piece = even(copied, factor * p.blocks, 0);
+        p.parts = p.piece / t.tn * t.along;
+        p.at_target = place((uint64_t)p.padded * 4);
+        p.running = place((uint64_t)p.padded * 8);
+        p.stats = place((uint64_t)p.parts * p.padded * 8);
+    } else {
+        p.piece = piece((uint64_t)n * p.padded * p.es);
+        p.piece = even(copied < p.piece ? copied : p.piece, factor * p.blocks, factor * loss_ceil(c->rows, p.whole));
+        const uint64_t widest = p.piece < c->vocab ? p.piece : c->vocab;
+        p.kind = loss_kind(p.es == 2, c->rows, widest);
+        // Few tiles: several workgroups share the sums of one over the vocabulary (Shares), as many as the device holds at once.  Then large tiles are as good
+        // where there are few, but for what hangs over the edges (2048 x 1600, of which 1448 tokens count, x 50257: 365 us in tiles of 128 x 128, 245 in 256 x 256).
+        const uint64_t stages = loss_ceil(widest, p.whole), large = loss_tiles(kLossLarge, c->rows, c->cols), middle = loss_tiles(kLossMiddle, c->rows, c->cols);
+        p.x_kind = c->rows <= 32 ? kLossFew : p.es == 2 && 3 * large <= middle && large * stages >= 256 * 16 ? kLossLarge : kLossMiddle;
+        p.x_stages = (uint32_t)stages;
+        p.x_slots = p.x_kind == kLossLarge ? 256 : 512;
+        const uint64_t tiles = loss_tiles(p.x_kind, c->rows, c->cols);
+        p.x_groups = tiles > p.x_slots ? tiles : p.x_slots;
+        p.g_plane = (uint64_t)p.padded * stages * 64;
+        p.grads = place(n * p.g_plane);
+        p.sums = place(p.x_groups * kLossTiles[p.x_kind].tm * kLossTiles[p.x_kind].tn * 4);
+    }
+    p.weight = place(p.copy ? (uint64_t)n * p.piece * p.blocks * 64 : 0);
+    p.total = at;
     return p;
 }
 

@@ -24,7 +24,27 @@ struct Operand {
     uint64_t ld;               // bytes: row-major from row to row, blocks from block to block
     uint32_t rows;             // that may be read in memory
     uint32_t blocks;           // kBlocksTurned: that may be read
+    uint64_t plane;            // bytes from plane to plane
 };
+
+// fp32 in planes: x = x1 + x2 + x3, bf16 each, every one what is left rounded to nearest; exact, as 8 bits, and twice 8 bits and a sign, are 24 and more.  Of the
+// nine products of two such sums six are taken, x1 y1, x1 y2, x1 y3, x2 y1, x2 y2, x3 y1; the others are below 2^-25 of |x y| together.  They are summed in
+// fp32 like the columns of one product six times as long: stage 6 k + i has columns 32 k on of the i-th of these.
+__device__ __forceinline__ uint32_t plane_of_a(uint32_t i) { return i < 3 ? 0 : i < 5 ? 1 : 2; }
+__device__ __forceinline__ uint32_t plane_of_b(uint32_t i) { return i < 3 ? i : i < 5 ? i - 3 : 0; }
+__device__ __forceinline__ void split_planes(const float (&x)[8], uint4 (&planes)[3])
+{
+    float left[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) left[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        const uint32_t w[4] = {two_bf16(left[0], left[1]), two_bf16(left[2], left[3]), two_bf16(left[4], left[5]), two_bf16(left[6], left[7])};
+        planes[p] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) left[i] -= __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+}
 
 // The tile of a workgroup: WM * MF units of 32 rows of A by WN * NF units of B; its four wavefronts take MF x NF units each.  A stage is
 // 64 bytes of every row (32 columns of bf16, 16 of fp32); four of them are in LDS, one in use, three on their way (loads straight to LDS), of
@@ -176,12 +196,14 @@ struct Feed {
     }
 };
 
-// Stages `from` .. `from + count - 1` of the product of tile (tm, tn); count >= 1.  A lies in blocks.  B's rows of k behind its last one, kTurned, are the
+// Stages `from` .. `from + count - 1` of the product of tile (tm, tn); count >= 1.  PLANES 3: each for six, of operands in planes.  A lies in blocks.  B's rows of k behind its last one, kTurned, are the
 // last one again (A's columns there are zeros).
-template <class T, bool BF16, Lies LIES_A, Lies LIES_B>
-__device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &ob, uint32_t tm, uint32_t tn, uint32_t from, uint32_t count, const Stages &stages,
+template <class T, bool BF16, int PLANES, Lies LIES_A, Lies LIES_B>
+__device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &ob, uint32_t tm, uint32_t tn, uint32_t from, uint32_t columns, const Stages &stages,
                                               TileResult<T> &result)
 {
+    static_assert(PLANES == 1 || (BF16 && (LIES_B == kBlocks || LIES_B == kBlocksTurned)), "planes lie in blocks");
+    const uint32_t count = PLANES == 3 ? 6 * columns : columns;
     static_assert(LIES_A == kBlocks || LIES_A == kBlocksTurned, "a line at a time, a stage at a time");
     constexpr int NB = 4, EACH = T::EACH, MF = T::MF, NF = T::NF, PERIOD = LIES_B == kRows ? 12 : NB;
     const uint32_t wave = uniform(threadIdx.x / 64);
@@ -218,6 +240,10 @@ __device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &
     auto batch_of = [&](auto at, uint32_t s) -> Batch {
         constexpr int ODD = (decltype(at)::value + PERIOD) % 2;
         const uint32_t stage = min(s + NB, count - 1), stage_b = LIES_B == kRows ? min((s + NB + ODD) / 2, (count - 1) / 2) : stage;
+        if constexpr (PLANES == 3) {
+            const uint32_t k = stage / 6, i = stage % 6;
+            return {a.at + k * a.step + plane_of_a(i) * oa.plane, b.at + k * b.step + plane_of_b(i) * ob.plane, 0u};
+        }
         return {a.at + stage * a.step, b.at + stage_b * b.step, stage_b == last_b ? ~0u : 0u};
     };
     auto issue = [&](auto at, const Batch &from_here, int j) {

@@ -114,7 +114,9 @@ def test_large(rows, cols, vocab):
     _check(rows, cols, vocab, "bf16")
 
 
-@pytest.mark.parametrize("rows, cols, vocab", [(1030, 260, 4099), (4100, 30, 17001)])
+# fp32 as three planes of bf16, in every kind of tile: of logits, of both gradients; in one direction alone; several pieces of the vocabulary
+@pytest.mark.parametrize("rows, cols, vocab", [(1030, 260, 4099), (4100, 30, 17001), (700, 64, 33003), (1030, 2056, 4099), (300, 4104, 4200), (230, 48, 777), (640, 33, 500),
+                                               (161, 31, 300), (6200, 16, 30001)])
 def test_large_f32(rows, cols, vocab):
     _check(rows, cols, vocab, "f32")
 
@@ -135,6 +137,11 @@ def test_weight_gradient_is_added_to(kind, wide):
 @pytest.mark.parametrize("x_wanted, w_wanted", [(True, False), (False, True)])
 def test_one_gradient_alone(x_wanted, w_wanted):
     _check(70, 72, 300, "bf16", x_wanted=x_wanted, w_wanted=w_wanted)
+
+
+def test_shares_of_several_pieces():
+    """Few tiles whose sums over the vocabulary are shared by many workgroups, over two pieces of it of unlike length."""
+    _check(544, 33, 246528 + 65600, "bf16")
 
 
 def test_statistics_of_several_pieces():
