@@ -77,11 +77,11 @@ uint32_t groups_of(const HeadShape &s, int which)
     const uint32_t each = 64 / s.lanes;
     return (s.heads[which] + each - 1) / each;
 }
-// workgroups that give every wavefront one token, or one group
+// workgroups that give every wavefront one token, or one group, but so few that queries' and keys' together are a launch of less than 2^32 lanes
 uint32_t workgroups_of(const HeadShape &s, uint32_t groups)
 {
     const uint64_t all = ((uint64_t)s.tokens * (s.split ? groups : 1) + kHeadWaves - 1) / kHeadWaves;
-    return (uint32_t)(all < (1u << 23) ? all : 1u << 23);
+    return (uint32_t)(all < (1u << 22) ? all : 1u << 22);
 }
 
 // Workgroups of the backward pass, queries' and keys'.  With norms each leaves a part of a weight's gradient, so there are no more than are at work at

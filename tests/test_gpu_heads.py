@@ -209,3 +209,30 @@ def test_slots_streams_and_graphs():
         assert all(torch.equal(a, b) for a, b in zip(out, run(heads)))
         want = back(heads)
         assert all(torch.equal(grads[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("norm", (0, 1))
+def test_more_tokens_than_a_launch_has_wavefronts(norm):
+    """Queries' and keys' workgroups together stay a launch that the runtime takes; every token has what it has in a call of a few."""
+    tokens, few, place = (1 << 25) + 5, 1003, {"norm": norm}
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k = (torch.randn(tokens, 1, 2, generator=g, device="cuda").bfloat16() for _ in range(2))
+    w = torch.ones(8, dtype=torch.bfloat16, device="cuda")[:2] if norm else None
+    positions, frequencies = torch.arange(tokens, device="cuda") * 12345, _frequencies(2, "plain", 1.0)[0]
+
+    def results(n, of):
+        cfg = tahq.make_heads_config(n, 1, 1, 2, 2, tahq.BF16, **place)
+        x, y, at = of(q).contiguous(), of(k).contiguous(), of(positions).contiguous()
+        out = [torch.full((n + 2, 1, 2), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+        tahq.tahq_heads_forward(cfg, x, y, w, w, at, frequencies, out[0][:n], out[1][:n])
+        sums = [torch.empty(4, device="cuda") for _ in range(2)] if norm else (None, None)
+        workspace = torch.empty(max(tahq.tahq_heads_workspace_size(cfg), 16), dtype=torch.uint8, device="cuda")
+        tahq.tahq_heads_backward(cfg, y, x, x if norm else None, y if norm else None, w, w, at, frequencies, out[2][:n], out[3][:n], *sums, workspace)
+        torch.cuda.synchronize()
+        assert all((t[n:] == 7).all() for t in out)
+        return [t[:n] for t in out]
+
+    all_of = results(tokens, lambda t: t)
+    for at in (0, (1 << 24) - 500, tokens - few):
+        for a, b in zip(all_of, results(few, lambda t: t[at:at + few])):
+            assert torch.equal(a[at:at + few], b)
