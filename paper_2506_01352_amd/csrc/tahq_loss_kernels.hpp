@@ -240,11 +240,10 @@ void k_loss_logits(LogitArgs g)
                 asm volatile("" : "+v"(m));
                 const bool there = m < count;
                 const uint32_t row = there ? g.tokens.rows[m] : 0, target = there ? g.tokens.targets[m] : kBadTarget;
-                // tokens that there are not have logits of 0 and probabilities of 0
-                const float shift = there ? -g.lse[row] * kLog2e : -INFINITY;
+                const float shift = there ? -g.lse[row] * kLog2e : 0.0f;
                 float factor = there && g.grad_loss ? g.grad_loss[row] : 1.0f;
                 if (there && target == kBadTarget) factor = NAN;
-                const bool here = target - n0 < (uint32_t)NF * 32, any = __ballot(here) != 0;
+                const bool here = target - n0 < (uint32_t)NF * 32, any = __ballot(here) != 0, behind = __ballot(!there) != 0;
 #pragma unroll
                 for (int j = 0; j < NF; ++j) {
                     __builtin_amdgcn_sched_barrier(0);
@@ -261,6 +260,10 @@ void k_loss_logits(LogitArgs g)
                     }
 #pragma unroll
                     for (int k = 0; k < 16; ++k) d[k] *= factor;
+                    if (behind) {                            // the last token; these rows' logits may be NaN, as products of zeros and infinite weights
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) d[k] = there ? d[k] : 0.0f;
+                    }
                     // of the vocabulary's last block all columns: zeros behind its end
                     const uint32_t n = n0 - g.first + 32 * j;                // in the piece
                     if constexpr (BF16) {

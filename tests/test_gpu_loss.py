@@ -216,6 +216,21 @@ def test_infinite_and_large_logits(kind):
     assert loss.losses[nan].isnan().all() and loss.losses[~nan].isfinite().all()
 
 
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+@pytest.mark.parametrize("counted", (0, 1, 5))
+def test_infinite_weights_and_rows_that_are_no_tokens(kind, counted):
+    """Products with a row of -infinity are -infinity or, of zeros, NaN: where fewer tokens count than a stage has rows, what fills it up adds nothing
+    to the weight's gradient, that row's neither."""
+    x, weight, target, _ = _make(40, 64, 300, kind, 0.0)
+    weight[7] = float("-inf")
+    x, target = x.abs() + 0.5, torch.where(target == 7, 8, target)
+    target[counted:] = IGNORE
+    loss = tahq.LinearLoss(tahq.make_loss_config(40, 64, 300, KINDS[kind][0], reduction=tahq.LOSS_SUM))
+    loss.forward(x, weight, target)
+    _, grad_w = loss.backward(x, weight, target)
+    assert grad_w.isfinite().all() and (grad_w[7] == 0).all() and (counted == 0) == bool((grad_w == 0).all())
+
+
 def test_class_slots_streams_and_refusals():
     rows, cols, vocab = 70, 64, 300
     loss = tahq.LinearLoss(tahq.make_loss_config(rows, cols, vocab, tahq.BF16), in_flight=2)
