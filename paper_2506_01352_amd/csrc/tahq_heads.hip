@@ -68,8 +68,10 @@ uint32_t lanes_of(const tahq_heads_config *c, bool wide)
     return lanes;
 }
 
-// Where tokens alone would leave vector units idle, each of a token's groups of heads has a wavefront of its own.
-constexpr uint32_t kSplitBelow = 4096;
+// Where tokens alone would leave vector units idle, each of a token's groups of heads has a wavefront of its own, which works out the token's angles again.
+// bf16, 40 + 8 heads of 128: 512 tokens split 6.8 us forward and 12.6 backward, not split 8.1 and 13.5; 1024 8.4 and 15.4, 8.6 and 14.2; 2048 13.0 and 21.4, 11.7
+// and 18.1; 4096 22.2 and 32.3, 18.5 and 26.6.
+constexpr uint32_t kSplitBelow = 1024;
 
 // groups of queries' (0) and of keys' heads (1) that a wavefront takes side by side
 uint32_t groups_of(const HeadShape &s, int which)

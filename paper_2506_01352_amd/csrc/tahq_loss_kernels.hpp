@@ -164,7 +164,7 @@ struct LogitArgs {
     uint32_t tiles_n;
     float2 *parts;                           // forward: (largest logit, sum of exp(l - it)), [part][padded tokens]
     float *at_target;                        // logits of the targets
-    uint32_t part, padded;                   // number of the piece's first part
+    uint32_t padded;
     const float *lse, *grad_loss;            // backward; grad_loss: of every token, or NULL
     uint8_t *grads;                          // p - [v = t] of the piece, in blocks
 };
@@ -225,7 +225,7 @@ void k_loss_logits(LogitArgs g)
                     for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(l[j][k], kLog2e, shift));
                 float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 all += __shfl_xor(all, 32);
-                if (half == 0 && m < count) g.parts[(uint64_t)(g.part + tn * WN + wave % WN) * g.padded + m] = make_float2(top, all);
+                if (half == 0 && m < count) g.parts[(uint64_t)(tn * WN + wave % WN) * g.padded + m] = make_float2(top, all);
             }
         };
         if (n0 + NF * 32 > g.vocab) stats(std::true_type{});

@@ -106,7 +106,7 @@ def test_small(rows, cols, vocab, kind, reduction):
 # what takes the largest tiles: of logits, of the hidden states' gradient, of the weight's, with rows of whole stages (an odd number of them) and without;
 # several pieces of the vocabulary backward, with the last one ragged; shared sums over the vocabulary; more tokens than one workgroup counts
 LARGE = [(300, 40, 33003), (4100, 4100, 70), (40, 4104, 4200), (4100, 40, 40001), (257, 512, 9000), (9000, 24, 300), (1030, 2056, 4099), (300, 96, 33003), (1030, 2080, 4099),
-         (4100, 64, 40001), (40, 4128, 4201)]
+         (4100, 64, 40001), (40, 4128, 4201), (500, 40, 32601), (500, 96, 32601)]
 
 
 @pytest.mark.parametrize("rows, cols, vocab", LARGE)

@@ -117,7 +117,7 @@ def test_which_tiles_the_gpu_tests_take(plan):
         f, b = plan(0, *s, dtype), plan(1, *s, dtype)
         return f["kind"], b["kind"], b["x_kind"]
 
-    assert kinds(5, 32, 127) == (2, 2, 2) and kinds(130, 1600, 257) == (1, 1, 1) and kinds(300, 40, 33003) == (0, 0, 1) and kinds(257, 512, 9000)[2] == 1
+    assert kinds(5, 32, 127) == (2, 2, 2) and kinds(130, 1600, 257) == (1, 1, 1) and kinds(500, 40, 32601) == kinds(500, 96, 32601) == (0, 0, 1) and kinds(257, 512, 9000)[2] == 1
     assert kinds(1030, 2056, 4099)[2] == kinds(1030, 2080, 4099)[2] == 0 and kinds(2048, 1600, 50257) == (0, 0, 0)
     assert plan(1, 4100, 40, 40001, tahq.BF16)["piece"] < 40001 and plan(0, 65536, 8, 70001, tahq.BF16)["piece"] < 70001
     assert plan(0, 300, 64, 5003, tahq.F32)["copy"] == 0 and plan(0, 300, 40, 33003, tahq.BF16)["copy"] == 1
