@@ -47,22 +47,18 @@ HeadShape shape_of(const tahq_heads_config *c)
     return s;
 }
 
-// Whether heads go by chunks of 16 bytes: halves of whole chunks, or rotated channels of whole chunks, and everything aligned.
-bool wide(const tahq_heads_config *c, const HeadShape &s, std::initializer_list<const void *> tensors)
+// Channels of a chunk: the most, up to 16 bytes, that halves, or pairs, are whole ones of; 1 where there are none.  Alignment does not matter for that.
+int chunk_of(const tahq_heads_config *c)
 {
-    const uint32_t chunk = 16 / esize(c);
-    if (c->head % chunk || c->rotated % (c->layout == TAHQ_HEADS_PAIRS ? chunk : 2 * chunk)) return false;
-    for (int i = 0; i < (c->k_heads ? 2 : 1); ++i)
-        if (s.ld[i] % chunk || s.ld_out[i] % chunk) return false;
-    for (const void *p : tensors)
-        if (misaligned(p)) return false;
-    return true;
+    for (uint32_t chunk = 16 / esize(c); chunk > 1; chunk /= 2)
+        if (c->head % chunk == 0 && c->rotated % (c->layout == TAHQ_HEADS_PAIRS ? chunk : 2 * chunk) == 0 && c->head <= 128 * chunk) return (int)chunk;
+    return 1;
 }
 
 // lanes to a head: two chunks, or four pairs, to each
-uint32_t lanes_of(const tahq_heads_config *c, bool wide)
+uint32_t lanes_of(const tahq_heads_config *c, uint32_t chunk)
 {
-    const uint32_t chunk = 16 / esize(c), need = wide ? (c->head / chunk + 1) / 2 : ((c->head + 1) / 2 + 3) / 4;
+    const uint32_t need = chunk > 1 ? (c->head / chunk + 1) / 2 : ((c->head + 1) / 2 + 3) / 4;
     uint32_t lanes = 1;
     while (lanes < need) lanes *= 2;
     return lanes;
@@ -73,35 +69,41 @@ uint32_t lanes_of(const tahq_heads_config *c, bool wide)
 // and 18.1; 4096 22.2 and 32.3, 18.5 and 26.6.
 constexpr uint32_t kSplitBelow = 1024;
 
-// groups of queries' (0) and of keys' heads (1) that a wavefront takes side by side
-uint32_t groups_of(const HeadShape &s, int which)
+// groups of `heads` heads that a wavefront takes side by side
+uint32_t groups_of(const HeadShape &s, uint32_t heads)
 {
     const uint32_t each = 64 / s.lanes;
-    return (s.heads[which] + each - 1) / each;
+    return (heads + each - 1) / each;
 }
-// workgroups that give every wavefront one token, or one group, but so few that queries' and keys' together are a launch of less than 2^32 lanes
-uint32_t workgroups_of(const HeadShape &s, uint32_t groups)
+// tokens whose heads a wavefront takes side by side
+uint32_t side_of(const HeadShape &s, uint32_t heads) { return 64 / s.lanes / heads > 1 ? 64 / s.lanes / heads : 1; }
+// workgroups that give every wavefront one token, or one group, or a group of several tokens, but so few that queries' and keys' together are a launch
+// of less than 2^32 lanes
+uint32_t workgroups_of(const HeadShape &s, uint32_t heads)
 {
-    const uint64_t all = ((uint64_t)s.tokens * (s.split ? groups : 1) + kHeadWaves - 1) / kHeadWaves;
+    if (heads == 0) return 0;
+    const uint32_t side = side_of(s, heads), groups = groups_of(s, heads);
+    const uint64_t all = (((uint64_t)s.tokens + side - 1) / side * (s.split ? groups : 1) + kHeadWaves - 1) / kHeadWaves;
     return (uint32_t)(all < (1u << 22) ? all : 1u << 22);
 }
 
 // Workgroups of the backward pass, queries' and keys'.  With norms each leaves a part of a weight's gradient, so there are no more than are at work at
-// once: three to a compute unit of bf16 in chunks of 16 bytes, which has up to 144 registers (32768 x 48 x 128: 768 workgroups 250 us, 1024 311, and with 128
-// registers, some of them in memory, 367), five of the others with up to 105 (fp32 2331 x 25 x 80: 768 17.6 us, 1280 16.1).
-// They are shared as the work is, a token's angles counting as a group.
+// once (bf16 32768 x 48 x 128, three to a compute unit: 768 245 us, 1024 311; fp32 2331 x 25 x 80, five: 768 17.6 us, 1024 16.4, 1280 16.1; bf16 7432 x 40 x 58,
+// four: 1024 72 us, 1280 85).  They are shared as the work is, a token's angles counting as a group.
 constexpr uint32_t kBackwardMost = 1280;
 struct BackwardGroups {
     uint32_t queries, keys;
 };
-BackwardGroups backward_groups(const tahq_heads_config *c, const HeadShape &s, bool by_chunks)
+BackwardGroups backward_groups(const tahq_heads_config *c, const HeadShape &s, int chunk)
 {
-    const uint32_t at_once = by_chunks && c->dtype == TAHQ_BF16 ? 768 : kBackwardMost;
-    const uint32_t gq = groups_of(s, 0), gk = groups_of(s, 1);
-    BackwardGroups g = {workgroups_of(s, gq), gk ? workgroups_of(s, gk) : 0};
+    const uint32_t at_once = 256 * backward_per_cu(c->dtype == TAHQ_BF16, chunk, c->layout == TAHQ_HEADS_PAIRS);
+    const uint32_t gq = groups_of(s, c->q_heads), gk = groups_of(s, c->k_heads);
+    BackwardGroups g = {workgroups_of(s, c->q_heads), workgroups_of(s, c->k_heads)};
     if (!c->norm || g.queries + g.keys <= at_once) return g;
-    const uint32_t angles = s.split ? 0 : 1, all = gq + gk + 2 * angles;
-    const uint32_t keys = gk ? (at_once * (gk + angles) + all / 2) / all : 0;
+    // of a token, in fractions of a group where a group has several tokens
+    auto work = [&](uint32_t heads, uint32_t groups) { return heads ? (groups + (s.split ? 0.0 : 1.0)) / side_of(s, heads) : 0.0; };
+    const double wq = work(c->q_heads, gq), wk = work(c->k_heads, gk);
+    const uint32_t keys = (uint32_t)(at_once * wk / (wq + wk) + 0.5);
     const uint32_t least = keys < 1 && gk ? 1 : keys, most = least < at_once ? least : at_once - 1;
     if (g.keys > most) g.keys = most;
     if (g.queries > at_once - g.keys) g.queries = at_once - g.keys;
@@ -110,7 +112,7 @@ BackwardGroups backward_groups(const tahq_heads_config *c, const HeadShape &s, b
 
 // what a configuration's kernel is compiled for
 template <typename Run>
-void with_kind(const tahq_heads_config *c, bool wide, Run run)
+void with_kind(const tahq_heads_config *c, int chunk, Run run)
 {
     auto norm = [&](auto b, auto w, auto p) {
         if (c->norm) run(b, w, p, std::true_type{});
@@ -121,11 +123,13 @@ void with_kind(const tahq_heads_config *c, bool wide, Run run)
         else norm(b, w, std::false_type{});
     };
     auto by = [&](auto b) {
-        if (wide) pairs(b, std::true_type{});
-        else pairs(b, std::false_type{});
+        if (chunk == 4) pairs(b, std::integral_constant<int, 4>{});
+        else if (chunk == 2) pairs(b, std::integral_constant<int, 2>{});
+        else pairs(b, std::integral_constant<int, 1>{});
     };
-    if (c->dtype == TAHQ_BF16) by(std::true_type{});
-    else by(std::false_type{});
+    if (c->dtype != TAHQ_BF16) by(std::false_type{});
+    else if (chunk == 8) pairs(std::true_type{}, std::integral_constant<int, 8>{});
+    else by(std::true_type{});
 }
 
 // Elements' alignment for queries, keys and their like and for positions, 16 bytes for the rest
@@ -216,12 +220,12 @@ tahq_status tahq_heads_forward(const tahq_heads_config *cfg, const void *d_q, co
     if (rc != TAHQ_OK) return rc;
     if (misplaced(cfg, d_positions, {d_q, d_k, d_q_out, d_k_out}, {d_w_q, d_w_k, d_frequencies})) return TAHQ_ERR_MISALIGNED;
     HeadShape s = shape_of(cfg);
-    const bool by_chunks = wide(cfg, s, {d_q, d_k, d_q_out, d_k_out});
-    s.lanes = lanes_of(cfg, by_chunks);
+    const int chunk = chunk_of(cfg);
+    s.lanes = lanes_of(cfg, chunk);
     s.split = cfg->tokens < kSplitBelow;
     Enqueue q{(hipStream_t)stream};
-    with_kind(cfg, by_chunks, [&](auto bf16, auto w, auto pairs, auto normed) {
-        q(k_heads_forward<bf16, w, pairs, normed>, dim3(workgroups_of(s, groups_of(s, 0) + groups_of(s, 1))), dim3(64 * kHeadWaves), HeadTensors{{d_q, d_k}}, HeadTensors{{d_w_q, d_w_k}}, d_positions,
+    with_kind(cfg, chunk, [&](auto bf16, auto w, auto pairs, auto normed) {
+        q(k_heads_forward<bf16, w, pairs, normed>, dim3(workgroups_of(s, cfg->q_heads + cfg->k_heads)), dim3(64 * kHeadWaves), HeadTensors{{d_q, d_k}}, HeadTensors{{d_w_q, d_w_k}}, d_positions,
           d_frequencies, HeadOutputs{{d_q_out, d_k_out}}, s);
     });
     return q.result();
@@ -249,13 +253,13 @@ tahq_status tahq_heads_backward(const tahq_heads_config *cfg, const void *d_grad
                   {d_w_q, d_w_k, d_frequencies, d_grad_w_q, d_grad_w_k, norm ? d_workspace : nullptr}))
         return TAHQ_ERR_MISALIGNED;
     HeadShape s = shape_of(cfg);
-    const bool by_chunks = wide(cfg, s, {d_grad_q_out, d_grad_k_out, d_q, d_k, d_grad_q, d_grad_k});
-    s.lanes = lanes_of(cfg, by_chunks);
+    const int chunk = chunk_of(cfg);
+    s.lanes = lanes_of(cfg, chunk);
     s.split = cfg->tokens < kSplitBelow;
-    const BackwardGroups g = backward_groups(cfg, s, by_chunks);
+    const BackwardGroups g = backward_groups(cfg, s, chunk);
     float *parts = static_cast<float *>(d_workspace);
     Enqueue q{(hipStream_t)stream};
-    with_kind(cfg, by_chunks, [&](auto bf16, auto w, auto pairs, auto normed) {
+    with_kind(cfg, chunk, [&](auto bf16, auto w, auto pairs, auto normed) {
         q(k_heads_backward<bf16, w, pairs, normed>, dim3(g.queries + g.keys), dim3(64 * kHeadWaves), HeadTensors{{d_grad_q_out, d_grad_k_out}}, HeadTensors{{d_q, d_k}},
           HeadTensors{{d_w_q, d_w_k}}, d_positions, d_frequencies, HeadOutputs{{d_grad_q, d_grad_k}}, parts, g.queries, s);
     });

@@ -39,11 +39,12 @@ __device__ __forceinline__ void cos_sin(uint32_t turn, float &c, float &s)
     s = quarter & 2 ? -s : s;
 }
 
-// The channels that a lane holds of every head: E pairs.  WIDE: two chunks of 16 bytes, at channels `at[0]` and `at[1]`; otherwise pair by pair,
-// whatever the sizes and strides.
-template <bool BF16, bool WIDE, bool PAIRS>
+// The channels that a lane holds of every head: E pairs.  CHUNK > 1: two chunks of so many channels, at channels `at[0]` and `at[1]`; otherwise pair by pair,
+// whatever the sizes.
+template <bool BF16, int CHUNK, bool PAIRS>
 struct HeadLane {
-    static constexpr int E = WIDE && BF16 ? 8 : 4;
+    static constexpr bool WIDE = CHUNK > 1;
+    static constexpr int E = WIDE ? CHUNK : 4, ES = BF16 ? 2 : 4, WORDS = CHUNK * ES / 4;
     uint32_t u, at[2];
     bool there[2];
     __device__ __forceinline__ HeadLane(const HeadShape &s) : u(threadIdx.x % s.lanes), at{0, 0}, there{false, false}
@@ -78,17 +79,17 @@ struct HeadLane {
     }
     // A head's channels as they lie in memory, and as numbers: pair i is a[i], b[i]; zeros for what there is not
     struct Raw {
-        uint4 q[2];
+        uint32_t q[2][WIDE ? WORDS : 1];
         float x[WIDE ? 1 : 2 * E];
     };
     __device__ __forceinline__ Raw load(const HeadShape &s, const void *base, uint64_t from, bool mine) const
     {
         Raw r = {};
         if constexpr (WIDE) {
-            const uint8_t *p = static_cast<const uint8_t *>(base) + from * (16 / E);
+            const uint8_t *p = static_cast<const uint8_t *>(base) + from * ES;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-                if (mine && there[k]) r.q[k] = *reinterpret_cast<const uint4 *>(p + at[k] * (16 / E));
+                if (mine && there[k]) __builtin_memcpy(r.q[k], p + at[k] * ES, sizeof r.q[k]);
         } else {
 #pragma unroll
             for (int i = 0; i < 2 * E; ++i) {
@@ -104,9 +105,8 @@ struct HeadLane {
             float x[2][E];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const uint32_t w[4] = {r.q[k].x, r.q[k].y, r.q[k].z, r.q[k].w};
 #pragma unroll
-                for (int i = 0; i < E; ++i) x[k][i] = __uint_as_float(!BF16 ? w[i % 4] : i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+                for (int i = 0; i < E; ++i) x[k][i] = __uint_as_float(!BF16 ? r.q[k][i % WORDS] : i % 2 ? r.q[k][i / 2] & 0xffff0000u : r.q[k][i / 2] << 16);
             }
 #pragma unroll
             for (int i = 0; i < E; ++i) {
@@ -135,13 +135,13 @@ struct HeadLane {
                     x[1][i] = b[i];
                 }
             }
-            uint8_t *p = static_cast<uint8_t *>(base) + from * (16 / E);
+            uint8_t *p = static_cast<uint8_t *>(base) + from * ES;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                uint32_t w[4];
+                uint32_t w[WORDS];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = BF16 ? two_bf16(x[k][2 * i % E], x[k][(2 * i + 1) % E]) : __float_as_uint(x[k][i]);
-                if (mine && there[k]) *reinterpret_cast<uint4 *>(p + at[k] * (16 / E)) = make_uint4(w[0], w[1], w[2], w[3]);
+                for (int i = 0; i < WORDS; ++i) w[i] = BF16 ? two_bf16(x[k][2 * i % E], x[k][(2 * i + 1) % E]) : __float_as_uint(x[k][i]);
+                if (mine && there[k]) __builtin_memcpy(p + at[k] * ES, w, sizeof w);
             }
         } else {
 #pragma unroll
@@ -151,15 +151,20 @@ struct HeadLane {
             }
         }
     }
-    __device__ __forceinline__ void angles(const HeadShape &s, const int64_t *positions, const uint64_t *frequencies, uint32_t token, float (&c)[E], float (&n)[E]) const
+    // of its pairs, 0 of those that are not turned
+    __device__ __forceinline__ void ask_frequencies(const HeadShape &s, const uint64_t *frequencies, uint64_t (&f)[E]) const
     {
-        const uint64_t position = s.rotated ? (uint64_t)positions[token] : 0;
-        uint64_t f[E] = {};
         // WIDE: runs of pairs are turned as a whole or not at all, and are asked for as a whole
         constexpr int RUN = !WIDE ? 1 : PAIRS ? E / 2 : E;
 #pragma unroll
-        for (int i = 0; i < E; i += RUN)
+        for (int i = 0; i < E; i += RUN) {
+#pragma unroll
+            for (int k = 0; k < RUN; ++k) f[i + k] = 0;
             if (turned(s, i)) __builtin_memcpy(f + i, frequencies + pair(s, i), RUN * sizeof *f);
+        }
+    }
+    __device__ __forceinline__ void angles(const HeadShape &s, uint64_t position, const uint64_t (&f)[E], float (&c)[E], float (&n)[E]) const
+    {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             cos_sin((uint32_t)((position * f[i] + 0x80000000u) >> 32), c[i], n[i]);
@@ -181,65 +186,77 @@ __device__ __forceinline__ float head_sum(float v, uint32_t lanes)
     return v;
 }
 
-// A wavefront's way through tokens and groups of heads: every splits-th group of a token, then the token that all wavefronts are further.  Forward groups
-// of queries, then of keys; backward (`only`) of one of them.
+// A wavefront's way through tokens and groups of `heads` heads: every splits-th group of a token, then the token that all wavefronts are further.  Where
+// a group has room for all heads of several tokens, it takes those; `at` is where the lane is, token and head.
 struct HeadWay {
-    uint32_t each, groups_q, groups, splits, split, step_split;
-    uint64_t token, step_token;
+    uint32_t heads, tokens, groups, splits, split, step_split, each, mine, side;
+    uint64_t first, step_first;              // of `side` tokens
     uint32_t group;
-    __device__ __forceinline__ HeadWay(const HeadShape &s, int only, uint32_t waves, uint32_t wave)
+    __device__ __forceinline__ HeadWay(const HeadShape &s, uint32_t heads_, uint32_t waves, uint32_t wave) : heads(heads_), tokens(s.tokens)
     {
         each = 64 / s.lanes;
-        const uint32_t groups_k = (s.heads[1] + each - 1) / each;
-        groups_q = (s.heads[0] + each - 1) / each;
-        groups = only < 0 ? groups_q + groups_k : only ? groups_k : groups_q;
-        splits = max(s.split ? groups : 1u, 1u);
-        token = wave / splits;
+        groups = (heads + each - 1) / each;
+        side = max(each / heads, 1u);
+        splits = s.split ? groups : 1u;
+        first = (uint64_t)(wave / splits) * side;
         group = split = wave % splits;
-        step_token = waves / splits;
+        step_first = (uint64_t)(waves / splits) * side;
         step_split = waves % splits;
+        const uint32_t place = threadIdx.x % 64 / s.lanes, off = place / heads;
+        // the token that it is further in a group of several, and its head; behind the last token of a group: no token at all
+        mine = side > 1 ? place - off * heads : place;
+        ahead = side == 1 ? 0 : off < side ? off : ~0u;
     }
+    uint32_t ahead;
+    __device__ __forceinline__ bool more() const { return first < tokens; }
+    __device__ __forceinline__ uint64_t token() const { return first + ahead; }
+    __device__ __forceinline__ uint32_t head() const { return group * each + mine; }
+    __device__ __forceinline__ bool valid() const { return head() < heads && token() < tokens; }
+    __device__ __forceinline__ uint64_t position(const int64_t *positions) const { return (uint64_t)positions[min(token(), (uint64_t)tokens - 1)]; }
     // to the next group; whether it is another token's
     __device__ __forceinline__ bool next()
     {
         group += splits;
         if (group < groups) return false;
-        token += step_token;
+        first += step_first;
         split += step_split;
         if (split >= splits) {
             split -= splits;
-            ++token;
+            first += side;
         }
         group = split;
         return true;
     }
 };
 
-template <bool BF16, bool WIDE, bool PAIRS, bool NORM>
+// Queries and keys are one row of heads.
+template <bool BF16, int CHUNK, bool PAIRS, bool NORM>
 __global__ __launch_bounds__(64 * kHeadWaves)
 void k_heads_forward(HeadTensors in, HeadTensors weights, const int64_t *positions, const uint64_t *frequencies, HeadOutputs out, HeadShape s)
 {
-    using Lane = HeadLane<BF16, WIDE, PAIRS>;
+    using Lane = HeadLane<BF16, CHUNK, PAIRS>;
     constexpr int E = Lane::E;
     const Lane lane(s);
-    const uint32_t mine = threadIdx.x % 64 / s.lanes;
-    HeadWay way(s, -1, gridDim.x * kHeadWaves, blockIdx.x * kHeadWaves + uniform(threadIdx.x / 64));
+    HeadWay way(s, s.heads[0] + s.heads[1], gridDim.x * kHeadWaves, blockIdx.x * kHeadWaves + uniform(threadIdx.x / 64));
     const float inv = 1.0f / (float)s.head;
     float c[E], n[E];
     bool another = true;
-    while (way.token < s.tokens) {
-        const int which = way.group < way.groups_q ? 0 : 1;
-        const uint32_t h = (which ? way.group - way.groups_q : way.group) * way.each + mine;
-        const bool valid = h < s.heads[which];
-        const typename Lane::Raw raw = lane.load(s, in.of[which], way.token * s.ld[which] + (uint64_t)h * s.head, valid);
-        const uint64_t to = way.token * s.ld_out[which] + (uint64_t)h * s.head;
-        if (another) lane.angles(s, positions, frequencies, (uint32_t)way.token, c, n);
+    while (way.more()) {
+        const bool valid = way.valid(), key = way.head() >= s.heads[0];
+        const uint32_t h = key ? way.head() - s.heads[0] : way.head();
+        const typename Lane::Raw raw = lane.load(s, key ? in.of[1] : in.of[0], way.token() * (key ? s.ld[1] : s.ld[0]) + (uint64_t)h * s.head, valid);
+        const uint64_t to = way.token() * (key ? s.ld_out[1] : s.ld_out[0]) + (uint64_t)h * s.head;
+        if (another) {
+            uint64_t f[E];
+            lane.ask_frequencies(s, frequencies, f);
+            lane.angles(s, s.rotated ? way.position(positions) : 0, f, c, n);
+        }
         another = way.next();
         float a[E], b[E];
         lane.unpack(raw, a, b);
         if constexpr (NORM) {
             float wa[E], wb[E], sum = 0.0f;
-            lane.unpack(lane.load(s, weights.of[which], 0, true), wa, wb);
+            lane.unpack(lane.load(s, key ? weights.of[1] : weights.of[0], 0, valid), wa, wb);
 #pragma unroll
             for (int i = 0; i < E; ++i) sum = __builtin_fmaf(b[i], b[i], __builtin_fmaf(a[i], a[i], sum));
             const float rstd = rsqrtf(head_sum(sum, s.lanes) * inv + s.eps);
@@ -255,44 +272,56 @@ void k_heads_forward(HeadTensors in, HeadTensors weights, const int64_t *positio
             a[i] = x * c[i] - y * n[i];
             b[i] = x * n[i] + y * c[i];
         }
-        lane.store(s, out.of[which], to, valid, a, b);
+        lane.store(s, key ? out.of[1] : out.of[0], to, valid, a, b);
     }
 }
+
+// Workgroups of the backward pass that a compute unit's registers hold: 168, 128 or 96 of them to a lane.  (In 96, fp32 pairs and numbers one by one would
+// be in memory: 1507 x 48 x 192 53 us and not 45, 5000 x 25 x 50 47 and not 28.)
+constexpr uint32_t backward_per_cu(bool bf16, int chunk, bool pairs) { return chunk == 8 ? 3 : chunk == 1 || (!bf16 && chunk == 4 && pairs) ? 4 : 5; }
 
 // With u the gradient of the normed head, turned back and times w: dx = rstd (u - n mean(u n)), n = x rstd; w's gradient is the sum of the turned
 // gradient times n over tokens and heads: in a lane's registers, then over the wavefront and the workgroup, which leaves its part in the workspace,
 // [workgroup][head].  The first `queries` workgroups take queries, the others keys, as sums for both would take a quarter of the registers; the next
 // group's numbers are on their way while a group is worked on.
-template <bool BF16, bool WIDE, bool PAIRS, bool NORM>
-__global__ __launch_bounds__(64 * kHeadWaves)
+template <bool BF16, int CHUNK, bool PAIRS, bool NORM>
+__global__ __launch_bounds__(64 * kHeadWaves, backward_per_cu(BF16, CHUNK, PAIRS))
 void k_heads_backward(HeadTensors grads, HeadTensors in, HeadTensors weights, const int64_t *positions, const uint64_t *frequencies, HeadOutputs out, float *parts, uint32_t queries, HeadShape s)
 {
-    using Lane = HeadLane<BF16, WIDE, PAIRS>;
+    using Lane = HeadLane<BF16, CHUNK, PAIRS>;
     constexpr int E = Lane::E;
     __shared__ float sums[NORM ? kHeadWaves : 1][NORM ? TAHQ_HEADS_MAX : 1];
     const Lane lane(s);
-    const uint32_t mine = threadIdx.x % 64 / s.lanes, wave = uniform(threadIdx.x / 64);
+    const uint32_t wave = uniform(threadIdx.x / 64);
     const float inv = 1.0f / (float)s.head;
     const int which = blockIdx.x < queries ? 0 : 1;
-    HeadWay way(s, which, (which ? gridDim.x - queries : queries) * kHeadWaves, (which ? blockIdx.x - queries : blockIdx.x) * kHeadWaves + wave);
+    HeadWay way(s, s.heads[which], (which ? gridDim.x - queries : queries) * kHeadWaves, (which ? blockIdx.x - queries : blockIdx.x) * kHeadWaves + wave);
     float da[E] = {}, db[E] = {}, c[E], n[E];
+    // frequencies stay in registers where that leaves room for as many workgroups
+    constexpr bool HELD = !NORM || CHUNK == 2 || (BF16 && CHUNK == 4);
+    uint64_t f[E], next_position = 0;
+    if constexpr (HELD) lane.ask_frequencies(s, frequencies, f);
     typename Lane::Raw next_grad = {}, next_x = {};
     const typename Lane::Raw weight = NORM ? lane.load(s, weights.of[which], 0, true) : typename Lane::Raw{};
     auto ask = [&] {
-        if (way.token >= s.tokens) return;
-        const uint32_t h = way.group * way.each + mine;
-        next_grad = lane.load(s, grads.of[which], way.token * s.ld_out[which] + (uint64_t)h * s.head, h < s.heads[which]);
-        if constexpr (NORM) next_x = lane.load(s, in.of[which], way.token * s.ld[which] + (uint64_t)h * s.head, h < s.heads[which]);
+        if (!way.more()) return;
+        const uint64_t at = (uint64_t)way.head() * s.head;
+        next_grad = lane.load(s, grads.of[which], way.token() * s.ld_out[which] + at, way.valid());
+        if constexpr (NORM) next_x = lane.load(s, in.of[which], way.token() * s.ld[which] + at, way.valid());
+        if (s.rotated) next_position = way.position(positions);
     };
     ask();
     bool another = true;
-    while (way.token < s.tokens) {
-        const uint32_t h = way.group * way.each + mine;
-        const uint64_t to = way.token * s.ld[which] + (uint64_t)h * s.head;
+    while (way.more()) {
+        const bool valid = way.valid();
+        const uint64_t to = way.token() * s.ld[which] + (uint64_t)way.head() * s.head;
         float a[E], b[E], xa[E], xb[E];
         lane.unpack(next_grad, a, b);
         if constexpr (NORM) lane.unpack(next_x, xa, xb);
-        if (another) lane.angles(s, positions, frequencies, (uint32_t)way.token, c, n);
+        if (another) {
+            if constexpr (!HELD) lane.ask_frequencies(s, frequencies, f);
+            lane.angles(s, next_position, f, c, n);
+        }
         another = way.next();
         ask();
 #pragma unroll
@@ -324,7 +353,7 @@ void k_heads_backward(HeadTensors grads, HeadTensors in, HeadTensors weights, co
                 b[i] = rstd * __builtin_fmaf(-xb[i], mean, b[i]);
             }
         }
-        lane.store(s, out.of[which], to, h < s.heads[which], a, b);
+        lane.store(s, out.of[which], to, valid, a, b);
     }
     if constexpr (NORM) {
 #pragma unroll
@@ -334,7 +363,7 @@ void k_heads_backward(HeadTensors grads, HeadTensors in, HeadTensors weights, co
                 a += __shfl_xor(a, (int)step);
                 b += __shfl_xor(b, (int)step);
             }
-            if (mine == 0) {
+            if (threadIdx.x % 64 < s.lanes) {
                 const uint32_t ca = lane.channel(s, i, 0), cb = lane.channel(s, i, 1);
                 if (ca < s.head) sums[wave][ca] = a;
                 if (cb < s.head) sums[wave][cb] = b;
