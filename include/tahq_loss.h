@@ -9,10 +9,11 @@
  * A token whose target is cfg->ignore does not count: its loss and lse are 0, it adds nothing to any gradient and its own is 0, whatever its
  * hidden state holds, NaN included.  A target outside 0 .. vocab - 1 that is not `ignore` makes the token's loss NaN, and its gradients.
  *
- * Products of bf16 are exact and summed in fp32; softmax statistics and losses are fp32.  Products of fp32 are fp32's or, for many tokens, those of sums of three
- * bf16, off by 2^-25 of their size; infinite hidden states and weights of fp32, and magnitudes from 3.39e38 on, then make NaN of every logit that they are in.  In the backward pass logits are computed again, a piece of
- * the vocabulary at a time, and p_v - [v = t] (times g with LOSS_NONE, otherwise g comes last) is rounded to cfg->dtype for the matrix
- * cores, as a hidden state or weight would be.
+ * Products of bf16 are exact and summed in fp32; softmax statistics and losses are fp32.  Products of fp32 are fp32's or, for many tokens
+ * and rows of the vocabulary, those of sums of three bf16: off by 2^-25 of their size, or, below magnitudes of 2^-100, by 2^-126 of the other
+ * number's; infinite hidden states and weights of fp32, and magnitudes from 3.39e38 on, then make NaN of every logit that they are in.  In the
+ * backward pass logits are computed again, a piece of the vocabulary at a time, and p_v - [v = t] (times g with LOSS_NONE, otherwise g comes
+ * last) is rounded to cfg->dtype for the matrix cores, as a hidden state or weight would be.
  *
  * Tensors are contiguous and row-major: hidden states [rows, cols], weight [vocab, cols].  Conventions as in tahq.h; targets and
  * grad_loss need no more alignment than their elements'.

@@ -113,7 +113,7 @@ struct Call {
     }
     void grad_w(GradWArgs g)
     {
-        const int kind = g.rows <= 32 ? kLossMiddle : loss_kind(p.es == 2, g.rows, g.cols);
+        const int kind = p.es == 2 && loss_large(g.rows, g.cols) ? kLossLarge : kLossMiddle;
         g.tiles_m = (uint32_t)loss_ceil(g.rows, kLossTiles[kind].tm);
         g.tiles_n = (uint32_t)loss_ceil(g.cols, kLossTiles[kind].tn);
         const dim3 grid(g.tiles_m * g.tiles_n), block(256);

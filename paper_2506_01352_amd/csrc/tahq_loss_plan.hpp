@@ -17,9 +17,11 @@ constexpr uint64_t kLossBudget = 256u << 20; // bytes of a piece, where the hidd
 constexpr uint64_t kLossMostRows = 1u << 22; // rows of the vocabulary in a piece
 
 // fp32 is multiplied as such (v_mfma_f32_32x32x2_f32, 110 to 135 TFLOP/s here), or as three bf16 whose sum it is, six products of bf16 for one (at the tiles; 155
-// to 200 TFLOP/s of fp32), for which the weight is copied into planes first.  So many tokens pay for that, 2048 x 32000: forward with rows of no whole stages, which
-// are copied in any case (2047: 100 tokens 273 us and as such 274, 130 324 and 382); forward (260 413 and 386, 400 487 and 501, 1000 738 and 986); backward, where three
-// products share a copy (200 1018 and 1004 with the forward pass, 260 1342 and 1454, 1000 2808 and 3890).
+// to 200 TFLOP/s of fp32), for which the weight is copied into planes first.  So many tokens pay for that, as such and in planes: forward (2048 x 32000: 260 tokens 328 and 402 us, 400
+// 500 and 476), with rows of no whole stages, which are copied in any case (2047: 100 tokens 264 and 263, 200 378 and 329); backward, where three products share a copy (160
+// 637 and 650, 200 743 and 694, 400 1382 and 1136).  And so many tiles of 128 x 128: six products take six times the stages, one after another (400 x 5120 x 2000, 64 tiles:
+// 116 and 290 forward, 284 and 422 backward; 400 x 2048 x 32000 has 1000).
+constexpr uint64_t kPlanesTiles = 256;
 constexpr uint32_t kPlanesPadded = 112, kPlanesForward = 384, kPlanesBackward = 224;
 
 // Tiles, and what a wavefront has of one; `along`: wavefronts side by side along the second
@@ -32,13 +34,22 @@ enum { kLossLarge = 0, kLossMiddle = 1, kLossFew = 2 };
 inline uint64_t loss_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 inline uint64_t loss_tiles(int kind, uint64_t m, uint64_t n) { return loss_ceil(m, kLossTiles[kind].tm) * loss_ceil(n, kLossTiles[kind].tn); }
 
-// The kind of tile of a product [m, n]; `large`: there are large ones (of bf16).  Large ones go 256 at a time, middle ones 512 in three fifths of the time.  Forward, 1024 x
-// 4096 x n in tiles of 256 x 256 and of 128 x 128: 128 large tiles 94 and 76 us, 192 105 and 107, 256 120 and 135, 320 191 and 165, 512 226 and 273.
-inline int loss_kind(bool large, uint64_t m, uint64_t n)
+// Whether a product [m, n] of bf16 goes in large tiles, 256 at a time, or middle ones, 512 in three fifths of the time.  Forward, 1024 x 4096 x n in tiles of 256 x
+// 256 and of 128 x 128: 128 large tiles 94 and 76 us, 192 105 and 107, 256 120 and 135, 320 191 and 165, 512 226 and 273.
+inline bool loss_large(uint64_t m, uint64_t n)
 {
-    if (m <= 32) return kLossFew;
     const uint64_t tiles = loss_tiles(kLossLarge, m, n), middle = loss_tiles(kLossMiddle, m, n);
-    return large && tiles >= 256 && 5 * loss_ceil(tiles, 256) <= 3 * loss_ceil(middle, 512) ? kLossLarge : kLossMiddle;
+    return tiles >= 256 && 5 * loss_ceil(tiles, 256) <= 3 * loss_ceil(middle, 512);
+}
+
+// The kind of tile of logits; `wide`: of bf16.  Products of fp32 as such keep the matrix cores busy whatever the tile, so smaller tiles, a quarter of a middle one each, pay where
+// they spread better over 256 compute units (forward in middle and in small ones: 163 x 5120 x 1355 339 and 117 us, 200 x 1600 x 9000 115 and 70, 200 x 1600 x 50257 391 and 327; but
+// 220 x 4096 x 32000, seven rounds in the place of eight, 517 and 542).
+inline int loss_kind(bool wide, uint64_t m, uint64_t n)
+{
+    const uint64_t few = loss_tiles(kLossFew, m, n), middle = loss_tiles(kLossMiddle, m, n);
+    if (m <= 32 || (!wide && 5 * loss_ceil(few, 256) <= 16 * loss_ceil(middle, 256))) return kLossFew;
+    return wide && loss_large(m, n) ? kLossLarge : kLossMiddle;
 }
 
 // How sums over a piece's `stages` are shared: `parts` of `run` stages, so many that `slots` workgroups, what the device holds at once, have one each of
@@ -77,7 +88,7 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
     LossPlan p = {};
     p.bf16 = c->dtype == TAHQ_BF16;
     const bool odd = c->cols % (p.bf16 ? 32 : 16) != 0;
-    p.planes = !p.bf16 && c->rows >= (odd ? kPlanesPadded : backward ? kPlanesBackward : kPlanesForward);
+    p.planes = !p.bf16 && c->rows >= (odd ? kPlanesPadded : backward ? kPlanesBackward : kPlanesForward) && loss_tiles(kLossMiddle, c->rows, c->vocab) >= kPlanesTiles;
     p.copy = odd || p.planes;
     p.es = p.bf16 || p.planes ? 2 : 4;
     p.whole = 64 / p.es;

@@ -116,7 +116,7 @@ def test_large(rows, cols, vocab):
 
 # fp32 as three planes of bf16, in every kind of tile: of logits, of both gradients; in one direction alone; several pieces of the vocabulary
 @pytest.mark.parametrize("rows, cols, vocab", [(1030, 260, 4099), (4100, 30, 17001), (700, 64, 33003), (1030, 2056, 4099), (300, 4104, 4200), (230, 48, 777), (640, 33, 500),
-                                               (161, 31, 300), (6200, 16, 30001)])
+                                               (161, 31, 300), (6200, 16, 30001), (200, 64, 16001), (100, 33, 32001), (66, 260, 4099), (300, 64, 11003), (161, 31, 17000)])
 def test_large_f32(rows, cols, vocab):
     _check(rows, cols, vocab, "f32")
 

@@ -121,7 +121,8 @@ def test_which_tiles_the_gpu_tests_take(plan):
     assert kinds(1030, 2056, 4099)[2] == kinds(1030, 2080, 4099)[2] == 0 and kinds(2048, 1600, 50257) == (0, 0, 0)
     assert plan(1, 4100, 40, 40001, tahq.BF16)["piece"] < 40001 and plan(0, 65536, 8, 70001, tahq.BF16)["piece"] < 70001
     assert plan(0, 300, 64, 5003, tahq.F32)["copy"] == 0 and plan(0, 300, 40, 33003, tahq.BF16)["copy"] == 1
-    planes = [(plan(0, *s, tahq.F32)["planes"], plan(1, *s, tahq.F32)["planes"]) for s in ((130, 1600, 257), (300, 64, 5003), (1030, 260, 4099))]
-    assert planes == [(0, 0), (0, 1), (1, 1)]
+    planes = [(plan(0, *s, tahq.F32)["planes"], plan(1, *s, tahq.F32)["planes"]) for s in ((130, 1600, 257), (300, 64, 11003), (1030, 260, 4099), (161, 31, 17000), (161, 31, 300))]
+    assert planes == [(0, 0), (0, 1), (1, 1), (1, 1), (0, 0)]
     f32 = lambda *s: kinds(*s, dtype=tahq.F32)      # noqa: E731
+    assert f32(200, 64, 16001) == f32(100, 33, 32001) == (1, 1, 1) and f32(66, 260, 4099)[:2] == f32(130, 1600, 257)[:2] == f32(64, 257, 1000)[:2] == (2, 2)
     assert f32(1030, 260, 4099) == (1, 1, 1) and f32(700, 64, 33003)[:2] == (0, 0) and f32(1030, 2056, 4099)[2] == 0 and f32(300, 4104, 4200)[2] == 1
