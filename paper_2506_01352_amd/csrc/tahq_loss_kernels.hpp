@@ -328,10 +328,11 @@ void k_loss_grad_x(GradXArgs g)
     const Stages stages = stages_of<T, LIES>();
     const uint32_t count = *g.tokens.count, tiles_m = (count + T::UM * 32 - 1) / (T::UM * 32);
     const Shares shares(tiles_m * g.tiles_n, g.first_stages, g.stages, g.slots);
-    const uint32_t part = shares.tiles ? blockIdx.x / shares.tiles : shares.parts;
-    if (part >= shares.parts) return;
+    const uint32_t all = shares.tiles * shares.parts;
+    if (blockIdx.x >= all) return;
+    const uint32_t id = by_die(blockIdx.x, all), part = id / shares.tiles;      // a die has as few parts, which share their operands, as there are
     uint32_t tm, tn;
-    tile_of(blockIdx.x % shares.tiles, tiles_m, g.tiles_n, tm, tn);
+    tile_at(id % shares.tiles, tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
     const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, 0, g.g_plane}, b = {g.weight, g.ldw, g.rows, (g.cols + T::COLS - 1) / T::COLS, g.w_plane};
     const uint32_t from = part * shares.run;

@@ -9,14 +9,23 @@ namespace tahq {
 
 typedef float float16v __attribute__((ext_vector_type(16)));
 
-// Workgroups go around the eight dies, each with a cache of its own: a die gets neighbouring tiles, in strips of eight rows of tiles.
-__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn)
+// Workgroups go around the eight dies, each with a cache of its own: numbers that a die gets follow each other.
+__device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total)
 {
-    const uint32_t total = tiles_m * tiles_n, die = id % 8, extra = total % 8;
-    id = die * (total / 8) + min(die, extra) + id / 8;
+    const uint32_t die = id % 8, extra = total % 8;
+    return die * (total / 8) + min(die, extra) + id / 8;
+}
+// Tiles one after another in strips of eight rows of tiles
+__device__ __forceinline__ void tile_at(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn)
+{
     const uint32_t strip = id / (8 * tiles_n), at = id % (8 * tiles_n), height = min(tiles_m - strip * 8, 8u);
     tm = strip * 8 + at % height;
     tn = at / height;
+}
+// A die gets neighbouring tiles
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn)
+{
+    tile_at(by_die(id, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
 }
 
 // s_waitcnt's operand: at most `vm` loads and `lgkm` LDS accesses outstanding (no exports are)
