@@ -149,9 +149,10 @@ __global__ __launch_bounds__(256)
 void k_loss_blocks(const void *weight, uint8_t *blocks, uint32_t rows, uint32_t cols, uint32_t padded)
 {
     constexpr uint32_t ES = BF16 ? 2 : 4, WHOLE = kStageCols<BF16 || PLANES == 3>, RUNS = WHOLE / 8;
+    constexpr uint32_t TOGETHER = 256 / (16 * RUNS);
     const uint32_t row = blockIdx.x * 16 + threadIdx.x / RUNS % 16, count = (cols + WHOLE - 1) / WHOLE;
     if (row >= padded) return;
-    for (uint32_t c = (threadIdx.x / (16 * RUNS)) * WHOLE + threadIdx.x % RUNS * 8; c < count * WHOLE; c += 256 / (16 * RUNS) * WHOLE) {
+    for (uint32_t c = (blockIdx.y * TOGETHER + threadIdx.x / (16 * RUNS)) * WHOLE + threadIdx.x % RUNS * 8; c < count * WHOLE; c += gridDim.y * TOGETHER * WHOLE) {
         Eight<BF16> e = {};
         if (row < rows && c < cols)
             e = fetch<BF16, false>(static_cast<const uint8_t *>(weight) + (uint64_t)row * cols * ES, c, cols, more_behind(row, rows, cols));
