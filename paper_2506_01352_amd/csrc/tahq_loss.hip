@@ -66,7 +66,8 @@ struct Call {
         const dim3 grid((uint32_t)(loss_ceil(cfg->rows, kLossTiles[p.kind].tm) * g.tiles_n)), block(256);
         if (p.kind == kLossLarge) q(k_loss_logits<true, 1, 2, 2, 4, 4, 1, LIES, MODE>, grid, block, g);
         else if (p.kind == kLossMiddle) p.bf16 ? q(k_loss_logits<true, 1, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 2, 2, 2, 2, 2, LIES, MODE>, grid, block, g);
-        else p.bf16 ? q(k_loss_logits<true, 1, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g) : q(k_loss_logits<false, 1, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g);
+        else if (!p.bf16) q(k_loss_logits<false, 1, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g);
+        else if constexpr (MODE == kGrads || LIES == kRows) q(k_loss_logits<true, 1, 1, 4, 1, 1, 2, LIES, MODE>, grid, block, g);       // otherwise: few
     }
     template <int MODE>
     void logits(const LogitArgs &g)
@@ -81,6 +82,7 @@ struct Call {
             logits_of<MODE, kRows>(g);
         }
     }
+    void few(const FewArgs &g) { q(p.bf16 ? k_loss_few<true> : k_loss_few<false>, dim3((uint32_t)loss_ceil(g.end - g.first, 32)), dim3(64), g); }
     LogitArgs logit_args(const Weight &w, uint32_t first, uint32_t rows) const
     {
         LogitArgs g = {};
@@ -155,7 +157,7 @@ tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, cons
     for (const void *x : {d_x, d_weight, (const void *)d_losses, (const void *)d_lse, (const void *)d_total, (const void *)d_workspace})
         if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
     if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target) return TAHQ_ERR_MISALIGNED;
-    call.gather(d_x, d_target, d_losses, d_lse, nullptr);
+    if (!p.few) call.gather(d_x, d_target, d_losses, d_lse, nullptr);
     // Tokens of a workgroup that joins statistics: up to 32 in one, then 64 workgroups and more, as a workgroup reads lines of 32 bytes of 4 tokens, and each
     // compute unit works on two (vocabulary of 50257: 256 workgroups and more, 500 tokens 37 us, 64 34; 1024 workgroups, 2048 tokens 91 us, 64 and 256 83).
     uint32_t width = 32;
@@ -163,11 +165,19 @@ tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, cons
     const bool alone = cfg->rows <= width;
     for (uint32_t first = 0; first < cfg->vocab; first += p.piece) {
         const uint32_t rows = cfg->vocab - first < p.piece ? cfg->vocab - first : p.piece;
-        LogitArgs g = call.logit_args(call.weight(d_weight, first, rows), first, rows);
-        g.parts = call.at<float2>(p.stats);
-        g.at_target = call.at<float>(p.at_target);
-        call.logits<kStats>(g);
-        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, width)), dim3(kJoinLanes), g.parts, g.tiles_n * kLossTiles[p.kind].along, p.padded, call.tokens, g.at_target,
+        float2 *const parts = call.at<float2>(p.stats);
+        float *const at_target = call.at<float>(p.at_target);
+        if (p.few) {
+            call.few({d_x, static_cast<const uint8_t *>(d_weight) + (uint64_t)first * cfg->cols * p.es, d_target, cfg->ignore, cfg->rows, cfg->cols, first, first + rows, cfg->vocab,
+                      p.padded, call.tokens, parts, at_target, d_losses, d_lse});
+        } else {
+            LogitArgs g = call.logit_args(call.weight(d_weight, first, rows), first, rows);
+            g.parts = parts;
+            g.at_target = at_target;
+            call.logits<kStats>(g);
+        }
+        const uint32_t count = (uint32_t)loss_ceil(rows, kLossTiles[p.kind].tn) * kLossTiles[p.kind].along;
+        call.q(k_loss_join, dim3((uint32_t)loss_ceil(cfg->rows, width)), dim3(kJoinLanes), parts, p.few ? (uint32_t)loss_ceil(rows, 32) : count, p.padded, call.tokens, at_target,
                call.at<float2>(p.running), first != 0, first + rows == cfg->vocab, width, d_losses, d_lse, cfg->reduction == TAHQ_LOSS_MEAN,
                alone && first + rows == cfg->vocab ? d_total : nullptr);
     }

@@ -178,6 +178,57 @@ struct LogitArgs {
 
 enum { kStats = 0, kGrads = 1 };
 
+// Exponentials as 2^(l log2(e) - shift log2(e)), one fused multiply-add each: off by the rounding of the second term, |shift| 2^-24 of the result.
+constexpr float kLog2e = 1.4426950408889634f;
+
+// A wavefront's part of the statistics of its logits, of tokens from m0 and rows of the vocabulary from n0 on, up to `vocab` of them.  Columns behind the vocabulary are asked for
+// in the tiles that have them alone, targets in the 32 tokens that have one here.
+template <class T, class Target>
+__device__ __forceinline__ void leave_stats(const TileResult<T> &r, uint32_t m0, uint32_t n0, uint32_t vocab, uint32_t count, Target target_of, float *at_target, float2 *parts)
+{
+    constexpr int MF = T::MF, NF = T::NF;
+    uint32_t lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));                           // what follows from it is not kept in registers all along
+    const uint32_t half = lane / 32;
+    auto column = [&](int j, int k) { return n0 + 32 * j + 8 * (k / 4) + 4 * half + k % 4; };
+    auto stats = [&](auto edge) {
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t m = m0 + 32 * i + lane % 32;
+            asm volatile("" : "+v"(m));
+            const uint32_t target = m < count ? target_of(m) : kBadTarget;
+            float l[NF][16], top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    l[j][k] = !decltype(edge)::value || column(j, k) < vocab ? r.acc[i][j][k] : -INFINITY;
+                    top = fmaxf(top, l[j][k]);
+                }
+            if (target - n0 < (uint32_t)NF * 32) {
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (column(j, k) == target) at_target[m] = l[j][k];
+            }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float shift = top == -INFINITY ? 0.0f : -top * kLog2e;             // a part without a logit above -infinity: its sum is 0
+            float sum[4] = {};
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(l[j][k], kLog2e, shift));
+            float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            all += __shfl_xor(all, 32);
+            if (half == 0 && m < count) parts[m] = make_float2(top, all);
+        }
+    };
+    if (n0 + NF * 32 > vocab) stats(std::true_type{});
+    else stats(std::false_type{});
+}
+
 // LIES: how the weight does
 template <bool BF16, int PLANES, int WM, int WN, int MF, int NF, int PER_CU, Lies LIES, int MODE>
 __global__ __launch_bounds__(256, PER_CU)
@@ -197,46 +248,8 @@ void k_loss_logits(LogitArgs g)
     const uint32_t half = lane / 32, wave = uniform(threadIdx.x / 64);
     const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = g.first + tn * T::UN * 32 + r.n0;         // n0: in the vocabulary
     auto column = [&](int j, int k) { return n0 + 32 * j + 8 * (k / 4) + 4 * half + k % 4; };
-    constexpr float kLog2e = 1.4426950408889634f;
-    // Exponentials as 2^(l log2(e) - shift log2(e)), one fused multiply-add each: off by the rounding of the second term, |shift| 2^-24 of the result.
-    // Columns behind the vocabulary are asked for in the tiles that have them alone, targets in the 32 tokens that have one here.
     if constexpr (MODE == kStats) {
-        auto stats = [&](auto edge) {
-#pragma unroll
-            for (int i = 0; i < MF; ++i) {
-                __builtin_amdgcn_sched_barrier(0);
-                uint32_t m = m0 + 32 * i + lane % 32;
-                asm volatile("" : "+v"(m));
-                const uint32_t target = m < count ? g.tokens.targets[m] : kBadTarget;
-                float l[NF][16], top = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < NF; ++j)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        l[j][k] = !decltype(edge)::value || column(j, k) < g.vocab ? r.acc[i][j][k] : -INFINITY;
-                        top = fmaxf(top, l[j][k]);
-                    }
-                if (target - n0 < (uint32_t)NF * 32) {
-#pragma unroll
-                    for (int j = 0; j < NF; ++j)
-#pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            if (column(j, k) == target) g.at_target[m] = l[j][k];
-                }
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float shift = top == -INFINITY ? 0.0f : -top * kLog2e;         // a part without a logit above -infinity: its sum is 0
-                float sum[4] = {};
-#pragma unroll
-                for (int j = 0; j < NF; ++j)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(l[j][k], kLog2e, shift));
-                float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                all += __shfl_xor(all, 32);
-                if (half == 0 && m < count) g.parts[(uint64_t)(tn * WN + wave % WN) * g.padded + m] = make_float2(top, all);
-            }
-        };
-        if (n0 + NF * 32 > g.vocab) stats(std::true_type{});
-        else stats(std::false_type{});
+        leave_stats(r, m0, n0, g.vocab, count, [&](uint32_t m) { return g.tokens.targets[m]; }, g.at_target, g.parts + (uint64_t)(tn * WN + wave % WN) * g.padded);
     } else {
         constexpr uint32_t WHOLE = kStageCols<BF16>;
         const uint32_t end = (max(count, 1u) + WHOLE - 1) / WHOLE * WHOLE;   // rows that are summed over: zeros behind the last token
@@ -308,6 +321,110 @@ void k_loss_logits(LogitArgs g)
         };
         if (n0 + NF * 32 > g.vocab) gradients(std::true_type{});
         else gradients(std::false_type{});
+    }
+}
+
+// Up to 32 tokens forward with rows of no whole stages, from where they lie: the weight goes straight to registers, a wavefront 32 rows of the vocabulary and 256 bytes of each at a
+// time, the next 256 on their way.  Which columns a product's operands hold does not matter as long as both hold the same: a lane has 128 bytes of a row, or the other 128.
+// Bound by addresses, a line for each lane: bf16 21 x 7999 x 50257 282 us, 2.9 TB/s, by way of a copy 605; 32 x 1001 x 131071 116 and 181; fp32 20 x 3001 x 32000 101 and 325.  Rows of whole stages are faster through LDS, four lanes to a line of them (11 x 2560 x
+// 131072 137 us, straight to registers 158).
+struct FewArgs {
+    const void *x, *weight;                  // the piece's first row
+    const int64_t *target;
+    int64_t ignore;
+    uint32_t rows, cols, first, end, vocab;  // the piece's rows of the vocabulary
+    uint32_t padded;
+    LossTokens tokens;                       // written, as by k_loss_gather
+    float2 *parts;
+    float *at_target, *zero, *zero_also;     // results of tokens that do not count
+};
+template <bool BF16>
+__global__ __launch_bounds__(64)
+void k_loss_few(FewArgs g)
+{
+    using T = TileKind<BF16, 1, 4, 1, 1>;
+    constexpr uint32_t ES = BF16 ? 2 : 4, EACH = 16 / ES, RUN = 8;
+    __shared__ uint32_t places[32];
+    const uint32_t lane = threadIdx.x, half = lane / 32, n = lane % 32, n0 = g.first + blockIdx.x * 32;
+    const int64_t t = n < g.rows ? g.target[n] : g.ignore;
+    const uint8_t *const w = static_cast<const uint8_t *>(g.weight) + (uint64_t)(min(n0 + n, g.end - 1) - g.first) * g.cols * ES;
+    // bf16 lie at any even address: words from the one before on, shifted by half a word.  At least one number is left behind the last run, so they stay within the row.
+    uint4 a[2][RUN], b[2][RUN];
+    uint32_t a_end[2] = {}, b_end[2] = {};
+    const uint32_t runs = (g.cols - 1) / (2 * RUN * EACH);
+    auto ask = [&](uint4 (&to)[RUN], uint32_t &end, const uint8_t *row, uint32_t run) {
+        const uint8_t *from = row + (uint64_t)run * RUN * 32 + half * RUN * 16;
+        const uint32_t off = BF16 ? (uint32_t)reinterpret_cast<uintptr_t>(from) & 2 : 0;
+        from -= off;
+#pragma unroll
+        for (uint32_t k = 0; k < RUN; ++k) __builtin_memcpy(&to[k], __builtin_assume_aligned(from + k * 16, 4), 16);
+        if (BF16 && off) __builtin_memcpy(&end, __builtin_assume_aligned(from + RUN * 16, 4), 4);
+    };
+    // what was asked for, as the products take it
+    auto shifted = [&](const uint4 (&v)[RUN], uint32_t end, uint32_t k, const uint8_t *row) {
+        if constexpr (!BF16) return v[k];
+        const uint32_t by = ((uint32_t)reinterpret_cast<uintptr_t>(row) & 2) * 8, next = k + 1 < RUN ? v[(k + 1) % RUN].x : end;
+        return make_uint4(__builtin_amdgcn_alignbit(v[k].y, v[k].x, by), __builtin_amdgcn_alignbit(v[k].z, v[k].y, by), __builtin_amdgcn_alignbit(v[k].w, v[k].z, by),
+                          __builtin_amdgcn_alignbit(next, v[k].w, by));
+    };
+    if (runs) ask(b[0], b_end[0], w, 0);
+    const uint32_t counted = (uint32_t)__ballot(t != g.ignore), count = __popc(counted), rank = __popc(counted & ((1u << n) - 1));
+    if (half == 0) places[n] = 0;
+    __syncthreads();
+    if (half == 0 && (counted >> n & 1)) places[rank] = n;
+    __syncthreads();
+    const uint32_t row = places[n];          // of the n-th token that counts; behind the last one any, whose results nobody takes
+    const uint32_t mine = (uint32_t)__shfl((int)(t >= 0 && t < (int64_t)g.vocab ? (uint32_t)t : kBadTarget), (int)row);
+    const uint8_t *const x = static_cast<const uint8_t *>(g.x) + (uint64_t)row * g.cols * ES;
+    TileResult<T> r;
+    r.acc[0][0] = float16v{};
+    r.m0 = r.n0 = 0;
+    if (runs) ask(a[0], a_end[0], x, 0);
+    for (uint32_t i = 0; i < runs; i += 2) {
+#pragma unroll
+        for (uint32_t k = 0; k < 2; ++k)
+            if (i + k < runs) {
+                const uint32_t next = min(i + k + 1, runs - 1);              // behind the last run that one again
+                ask(b[1 - k], b_end[1 - k], w, next);
+                ask(a[1 - k], a_end[1 - k], x, next);
+#pragma unroll
+                for (uint32_t j = 0; j < RUN; ++j) r.acc[0][0] = multiply32<BF16>(shifted(b[k], b_end[k], j, w), shifted(a[k], a_end[k], j, x), r.acc[0][0]);
+            }
+    }
+    // what is left of the rows, and zeros behind their end
+    {
+        const uint32_t from = runs * 2 * RUN * EACH;
+        auto rest = [&](uint4 (&to)[RUN], const uint8_t *of) {
+#pragma unroll
+            for (uint32_t k = 0; k < RUN; ++k) {
+                const uint32_t c = from + (2 * k + half) * EACH;
+                uint32_t v[4] = {};
+                if (c + EACH <= g.cols) {
+                    __builtin_memcpy(v, of + (uint64_t)c * ES, 16);
+                } else {
+#pragma unroll
+                    for (uint32_t e = 0; e < EACH; ++e)
+                        if (c + e < g.cols) {
+                            if constexpr (BF16) v[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(of)[c + e] << e % 2 * 16;
+                            else v[e] = reinterpret_cast<const uint32_t *>(of)[c + e];
+                        }
+                }
+                to[k] = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+        };
+        rest(b[0], w);
+        rest(a[0], x);
+#pragma unroll
+        for (uint32_t j = 0; j < RUN; ++j) r.acc[0][0] = multiply32<BF16>(b[0][j], a[0][j], r.acc[0][0]);
+    }
+    leave_stats(r, 0, n0, g.end, count, [&](uint32_t) { return mine; }, g.at_target, g.parts + (uint64_t)blockIdx.x * g.padded);
+    if (blockIdx.x == 0 && half == 0) {
+        if (n < count) {
+            g.tokens.rows[n] = row;
+            g.tokens.targets[n] = mine;
+        }
+        if (n < g.rows && !(counted >> n & 1)) g.zero[n] = g.zero_also[n] = 0.0f;
+        if (n == 0) *g.tokens.count = count;
     }
 }
 

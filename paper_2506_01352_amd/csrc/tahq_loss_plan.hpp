@@ -71,6 +71,7 @@ struct Shares {
 struct LossPlan {
     bool bf16, planes;                       // the tensors' type; fp32 as three planes of bf16
     bool copy;                               // the weight is copied into blocks of whole stages
+    bool few;                                // forward, up to 32 tokens: instead of that the weight as it lies, and hidden states are not gathered either
     uint32_t es, whole, blocks, padded;      // bytes of an element in a tile; columns of a stage; stages of a row of x; tokens up to whole stages
     uint32_t spans;                          // of kLossSpan tokens
     uint32_t piece;                          // rows of the vocabulary
@@ -89,7 +90,8 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
     p.bf16 = c->dtype == TAHQ_BF16;
     const bool odd = c->cols % (p.bf16 ? 32 : 16) != 0;
     p.planes = !p.bf16 && c->rows >= (odd ? kPlanesPadded : backward ? kPlanesBackward : kPlanesForward) && loss_tiles(kLossMiddle, c->rows, c->vocab) >= kPlanesTiles;
-    p.copy = odd || p.planes;
+    p.few = odd && !backward && c->rows <= 32;
+    p.copy = (odd || p.planes) && !p.few;
     p.es = p.bf16 || p.planes ? 2 : 4;
     p.whole = 64 / p.es;
     p.blocks = (uint32_t)loss_ceil(c->cols, p.whole);

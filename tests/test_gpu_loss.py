@@ -121,6 +121,33 @@ def test_large_f32(rows, cols, vocab):
     _check(rows, cols, vocab, "f32")
 
 
+# up to 32 tokens: runs of 256 bytes of a row, an even and an odd number of them, and what is left; several pieces of the vocabulary
+@pytest.mark.parametrize("rows, cols, vocab", [(7, 1001, 700), (32, 1600, 999), (3, 4099, 515), (20, 384, 300), (9, 256, 33), (32, 127, 64), (1, 64, 31), (17, 130, 65), (2, 8, (1 << 22) + 700)])
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+def test_few(rows, cols, vocab, kind):
+    _check(rows, cols, vocab, kind, ignored=0.3)
+
+
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+@pytest.mark.parametrize("cols", (31, 256, 1600))
+def test_few_tokens_that_do_not_count_and_targets_that_are_none(kind, cols):
+    x, weight, target, _ = _make(13, cols, 301, kind, 0.0)
+    target[::3] = IGNORE
+    target[1], target[4] = 301, -7
+    clean = tahq.LinearLoss(tahq.make_loss_config(13, cols, 301, KINDS[kind][0], reduction=tahq.LOSS_SUM), training=False)
+    clean.forward(x, weight, target)
+    losses, lse = clean.losses.clone(), clean.lse.clone()
+    x[::3] = float("nan")
+    clean.forward(x, weight, target)
+    bad = torch.zeros(13, dtype=torch.bool, device="cuda")
+    bad[1] = bad[4] = True
+    assert torch.equal(clean.lse, lse) and lse.isfinite().all() and (lse[::3] == 0).all() and (losses[::3] == 0).all()
+    assert clean.losses[bad].isnan().all() and torch.equal(clean.losses[~bad], losses[~bad]) and clean.total[1] == 8 and clean.total[0].isnan()
+    want, want_lse = loss64.forward(x[~bad], weight, target[~bad], IGNORE)
+    off, lse_off, _ = _bounds(torch.nan_to_num(x[~bad]), weight, target[~bad], kind)
+    assert ((losses[~bad].double() - want).abs() <= off + lse_off + UNIT * want.abs()).all() and ((lse[~bad].double() - want_lse).abs() <= lse_off).all()
+
+
 @pytest.mark.parametrize("kind", ("f32", "bf16"))
 @pytest.mark.parametrize("ignored", (0.0, 1.1))
 def test_all_or_none_count(kind, ignored):
