@@ -33,9 +33,9 @@ __device__ __forceinline__ uint4 philox(uint64_t counter, uint64_t offset, uint6
     return make_uint4(c0, c1, c2, c3);
 }
 
-// Eight elements to a lane, which are one counter's (ten rounds of two products): bound by memory, three tensors with a residual and two without.  bf16 32768 x 8192
-// with a residual 266 us, 6.05 TB/s; fp32 2331 x 1600 without 7.8 us out of the last cache, 10.0 out of HBM; 128 x 512 2.5 us, a launch.  A workgroup to every 2048
-// elements: they are so many, and so short, that they balance by themselves.
+// Eight elements to a lane, which are one counter's (ten rounds of two products): bound by memory, three tensors with a residual and two without.  bf16
+// 32768 x 8192 with a residual 266 us, 6.05 TB/s; fp32 2331 x 1600 without 7.8 us out of the last cache, 10.0 out of HBM; 128 x 512 2.5 us, a launch.  A
+// workgroup to every 2048 elements: they are so many, and so short, that they balance by themselves.
 template <bool BF16, bool RESIDUAL>
 __global__ __launch_bounds__(kDropLanes)
 void k_dropout(const void *x, const void *residual, void *out, const uint64_t *more_offset, Mask mask, uint64_t elements)

@@ -65,8 +65,8 @@ uint32_t lanes_of(const tahq_heads_config *c, uint32_t chunk)
 }
 
 // Where tokens alone would leave vector units idle, each of a token's groups of heads has a wavefront of its own, which works out the token's angles again.
-// bf16, 40 + 8 heads of 128: 512 tokens split 6.8 us forward and 12.6 backward, not split 8.1 and 13.5; 1024 8.4 and 15.4, 8.6 and 14.2; 2048 13.0 and 21.4, 11.7
-// and 18.1; 4096 22.2 and 32.3, 18.5 and 26.6.
+// bf16, 40 + 8 heads of 128: 512 tokens split 6.8 us forward and 12.6 backward, not split 8.1 and 13.5; 1024 8.4 and 15.4, 8.6 and 14.2; 2048 13.0 and
+// 21.4, 11.7 and 18.1; 4096 22.2 and 32.3, 18.5 and 26.6.
 constexpr uint32_t kSplitBelow = 1024;
 
 // groups of `heads` heads that a wavefront takes side by side
@@ -87,8 +87,8 @@ uint32_t workgroups_of(const HeadShape &s, uint32_t heads)
     return (uint32_t)(all < (1u << 22) ? all : 1u << 22);
 }
 
-// Workgroups of the backward pass, queries' and keys'.  With norms each leaves a part of a weight's gradient, so there are no more than are at work at
-// once (bf16 32768 x 48 x 128, three to a compute unit: 768 245 us, 1024 311; fp32 2331 x 25 x 80, five: 768 17.6 us, 1024 16.4, 1280 16.1; bf16 7432 x 40 x 58,
+// Workgroups of the backward pass, queries' and keys'.  With norms each leaves a part of a weight's gradient, so there are no more than are at work at once
+// (bf16 32768 x 48 x 128, three to a compute unit: 768 245 us, 1024 311; fp32 2331 x 25 x 80, five: 768 17.6 us, 1024 16.4, 1280 16.1; bf16 7432 x 40 x 58,
 // four: 1024 72 us, 1280 85).  They are shared as the work is, a token's angles counting as a group.
 constexpr uint32_t kBackwardMost = 1280;
 struct BackwardGroups {

@@ -1,11 +1,11 @@
 // Heads of queries and keys, normed and rotated (include/tahq_heads.h), forward and backward.
 //
-// Bound by memory: forward two tensors, backward three, each once.  A wavefront takes a token at a time and several of its heads side by side, a
-// group of `lanes` lanes to a head, or several tokens where they have few heads.  A lane holds both channels of each of its pairs, so that rotations stay within it,
-// and the same channels of every head, so that it works out its angles once for a token.
-// bf16 32768 x (40 + 8) x 128: forward 151 us, 5.3 TB/s; backward 243 and 5, 5.0 TB/s.  One token: 3.4 us, a launch and its loads one after another.  fp32 777 x 50 x 64
-// forward 7.2 us, 2331 x 25 x 80 backward 14.2 and 3.8: 40 and 56 MB, a launch's start and two rounds of memory's latency, positions before angles, in it.
-// Numbers one by one, for halves of odd size, take three times the bytes' time (bf16 7432 x 40 x 58 backward 65 us).
+// Bound by memory: forward two tensors, backward three, each once.  A wavefront takes a token at a time and several of its heads side by side, a group of
+// `lanes` lanes to a head, or several tokens where they have few heads.  A lane holds both channels of each of its pairs, so that rotations stay within it,
+// and the same channels of every head, so that it works out its angles once for a token. bf16 32768 x (40 + 8) x 128: forward 151 us, 5.3 TB/s; backward
+// 243 and 5, 5.0 TB/s.  One token: 3.4 us, a launch and its loads one after another.  fp32 777 x 50 x 64 forward 7.2 us, 2331 x 25 x 80 backward 14.2 and
+// 3.8: 40 and 56 MB, a launch's start and two rounds of memory's latency, positions before angles, in it. Numbers one by one, for halves of odd size, take
+// three times the bytes' time (bf16 7432 x 40 x 58 backward 65 us).
 #pragma once
 #include "tahq_heads.h"
 #include "tahq_lanes.hpp"
@@ -42,8 +42,8 @@ __device__ __forceinline__ void cos_sin(uint32_t turn, float &c, float &s)
     s = quarter & 2 ? -s : s;
 }
 
-// The channels that a lane holds of every head: E pairs.  CHUNK > 1: two chunks of so many channels, at channels `at[0]` and `at[1]`; otherwise pair by pair,
-// whatever the sizes.
+// The channels that a lane holds of every head: E pairs.  CHUNK > 1: two chunks of so many channels, at channels `at[0]` and `at[1]`; otherwise pair by
+// pair, whatever the sizes.
 template <bool BF16, int CHUNK, bool PAIRS>
 struct HeadLane {
     static constexpr bool WIDE = CHUNK > 1;

@@ -158,8 +158,9 @@ tahq_status tahq_loss_forward(const tahq_loss_config *cfg, const void *d_x, cons
         if (misaligned(x)) return TAHQ_ERR_MISALIGNED;
     if (reinterpret_cast<uintptr_t>(d_target) % sizeof *d_target) return TAHQ_ERR_MISALIGNED;
     if (!p.few) call.gather(d_x, d_target, d_losses, d_lse, nullptr);
-    // Tokens of a workgroup that joins statistics: up to 32 in one, then 64 workgroups and more, as a workgroup reads lines of 32 bytes of 4 tokens, and each
-    // compute unit works on two (vocabulary of 50257: 256 workgroups and more, 500 tokens 37 us, 64 34; 1024 workgroups, 2048 tokens 91 us, 64 and 256 83).
+    // Tokens of a workgroup that joins statistics: up to 32 in one, then 64 workgroups and more, as a workgroup reads lines of 32 bytes of 4 tokens, and
+    // each compute unit works on two (vocabulary of 50257: 256 workgroups and more, 500 tokens 37 us, 64 34; 1024 workgroups, 2048 tokens 91 us, 64 and 256
+    // 83).
     uint32_t width = 32;
     while (width > 1 && (cfg->rows <= 32 ? cfg->rows <= width / 2 : cfg->rows < 64 * width)) width /= 2;
     const bool alone = cfg->rows <= width;

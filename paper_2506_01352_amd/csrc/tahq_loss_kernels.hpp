@@ -1,14 +1,14 @@
 // Softmax cross entropy over a vocabulary and its gradients (include/tahq_loss.h).
 //
-// Forward: the hidden states of the tokens that count are gathered, with their rows filled up to whole stages; every tile of logits leaves the
-// largest logit and the sum of exp(l - largest) of each of its rows and the logits of the targets in it; these are joined.  Backward, for a
-// piece of the vocabulary at a time: the piece's logits again, turned into p - [v = t], which go to the workspace; their product with the
-// weight's piece, added up over the pieces; their product with the hidden states, the piece of the weight's gradient.
+// Forward: the hidden states of the tokens that count are gathered, with their rows filled up to whole stages; every tile of logits leaves the largest
+// logit and the sum of exp(l - largest) of each of its rows and the logits of the targets in it; these are joined.  Backward, for a piece of the vocabulary
+// at a time: the piece's logits again, turned into p - [v = t], which go to the workspace; their product with the weight's piece, added up over the pieces;
+// their product with the hidden states, the piece of the weight's gradient.
 //
-// Bound by the matrix cores where there are hundreds of tokens and more: four products of 2 rows cols vocab operations each, one of them the logits again, which costs a fourth
-// of the time and saves logits of 2 rows vocab bytes and more (8192 x 131072 in bf16: 2.1 GB).  8192 x 4096 x 131072 in bf16: logits 6.49 ms, 1.36 PFLOP/s; backward, in pieces of
-// 16384 rows, logits 852 us, 1.29 PFLOP/s, the hidden states' gradient 814, 1.35, the weight's 808, 1.36.  The matrix cores are busy in 70 to 75 % of the cycles, at 1.6 to 1.8 GHz.
-// By the weight's bytes where there are few: 5 x 1600 x 50257 33 us, 4.9 TB/s.
+// Bound by the matrix cores where there are hundreds of tokens and more: four products of 2 rows cols vocab operations each, one of them the logits again,
+// which costs a fourth of the time and saves logits of 2 rows vocab bytes and more (8192 x 131072 in bf16: 2.1 GB).  8192 x 4096 x 131072 in bf16: logits
+// 6.49 ms, 1.36 PFLOP/s; backward, in pieces of 16384 rows, logits 852 us, 1.29 PFLOP/s, the hidden states' gradient 814, 1.35, the weight's 808, 1.36.
+// The matrix cores are busy in 70 to 75 % of the cycles, at 1.6 to 1.8 GHz. By the weight's bytes where there are few: 5 x 1600 x 50257 33 us, 4.9 TB/s.
 #pragma once
 #include "tahq_lanes.hpp"
 #include "tahq_loss.h"
@@ -70,8 +70,8 @@ __device__ __forceinline__ void put_eight(const Eight<BF16> &e, uint8_t *base, u
 
 constexpr uint32_t kGatherRows = 4;          // of a workgroup, one to a wavefront
 
-// gathered: blocks of 64 bytes of every row, `padded` rows each, `blocks` of them, of fp32 in planes of bf16 three times.  counts: of the spans of kLossSpan tokens, NULL if there is one.
-// Four rows to a workgroup: 8192 x 4096 28 us, 4.8 TB/s; eight would leave compute units idle below 2048 tokens.
+// gathered: blocks of 64 bytes of every row, `padded` rows each, `blocks` of them, of fp32 in planes of bf16 three times.  counts: of the spans of
+// kLossSpan tokens, NULL if there is one. Four rows to a workgroup: 8192 x 4096 28 us, 4.8 TB/s; eight would leave compute units idle below 2048 tokens.
 // zero, zero_also: float results of tokens that do not count (NULL: none); grad_x: their gradients.
 template <bool BF16, int PLANES>
 __global__ __launch_bounds__(256)
@@ -142,8 +142,8 @@ void k_loss_gather(const void *x, const int64_t *target, const uint32_t *counts,
     }
 }
 
-// A piece of the weight in blocks, for numbers of channels that are not whole stages, and of fp32 in planes; rows up to whole stages, and channels, are filled up
-// with zeros.  Sixteen rows to a workgroup, so that it writes runs of 1 KB.  Bound by memory: fp32 32003 x 1001 to planes 58 us, 5.5 TB/s.
+// A piece of the weight in blocks, for numbers of channels that are not whole stages, and of fp32 in planes; rows up to whole stages, and channels, are
+// filled up with zeros.  Sixteen rows to a workgroup, so that it writes runs of 1 KB.  Bound by memory: fp32 32003 x 1001 to planes 58 us, 5.5 TB/s.
 template <bool BF16, int PLANES>
 __global__ __launch_bounds__(256)
 void k_loss_blocks(const void *weight, uint8_t *blocks, uint32_t rows, uint32_t cols, uint32_t padded)
@@ -181,8 +181,8 @@ enum { kStats = 0, kGrads = 1 };
 // Exponentials as 2^(l log2(e) - shift log2(e)), one fused multiply-add each: off by the rounding of the second term, |shift| 2^-24 of the result.
 constexpr float kLog2e = 1.4426950408889634f;
 
-// A wavefront's part of the statistics of its logits, of tokens from m0 and rows of the vocabulary from n0 on, up to `vocab` of them.  Columns behind the vocabulary are asked for
-// in the tiles that have them alone, targets in the 32 tokens that have one here.
+// A wavefront's part of the statistics of its logits, of tokens from m0 and rows of the vocabulary from n0 on, up to `vocab` of them.  Columns behind the
+// vocabulary are asked for in the tiles that have them alone, targets in the 32 tokens that have one here.
 template <class T, class Target>
 __device__ __forceinline__ void leave_stats(const TileResult<T> &r, uint32_t m0, uint32_t n0, uint32_t vocab, uint32_t count, Target target_of, float *at_target, float2 *parts)
 {
@@ -324,10 +324,11 @@ void k_loss_logits(LogitArgs g)
     }
 }
 
-// Up to 32 tokens forward with rows of no whole stages, from where they lie: the weight goes straight to registers, a wavefront 32 rows of the vocabulary and 256 bytes of each at a
-// time, the next 256 on their way.  Which columns a product's operands hold does not matter as long as both hold the same: a lane has 128 bytes of a row, or the other 128.
-// Bound by addresses, a line for each lane: bf16 21 x 7999 x 50257 282 us, 2.9 TB/s, by way of a copy 605; 32 x 1001 x 131071 116 and 181; fp32 20 x 3001 x 32000 101 and 325.  Rows of whole stages are faster through LDS, four lanes to a line of them (11 x 2560 x
-// 131072 137 us, straight to registers 158).
+// Up to 32 tokens forward with rows of no whole stages, from where they lie: the weight goes straight to registers, a wavefront 32 rows of the vocabulary
+// and 256 bytes of each at a time, the next 256 on their way.  Which columns a product's operands hold does not matter as long as both hold the same: a
+// lane has 128 bytes of a row, or the other 128. Bound by addresses, a line for each lane: bf16 21 x 7999 x 50257 282 us, 2.9 TB/s, by way of a copy 605;
+// 32 x 1001 x 131071 116 and 181; fp32 20 x 3001 x 32000 101 and 325.  Rows of whole stages are faster through LDS, four lanes to a line of them (11 x 2560
+// x 131072 137 us, straight to registers 158).
 struct FewArgs {
     const void *x, *weight;                  // the piece's first row
     const int64_t *target;
@@ -348,7 +349,8 @@ void k_loss_few(FewArgs g)
     const uint32_t lane = threadIdx.x, half = lane / 32, n = lane % 32, n0 = g.first + blockIdx.x * 32;
     const int64_t t = n < g.rows ? g.target[n] : g.ignore;
     const uint8_t *const w = static_cast<const uint8_t *>(g.weight) + (uint64_t)(min(n0 + n, g.end - 1) - g.first) * g.cols * ES;
-    // bf16 lie at any even address: words from the one before on, shifted by half a word.  At least one number is left behind the last run, so they stay within the row.
+    // bf16 lie at any even address: words from the one before on, shifted by half a word.  At least one number is left behind the last run, so they stay
+    // within the row.
     uint4 a[2][RUN], b[2][RUN];
     uint32_t a_end[2] = {}, b_end[2] = {};
     const uint32_t runs = (g.cols - 1) / (2 * RUN * EACH);
@@ -499,9 +501,9 @@ __device__ __forceinline__ void store_four(void *to, uint64_t at, uint32_t valid
     }
 }
 
-// The hidden states' gradient from its sums, to the tokens' own rows.  How the sums lie: tiles of tm x tn, wavefronts of wm x wn in them.  A wavefront takes
-// eight tokens, whose numbers lie side by side, and 32 columns at a time; workgroups have up to eight runs of 128 columns one after another (2048 x 1600 of six parts:
-// 20 us; a workgroup to each run, parts one by one, 77).
+// The hidden states' gradient from its sums, to the tokens' own rows.  How the sums lie: tiles of tm x tn, wavefronts of wm x wn in them.  A wavefront
+// takes eight tokens, whose numbers lie side by side, and 32 columns at a time; workgroups have up to eight runs of 128 columns one after another (2048 x
+// 1600 of six parts: 20 us; a workgroup to each run, parts one by one, 77).
 struct SumsLayout {
     uint32_t tm, tn, wm, wn;
 };

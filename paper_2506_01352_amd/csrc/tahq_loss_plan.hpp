@@ -16,11 +16,12 @@ constexpr uint32_t kLossSpan = 4096;         // tokens that are counted together
 constexpr uint64_t kLossBudget = 256u << 20; // bytes of a piece, where the hidden states have no more
 constexpr uint64_t kLossMostRows = 1u << 22; // rows of the vocabulary in a piece
 
-// fp32 is multiplied as such (v_mfma_f32_32x32x2_f32, 110 to 135 TFLOP/s here), or as three bf16 whose sum it is, six products of bf16 for one (at the tiles; 155
-// to 200 TFLOP/s of fp32), for which the weight is copied into planes first.  So many tokens pay for that, as such and in planes: forward (2048 x 32000: 260 tokens 328 and 402 us, 400
-// 500 and 476), with rows of no whole stages, which are copied in any case (2047: 100 tokens 264 and 263, 200 378 and 329); backward, where three products share a copy (160
-// 637 and 650, 200 743 and 694, 400 1382 and 1136).  And so many tiles of 128 x 128: six products take six times the stages, one after another (400 x 5120 x 2000, 64 tiles:
-// 116 and 290 forward, 284 and 422 backward; 400 x 2048 x 32000 has 1000).
+// fp32 is multiplied as such (v_mfma_f32_32x32x2_f32, 110 to 135 TFLOP/s here), or as three bf16 whose sum it is, six products of bf16 for one (at the
+// tiles; 155 to 200 TFLOP/s of fp32), for which the weight is copied into planes first.  So many tokens pay for that, as such and in planes: forward (2048
+// x 32000: 260 tokens 328 and 402 us, 400 500 and 476), with rows of no whole stages, which are copied in any case (2047: 100 tokens 264 and 263, 200 378
+// and 329); backward, where three products share a copy (160 637 and 650, 200 743 and 694, 400 1382 and 1136).  And so many tiles of 128 x 128: six
+// products take six times the stages, one after another (400 x 5120 x 2000, 64 tiles: 116 and 290 forward, 284 and 422 backward; 400 x 2048 x 32000 has
+// 1000).
 constexpr uint64_t kPlanesTiles = 256;
 constexpr uint32_t kPlanesPadded = 112, kPlanesForward = 384, kPlanesBackward = 224;
 
@@ -34,17 +35,17 @@ enum { kLossLarge = 0, kLossMiddle = 1, kLossFew = 2 };
 inline uint64_t loss_ceil(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 inline uint64_t loss_tiles(int kind, uint64_t m, uint64_t n) { return loss_ceil(m, kLossTiles[kind].tm) * loss_ceil(n, kLossTiles[kind].tn); }
 
-// Whether a product [m, n] of bf16 goes in large tiles, 256 at a time, or middle ones, 512 in three fifths of the time.  Forward, 1024 x 4096 x n in tiles of 256 x
-// 256 and of 128 x 128: 128 large tiles 94 and 76 us, 192 105 and 107, 256 120 and 135, 320 191 and 165, 512 226 and 273.
+// Whether a product [m, n] of bf16 goes in large tiles, 256 at a time, or middle ones, 512 in three fifths of the time.  Forward, 1024 x 4096 x n in tiles
+// of 256 x 256 and of 128 x 128: 128 large tiles 94 and 76 us, 192 105 and 107, 256 120 and 135, 320 191 and 165, 512 226 and 273.
 inline bool loss_large(uint64_t m, uint64_t n)
 {
     const uint64_t tiles = loss_tiles(kLossLarge, m, n), middle = loss_tiles(kLossMiddle, m, n);
     return tiles >= 256 && 5 * loss_ceil(tiles, 256) <= 3 * loss_ceil(middle, 512);
 }
 
-// The kind of tile of logits; `wide`: of bf16.  Products of fp32 as such keep the matrix cores busy whatever the tile, so smaller tiles, a quarter of a middle one each, pay where
-// they spread better over 256 compute units (forward in middle and in small ones: 163 x 5120 x 1355 339 and 117 us, 200 x 1600 x 9000 115 and 70, 200 x 1600 x 50257 391 and 327; but
-// 220 x 4096 x 32000, seven rounds in the place of eight, 517 and 542).
+// The kind of tile of logits; `wide`: of bf16.  Products of fp32 as such keep the matrix cores busy whatever the tile, so smaller tiles, a quarter of a
+// middle one each, pay where they spread better over 256 compute units (forward in middle and in small ones: 163 x 5120 x 1355 339 and 117 us, 200 x 1600 x
+// 9000 115 and 70, 200 x 1600 x 50257 391 and 327; but 220 x 4096 x 32000, seven rounds in the place of eight, 517 and 542).
 inline int loss_kind(bool wide, uint64_t m, uint64_t n)
 {
     const uint64_t few = loss_tiles(kLossFew, m, n), middle = loss_tiles(kLossMiddle, m, n);
@@ -117,9 +118,9 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
         rows = rows < kLossMostRows ? rows : kLossMostRows;
         return (uint32_t)(rows < 256 ? 256 : rows < vocab ? rows : vocab);
     };
-    // Pieces of at most `most` rows, so long that their tiles make whole rounds of the compute units where that is possible: launches take a round for every 256
-    // tiles, begun or not, of as many stages as `logits` and `weights` say and a start as long as twenty more.  (Tiles of 256 x 256; fp32 4319 x 1024 x 50257, pieces of
-    // 20480 rows, 320 tiles of the weight's gradient: 9.99 ms, chosen so 9.87.)
+    // Pieces of at most `most` rows, so long that their tiles make whole rounds of the compute units where that is possible: launches take a round for
+    // every 256 tiles, begun or not, of as many stages as `logits` and `weights` say and a start as long as twenty more.  (Tiles of 256 x 256; fp32 4319 x
+    // 1024 x 50257, pieces of 20480 rows, 320 tiles of the weight's gradient: 9.99 ms, chosen so 9.87.)
     const uint64_t factor = p.planes ? 6 : 1, tiles_m = loss_tiles(kLossLarge, c->rows, 1), tiles_c = loss_tiles(kLossLarge, c->cols, 1);
     auto even = [&](uint32_t most, uint64_t logits, uint64_t weights) {
         if (p.es != 2 || c->rows <= 32 || most >= vocab) return most;
@@ -152,8 +153,9 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
         p.piece = even(copied < p.piece ? copied : p.piece, factor * p.blocks, factor * loss_ceil(c->rows, p.whole));
         const uint64_t widest = p.piece < c->vocab ? p.piece : c->vocab;
         p.kind = loss_kind(p.es == 2, c->rows, widest);
-        // Few tiles: several workgroups share the sums of one over the vocabulary (Shares), as many as the device holds at once.  Then large tiles are as good
-        // where there are few, but for what hangs over the edges (2048 x 1600, of which 1448 tokens count, x 50257: 365 us in tiles of 128 x 128, 245 in 256 x 256).
+        // Few tiles: several workgroups share the sums of one over the vocabulary (Shares), as many as the device holds at once.  Then large tiles are as
+        // good where there are few, but for what hangs over the edges (2048 x 1600, of which 1448 tokens count, x 50257: 365 us in tiles of 128 x 128, 245
+        // in 256 x 256).
         const uint64_t stages = loss_ceil(widest, p.whole), large = loss_tiles(kLossLarge, c->rows, c->cols), middle = loss_tiles(kLossMiddle, c->rows, c->cols);
         p.x_kind = c->rows <= 32 ? kLossFew : p.es == 2 && 3 * large <= middle && large * stages >= 256 * 16 ? kLossLarge : kLossMiddle;
         p.x_stages = (uint32_t)stages;

@@ -27,9 +27,9 @@ struct Operand {
     uint64_t plane;            // bytes from plane to plane
 };
 
-// fp32 in planes: x = x1 + x2 + x3, bf16 each, every one what is left rounded to nearest; exact, as 8 bits, and twice 8 bits and a sign, are 24 and more.  Of the
-// nine products of two such sums six are taken, x1 y1, x1 y2, x1 y3, x2 y1, x2 y2, x3 y1; the others are below 2^-25 of |x y| together.  They are summed in
-// fp32 like the columns of one product six times as long: stage 6 k + i has columns 32 k on of the i-th of these.
+// fp32 in planes: x = x1 + x2 + x3, bf16 each, every one what is left rounded to nearest; exact, as 8 bits, and twice 8 bits and a sign, are 24 and more.
+// Of the nine products of two such sums six are taken, x1 y1, x1 y2, x1 y3, x2 y1, x2 y2, x3 y1; the others are below 2^-25 of |x y| together.  They are
+// summed in fp32 like the columns of one product six times as long: stage 6 k + i has columns 32 k on of the i-th of these.
 __device__ __forceinline__ uint32_t plane_of_a(uint32_t i) { return i < 3 ? 0 : i < 5 ? 1 : 2; }
 __device__ __forceinline__ uint32_t plane_of_b(uint32_t i) { return i < 3 ? i : i < 5 ? i - 3 : 0; }
 __device__ __forceinline__ void split_planes(const float (&x)[8], uint4 (&planes)[3])
@@ -46,18 +46,18 @@ __device__ __forceinline__ void split_planes(const float (&x)[8], uint4 (&planes
     }
 }
 
-// The tile of a workgroup: WM * MF units of 32 rows of A by WN * NF units of B; its four wavefronts take MF x NF units each.  A stage is
-// 64 bytes of every row (32 columns of bf16, 16 of fp32); four of them are in LDS, one in use, three on their way (loads straight to LDS), of
-// kRows three pairs.
+// The tile of a workgroup: WM * MF units of 32 rows of A by WN * NF units of B; its four wavefronts take MF x NF units each.  A stage is 64 bytes of every
+// row (32 columns of bf16, 16 of fp32); four of them are in LDS, one in use, three on their way (loads straight to LDS), of kRows three pairs.
 //   What lies in LDS: a unit's 32 rows of 64 bytes (pairs: 128) in chunks of 16; turned, blocks' rows of k, or whole rows of k of the tile.  Loads write
-// LDS in a row; which 16 bytes a lane loads is chosen so that the operands' reads meet no bank twice, among eight lanes and among sixteen:
+//   LDS in a row; which 16 bytes a lane loads is chosen so that the operands' reads meet no bank twice, among eight lanes and among sixteen:
 //   chunk c of row r is at place c ^ swap(r)
 //   turned, bf16: 32 bytes (16 rows) number c of k are at place c ^ swap(k): four rows of k are read at a time, transposed on the way
 //   to registers (ds_read_b64_tr_b16: sixteen lanes address 4 x 16 elements and each gets a column).  fp32: one number at a time.
-//   Tiles of 256 x 256 take all of a compute unit's LDS and four wavefronts with 128 x 128 results each: an operand read from LDS goes into four products.  A stage takes
-// 0.75 us, the products alone 0.55; a tile's start and end 11 us.  Workgroups that go on to further tiles, whose loads begin before the results are stored, were 8 % slower.
-//   Order of work as in the mx4 products: operands of a step (two to a stage) are read while the step before is multiplied; at the last step of
-// a stage all wavefronts have the operands in registers, the next stage's loads are waited for, and the stage just read is loaded over.
+//   Tiles of 256 x 256 take all of a compute unit's LDS and four wavefronts with 128 x 128 results each: an operand read from LDS goes into four products.
+//   A stage takes 0.75 us, the products alone 0.55; a tile's start and end 11 us.  Workgroups that go on to further tiles, whose loads begin before the
+//   results are stored, were 8 % slower.
+//   Order of work as in the mx4 products: operands of a step (two to a stage) are read while the step before is multiplied; at the last step of a stage all
+//   wavefronts have the operands in registers, the next stage's loads are waited for, and the stage just read is loaded over.
 template <bool BF16, int WM_, int WN_, int MF_, int NF_>
 struct TileKind {
     static constexpr int WM = WM_, WN = WN_, MF = MF_, NF = NF_, W = WM * WN, UM = WM * MF, UN = WN * NF;
@@ -198,8 +198,8 @@ struct Feed {
     }
 };
 
-// Stages `from` .. `from + count - 1` of the product of tile (tm, tn); count >= 1.  PLANES 3: each for six, of operands in planes.  A lies in blocks.  B's rows of k behind its last one, kTurned, are the
-// last one again (A's columns there are zeros).
+// Stages `from` .. `from + count - 1` of the product of tile (tm, tn); count >= 1.  PLANES 3: each for six, of operands in planes.  A lies in blocks.  B's
+// rows of k behind its last one, kTurned, are the last one again (A's columns there are zeros).
 template <class T, bool BF16, int PLANES, Lies LIES_A, Lies LIES_B>
 __device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &ob, uint32_t tm, uint32_t tn, uint32_t from, uint32_t columns, const Stages &stages,
                                               TileResult<T> &result)
