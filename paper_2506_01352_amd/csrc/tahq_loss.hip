@@ -82,7 +82,12 @@ struct Call {
             logits_of<MODE, kRows>(g);
         }
     }
-    void few(const FewArgs &g) { q(p.bf16 ? k_loss_few<true> : k_loss_few<false>, dim3((uint32_t)loss_ceil(g.end - g.first, 32)), dim3(64), g); }
+    void few(const FewArgs &g)
+    {
+        const dim3 grid((uint32_t)loss_ceil(g.end - g.first, 32));
+        if (p.split) q(p.bf16 ? k_loss_few<true, kFewWaves> : k_loss_few<false, kFewWaves>, grid, dim3(64 * kFewWaves), g);
+        else q(p.bf16 ? k_loss_few<true, 1> : k_loss_few<false, 1>, grid, dim3(64), g);
+    }
     LogitArgs logit_args(const Weight &w, uint32_t first, uint32_t rows) const
     {
         LogitArgs g = {};

@@ -324,11 +324,11 @@ void k_loss_logits(LogitArgs g)
     }
 }
 
-// Up to 32 tokens forward with rows of no whole stages, from where they lie: the weight goes straight to registers, a wavefront 32 rows of the vocabulary
-// and 256 bytes of each at a time, the next 256 on their way.  Which columns a product's operands hold does not matter as long as both hold the same: a
-// lane has 128 bytes of a row, or the other 128. Bound by addresses, a line for each lane: bf16 21 x 7999 x 50257 282 us, 2.9 TB/s, by way of a copy 605;
-// 32 x 1001 x 131071 116 and 181; fp32 20 x 3001 x 32000 101 and 325.  Rows of whole stages are faster through LDS, four lanes to a line of them (11 x 2560
-// x 131072 137 us, straight to registers 158).
+// Up to 32 tokens forward, with rows of no whole stages or few rows of the vocabulary (then WAVES wavefronts to the channels), from where they lie: the
+// weight goes straight to registers, a wavefront 32 rows of the vocabulary and 256 bytes of each at a time, the next 256 on their way.  Which columns a
+// product's operands hold does not matter as long as both hold the same: a lane has 128 bytes of a row, or the other 128. Bound by addresses, a line for
+// each lane: bf16 21 x 7999 x 50257 282 us, 2.9 TB/s, by way of a copy 605; 32 x 1001 x 131071 116 and 181; fp32 20 x 3001 x 32000 101 and 325.  Rows of
+// whole stages are faster through LDS, four lanes to a line of them (11 x 2560 x 131072 137 us, straight to registers 158).
 struct FewArgs {
     const void *x, *weight;                  // the piece's first row
     const int64_t *target;
@@ -339,14 +339,15 @@ struct FewArgs {
     float2 *parts;
     float *at_target, *zero, *zero_also;     // results of tokens that do not count
 };
-template <bool BF16>
-__global__ __launch_bounds__(64)
+constexpr int kFewWaves = 8;
+template <bool BF16, int WAVES>
+__global__ __launch_bounds__(64 * WAVES)
 void k_loss_few(FewArgs g)
 {
     using T = TileKind<BF16, 1, 4, 1, 1>;
     constexpr uint32_t ES = BF16 ? 2 : 4, EACH = 16 / ES, RUN = 8;
     __shared__ uint32_t places[32];
-    const uint32_t lane = threadIdx.x, half = lane / 32, n = lane % 32, n0 = g.first + blockIdx.x * 32;
+    const uint32_t lane = threadIdx.x % 64, wave = uniform(threadIdx.x / 64), half = lane / 32, n = lane % 32, n0 = g.first + blockIdx.x * 32;
     const int64_t t = n < g.rows ? g.target[n] : g.ignore;
     const uint8_t *const w = static_cast<const uint8_t *>(g.weight) + (uint64_t)(min(n0 + n, g.end - 1) - g.first) * g.cols * ES;
     // bf16 lie at any even address: words from the one before on, shifted by half a word.  At least one number is left behind the last run, so they stay
@@ -369,11 +370,11 @@ void k_loss_few(FewArgs g)
         return make_uint4(__builtin_amdgcn_alignbit(v[k].y, v[k].x, by), __builtin_amdgcn_alignbit(v[k].z, v[k].y, by), __builtin_amdgcn_alignbit(v[k].w, v[k].z, by),
                           __builtin_amdgcn_alignbit(next, v[k].w, by));
     };
-    if (runs) ask(b[0], b_end[0], w, 0);
+    if (wave < runs) ask(b[0], b_end[0], w, wave);
     const uint32_t counted = (uint32_t)__ballot(t != g.ignore), count = __popc(counted), rank = __popc(counted & ((1u << n) - 1));
-    if (half == 0) places[n] = 0;
+    if (threadIdx.x < 32) places[n] = 0;
     __syncthreads();
-    if (half == 0 && (counted >> n & 1)) places[rank] = n;
+    if (threadIdx.x < 32 && (counted >> n & 1)) places[rank] = n;
     __syncthreads();
     const uint32_t row = places[n];          // of the n-th token that counts; behind the last one any, whose results nobody takes
     const uint32_t mine = (uint32_t)__shfl((int)(t >= 0 && t < (int64_t)g.vocab ? (uint32_t)t : kBadTarget), (int)row);
@@ -381,12 +382,12 @@ void k_loss_few(FewArgs g)
     TileResult<T> r;
     r.acc[0][0] = float16v{};
     r.m0 = r.n0 = 0;
-    if (runs) ask(a[0], a_end[0], x, 0);
-    for (uint32_t i = 0; i < runs; i += 2) {
+    if (wave < runs) ask(a[0], a_end[0], x, wave);
+    for (uint32_t i = wave; i < runs; i += 2 * WAVES) {
 #pragma unroll
         for (uint32_t k = 0; k < 2; ++k)
-            if (i + k < runs) {
-                const uint32_t next = min(i + k + 1, runs - 1);              // behind the last run that one again
+            if (i + k * WAVES < runs) {
+                const uint32_t next = min(i + (k + 1) * WAVES, runs - 1);    // behind the last run that one again
                 ask(b[1 - k], b_end[1 - k], w, next);
                 ask(a[1 - k], a_end[1 - k], x, next);
 #pragma unroll
@@ -394,7 +395,7 @@ void k_loss_few(FewArgs g)
             }
     }
     // what is left of the rows, and zeros behind their end
-    {
+    if (wave == 0) {
         const uint32_t from = runs * 2 * RUN * EACH;
         auto rest = [&](uint4 (&to)[RUN], const uint8_t *of) {
 #pragma unroll
@@ -418,6 +419,19 @@ void k_loss_few(FewArgs g)
         rest(a[0], x);
 #pragma unroll
         for (uint32_t j = 0; j < RUN; ++j) r.acc[0][0] = multiply32<BF16>(b[0][j], a[0][j], r.acc[0][0]);
+    }
+    if constexpr (WAVES > 1) {
+        __shared__ float sums[WAVES - 1][16][64];
+        if (wave) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) sums[wave - 1][k][lane] = r.acc[0][0][k];
+        }
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int v = 0; v < WAVES - 1; ++v)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) r.acc[0][0][k] += sums[v][k][lane];
     }
     leave_stats(r, 0, n0, g.end, count, [&](uint32_t) { return mine; }, g.at_target, g.parts + (uint64_t)blockIdx.x * g.padded);
     if (blockIdx.x == 0 && half == 0) {

@@ -25,6 +25,11 @@ constexpr uint64_t kLossMostRows = 1u << 22; // rows of the vocabulary in a piec
 constexpr uint64_t kPlanesTiles = 256;
 constexpr uint32_t kPlanesPadded = 112, kPlanesForward = 384, kPlanesBackward = 224;
 
+// Up to 32 tokens forward go by tiles of 128 rows of the vocabulary through LDS, or, against so many rows, by 32 rows from registers with eight wavefronts
+// to the channels, as there are few tiles of one stage after another (5 x 8192 x n: fp32 n 2345 173 and 72 us, 8192 180 and 99, 16384 183 and 200; bf16 51
+// and 29, 67 and 36, 86 and 71; 30 x 1600 x 16384 20 and 32).
+constexpr uint32_t kFewSplit = 8192;
+
 // Tiles, and what a wavefront has of one; `along`: wavefronts side by side along the second
 struct LossTile {
     uint32_t tm, tn, wm, wn, along;
@@ -73,6 +78,7 @@ struct LossPlan {
     bool bf16, planes;                       // the tensors' type; fp32 as three planes of bf16
     bool copy;                               // the weight is copied into blocks of whole stages
     bool few;                                // forward, up to 32 tokens: instead of that the weight as it lies, and hidden states are not gathered either
+    bool split;                              // with several wavefronts to the channels
     uint32_t es, whole, blocks, padded;      // bytes of an element in a tile; columns of a stage; stages of a row of x; tokens up to whole stages
     uint32_t spans;                          // of kLossSpan tokens
     uint32_t piece;                          // rows of the vocabulary
@@ -91,7 +97,8 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
     p.bf16 = c->dtype == TAHQ_BF16;
     const bool odd = c->cols % (p.bf16 ? 32 : 16) != 0;
     p.planes = !p.bf16 && c->rows >= (odd ? kPlanesPadded : backward ? kPlanesBackward : kPlanesForward) && loss_tiles(kLossMiddle, c->rows, c->vocab) >= kPlanesTiles;
-    p.few = odd && !backward && c->rows <= 32;
+    p.split = !backward && c->rows <= 32 && c->vocab <= kFewSplit;
+    p.few = !backward && c->rows <= 32 && (odd || p.split);
     p.copy = (odd || p.planes) && !p.few;
     p.es = p.bf16 || p.planes ? 2 : 4;
     p.whole = 64 / p.es;

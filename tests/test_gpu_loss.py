@@ -121,8 +121,10 @@ def test_large_f32(rows, cols, vocab):
     _check(rows, cols, vocab, "f32")
 
 
-# up to 32 tokens: runs of 256 bytes of a row, an even and an odd number of them, and what is left; several pieces of the vocabulary
-@pytest.mark.parametrize("rows, cols, vocab", [(7, 1001, 700), (32, 1600, 999), (3, 4099, 515), (20, 384, 300), (9, 256, 33), (32, 127, 64), (1, 64, 31), (17, 130, 65), (2, 8, (1 << 22) + 700)])
+# up to 32 tokens: runs of 256 bytes of a row, an even and an odd number of them, and what is left, with one wavefront to the channels and with eight;
+# several pieces of the vocabulary; through LDS
+@pytest.mark.parametrize("rows, cols, vocab", [(7, 1001, 700), (32, 1600, 999), (3, 4099, 515), (20, 384, 300), (9, 256, 33), (32, 127, 64), (1, 64, 31), (17, 130, 65), (2, 8, (1 << 22) + 700), (5, 1001, 9001), (32, 259, 8193), (20, 384, 9001), (3, 1600, 8200),
+                                               (5, 4097, 100), (31, 2048, 640)])
 @pytest.mark.parametrize("kind", ("f32", "bf16"))
 def test_few(rows, cols, vocab, kind):
     _check(rows, cols, vocab, kind, ignored=0.3)

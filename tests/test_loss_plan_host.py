@@ -13,7 +13,7 @@ SOURCE = r"""
 extern "C" void plan(const tahq_loss_config *c, int backward, uint64_t *out)
 {
     const tahq::LossPlan p = tahq::plan_loss(c, backward != 0);
-    const uint64_t v[] = {p.planes, p.copy, p.few, p.es, p.whole, p.blocks, p.padded, p.piece, (uint64_t)p.kind, (uint64_t)p.x_kind, p.parts, p.x_stages, p.x_slots, p.x_groups, p.x_plane,
+    const uint64_t v[] = {p.planes, p.copy, p.few, p.split, p.es, p.whole, p.blocks, p.padded, p.piece, (uint64_t)p.kind, (uint64_t)p.x_kind, p.parts, p.x_stages, p.x_slots, p.x_groups, p.x_plane,
                           p.g_plane, p.rows, p.targets, p.counts, p.x, p.at_target, p.running, p.stats, p.grads, p.sums, p.weight, p.total};
     for (unsigned i = 0; i < sizeof v / sizeof *v; ++i) out[i] = v[i];
 }
@@ -24,7 +24,7 @@ extern "C" void shares(uint32_t tiles, uint32_t first, uint32_t stages, uint32_t
     out[1] = s.run;
 }
 """
-NAMES = ("planes copy few es whole blocks padded piece kind x_kind parts x_stages x_slots x_groups x_plane g_plane rows targets counts x at_target running stats grads sums "
+NAMES = ("planes copy few split es whole blocks padded piece kind x_kind parts x_stages x_slots x_groups x_plane g_plane rows targets counts x at_target running stats grads sums "
          "weight total").split()
 TILES = {0: (256, 256), 1: (128, 128), 2: (32, 128)}
 
@@ -59,7 +59,7 @@ def test_places_hold_what_they_are_for(plan, rows, cols, vocab, dtype, backward)
     n = 3 if p["planes"] else 1
     assert p["es"] == (4 if dtype == tahq.F32 and not p["planes"] else 2) and p["whole"] * p["es"] == 64 and not (p["planes"] and dtype == tahq.BF16)
     assert p["blocks"] == -(-cols // p["whole"]) and rows <= p["padded"] < rows + p["whole"] and p["padded"] % p["whole"] == 0
-    assert p["few"] == (not backward and rows <= 32 and cols % p["whole"] != 0) and p["copy"] == (not p["few"] and (cols % p["whole"] != 0 or p["planes"]))
+    assert p["few"] == (not backward and rows <= 32 and (cols % p["whole"] != 0 or vocab <= 8192)) and p["copy"] == (not p["few"] and (cols % p["whole"] != 0 or p["planes"]))
     x_plane = p["padded"] * p["blocks"] * 64
     places = [("rows", 4 * p["padded"]), ("targets", 4 * p["padded"]), ("counts", 4 * -(-rows // 4096)), ("x", n * x_plane)]
     widest = min(vocab, p["piece"])
@@ -119,6 +119,8 @@ def test_which_tiles_the_gpu_tests_take(plan):
 
     assert kinds(5, 32, 127) == (2, 2, 2) and kinds(130, 1600, 257) == (1, 1, 1) and kinds(500, 40, 32601) == kinds(500, 96, 32601) == (0, 0, 1) and kinds(257, 512, 9000)[2] == 1
     assert kinds(1030, 2056, 4099)[2] == kinds(1030, 2080, 4099)[2] == 0 and kinds(2048, 1600, 50257) == (0, 0, 0)
+    few = [(plan(0, *s, dtype)["few"], plan(0, *s, dtype)["split"]) for s in ((5, 1600, 8192), (7, 1001, 700), (5, 1001, 9001), (20, 384, 9001)) for dtype in (tahq.F32, tahq.BF16)]
+    assert few == [(1, 1)] * 4 + [(1, 0)] * 2 + [(0, 0)] * 2
     assert plan(1, 4100, 40, 40001, tahq.BF16)["piece"] < 40001 and plan(0, 65536, 8, 70001, tahq.BF16)["piece"] < 70001
     assert plan(0, 300, 64, 5003, tahq.F32)["copy"] == 0 and plan(0, 300, 40, 33003, tahq.BF16)["copy"] == 1
     planes = [(plan(0, *s, tahq.F32)["planes"], plan(1, *s, tahq.F32)["planes"]) for s in ((130, 1600, 257), (300, 64, 11003), (1030, 260, 4099), (161, 31, 17000), (161, 31, 300))]
