@@ -383,6 +383,7 @@ void k_loss_few(FewArgs g)
     r.acc[0][0] = float16v{};
     r.m0 = r.n0 = 0;
     if (wave < runs) ask(a[0], a_end[0], x, wave);
+    float16v parts = {};                     // of fp32, as in multiply_tile
     for (uint32_t i = wave; i < runs; i += 2 * WAVES) {
 #pragma unroll
         for (uint32_t k = 0; k < 2; ++k)
@@ -393,6 +394,14 @@ void k_loss_few(FewArgs g)
 #pragma unroll
                 for (uint32_t j = 0; j < RUN; ++j) r.acc[0][0] = multiply32<BF16>(shifted(b[k], b_end[k], j, w), shifted(a[k], a_end[k], j, x), r.acc[0][0]);
             }
+        if (!BF16 && i / (2 * WAVES) % 8 == 7) {
+            parts += r.acc[0][0];
+            r.acc[0][0] = float16v{};
+        }
+    }
+    if (!BF16) {
+        parts += r.acc[0][0];
+        r.acc[0][0] = float16v{};
     }
     // what is left of the rows, and zeros behind their end
     if (wave == 0) {
@@ -420,6 +429,7 @@ void k_loss_few(FewArgs g)
 #pragma unroll
         for (uint32_t j = 0; j < RUN; ++j) r.acc[0][0] = multiply32<BF16>(b[0][j], a[0][j], r.acc[0][0]);
     }
+    if (!BF16) r.acc[0][0] += parts;
     if constexpr (WAVES > 1) {
         __shared__ float sums[WAVES - 1][16][64];
         if (wave) {

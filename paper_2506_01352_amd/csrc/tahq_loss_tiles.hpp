@@ -357,8 +357,33 @@ __device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &
         if constexpr (AT + 1 < PERIOD) self(self, std::integral_constant<int, AT + 1>{}, s);
     };
     uint32_t s = 0;
-    for (; count - s >= PERIOD; s += PERIOD) whole(whole, std::integral_constant<int, 0>{}, s);
-    some(std::integral_constant<int, PERIOD - 1>{}, s, count - s);
+    if constexpr (BF16) {
+        for (; count - s >= PERIOD; s += PERIOD) whole(whole, std::integral_constant<int, 0>{}, s);
+        some(std::integral_constant<int, PERIOD - 1>{}, s, count - s);
+    } else {
+        // Sums of fp32 in parts of a few hundred columns, which are added up: thousands one after another would be off by three times as much.
+        constexpr uint32_t PART = 48 / PERIOD;
+        float16v sums[MF][NF] = {};
+        auto part = [&] {
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int j = 0; j < NF; ++j) {
+                    sums[i][j] += result.acc[i][j];
+                    result.acc[i][j] = float16v{};
+                }
+        };
+        for (uint32_t n = 1; count - s >= PERIOD; s += PERIOD, ++n) {
+            whole(whole, std::integral_constant<int, 0>{}, s);
+            if (n % PART == 0) part();
+        }
+        some(std::integral_constant<int, PERIOD - 1>{}, s, count - s);
+        part();
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j) result.acc[i][j] = sums[i][j];
+    }
     // loads to LDS that nobody reads are waited for, too: what comes now uses LDS otherwise
     arrived(std::integral_constant<int, 0>{});
 }
