@@ -327,7 +327,7 @@ void k_loss_logits(LogitArgs g)
 // Up to 32 tokens forward, with rows of no whole stages or few rows of the vocabulary (then WAVES wavefronts to the channels), from where they lie: the
 // weight goes straight to registers, a wavefront 32 rows of the vocabulary and 256 bytes of each at a time, the next 256 on their way.  Which columns a
 // product's operands hold does not matter as long as both hold the same: a lane has 128 bytes of a row, or the other 128. Bound by addresses, a line for
-// each lane: bf16 21 x 7999 x 50257 282 us, 2.9 TB/s, by way of a copy 605; 32 x 1001 x 131071 116 and 181; fp32 20 x 3001 x 32000 101 and 325.  Rows of
+// each lane: bf16 21 x 7999 x 50257 282 us, 2.9 TB/s, by way of a copy 605; 32 x 1001 x 131071 116 and 181; fp32 20 x 3001 x 32000 123 and 325.  Rows of
 // whole stages are faster through LDS, four lanes to a line of them (11 x 2560 x 131072 137 us, straight to registers 158).
 struct FewArgs {
     const void *x, *weight;                  // the piece's first row
@@ -380,10 +380,9 @@ void k_loss_few(FewArgs g)
     const uint32_t mine = (uint32_t)__shfl((int)(t >= 0 && t < (int64_t)g.vocab ? (uint32_t)t : kBadTarget), (int)row);
     const uint8_t *const x = static_cast<const uint8_t *>(g.x) + (uint64_t)row * g.cols * ES;
     TileResult<T> r;
-    r.acc[0][0] = float16v{};
     r.m0 = r.n0 = 0;
     if (wave < runs) ask(a[0], a_end[0], x, wave);
-    float16v parts = {};                     // of fp32, as in multiply_tile
+    float16v sums_of[BF16 ? 1 : 4] = {};     // four of fp32, as sums of thousands of columns one after another would be off by more
     for (uint32_t i = wave; i < runs; i += 2 * WAVES) {
 #pragma unroll
         for (uint32_t k = 0; k < 2; ++k)
@@ -391,17 +390,10 @@ void k_loss_few(FewArgs g)
                 const uint32_t next = min(i + (k + 1) * WAVES, runs - 1);    // behind the last run that one again
                 ask(b[1 - k], b_end[1 - k], w, next);
                 ask(a[1 - k], a_end[1 - k], x, next);
+                __builtin_amdgcn_sched_barrier(0);           // not after the products
 #pragma unroll
-                for (uint32_t j = 0; j < RUN; ++j) r.acc[0][0] = multiply32<BF16>(shifted(b[k], b_end[k], j, w), shifted(a[k], a_end[k], j, x), r.acc[0][0]);
+                for (uint32_t j = 0; j < RUN; ++j) sums_of[BF16 ? 0 : j % 4] = multiply32<BF16>(shifted(b[k], b_end[k], j, w), shifted(a[k], a_end[k], j, x), sums_of[BF16 ? 0 : j % 4]);
             }
-        if (!BF16 && i / (2 * WAVES) % 8 == 7) {
-            parts += r.acc[0][0];
-            r.acc[0][0] = float16v{};
-        }
-    }
-    if (!BF16) {
-        parts += r.acc[0][0];
-        r.acc[0][0] = float16v{};
     }
     // what is left of the rows, and zeros behind their end
     if (wave == 0) {
@@ -427,9 +419,10 @@ void k_loss_few(FewArgs g)
         rest(b[0], w);
         rest(a[0], x);
 #pragma unroll
-        for (uint32_t j = 0; j < RUN; ++j) r.acc[0][0] = multiply32<BF16>(b[0][j], a[0][j], r.acc[0][0]);
+        for (uint32_t j = 0; j < RUN; ++j) sums_of[BF16 ? 0 : j % 4] = multiply32<BF16>(b[0][j], a[0][j], sums_of[BF16 ? 0 : j % 4]);
     }
-    if (!BF16) r.acc[0][0] += parts;
+    r.acc[0][0] = sums_of[0];
+    if constexpr (!BF16) r.acc[0][0] = (sums_of[0] + sums_of[1]) + (sums_of[2] + sums_of[3]);
     if constexpr (WAVES > 1) {
         __shared__ float sums[WAVES - 1][16][64];
         if (wave) {

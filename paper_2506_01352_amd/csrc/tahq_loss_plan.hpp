@@ -26,7 +26,7 @@ constexpr uint64_t kPlanesTiles = 256;
 constexpr uint32_t kPlanesPadded = 112, kPlanesForward = 384, kPlanesBackward = 224;
 
 // Up to 32 tokens forward go by tiles of 128 rows of the vocabulary through LDS, or, against so many rows, by 32 rows from registers with eight wavefronts
-// to the channels, as there are few tiles of one stage after another (5 x 8192 x n: fp32 n 2345 173 and 72 us, 8192 180 and 99, 16384 183 and 200; bf16 51
+// to the channels, as there are few tiles of one stage after another (5 x 8192 x n: fp32 n 2345 173 and 68 us, 8192 180 and 99, 16384 183 and 200; bf16 51
 // and 29, 67 and 36, 86 and 71; 30 x 1600 x 16384 20 and 32).
 constexpr uint32_t kFewSplit = 8192;
 
