@@ -122,7 +122,9 @@ struct Call {
     }
     void grad_w(GradWArgs g)
     {
-        const int kind = p.es == 2 && loss_large(g.rows, g.cols) ? kLossLarge : kLossMiddle;
+        // sums run after run are added up in the gradient itself, if that is of fp32
+        const bool chain = p.planes && g.out_bf16 && cfg->rows > kPlanesChain * p.whole;
+        const int kind = p.es == 2 && !chain && loss_large(g.rows, g.cols) ? kLossLarge : kLossMiddle;
         g.tiles_m = (uint32_t)loss_ceil(g.rows, kLossTiles[kind].tm);
         g.tiles_n = (uint32_t)loss_ceil(g.cols, kLossTiles[kind].tn);
         const dim3 grid(g.tiles_m * g.tiles_n), block(256);

@@ -478,26 +478,32 @@ void k_loss_grad_x(GradXArgs g)
     tile_at(id % shares.tiles, tiles_m, g.tiles_n, tm, tn);
     TileResult<T> r;
     const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, 0, g.g_plane}, b = {g.weight, g.ldw, g.rows, (g.cols + T::COLS - 1) / T::COLS, g.w_plane};
-    const uint32_t from = part * shares.run;
-    multiply_tile<T, BF16, PLANES, kBlocks, LIES>(a, b, tm, tn, from, min(shares.run, g.stages - from), stages, r);
-    uint32_t lane = threadIdx.x % 64;
-    asm volatile("" : "+v"(lane));                           // not an address to keep in registers all along
-    float4 *to = g.sums + (((uint64_t)part * shares.tiles + (uint64_t)tm * g.tiles_n + tn) * 4 + uniform(threadIdx.x / 64)) * (MF * NF * 256) + lane;
+    const uint32_t from = part * shares.run, count_stages = min(shares.run, g.stages - from);
+    auto run = [&](uint32_t begin, uint32_t columns, bool add) {
+        multiply_tile<T, BF16, PLANES, kBlocks, LIES>(a, b, tm, tn, begin, columns, stages, r);
+        uint32_t lane = threadIdx.x % 64;
+        asm volatile("" : "+v"(lane));                       // not an address to keep in registers all along
+        float4 *to = g.sums + (((uint64_t)part * shares.tiles + (uint64_t)tm * g.tiles_n + tn) * 4 + uniform(threadIdx.x / 64)) * (MF * NF * 256) + lane;
 #pragma unroll
-    for (int i = 0; i < MF; ++i)
+        for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) {
-            __builtin_amdgcn_sched_barrier(0);
-            asm volatile("" : "+v"(to));                     // one by one: addresses of all of them would not fit the registers
-            float4 x[4];
+            for (int j = 0; j < NF; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("" : "+v"(to));                 // one by one: addresses of all of them would not fit the registers
+                float4 x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = g.add ? to[((i * NF + j) * 4 + k) * 64] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                for (int k = 0; k < 4; ++k) x[k] = add ? to[((i * NF + j) * 4 + k) * 64] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float16v &v = r.acc[i][j];
-                to[((i * NF + j) * 4 + k) * 64] = make_float4(x[k].x + v[4 * k], x[k].y + v[4 * k + 1], x[k].z + v[4 * k + 2], x[k].w + v[4 * k + 3]);
+                for (int k = 0; k < 4; ++k) {
+                    const float16v &v = r.acc[i][j];
+                    to[((i * NF + j) * 4 + k) * 64] = make_float4(x[k].x + v[4 * k], x[k].y + v[4 * k + 1], x[k].z + v[4 * k + 2], x[k].w + v[4 * k + 3]);
+                }
             }
-        }
+    };
+    if constexpr (T::template runs<PLANES>())
+        for (uint32_t done = 0; done < count_stages; done += kPlanesChain) run(from + done, min(kPlanesChain, count_stages - done), done || g.add);
+    else
+        run(from, count_stages, g.add != 0);
 }
 
 // Up to four neighbours
@@ -581,11 +587,17 @@ void k_loss_grad_w(GradWArgs g)
     TileResult<T> r;
     const Operand a = {g.grads, (uint64_t)g.padded * 64, g.padded, (g.rows + T::COLS - 1) / T::COLS, g.g_plane},
                   b = {g.x, (uint64_t)g.padded * 64, g.padded, (g.cols + T::COLS - 1) / T::COLS, g.x_plane};
-    multiply_tile<T, BF16, PLANES, kBlocksTurned, kBlocksTurned>(a, b, tm, tn, 0, depth, stages, r);
     const float scale = loss_scale(g.grad_loss, g.mean, count);
-    const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = tn * T::UN * 32 + r.n0;
-    if (g.out_bf16) store_rows<true, T>(r, m0, n0, g.rows, g.cols, scale, g.out, g.accumulate != 0);
-    else store_rows<false, T>(r, m0, n0, g.rows, g.cols, scale, g.out, g.accumulate != 0);
+    auto run = [&](uint32_t begin, uint32_t columns, bool add) {
+        multiply_tile<T, BF16, PLANES, kBlocksTurned, kBlocksTurned>(a, b, tm, tn, begin, columns, stages, r);
+        const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = tn * T::UN * 32 + r.n0;
+        if (g.out_bf16) store_rows<true, T>(r, m0, n0, g.rows, g.cols, scale, g.out, add);
+        else store_rows<false, T>(r, m0, n0, g.rows, g.cols, scale, g.out, add);
+    };
+    if constexpr (T::template runs<PLANES>())               // bf16: a single run
+        for (uint32_t done = 0; done < depth; done += kPlanesChain) run(done, min(kPlanesChain, depth - done), done || g.accumulate);
+    else
+        run(0, depth, g.accumulate != 0);
 }
 
 // ---------------------------------------------------------------- joining

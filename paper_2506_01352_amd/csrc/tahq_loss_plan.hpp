@@ -25,6 +25,12 @@ constexpr uint64_t kLossMostRows = 1u << 22; // rows of the vocabulary in a piec
 constexpr uint64_t kPlanesTiles = 256;
 constexpr uint32_t kPlanesPadded = 112, kPlanesForward = 384, kPlanesBackward = 224;
 
+// Large tiles of fp32 in planes have no registers for sums in parts: they sum so many stages of 32 columns one after another, 384 instructions as in a
+// part of fp32 as such.  Longer sums of logits go in middle tiles (2048 x 1600 x 32000 forward 1.06 and 1.28 ms, losses off by 8.8e-7 and 6.9e-7; 4194 x
+// 4096 x 32000 5.7 and 6.5 ms, 1.13e-6 and 6.3e-7), those of gradients run after run, which are added up in memory (hidden states' gradients of these
+// two off by 1.06e-6 and 3.6e-7, 1.59e-6 and 4.0e-7; backward in all 3.4 and 3.9 ms, 20.2 and 22.5).
+constexpr uint32_t kPlanesChain = 32;
+
 // Up to 32 tokens forward go by tiles of 128 rows of the vocabulary through LDS, or, against so many rows, by 32 rows from registers with eight wavefronts
 // to the channels, as there are few tiles of one stage after another (5 x 8192 x n: fp32 n 2345 173 and 68 us, 8192 180 and 99, 16384 183 and 200; bf16 51
 // and 29, 67 and 36, 86 and 71; 30 x 1600 x 16384 20 and 32).
@@ -144,10 +150,14 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
         }
         return (uint32_t)(best * 256);
     };
+    auto kind_of = [&](uint64_t vocab_rows) {
+        const int kind = loss_kind(p.es == 2, c->rows, vocab_rows);
+        return p.planes && kind == kLossLarge && p.blocks > kPlanesChain ? (int)kLossMiddle : kind;
+    };
     const uint32_t copied = p.copy ? piece((uint64_t)n * p.blocks * 64) : ~0u;
     if (!backward) {
         // 8 bytes of statistics of every token and 32 rows of the vocabulary at least
-        p.kind = loss_kind(p.es == 2, c->rows, c->vocab);
+        p.kind = kind_of(c->vocab);
         const LossTile &t = kLossTiles[p.kind];
         p.piece = piece((uint64_t)p.padded * 8 * t.along / t.tn + 1);
         if (copied < p.piece) p.piece = even(copied, factor * p.blocks, 0);
@@ -159,7 +169,7 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
         p.piece = piece((uint64_t)n * p.padded * p.es);
         p.piece = even(copied < p.piece ? copied : p.piece, factor * p.blocks, factor * loss_ceil(c->rows, p.whole));
         const uint64_t widest = p.piece < c->vocab ? p.piece : c->vocab;
-        p.kind = loss_kind(p.es == 2, c->rows, widest);
+        p.kind = kind_of(widest);
         // Few tiles: several workgroups share the sums of one over the vocabulary (Shares), as many as the device holds at once.  Then large tiles are as
         // good where there are few, but for what hangs over the edges (2048 x 1600, of which 1448 tokens count, x 50257: 365 us in tiles of 128 x 128, 245
         // in 256 x 256).

@@ -64,6 +64,12 @@ struct TileKind {
     static constexpr int LOADS_A = 2 * UM, LOADS_B = 2 * UN, EACH_A = (LOADS_A + W - 1) / W, EACH_B = (LOADS_B + W - 1) / W, EACH = EACH_A + EACH_B, PRODUCTS = MF * NF;
     static constexpr int COLS = kStageCols<BF16>, ES = BF16 ? 2 : 4, STAGE_A = UM * 2048, STAGE_B = UN * 2048;
     static_assert(W == 4, "four wavefronts");
+    // whether multiply_tile takes sums in parts: of fp32, where registers hold results twice
+    template <int PLANES>
+    static constexpr bool parts() { return (!BF16 || PLANES == 3) && PRODUCTS <= 4; }
+    // and whether a kernel takes them run after run instead
+    template <int PLANES>
+    static constexpr bool runs() { return PLANES == 3 && !parts<PLANES>(); }
 };
 // What a workgroup has of LDS: a variable for each stage (kRows: of B for each pair), as the compiler then knows which loads a read has to wait for.
 struct Stages {
@@ -117,7 +123,7 @@ struct Feed {
     const uint8_t *at;         // the tile's part of the first stage
     uint64_t step;             // from stage to stage (of kRows: pair to pair)
     uint32_t first, lane;
-    __device__ __forceinline__ Feed(const Operand &operand, uint32_t tile, uint32_t from) : o(operand), first(tile * UNITS * 32), lane(threadIdx.x % 64)
+    __device__ __forceinline__ Feed(const Operand &operand, uint32_t tile, uint32_t from, uint32_t lane_) : o(operand), first(tile * UNITS * 32), lane(lane_)
     {
         if constexpr (LIES == kBlocks) {
             step = o.ld;
@@ -209,8 +215,10 @@ __device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &
     static_assert(LIES_A == kBlocks || LIES_A == kBlocksTurned, "a line at a time, a stage at a time");
     constexpr int NB = 4, EACH = T::EACH, MF = T::MF, NF = T::NF, PERIOD = LIES_B == kRows ? 12 : NB;
     const uint32_t wave = uniform(threadIdx.x / 64);
-    const Feed<T, LIES_A, T::UM> a(oa, tm, from);
-    const Feed<T, LIES_B, T::UN> b(ob, tn, from);
+    uint32_t lane = threadIdx.x % 64;
+    if constexpr (T::template runs<PLANES>()) asm volatile("" : "+v"(lane));             // no address is kept from run to run: they would not fit the registers
+    const Feed<T, LIES_A, T::UM> a(oa, tm, from, lane);
+    const Feed<T, LIES_B, T::UN> b(ob, tn, from, lane);
     // a wavefront's loads; where there are fewer than wavefronts, the last one again
     auto load_a = [&](int j) { return min(wave * T::EACH_A + j, (uint32_t)T::LOADS_A - 1); };
     auto load_b = [&](int j) { return min(wave * T::EACH_B + j, (uint32_t)T::LOADS_B - 1); };
@@ -357,12 +365,14 @@ __device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &
         if constexpr (AT + 1 < PERIOD) self(self, std::integral_constant<int, AT + 1>{}, s);
     };
     uint32_t s = 0;
-    if constexpr (BF16) {
+    if constexpr (!T::template parts<PLANES>()) {
         for (; count - s >= PERIOD; s += PERIOD) whole(whole, std::integral_constant<int, 0>{}, s);
         some(std::integral_constant<int, PERIOD - 1>{}, s, count - s);
     } else {
-        // Sums of fp32 in parts of a few hundred columns, which are added up: thousands one after another would be off by three times as much.
-        constexpr uint32_t PART = 48 / PERIOD;
+        // Sums of fp32, as such or in planes, in parts of a few hundred columns (768, 512), which are added up: thousands one after another would be off
+        // by several times as much (losses of 400 x 8192 x 32000 in planes, 1.5e-6 and so 7.4e-7, of which 6e-7 are the losses' own roundings; the time is
+        // the same).
+        constexpr uint32_t PART = (PLANES == 3 ? 96 : 48) / PERIOD;
         float16v sums[MF][NF] = {};
         auto part = [&] {
 #pragma unroll
@@ -413,7 +423,9 @@ __device__ __forceinline__ uint4 eight_of(uint2 x, uint2 y)
 template <bool OUT_BF16, class T>
 __device__ __forceinline__ void store_rows(const TileResult<T> &r, uint32_t m0, uint32_t n0, uint32_t rows, uint32_t cols, float scale, void *out, bool accumulate)
 {
-    const uint32_t lane = threadIdx.x % 64, half = lane / 32;
+    uint32_t lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));                           // what follows from it is not kept in registers all along
+    const uint32_t half = lane / 32;
 #pragma unroll
     for (int i = 0; i < T::MF; ++i) {
 #pragma unroll
