@@ -10,7 +10,7 @@
  * hidden state holds, NaN included.  A target outside 0 .. vocab - 1 that is not `ignore` makes the token's loss NaN, and its gradients.
  *
  * Products of bf16 are exact and summed in fp32; softmax statistics and losses are fp32.  Products of fp32 are fp32's or, for many tokens
- * and rows of the vocabulary, those of sums of three bf16: off by 2^-25 of their size, or, below magnitudes of 2^-100, by 2^-126 of the other
+ * and rows of the vocabulary, those of sums of three bf16: off by 2^-24 of their size, or, below magnitudes of 2^-100, by 2^-126 of the other
  * number's; infinite hidden states and weights of fp32, and magnitudes from 3.39e38 on, then make NaN of every logit that they are in.  In the
  * backward pass logits are computed again, a piece of the vocabulary at a time, and p_v - [v = t] (times g with LOSS_NONE, otherwise g comes
  * last) is rounded to cfg->dtype for the matrix cores, as a hidden state or weight would be.

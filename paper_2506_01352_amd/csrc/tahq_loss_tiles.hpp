@@ -28,8 +28,9 @@ struct Operand {
 };
 
 // fp32 in planes: x = x1 + x2 + x3, bf16 each, every one what is left rounded to nearest; exact, as 8 bits, and twice 8 bits and a sign, are 24 and more.
-// Of the nine products of two such sums six are taken, x1 y1, x1 y2, x1 y3, x2 y1, x2 y2, x3 y1; the others are below 2^-25 of |x y| together.  They are
-// summed in fp32 like the columns of one product six times as long: stage 6 k + i has columns 32 k on of the i-th of these.
+// Of the nine products of two such sums six are taken, x1 y1, x1 y2, x1 y3, x2 y1, x2 y2, x3 y1; the others are up to 2^-24 of |x y| together (|x2| reaches
+// 2^-8 |x|, |x3| 2^-17 |x|).  They are summed in fp32 like the columns of one product six times as long: stage 6 k + i has columns 32 k on of the i-th of
+// these.
 __device__ __forceinline__ uint32_t plane_of_a(uint32_t i) { return i < 3 ? 0 : i < 5 ? 1 : 2; }
 __device__ __forceinline__ uint32_t plane_of_b(uint32_t i) { return i < 3 ? i : i < 5 ? i - 3 : 0; }
 __device__ __forceinline__ void split_planes(const float (&x)[8], uint4 (&planes)[3])

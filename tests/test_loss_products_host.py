@@ -1,8 +1,23 @@
 """Products of fp32 as products of planes of bf16, on the CPU: what they lose, and that the bounds of the GPU tests tell six products from five or three."""
+from fractions import Fraction
+
 import pytest
 import torch
 
 import loss_products as lp
+
+
+def test_what_six_products_leave_out():
+    """x2 y3 + x3 y2 + x3 y3: |x2| reaches 2^-8 |x| and |x3| 2^-17 |x|, so 2^-24 of |x y| together, for numbers next to 1 that round the wrong way twice."""
+    worst = torch.tensor([float.fromhex("0x1.00ff8p+0")])
+    exact = Fraction(float(worst)) ** 2
+    assert [float(p) for p in lp.split(worst)] == [1.0, 2.0 ** -8, -(2.0 ** -17)]
+    left = abs(Fraction(float(lp.product(worst, worst))) - exact) / exact
+    assert Fraction(19, 10) * Fraction(1, 1 << 25) < left <= Fraction(1, 1 << 24)
+    g = torch.Generator().manual_seed(2)
+    x, y = ((1 + torch.rand(1 << 20, generator=g, dtype=torch.float64)).float() for _ in range(2))
+    assert ((lp.product(x, y) - x.double() * y.double()).abs() <= 2.0 ** -24 * x.double() * y.double()).all()
+    assert (sum(lp.split(x)) == x.double()).all()
 
 
 @pytest.mark.parametrize("products, good", [(6, True), (5, False), (3, False), (1, False)])
