@@ -181,10 +181,17 @@ enum { kStats = 0, kGrads = 1 };
 // Exponentials as 2^(l log2(e) - shift log2(e)), one fused multiply-add each: off by the rounding of the second term, |shift| 2^-24 of the result.
 constexpr float kLog2e = 1.4426950408889634f;
 
+__device__ __forceinline__ float2 joined(float2 a, float2 b)
+{
+    const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, a.y * __expf(a.x - shift) + b.y * __expf(b.x - shift));
+}
 // A wavefront's part of the statistics of its logits, of tokens from m0 and rows of the vocabulary from n0 on, up to `vocab` of them.  Columns behind the
-// vocabulary are asked for in the tiles that have them alone, targets in the 32 tokens that have one here.
+// vocabulary are asked for in the tiles that have them alone, targets in the 32 tokens that have one here.  `more`: joined to what is
+// there.
 template <class T, class Target>
-__device__ __forceinline__ void leave_stats(const TileResult<T> &r, uint32_t m0, uint32_t n0, uint32_t vocab, uint32_t count, Target target_of, float *at_target, float2 *parts)
+__device__ __forceinline__ void leave_stats(const TileResult<T> &r, uint32_t m0, uint32_t n0, uint32_t vocab, uint32_t count, Target target_of, float *at_target, float2 *parts,
+                                            bool more = false)
 {
     constexpr int MF = T::MF, NF = T::NF;
     uint32_t lane = threadIdx.x % 64;
@@ -222,11 +229,92 @@ __device__ __forceinline__ void leave_stats(const TileResult<T> &r, uint32_t m0,
                 for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(l[j][k], kLog2e, shift));
             float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
             all += __shfl_xor(all, 32);
-            if (half == 0 && m < count) parts[m] = make_float2(top, all);
+            if (half == 0 && m < count) parts[m] = more ? joined(parts[m], make_float2(top, all)) : make_float2(top, all);
         }
     };
     if (n0 + NF * 32 > vocab) stats(std::true_type{});
     else stats(std::false_type{});
+}
+
+// A wavefront's part of p - [v = t] of the piece, from its logits of tokens from m0 and rows of the vocabulary from n0 on
+template <bool BF16, int PLANES, class T>
+__device__ __forceinline__ void leave_gradients(const TileResult<T> &r, uint32_t m0, uint32_t n0, uint32_t count, const LogitArgs &g)
+{
+    constexpr int MF = T::MF, NF = T::NF;
+    uint32_t lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));                           // what follows from it is not kept in registers all along
+    const uint32_t half = lane / 32;
+    auto column = [&](int j, int k) { return n0 + 32 * j + 8 * (k / 4) + 4 * half + k % 4; };
+    constexpr uint32_t WHOLE = kStageCols<BF16>;
+    const uint32_t end = (max(count, 1u) + WHOLE - 1) / WHOLE * WHOLE;   // rows that are summed over: zeros behind the last token
+    auto gradients = [&](auto edge) {
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            uint32_t m = m0 + 32 * i + lane % 32;
+            asm volatile("" : "+v"(m));
+            const bool there = m < count;
+            const uint32_t row = there ? g.tokens.rows[m] : 0, target = there ? g.tokens.targets[m] : kBadTarget;
+            const float shift = there ? -g.lse[row] * kLog2e : 0.0f;
+            float factor = there && g.grad_loss ? g.grad_loss[row] : 1.0f;
+            if (there && target == kBadTarget) factor = NAN;
+            const bool here = target - n0 < (uint32_t)NF * 32, any = __ballot(here) != 0, behind = __ballot(!there) != 0;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                float d[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    d[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(r.acc[i][j][k], kLog2e, shift));
+                    if (decltype(edge)::value && column(j, k) >= g.vocab) d[k] = 0.0f;
+                }
+                if (any) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (column(j, k) == target) d[k] -= 1.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) d[k] *= factor;
+                if (behind) {                            // the last token; these rows' logits may be NaN, as products of zeros and infinite weights
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) d[k] = there ? d[k] : 0.0f;
+                }
+                // of the vocabulary's last block all columns: zeros behind its end
+                const uint32_t n = n0 - g.first + 32 * j;                // in the piece
+                if constexpr (BF16) {
+                    uint8_t *to = g.grads + ((uint64_t)(n / 32) * g.padded + m) * 64 + half * 16;
+#pragma unroll
+                    for (int plane = 0; plane < PLANES; ++plane) {
+                        uint2 w[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) w[q] = four_bf16(d, 4 * q);
+                        if (plane + 1 < PLANES) {                        // what is left for the next one
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                const uint32_t two = k % 4 < 2 ? w[k / 4].x : w[k / 4].y;
+                                d[k] -= __uint_as_float(k % 2 ? two & 0xffff0000u : two << 16);
+                            }
+                        }
+                        const uint4 w0 = eight_of(w[0], w[1]), w1 = eight_of(w[2], w[3]);
+                        if (m < end && g.first + n < g.vocab) {
+                            *reinterpret_cast<uint4 *>(to + plane * g.g_plane) = w0;
+                            *reinterpret_cast<uint4 *>(to + plane * g.g_plane + 32) = w1;
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        uint8_t *to = g.grads + ((uint64_t)(n / 16 + b) * g.padded + m) * 64 + half * 16;
+                        if (m < end && g.first + n + 16 * b < g.vocab) {
+                            *reinterpret_cast<float4 *>(to) = make_float4(d[8 * b], d[8 * b + 1], d[8 * b + 2], d[8 * b + 3]);
+                            *reinterpret_cast<float4 *>(to + 32) = make_float4(d[8 * b + 4], d[8 * b + 5], d[8 * b + 6], d[8 * b + 7]);
+                        }
+                    }
+                }
+            }
+        }
+    };
+    if (n0 + NF * 32 > g.vocab) gradients(std::true_type{});
+    else gradients(std::false_type{});
 }
 
 // LIES: how the weight does
@@ -243,85 +331,25 @@ void k_loss_logits(LogitArgs g)
     TileResult<T> r;
     const Operand a = {g.x, (uint64_t)g.padded * 64, g.padded, 0, g.x_plane}, b = {g.weight, g.ldw, g.vocab - g.first, 0, g.w_plane};
     multiply_tile<T, BF16, PLANES, kBlocks, LIES>(a, b, tm, tn, 0, g.stages, stages, r);
-    uint32_t lane = threadIdx.x % 64;
-    asm volatile("" : "+v"(lane));                           // what follows from it is not kept in registers all along
-    const uint32_t half = lane / 32, wave = uniform(threadIdx.x / 64);
-    const uint32_t m0 = tm * T::UM * 32 + r.m0, n0 = g.first + tn * T::UN * 32 + r.n0;         // n0: in the vocabulary
-    auto column = [&](int j, int k) { return n0 + 32 * j + 8 * (k / 4) + 4 * half + k % 4; };
-    if constexpr (MODE == kStats) {
-        leave_stats(r, m0, n0, g.vocab, count, [&](uint32_t m) { return g.tokens.targets[m]; }, g.at_target, g.parts + (uint64_t)(tn * WN + wave % WN) * g.padded);
-    } else {
-        constexpr uint32_t WHOLE = kStageCols<BF16>;
-        const uint32_t end = (max(count, 1u) + WHOLE - 1) / WHOLE * WHOLE;   // rows that are summed over: zeros behind the last token
-        auto gradients = [&](auto edge) {
-#pragma unroll
-            for (int i = 0; i < MF; ++i) {
-                uint32_t m = m0 + 32 * i + lane % 32;
-                asm volatile("" : "+v"(m));
-                const bool there = m < count;
-                const uint32_t row = there ? g.tokens.rows[m] : 0, target = there ? g.tokens.targets[m] : kBadTarget;
-                const float shift = there ? -g.lse[row] * kLog2e : 0.0f;
-                float factor = there && g.grad_loss ? g.grad_loss[row] : 1.0f;
-                if (there && target == kBadTarget) factor = NAN;
-                const bool here = target - n0 < (uint32_t)NF * 32, any = __ballot(here) != 0, behind = __ballot(!there) != 0;
-#pragma unroll
-                for (int j = 0; j < NF; ++j) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    float d[16];
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        d[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(r.acc[i][j][k], kLog2e, shift));
-                        if (decltype(edge)::value && column(j, k) >= g.vocab) d[k] = 0.0f;
-                    }
-                    if (any) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            if (column(j, k) == target) d[k] -= 1.0f;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) d[k] *= factor;
-                    if (behind) {                            // the last token; these rows' logits may be NaN, as products of zeros and infinite weights
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) d[k] = there ? d[k] : 0.0f;
-                    }
-                    // of the vocabulary's last block all columns: zeros behind its end
-                    const uint32_t n = n0 - g.first + 32 * j;                // in the piece
-                    if constexpr (BF16) {
-                        uint8_t *to = g.grads + ((uint64_t)(n / 32) * g.padded + m) * 64 + half * 16;
-#pragma unroll
-                        for (int plane = 0; plane < PLANES; ++plane) {
-                            uint2 w[4];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) w[q] = four_bf16(d, 4 * q);
-                            if (plane + 1 < PLANES) {                        // what is left for the next one
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) {
-                                    const uint32_t two = k % 4 < 2 ? w[k / 4].x : w[k / 4].y;
-                                    d[k] -= __uint_as_float(k % 2 ? two & 0xffff0000u : two << 16);
-                                }
-                            }
-                            const uint4 w0 = eight_of(w[0], w[1]), w1 = eight_of(w[2], w[3]);
-                            if (m < end && g.first + n < g.vocab) {
-                                *reinterpret_cast<uint4 *>(to + plane * g.g_plane) = w0;
-                                *reinterpret_cast<uint4 *>(to + plane * g.g_plane + 32) = w1;
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            uint8_t *to = g.grads + ((uint64_t)(n / 16 + b) * g.padded + m) * 64 + half * 16;
-                            if (m < end && g.first + n + 16 * b < g.vocab) {
-                                *reinterpret_cast<float4 *>(to) = make_float4(d[8 * b], d[8 * b + 1], d[8 * b + 2], d[8 * b + 3]);
-                                *reinterpret_cast<float4 *>(to + 32) = make_float4(d[8 * b + 4], d[8 * b + 5], d[8 * b + 6], d[8 * b + 7]);
-                            }
-                        }
-                    }
-                }
+    const uint32_t wave = uniform(threadIdx.x / 64), m0 = tm * T::UM * 32 + r.m0, n0 = g.first + tn * T::UN * 32 + r.n0;         // n0: in the vocabulary
+    auto leave = [&](const auto &results, uint32_t m, uint32_t n, bool more) {
+        if constexpr (MODE == kStats)
+            leave_stats(results, m, n, g.vocab, count, [&](uint32_t token) { return g.tokens.targets[token]; }, g.at_target, g.parts + (uint64_t)(tn * WN + wave % WN) * g.padded, more);
+        else
+            leave_gradients<BF16, PLANES>(results, m, n, count, g);
+    };
+    if constexpr (PLANES == 3) {
+        if (any_nan(r, m0, count)) {                         // an infinite operand, or a NaN: a unit after the other
+            for (uint32_t unit = 0; unit < MF * NF; ++unit) {
+                const uint32_t m = m0 + unit / NF * 32, n = n0 + unit % NF * 32;
+                TileResult<OneUnit> one;
+                one.acc[0][0] = as_fp32(a, b, m, n - g.first, g.stages);
+                leave(one, m, n, unit % NF != 0);
             }
-        };
-        if (n0 + NF * 32 > g.vocab) gradients(std::true_type{});
-        else gradients(std::false_type{});
+            return;
+        }
     }
+    leave(r, m0, n0, false);
 }
 
 // Up to 32 tokens forward, with rows of no whole stages or few rows of the vocabulary (then WAVES wavefronts to the channels), from where they lie: the
@@ -606,11 +634,6 @@ void k_loss_grad_w(GradWArgs g)
 // A workgroup takes `width` tokens, a power of two up to 32, and the parts in kJoinLanes / width runs, four at a time.
 constexpr uint32_t kJoinLanes = 1024;
 
-__device__ __forceinline__ float2 joined(float2 a, float2 b)
-{
-    const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.0f : top;
-    return make_float2(top, a.y * __expf(a.x - shift) + b.y * __expf(b.x - shift));
-}
 // Sum over a workgroup of kJoinLanes, in every lane
 __device__ __forceinline__ float lanes_sum(float v, float *sums)
 {

@@ -30,20 +30,22 @@ struct Operand {
 // fp32 in planes: x = x1 + x2 + x3, bf16 each, every one what is left rounded to nearest; exact, as 8 bits, and twice 8 bits and a sign, are 24 and more.
 // Of the nine products of two such sums six are taken, x1 y1, x1 y2, x1 y3, x2 y1, x2 y2, x3 y1; the others are up to 2^-24 of |x y| together (|x2| reaches
 // 2^-8 |x|, |x3| 2^-17 |x|).  They are summed in fp32 like the columns of one product six times as long: stage 6 k + i has columns 32 k on of the i-th of
-// these.
+// these.  Numbers from 3.39e38 on, which bf16 rounds to infinity, begin with its largest one; infinity and NaN are the first plane alone, and products of
+// an infinite number's planes are NaN where those of the number need not be (as_fp32).
 __device__ __forceinline__ uint32_t plane_of_a(uint32_t i) { return i < 3 ? 0 : i < 5 ? 1 : 2; }
 __device__ __forceinline__ uint32_t plane_of_b(uint32_t i) { return i < 3 ? i : i < 5 ? i - 3 : 0; }
 __device__ __forceinline__ void split_planes(const float (&x)[8], uint4 (&planes)[3])
 {
+    constexpr float MOST = 3.3895313892515355e38f;           // of bf16
     float left[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) left[i] = x[i];
+    for (int i = 0; i < 8; ++i) left[i] = __builtin_isfinite(x[i]) ? __builtin_fminf(__builtin_fmaxf(x[i], -MOST), MOST) : x[i];
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
         const uint32_t w[4] = {two_bf16(left[0], left[1]), two_bf16(left[2], left[3]), two_bf16(left[4], left[5]), two_bf16(left[6], left[7])};
         planes[p] = make_uint4(w[0], w[1], w[2], w[3]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) left[i] -= __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        for (int i = 0; i < 8; ++i) left[i] = __builtin_isfinite(x[i]) ? (p ? left[i] : x[i]) - __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16) : 0.0f;
     }
 }
 
@@ -397,6 +399,64 @@ __device__ __forceinline__ void multiply_tile(const Operand &oa, const Operand &
     }
     // loads to LDS that nobody reads are waited for, too: what comes now uses LDS otherwise
     arrived(std::integral_constant<int, 0>{});
+}
+
+// What is not a whole wavefront's results but 32 x 32 of them
+struct OneUnit {
+    static constexpr int MF = 1, NF = 1;
+};
+
+// Whether there is a NaN among a wavefront's results of rows of A from m0 up to `count`
+template <class T>
+__device__ __forceinline__ bool any_nan(const TileResult<T> &r, uint32_t m0, uint32_t count)
+{
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < T::MF; ++i) {
+        bool nan = false;
+#pragma unroll
+        for (int j = 0; j < T::NF; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) nan |= __builtin_isnan(r.acc[i][j][k]);
+        found |= nan && m0 + 32 * i + threadIdx.x % 32 < count;
+    }
+    return __ballot(found) != 0;
+}
+
+// Results of rows row_a and row_b on, 32 x 32 of operands in planes, as products of fp32, which the planes add up to, straight from memory, in parts as
+// elsewhere.  For wavefronts with a NaN: where an operand is infinite, products of its planes are NaN, and fp32's need not be.  (4194 x 4096 x 32000 forward
+// 6.5 ms, with an infinite row of the weight 7.0, with 300 of them 7.6, of NaN alone 20.7.)
+__device__ __forceinline__ float16v as_fp32(const Operand &a, const Operand &b, uint32_t row_a, uint32_t row_b, uint32_t blocks)
+{
+    uint32_t lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));                           // what follows from it is not kept in registers all along
+    const uint8_t *from_a = a.base + (uint64_t)min(row_a + lane % 32, a.rows - 1) * 64 + lane / 32 * 16;
+    const uint8_t *from_b = b.base + (uint64_t)min(row_b + lane % 32, b.rows - 1) * 64 + lane / 32 * 16;
+    float16v sum = {}, part = {};
+    for (uint32_t block = 0; block < blocks; ++block, from_a += a.ld, from_b += b.ld) {
+        uint4 x[2][3], y[2][3];                              // which columns a lane has does not matter as long as both operands' are the same
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                x[q][p] = *reinterpret_cast<const uint4 *>(from_a + p * a.plane + q * 32);
+                y[q][p] = *reinterpret_cast<const uint4 *>(from_b + p * b.plane + q * 32);
+            }
+        auto number = [](const uint4 (&v)[3], int i) {
+            auto one = [i](const uint4 &w) {
+                const uint32_t two = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+                return __uint_as_float(i % 2 ? two & 0xffff0000u : two << 16);
+            };
+            return (one(v[0]) + one(v[1])) + one(v[2]);
+        };
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part = __builtin_amdgcn_mfma_f32_32x32x2f32(number(y[i / 8], i % 8), number(x[i / 8], i % 8), part, 0, 0, 0);
+        if (block % 24 == 23) {
+            sum += part;
+            part = float16v{};
+        }
+    }
+    return sum + part;
 }
 
 // Results are stored straight from registers, where a lane has four neighbours of a row.  Of two groups x and y of four, after this exchange between the
