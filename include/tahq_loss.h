@@ -12,9 +12,10 @@
  * Products of bf16 are exact and summed in fp32; softmax statistics and losses are fp32.  Products of fp32 are fp32's or, for many tokens
  * and rows of the vocabulary, those of sums of three bf16: off by 2^-24 of their size, or, below magnitudes of 2^-100, by 2^-126 of the other
  * number's; logits of infinite numbers are what fp32's products make of them either way.  (A gradient that an infinite hidden state or weight
- * is a factor in, mostly 0 times it, may be NaN where fp32's is infinite.)  In the backward pass logits are computed again, a piece of the
- * vocabulary at a time, and p_v - [v = t] (times g with LOSS_NONE, otherwise g comes last) is rounded to cfg->dtype for the matrix cores, as a
- * hidden state or weight would be.
+ * is a factor in, mostly 0 times it, may be NaN where fp32's is infinite.)  Logits of -infinity and masks of any lowest number have p = 0; one
+ * of +infinity, or NaN, makes NaN of the token's loss and lse.  In the backward pass logits are computed again, a piece of the vocabulary at a
+ * time, and p_v - [v = t] (times g with LOSS_NONE, otherwise g comes last) is rounded to cfg->dtype for the matrix cores, as a hidden state or
+ * weight would be.
  *
  * Tensors are contiguous and row-major: hidden states [rows, cols], weight [vocab, cols].  Conventions as in tahq.h; targets and
  * grad_loss need no more alignment than their elements'.

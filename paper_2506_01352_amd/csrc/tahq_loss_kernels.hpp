@@ -178,8 +178,10 @@ struct LogitArgs {
 
 enum { kStats = 0, kGrads = 1 };
 
-// Exponentials as 2^(l log2(e) - shift log2(e)), one fused multiply-add each: off by the rounding of the second term, |shift| 2^-24 of the result.
-constexpr float kLog2e = 1.4426950408889634f;
+// exp(l - top) as 2^(l log2(e) + shift), one fused multiply-add, with shift = -top log2(e), whose rounding, 2^-24 of it, is in the exponent.  Where a shift
+// is larger than kFar (logits of thousands; nothing but masks, -1e30, whose rounding is more than any exponent, or the lowest number, whose shift is
+// infinite) as 2^((l - top) log2(e)).
+constexpr float kLog2e = 1.4426950408889634f, kFar = 4096.0f;
 
 __device__ __forceinline__ float2 joined(float2 a, float2 b)
 {
@@ -223,10 +225,18 @@ __device__ __forceinline__ void leave_stats(const TileResult<T> &r, uint32_t m0,
             top = fmaxf(top, __shfl_xor(top, 32));
             const float shift = top == -INFINITY ? 0.0f : -top * kLog2e;             // a part without a logit above -infinity: its sum is 0
             float sum[4] = {};
+            if (__ballot(__builtin_fabsf(shift) > kFar)) {
+                const float from = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-            for (int j = 0; j < NF; ++j)
+                for (int j = 0; j < NF; ++j)
 #pragma unroll
-                for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(l[j][k], kLog2e, shift));
+                    for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f((l[j][k] - from) * kLog2e);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NF; ++j)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) sum[k % 4] += __builtin_amdgcn_exp2f(__builtin_fmaf(l[j][k], kLog2e, shift));
+            }
             float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
             all += __shfl_xor(all, 32);
             if (half == 0 && m < count) parts[m] = more ? joined(parts[m], make_float2(top, all)) : make_float2(top, all);
@@ -254,7 +264,8 @@ __device__ __forceinline__ void leave_gradients(const TileResult<T> &r, uint32_t
             asm volatile("" : "+v"(m));
             const bool there = m < count;
             const uint32_t row = there ? g.tokens.rows[m] : 0, target = there ? g.tokens.targets[m] : kBadTarget;
-            const float shift = there ? -g.lse[row] * kLog2e : 0.0f;
+            const float lse = there ? g.lse[row] : 0.0f, shift = -lse * kLog2e;
+            const bool far = __ballot(__builtin_fabsf(shift) > kFar) != 0;
             float factor = there && g.grad_loss ? g.grad_loss[row] : 1.0f;
             if (there && target == kBadTarget) factor = NAN;
             const bool here = target - n0 < (uint32_t)NF * 32, any = __ballot(here) != 0, behind = __ballot(!there) != 0;
@@ -266,6 +277,13 @@ __device__ __forceinline__ void leave_gradients(const TileResult<T> &r, uint32_t
                 for (int k = 0; k < 16; ++k) {
                     d[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(r.acc[i][j][k], kLog2e, shift));
                     if (decltype(edge)::value && column(j, k) >= g.vocab) d[k] = 0.0f;
+                }
+                if (far) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        d[k] = __builtin_amdgcn_exp2f((r.acc[i][j][k] - lse) * kLog2e);
+                        if (decltype(edge)::value && column(j, k) >= g.vocab) d[k] = 0.0f;
+                    }
                 }
                 if (any) {
 #pragma unroll

@@ -78,6 +78,15 @@ def test_bias_of_the_lowest_number(rows, cols, vocab, kind):
 
 
 @pytest.mark.parametrize("rows, cols, vocab, kind", SIZES)
+@pytest.mark.parametrize("value", (None, -1e38, -1e30, -1e12, -1e5))
+def test_runs_of_large_negative_biases(rows, cols, vocab, kind, value):
+    """Masks (None: the lowest number) that leave nothing else in some tiles."""
+    x, weight, target, masked = _inputs(rows, cols, vocab, kind)
+    weight[masked, 0] = torch.finfo(weight.dtype).min if value is None else value
+    _check(_run(x, weight, target, kind), x, weight, target, masked, kind, slice(None))
+
+
+@pytest.mark.parametrize("rows, cols, vocab, kind", SIZES)
 def test_rows_of_minus_infinity(rows, cols, vocab, kind):
     """Of positive hidden states: logits of -infinity, losses of targets among them infinity."""
     x, weight, target, masked = _inputs(rows, cols, vocab, kind)
@@ -110,3 +119,25 @@ def test_a_token_that_is_none(rows, cols, vocab, kind, value):
     # as such instead of in planes where a tile has a NaN: either is as near to 64 bits as the bounds say
     assert ((loss.losses - clean.losses).double().abs() <= 2 * (off + lse_off) + 2 * UNIT * clean.losses.double().abs())[others].all()
     assert loss.grad_x[others].isfinite().all()
+
+
+@pytest.mark.parametrize("rows, cols, vocab, kind", SIZES)
+@pytest.mark.parametrize("size", (1e5, 1e8, 1e30))
+def test_large_logits(rows, cols, vocab, kind, size):
+    """Every token's largest logits are two equal ones of `size` and far above the others, and the target is one of the two: a loss of log 2, off by lse's
+    rounding; p is 1 / 2 twice, off by that of lse, or 1 where that is all of it."""
+    x, weight, target, _ = _inputs(rows, cols, vocab, kind, False)
+    weight[:, 0] = 0
+    counts = target != IGNORE
+    x[:, 0] = 1
+    x[:, 1:] = 0
+    weight[[3, vocab - 2], 0] = size
+    size = float(weight[3, 0])
+    target = torch.where(counts, torch.where(torch.arange(rows, device="cuda") % 2 == 0, 3, vocab - 2), target)
+    loss = _run(x, weight, target, kind)
+    ulp = 2.0 ** -23 * size
+    assert ((loss.lse[counts].double() - size).abs() <= ulp + 1).all() and ((loss.losses[counts].double()).abs() <= ulp + 1).all()
+    assert loss.grad_x.isfinite().all() and loss.grad_weight.isfinite().all()
+    rest = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    rest[[3, vocab - 2]] = False
+    assert (loss.grad_weight[rest] == 0).all()
