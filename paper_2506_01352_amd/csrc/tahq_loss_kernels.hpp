@@ -493,11 +493,12 @@ void k_loss_few(FewArgs g)
     }
 }
 
-// The gradient that the reduced loss came back with, over the number of tokens if it is their mean
+// The gradient that the reduced loss came back with, over the number of tokens if it is their mean; without a token 0, whatever it is
 __device__ __forceinline__ float loss_scale(const float *grad_loss, uint32_t mean, uint32_t count)
 {
+    if (count == 0) return 0.0f;
     const float g = grad_loss ? *grad_loss : 1.0f;
-    return mean ? g / (float)max(count, 1u) : g;
+    return mean ? g / (float)count : g;
 }
 
 // Sums over the vocabulary's piece, in parts; `add`: to what earlier pieces left.  They stay in the order that the lanes have them in, [part][tile]

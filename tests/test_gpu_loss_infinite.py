@@ -141,3 +141,17 @@ def test_large_logits(rows, cols, vocab, kind, size):
     rest = torch.ones(vocab, dtype=torch.bool, device="cuda")
     rest[[3, vocab - 2]] = False
     assert (loss.grad_weight[rest] == 0).all()
+
+
+@pytest.mark.parametrize("reduction", (tahq.LOSS_NONE, tahq.LOSS_SUM, tahq.LOSS_MEAN))
+@pytest.mark.parametrize("value", (float("nan"), float("inf")))
+@pytest.mark.parametrize("accumulate", (0, 1))
+def test_no_token_adds_nothing(reduction, value, accumulate):
+    """Gradients without a token that counts are 0, or what was there, whatever the loss came back with: 0 / 0 of a mean, say."""
+    x, weight, target, _ = _make(40, 64, 300, "bf16", 1.1)
+    loss = tahq.LinearLoss(tahq.make_loss_config(40, 64, 300, tahq.BF16, reduction=reduction, accumulate=accumulate))
+    loss.forward(x, weight, target)
+    if accumulate:
+        loss.grad_weight.fill_(3.0)
+    grad_x, grad_w = loss.backward(x, weight, target, torch.full((40 if reduction == tahq.LOSS_NONE else 1,), value, device="cuda"))
+    assert (grad_x == 0).all() and (grad_w == (3 if accumulate else 0)).all()
