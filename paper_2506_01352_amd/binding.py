@@ -944,9 +944,12 @@ def make_dropout_config(elements, dtype, p, seed=0, offset=0):
     return cfg
 
 
-def _check_offset(where, t):
-    if t is not None and not isinstance(t, int) and (t.element_size() != 8 or t.numel() < 1):
-        raise ValueError(f"{where}: d_offset is a {tuple(t.shape)} tensor of {t.dtype}, a 64-bit number is needed")
+def _check_whole_numbers(where, name, t, elements):
+    """64-bit whole numbers: another type of that size would be read bit by bit."""
+    if t is None or isinstance(t, int):
+        return
+    if t.element_size() != 8 or t.is_floating_point() or t.is_complex() or t.numel() < elements:
+        raise ValueError(f"{where}: {name} is a {tuple(t.shape)} tensor of {t.dtype}, {elements} int64 are needed")
 
 
 def tahq_dropout_forward(cfg, d_x, d_residual, d_out, d_offset=None, stream=None):
@@ -954,7 +957,7 @@ def tahq_dropout_forward(cfg, d_x, d_residual, d_out, d_offset=None, stream=None
     for name, t in (("d_x", d_x), ("d_residual", d_residual), ("d_out", d_out)):
         _check_not_half("tahq_dropout_forward", name, t, cfg.dtype)
         _check_tensor("tahq_dropout_forward", name, t, cfg.elements, cfg.dtype)
-    _check_offset("tahq_dropout_forward", d_offset)
+    _check_whole_numbers("tahq_dropout_forward", "d_offset", d_offset, 1)
     rc = (_lib or _load()).tahq_dropout_forward(C.byref(cfg), _dev_ptr(d_x), _dev_ptr(d_residual), _dev_ptr(d_out), _dev_ptr(d_offset), _stream_handle(stream))
     if rc != 0:
         raise TahqError(rc, "tahq_dropout_forward")
@@ -964,7 +967,7 @@ def tahq_dropout_backward(cfg, d_grad_out, d_grad_x, d_offset=None, stream=None)
     for name, t in (("d_grad_out", d_grad_out), ("d_grad_x", d_grad_x)):
         _check_not_half("tahq_dropout_backward", name, t, cfg.dtype)
         _check_tensor("tahq_dropout_backward", name, t, cfg.elements, cfg.dtype)
-    _check_offset("tahq_dropout_backward", d_offset)
+    _check_whole_numbers("tahq_dropout_backward", "d_offset", d_offset, 1)
     rc = (_lib or _load()).tahq_dropout_backward(C.byref(cfg), _dev_ptr(d_grad_out), _dev_ptr(d_grad_x), _dev_ptr(d_offset), _stream_handle(stream))
     if rc != 0:
         raise TahqError(rc, "tahq_dropout_backward")
@@ -1100,6 +1103,9 @@ def _heads_ptr(where, name, t, tokens, heads, head, ld, dtype):
 
 
 def _heads_tables(where, cfg, tensors):
+    for name, t, elements, size in tensors:
+        if name in ("d_positions", "d_frequencies"):
+            _check_whole_numbers(where, name, t, elements)
     for name, t, elements, size in tensors:
         if t is None or isinstance(t, int):
             continue
@@ -1279,8 +1285,7 @@ def _check_loss(where, cfg, tensors, targets, floats):
     for name, t, elements, dtype in tensors:
         _check_not_half(where, name, t, dtype)
         _check_tensor(where, name, t, elements, dtype)
-    if targets is not None and not isinstance(targets, int) and (targets.element_size() != 8 or targets.numel() < cfg.rows):
-        raise ValueError(f"{where}: d_target is a {tuple(targets.shape)} tensor of {targets.dtype}, {cfg.rows} int64 are needed")
+    _check_whole_numbers(where, "d_target", targets, cfg.rows)
     for name, t, elements in floats:
         _check_tensor(where, name, t, elements, F32)
 
