@@ -1,6 +1,8 @@
 """ctypes binding of libtahq.so: same names as the C ABI, marshalling only."""
 import ctypes as C
 import os
+import warnings
+import weakref
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 # TAHQ_LIBRARY lets an experiment load another build of the same library
@@ -975,7 +977,9 @@ def tahq_dropout_backward(cfg, d_grad_out, d_grad_x, d_offset=None, stream=None)
 
 class Dropout:
     """Dropout of one tensor of the stage, with or without the residual that it is added to.  Every forward pass takes the next offset, from
-    cfg.offset on, unless it is given one; a slot's backward pass takes that of the slot's last forward pass.
+    cfg.offset on, unless it is given one; a slot's backward pass takes that of the slot's last forward pass.  A mask follows from seed and offset alone, so
+    every layer, and every rank whose tensors are not copies, has a seed of its own (make_dropout_config(.., seed=base + layer), say): objects that count from the same
+    offset under the same seed drop the same elements, and the second one to do so warns.
     in_flight: micro-batches that go forward before the first of them comes back; each has a slot with an output of its own.  The gradient is the next
     backward call's: calls of one object follow each other, and calls on another stream than that which was torch's current one at construction come after
     that stream has waited for it.
@@ -993,9 +997,19 @@ class Dropout:
         self._outs = [torch.empty(cfg.elements, dtype=self._kind, device=device) for _ in range(in_flight)]
         self._grad = torch.empty(cfg.elements, dtype=self._kind, device=device)
         self._next, self._offsets = cfg.offset, [None] * in_flight
+        self._numbers = (cfg.seed, cfg.offset, self._graph)          # None once others have been looked for that count them
         self._config = _own_copy(cfg)        # a call's own: the offset changes
         self._by_ref = C.byref(self._config)
         self._views = {}
+
+    _counting = weakref.WeakValueDictionary()
+
+    def _count(self):
+        """Looks once for another object that takes the same numbers."""
+        numbers, self._numbers = self._numbers, None
+        if Dropout._counting.setdefault(numbers, self) is not self:
+            warnings.warn(f"Dropout: another object counts offsets from {numbers[1]} under seed {numbers[0]}, too, and drops the same elements: each needs a seed "
+                          "of its own (make_dropout_config(.., seed=..))", stacklevel=3)
 
     def _call(self, where, offset, *arguments):
         self._config.offset = offset % (1 << 64)
@@ -1020,6 +1034,8 @@ class Dropout:
         d_residual = None if residual is None else _whole("Dropout.forward", "residual", residual, self.cfg.elements, self._kind, self.device)
         if residual is not None and residual.shape != x.shape:
             raise ValueError(f"Dropout.forward: residual is a {tuple(residual.shape)} tensor, x a {tuple(x.shape)} tensor")
+        if offset is None and self._numbers is not None:
+            self._count()
         used = self._next if offset is None else offset
         self._offsets[slot] = None
         out = self._outs[slot]
