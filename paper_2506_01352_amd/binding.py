@@ -1388,7 +1388,8 @@ class LinearLoss:
         return self._results[slot]
 
     def backward(self, x, weight, target, grad_loss=None, stream=None, slot=0):
-        """(gradient of x, gradient of the weight or None) of the slot's last forward pass, which was of the same x, weight and target.  grad_loss:
+        """(gradient of x, gradient of the weight or None) of the slot's last forward pass, which was of the same x, weight and target: of the same values, in
+        whichever tensors.  That is not looked at, as it would take a pass over them; others get gradients against that pass's log-sum-exps.  grad_loss:
         float, that of the reduced loss (of every token with LOSS_NONE); None: ones."""
         _check_slot("LinearLoss.backward", slot, len(self._slots))
         if not self.training:
