@@ -55,7 +55,7 @@ void tahq_heads_config_default(tahq_heads_config *cfg);   /* bf16, halves, norm,
  *   TAHQ_ROTARY_PARTS      with r = original * f_i / 2 pi, the turns of the pair in the original context, and k = (r - low) / (high - low) cut to
  *                          0 .. 1: k f_i + (1 - k) f_i / factor
  * Published methods: the rotation with plain frequencies, Su, Lu, Pan, Murtadha, Wen, Liu 2021; linear, position interpolation, Chen, Wong, Chen, Tian
- * 2023; stretched, "NTK-aware" scaling, and by parts, "NTK-by-parts", Peng, Quesnelle, Fan, Shippole 2023, sections 3.1 and 3.2. */
+ * 2023; stretched, "NTK-aware" scaling, and by parts, "NTK-by-parts", Peng, Quesnelle, Fan, Shippole 2023. */
 typedef struct {
     uint32_t struct_size;      /* = sizeof(tahq_rotary_config)                                   */
     uint32_t rotated;          /* even, 2 .. TAHQ_HEADS_MAX                                      */

@@ -6,9 +6,10 @@
 // their product with the hidden states, the piece of the weight's gradient.
 //
 // Bound by the matrix cores where there are hundreds of tokens and more: four products of 2 rows cols vocab operations each, one of them the logits again,
-// which costs a fourth of the time and saves logits of 2 rows vocab bytes and more (8192 x 131072 in bf16: 2.1 GB).  8192 x 4096 x 131072 in bf16: logits
-// 6.49 ms, 1.36 PFLOP/s; backward, in pieces of 16384 rows, logits 852 us, 1.29 PFLOP/s, the hidden states' gradient 814, 1.35, the weight's 808, 1.36.
-// The matrix cores are busy in 70 to 75 % of the cycles, at 1.6 to 1.8 GHz. By the weight's bytes where there are few: 5 x 1600 x 50257 33 us, 4.9 TB/s.
+// which costs a fourth of the time and saves logits of 2 rows vocab bytes and more (8192 x 131072 in bf16: 2.1 GB).  8192 x 4096 x 131072 in bf16, by the
+// clock that power leaves: logits 6.5 to 6.9 ms, 1.36 to 1.28 PFLOP/s; backward, in pieces of 16384 rows, logits 852 to 887 us, 1.29 to 1.24 PFLOP/s, the
+// hidden states' gradient 814 to 841, the weight's 808 to 837.  The matrix cores are busy in 68 to 72 % of the cycles, at 1.7 to 1.8 GHz.  By the weight's
+// bytes where there are few: 5 x 1600 x 50257 33 us, 4.9 TB/s, out of the last cache in part; 47 out of HBM, 25 with the weight in the last cache.
 #pragma once
 #include "tahq_lanes.hpp"
 #include "tahq_loss.h"
@@ -246,7 +247,10 @@ __device__ __forceinline__ void leave_stats(const TileResult<T> &r, uint32_t m0,
     else stats(std::false_type{});
 }
 
-// A wavefront's part of p - [v = t] of the piece, from its logits of tokens from m0 and rows of the vocabulary from n0 on
+// A wavefront's part of p - [v = t] of the piece, from its logits of tokens from m0 and rows of the vocabulary from n0 on.  Of bf16 tensors it is rounded to
+// bf16, up to 2^-8 of it: a matrix instruction's operands are both of one type, and a second plane of bf16 would double two of the pass's products (8192 x
+// 4096 x 131072 27 to about 40 ms in all).  Gradients are off by 1.85e-3 of their norm, of which rounding the results makes 1.66e-3 alone (2048 x 1600 x
+// 50257, hidden states' and weight's; 8192 x 4096 x 131072 1.83e-3 of 1.66e-3, and 1.53e-3 of 1.34e-3).  fp32 is in three planes, or as it is.
 template <bool BF16, int PLANES, class T>
 __device__ __forceinline__ void leave_gradients(const TileResult<T> &r, uint32_t m0, uint32_t n0, uint32_t count, const LogitArgs &g)
 {

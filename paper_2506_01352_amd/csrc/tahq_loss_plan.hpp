@@ -133,7 +133,7 @@ inline LossPlan plan_loss(const tahq_loss_config *c, bool backward)
     };
     // Pieces of at most `most` rows, so long that their tiles make whole rounds of the compute units where that is possible: launches take a round for
     // every 256 tiles, begun or not, of as many stages as `logits` and `weights` say and a start as long as twenty more.  (Tiles of 256 x 256; fp32 4319 x
-    // 1024 x 50257, pieces of 20480 rows, 320 tiles of the weight's gradient: 9.99 ms, chosen so 9.87.)
+    // 1024 x 50257, pieces of 20480 rows, 320 tiles of the weight's gradient: 9.99 ms, chosen so 9.87, sums of gradients in one run.)
     const uint64_t factor = p.planes ? 6 : 1, tiles_m = loss_tiles(kLossLarge, c->rows, 1), tiles_c = loss_tiles(kLossLarge, c->cols, 1);
     auto even = [&](uint32_t most, uint64_t logits, uint64_t weights) {
         if (p.es != 2 || c->rows <= 32 || most >= vocab) return most;

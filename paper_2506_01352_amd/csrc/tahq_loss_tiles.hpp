@@ -15,7 +15,7 @@ constexpr int kStageCols = BF16 ? 32 : 16;
 //   kBlocks, kBlocksTurned: blocks of 64 bytes of every row, [block][row][64 bytes], so that whatever a tile takes at a time is whole cache lines;
 //     k along the blocks (m the rows), or, turned, k the rows (m along the blocks).  What a call makes itself lies like this.
 //   kRows: row-major, k along a row, rows of whole 64 bytes.  Lines are 128 bytes: two stages are loaded at a time, or each line would be
-//     fetched twice (logits of 8192 x 4096 x 131072 6.57 ms, stage by stage 6.79; of 5 x 1600 x 50257 25.4 us, 27.1).
+//     fetched twice (logits of 8192 x 4096 x 131072 6.57 ms, stage by stage 6.79; of 5 x 1600 x 50257 out of the last cache 25.4 us, 27.1).
 //   kTurned: row-major, k the rows.
 enum Lies { kBlocks, kBlocksTurned, kRows, kTurned };
 

@@ -75,3 +75,28 @@ def test_long_sums_of_gradients(rows, cols, vocab):
         bound = lp.long_sum(min(instructions, 384), max(instructions / 384, 1)) + 32 * UNIT / vocab ** 0.5 + 2 * UNIT
         off = float((got.double() - want).norm() / want.norm())
         assert off <= bound, (off, bound)
+
+
+@pytest.mark.parametrize("reduction", (tahq.LOSS_NONE, tahq.LOSS_SUM))
+@pytest.mark.parametrize("accumulate, wide", [(1, tahq.F32), (1, tahq.BF16), (0, tahq.BF16)])
+def test_runs_that_are_added_to_a_gradient(reduction, accumulate, wide):
+    """More tokens than one run of a large tile's sums: added to what is there once, in fp32, and rounded once where the gradient is bf16."""
+    rows, cols, vocab = 1100, 1104, 33003
+    x, weight, target, factor, winner = lp.single_products(rows, cols, vocab, "cuda")
+    if reduction == tahq.LOSS_SUM:
+        factor = factor[:1]
+    want = lp.wanted(x, weight, target, factor.expand(rows), winner)
+    cfg = tahq.make_loss_config(rows, cols, vocab, tahq.F32, wide, reduction, accumulate=accumulate)
+    loss = tahq.LinearLoss(cfg)
+    loss.forward(x, weight, target)
+    before = 3.0 if accumulate else 0.0
+    loss.grad_weight.fill_(before)
+    grad = loss.backward(x, weight, target, factor)[1].double()
+    half = 2.0 ** -8 if wide == tahq.BF16 else UNIT
+    n = torch.arange(rows, device="cuda")
+    for at, value in ((winner, want["grad_w"]), (target, -want["grad_w"])):
+        off = (lp.ONE_PRODUCT + lp.PROBABILITY + 4 * UNIT) * value.abs() + half * (value + before).abs() + 2 * UNIT * before
+        assert ((grad[at, n] - (value + before)).abs() <= off).all()
+    untouched = torch.ones_like(grad, dtype=torch.bool)
+    untouched[winner, n] = untouched[target, n] = False
+    assert (grad[untouched] - before).abs().max() <= 1e-9
